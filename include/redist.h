@@ -377,6 +377,149 @@ int64_t redist_bulk_timeouts(void);
  */
 redist_status redist_debug_bounds_report(int64_t out[5]);
 
+/* ---- operators on a device's tiles ------------------------------------------------------------ */
+
+/*
+ * What runs on a tile between two redistributions (the paper's spmd_op, Section 2.2, is any function of
+ * the local tiles): the linear layer and layer norm with their gradients, and the orthogonalisation of a
+ * weight update.  All three are asynchronous on `cuda_stream`, allocate nothing and can be captured into
+ * a CUDA graph.  Scratch comes from the caller: the matching ..._scratch_bytes query says how much (it
+ * depends on sizes, strides and the alignment of the pointers), 256-byte aligned; NULL where it says 0;
+ * its contents are undefined before and after.  Sums, means and norms are held in 32 bits or more.
+ * Errors of all of them: EINVAL (null pointer, size, type, stride), EALIGN (a pointer off its element
+ * size, scratch off 256 bytes), EOVERLAP (an output overlaps an input, scratch or another output, except
+ * where said), ESCRATCH, EUNSUPPORTED (2^31 rows, columns or stacked matrices; 65536 for the latter),
+ * ECUDA.
+ */
+typedef enum redist_dtype { REDIST_BF16 = 0, REDIST_F16 = 1, REDIST_F32 = 2 } redist_dtype;
+
+typedef enum redist_activation {
+    REDIST_ACT_NONE = 0,
+    REDIST_ACT_RELU = 1,
+    REDIST_ACT_GELU = 2,        /* z Phi(z), Phi by the error function                                 */
+    REDIST_ACT_SILU = 3         /* z / (1 + exp(-z))                                                   */
+} redist_activation;
+
+/* A matrix in device memory: element (r, c) at data[r * row_stride + c * col_stride], strides in elements.
+   "Row-major" below: col_stride 1 and row_stride >= the number of columns.  Inputs called "either order"
+   may also be column-major (row_stride 1, col_stride >= the number of rows).  data NULL: absent. */
+typedef struct redist_matrix {
+    void *data;
+    int64_t row_stride, col_stride;
+} redist_matrix;
+
+/*
+ * redist_linear_forward -- out = activation(x w^T + bias) + residual.
+ *
+ *   rows >= 0, in_features >= 1, out_features >= 1
+ *   type            REDIST_BF16 or REDIST_F16: x, w, residual, out and pre
+ *   x               rows x in_features, either order;  w  out_features x in_features, either order
+ *   bias            out_features elements of bias_type (any), or NULL
+ *   residual        rows x out_features, row-major, or absent; may be `out` itself
+ *   out             rows x out_features, row-major
+ *   pre             rows x out_features, row-major, or absent: receives z = x w^T + bias for the backward pass
+ * Products are accumulated and the epilogue computed in 32 bits; each output is rounded once.  Operands
+ * whose lines do not start on 16-byte boundaries are laid out anew in scratch first.
+ *
+ * redist_linear_backward -- the gradients.  With dz = dy activation'(pre):
+ *   dx = dz w  (rows x in_features)     dw = dz^T x  (out_features x in_features)     dbias = sum of dz's rows
+ *   (the gradient of residual is dy itself).  dy, dx, dw row-major, of `type`; dbias out_features 32-bit
+ *   floats; dx, dw and dbias may each be absent.  Of `op` the sizes, types and activation, x (unless dw is
+ *   absent), w (unless dx is absent) and pre (unless the activation is NONE) are read.  dz is rounded to
+ *   `type` where it becomes an operand of a product; dbias sums the unrounded values in a fixed order.
+ *   rows = 0 gives zeros in dw and dbias.
+ */
+typedef struct redist_linear {
+    int64_t rows, in_features, out_features;
+    int32_t type, bias_type, activation, reserved;   /* reserved: 0 */
+    redist_matrix x, w, residual, out, pre;
+    const void *bias;
+} redist_linear;
+
+typedef struct redist_linear_grads {
+    redist_matrix dy, dx, dw;
+    float *dbias;
+} redist_linear_grads;
+
+size_t redist_linear_scratch_bytes(const redist_linear *op, const redist_linear_grads *grads); /* NULL: forward */
+redist_status redist_linear_forward(const redist_linear *op, void *scratch, size_t scratch_bytes, void *cuda_stream);
+redist_status redist_linear_backward(const redist_linear *op, const redist_linear_grads *grads, void *scratch,
+                                     size_t scratch_bytes, void *cuda_stream);
+
+/*
+ * redist_layer_norm_forward -- y = (x - mean) rstd gamma + beta for every row, with mean and
+ * rstd = 1 / sqrt(variance + eps) over the row (the variance is the mean squared difference from the mean).
+ *
+ *   rows >= 0, cols >= 1, eps >= 0
+ *   type                 of x and y (and dy, dx): REDIST_BF16, REDIST_F16 or REDIST_F32
+ *   x, y                 rows x cols, row-major
+ *   gamma, beta          cols elements of weight_type (any), or NULL: 1 and 0
+ *   mean, rstd           rows 32-bit floats each; the forward pass writes them (either may be NULL), the
+ *                        backward pass reads them
+ *
+ * redist_layer_norm_backward -- with xh = (x - mean) rstd and c = dy gamma:
+ *   dx = rstd (c - mean(c) - xh mean(c xh))     dgamma = sum of rows of dy xh     dbeta = sum of rows of dy
+ *   dgamma and dbeta are cols 32-bit floats each, summed in a fixed order; either may be NULL.  y and beta
+ *   are not read.  rows = 0 gives zeros in dgamma and dbeta.
+ */
+typedef struct redist_layer_norm {
+    int64_t rows, cols;
+    int32_t type, weight_type;
+    float eps;
+    int32_t reserved;                                 /* 0 */
+    redist_matrix x, y;
+    const void *gamma, *beta;
+    float *mean, *rstd;
+} redist_layer_norm;
+
+typedef struct redist_layer_norm_grads {
+    redist_matrix dy, dx;
+    float *dgamma, *dbeta;
+} redist_layer_norm_grads;
+
+redist_status redist_layer_norm_forward(const redist_layer_norm *op, void *cuda_stream);
+size_t redist_layer_norm_scratch_bytes(const redist_layer_norm *op, const redist_layer_norm_grads *grads);
+redist_status redist_layer_norm_backward(const redist_layer_norm *op, const redist_layer_norm_grads *grads, void *scratch,
+                                         size_t scratch_bytes, void *cuda_stream);
+
+/*
+ * redist_orthogonalize -- Newton-Schulz orthogonalisation of a stack of matrices, as the Muon optimiser
+ * applies it to a momentum matrix: X <- X / (|X| + eps) (Frobenius norm), then per step, on the side on
+ * which the Gram matrix is the smaller,
+ *     A = X X^T,   X <- a X + (b A + c A A) X
+ * and finally out = scale X.  The singular values move towards 1, the singular vectors stay.
+ *
+ *   batch, rows, cols >= 1;  1 <= steps <= 64;  eps >= 1e-30
+ *   type            of x: REDIST_BF16, REDIST_F16 or REDIST_F32; out is REDIST_BF16
+ *   x, out          row-major, matrix i at data + i * x_batch_stride (out_batch_stride) elements
+ *   coefficients    host; steps triples (a, b, c), read during the call
+ * The products run on 16-bit floats with 32-bit accumulation; X itself is carried from step to step in 22
+ * bits, because small singular values grow by a factor of a per step and with them every error made in X.
+ * Intermediates are scaled by powers of two found on the host from the coefficients; coefficients under
+ * which a singular value could leave [0, 256] are refused (EINVAL).  A matrix with an infinity or NaN
+ * gives NaN throughout, a zero matrix zeros.
+ */
+typedef struct redist_orthogonal {
+    int64_t batch, rows, cols;
+    int32_t type, steps;
+    double eps;
+    float scale;
+    int32_t reserved;                                 /* 0 */
+    redist_matrix x, out;
+    int64_t x_batch_stride, out_batch_stride;
+    const float *coefficients;
+} redist_orthogonal;
+
+size_t redist_orthogonalize_scratch_bytes(const redist_orthogonal *op);
+redist_status redist_orthogonalize(const redist_orthogonal *op, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/*
+ * redist_product_timeouts -- health counter of the matrix products, as redist_bulk_timeouts is of the bulk
+ * copies: thread blocks whose bounded wait ("wait_polls") ran out on the current device.  Such a block
+ * leaves its tiles unwritten and returns.  0 in a healthy run; -1 on a CUDA error.  Synchronizes the device.
+ */
+int64_t redist_product_timeouts(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -40,7 +40,12 @@ EXPORTS = (
     "redist_plan_height", "redist_plan_cost", "redist_plan_num_steps", "redist_plan_num_launches",
     "redist_plan_step_info", "redist_plan_launch_info", "redist_plan_describe", "redist_base_offsets",
     "redist_status_string", "redist_last_cuda_error", "redist_bulk_timeouts",
+    "redist_linear_scratch_bytes", "redist_linear_forward", "redist_linear_backward",
+    "redist_layer_norm_forward", "redist_layer_norm_scratch_bytes", "redist_layer_norm_backward",
+    "redist_orthogonalize_scratch_bytes", "redist_orthogonalize", "redist_product_timeouts",
 )
+
+ACTIVATIONS = ("none", "relu", "gelu", "silu")
 
 
 class RedistError(RuntimeError):
@@ -67,6 +72,40 @@ class LaunchInfo(ctypes.Structure):
                 ("vector_bytes", ctypes.c_int32), ("run_bytes", ctypes.c_int64), ("bytes_read", ctypes.c_int64),
                 ("bytes_written", ctypes.c_int64), ("n_items", ctypes.c_int64), ("fanout", ctypes.c_int32),
                 ("variant", ctypes.c_int32)]
+
+
+class _Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("col_stride", ctypes.c_int64)]
+
+
+class _Linear(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("in_features", ctypes.c_int64), ("out_features", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("bias_type", ctypes.c_int32), ("activation", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("x", _Matrix), ("w", _Matrix), ("residual", _Matrix), ("out", _Matrix),
+                ("pre", _Matrix), ("bias", ctypes.c_void_p)]
+
+
+class _LinearGrads(ctypes.Structure):
+    _fields_ = [("dy", _Matrix), ("dx", _Matrix), ("dw", _Matrix), ("dbias", ctypes.c_void_p)]
+
+
+class _LayerNorm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("type", ctypes.c_int32),
+                ("weight_type", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("x", _Matrix), ("y", _Matrix), ("gamma", ctypes.c_void_p), ("beta", ctypes.c_void_p),
+                ("mean", ctypes.c_void_p), ("rstd", ctypes.c_void_p)]
+
+
+class _LayerNormGrads(ctypes.Structure):
+    _fields_ = [("dy", _Matrix), ("dx", _Matrix), ("dgamma", ctypes.c_void_p), ("dbeta", ctypes.c_void_p)]
+
+
+class _Orthogonal(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("steps", ctypes.c_int32), ("eps", ctypes.c_double),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_int32), ("x", _Matrix), ("out", _Matrix),
+                ("x_batch_stride", ctypes.c_int64), ("out_batch_stride", ctypes.c_int64),
+                ("coefficients", ctypes.c_void_p)]
 
 
 _lib = None
@@ -137,6 +176,24 @@ def load() -> ctypes.CDLL:
     lib.redist_tuning_reset.restype = None
     lib.redist_plan_gpu_split.argtypes = [vp, i32, i32, ctypes.POINTER(i64)]
     lib.redist_plan_gpu_split.restype = i32
+    lib.redist_linear_scratch_bytes.argtypes = [ctypes.POINTER(_Linear), ctypes.POINTER(_LinearGrads)]
+    lib.redist_linear_scratch_bytes.restype = sz
+    lib.redist_linear_forward.argtypes = [ctypes.POINTER(_Linear), vp, sz, vp]
+    lib.redist_linear_forward.restype = i32
+    lib.redist_linear_backward.argtypes = [ctypes.POINTER(_Linear), ctypes.POINTER(_LinearGrads), vp, sz, vp]
+    lib.redist_linear_backward.restype = i32
+    lib.redist_layer_norm_forward.argtypes = [ctypes.POINTER(_LayerNorm), vp]
+    lib.redist_layer_norm_forward.restype = i32
+    lib.redist_layer_norm_scratch_bytes.argtypes = [ctypes.POINTER(_LayerNorm), ctypes.POINTER(_LayerNormGrads)]
+    lib.redist_layer_norm_scratch_bytes.restype = sz
+    lib.redist_layer_norm_backward.argtypes = [ctypes.POINTER(_LayerNorm), ctypes.POINTER(_LayerNormGrads), vp, sz, vp]
+    lib.redist_layer_norm_backward.restype = i32
+    lib.redist_orthogonalize_scratch_bytes.argtypes = [ctypes.POINTER(_Orthogonal)]
+    lib.redist_orthogonalize_scratch_bytes.restype = sz
+    lib.redist_orthogonalize.argtypes = [ctypes.POINTER(_Orthogonal), vp, sz, vp]
+    lib.redist_orthogonalize.restype = i32
+    lib.redist_product_timeouts.argtypes = []
+    lib.redist_product_timeouts.restype = i64
     lib.redist_debug_bounds_report.argtypes = [ctypes.POINTER(i64)]
     lib.redist_debug_bounds_report.restype = i32
     _lib = lib
@@ -527,3 +584,223 @@ def shard_global(G, mesh_shape, dtype) -> list:
             t = t.narrow(k, int(o), int(c))
         out.append(t.contiguous())
     return out
+
+
+# ---- operators on a device's tiles -------------------------------------------------------------------
+#
+# Tensors in, tensors out; outputs that are not given are allocated.  Everything runs asynchronously on
+# ``stream`` (default: the current one); what a call allocates itself, scratch included, is allocated on
+# that stream, so the caching allocator hands it on in stream order.  Tensors of another stream than their
+# own need the usual care of the caller (wait_stream, record_stream).
+
+_TYPE_CODES = None
+_NO_MATRIX = (None, 0, 0)
+
+
+def _type_code(t, what: str) -> int:
+    global _TYPE_CODES
+    if _TYPE_CODES is None:
+        import torch
+        _TYPE_CODES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+    code = _TYPE_CODES.get(t.dtype)
+    if code is None:
+        raise RedistError(1, f"{what} is bfloat16, float16 or float32, not {t.dtype}")
+    return code
+
+
+def _need(condition: bool, what: str) -> None:
+    if not condition:
+        raise RedistError(1, what)
+
+
+def _matrix(t, rows: int, cols: int, like, what: str):
+    """``t`` as a redist_matrix of the given size, of the type and on the device of ``like``."""
+    if t is None:
+        return _NO_MATRIX
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise RedistError(1, f"{what} has to be {rows} x {cols}, not {tuple(t.shape)}")
+    if t.dtype != like.dtype or t.device != like.device:
+        raise RedistError(1, f"{what} has to be of {like.dtype} on {like.device}, not {t.dtype} on {t.device}")
+    return (t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _vector(t, length: int, like, what: str, dtype=None):
+    """Address and type code of a contiguous vector on the device of ``like``."""
+    if t is None:
+        return None, 0
+    _need(t.dim() == 1 and t.shape[0] == length and t.device == like.device and (length <= 1 or t.stride(0) == 1),
+          f"{what} has to be a contiguous vector of {length} elements on {like.device}")
+    _need(dtype is None or t.dtype == dtype, f"{what} has to be of {dtype}")
+    return t.data_ptr(), _type_code(t, what)
+
+
+class _On:
+    """The stream a call runs on; inside the context torch allocates for that stream."""
+
+    def __init__(self, like, stream):
+        import torch
+        _need(like.is_cuda, "CUDA tensors are required")
+        _need(like.device.index == torch.cuda.current_device(), "tensors have to be on the current device")
+        self.torch, self.given = torch, stream
+        self.context = torch.cuda.stream(stream) if stream is not None else None
+        self.ptr = (stream if stream is not None else torch.cuda.current_stream()).cuda_stream or None
+
+    def __enter__(self):
+        if self.context is not None:
+            self.context.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self.context is not None:
+            self.context.__exit__(*exc)
+
+    def scratch(self, need: int, given, like):
+        if not need:
+            return None, None, 0
+        t = given if given is not None else self.torch.empty(need, dtype=self.torch.uint8, device=like.device)
+        _need(t.is_cuda and t.is_contiguous(), "scratch has to be a contiguous CUDA tensor")
+        return t, t.data_ptr(), t.numel() * t.element_size()
+
+
+def _activation(name: str) -> int:
+    if name not in ACTIVATIONS:
+        raise RedistError(1, f"activation is one of {ACTIVATIONS}, not {name!r}")
+    return ACTIVATIONS.index(name)
+
+
+def linear_forward(x, w, bias=None, residual=None, activation: str = "none", out=None, pre=None, scratch=None, stream=None):
+    """``redist_linear_forward``: ``activation(x @ w.T + bias) + residual``, in one pass over the products.
+
+    ``x`` (rows, in) and ``w`` (out, in), bfloat16 or float16, rows or columns contiguous; ``bias`` (out,) of any
+    type; ``residual`` (rows, out); ``pre`` (rows, out), if given, receives ``x @ w.T + bias`` for the backward pass.
+    Returns ``out`` (rows, out)."""
+    lib = _lib or load()
+    _need(x.dim() == 2 and w.dim() == 2, "x and w are matrices")
+    rows, k = x.shape
+    n = w.shape[0]
+    with _On(x, stream) as on:
+        if out is None:
+            out = on.torch.empty((rows, n), dtype=x.dtype, device=x.device)
+        b, bt = _vector(bias, n, x, "bias")
+        op = _Linear(rows, k, n, _type_code(x, "x"), bt, _activation(activation), 0, _matrix(x, rows, k, x, "x"),
+                     _matrix(w, n, k, x, "w"), _matrix(residual, rows, n, x, "residual"), _matrix(out, rows, n, x, "out"),
+                     _matrix(pre, rows, n, x, "pre"), b)
+        keep, sp, sn = on.scratch(lib.redist_linear_scratch_bytes(op, None), scratch, x)
+        rc = lib.redist_linear_forward(op, sp, sn, on.ptr)
+    if rc:
+        raise RedistError(rc, "redist_linear_forward")
+    return out
+
+
+def linear_backward(dy, x, w, pre=None, activation: str = "none", need=(True, True, True), dx=None, dw=None, dbias=None,
+                    scratch=None, stream=None):
+    """``redist_linear_backward``: ``(dx, dw, dbias)``, the gradients of :func:`linear_forward` (that of ``residual`` is
+    ``dy`` itself).  ``need`` says which of the three are wanted; the others are None.  ``pre`` is what the forward pass
+    kept (not needed without an activation).  dx and dw have the type of ``dy``, dbias is float32."""
+    lib = _lib or load()
+    _need(dy.dim() == 2 and x.dim() == 2 and w.dim() == 2, "dy, x and w are matrices")
+    rows, n = dy.shape
+    k = x.shape[1]
+    act = _activation(activation)
+    with _On(dy, stream) as on:
+        empty = on.torch.empty
+        if need[0] and dx is None:
+            dx = empty((rows, k), dtype=dy.dtype, device=dy.device)
+        if need[1] and dw is None:
+            dw = empty((n, k), dtype=dy.dtype, device=dy.device)
+        if need[2] and dbias is None:
+            dbias = empty((n,), dtype=on.torch.float32, device=dy.device)
+        op = _Linear(rows, k, n, _type_code(dy, "dy"), 0, act, 0, _matrix(x, rows, k, dy, "x"), _matrix(w, n, k, dy, "w"),
+                     _NO_MATRIX, _NO_MATRIX, _matrix(pre, rows, n, dy, "pre"), None)
+        g = _LinearGrads(_matrix(dy, rows, n, dy, "dy"), _matrix(dx if need[0] else None, rows, k, dy, "dx"),
+                         _matrix(dw if need[1] else None, n, k, dy, "dw"),
+                         _vector(dbias if need[2] else None, n, dy, "dbias", on.torch.float32)[0])
+        keep, sp, sn = on.scratch(lib.redist_linear_scratch_bytes(op, g), scratch, dy)
+        rc = lib.redist_linear_backward(op, g, sp, sn, on.ptr)
+    if rc:
+        raise RedistError(rc, "redist_linear_backward")
+    return dx if need[0] else None, dw if need[1] else None, dbias if need[2] else None
+
+
+def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, out=None, stream=None):
+    """``redist_layer_norm_forward``: ``(y, mean, rstd)``.  ``x`` (rows, cols) in bfloat16, float16 or float32 with
+    contiguous rows; ``gamma`` and ``beta`` (cols,), both of one type; ``mean`` and ``rstd`` (rows,) in float32 are
+    what the backward pass needs."""
+    lib = _lib or load()
+    _need(x.dim() == 2, "x is a matrix")
+    rows, cols = x.shape
+    with _On(x, stream) as on:
+        if out is None:
+            out = on.torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        stats = on.torch.empty((2, rows), dtype=on.torch.float32, device=x.device)
+        _need(gamma is None or beta is None or gamma.dtype == beta.dtype, "gamma and beta have to be of one type")
+        g, gt = _vector(gamma, cols, x, "gamma")
+        b, bt = _vector(beta, cols, x, "beta")
+        at = stats.data_ptr()
+        op = _LayerNorm(rows, cols, _type_code(x, "x"), gt if g else bt, eps, 0, _matrix(x, rows, cols, x, "x"),
+                        _matrix(out, rows, cols, x, "out"), g, b, at or None, at + 4 * rows if at else None)
+        rc = lib.redist_layer_norm_forward(op, on.ptr)
+    if rc:
+        raise RedistError(rc, "redist_layer_norm_forward")
+    return out, stats[0], stats[1]
+
+
+def layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, scratch=None, stream=None):
+    """``redist_layer_norm_backward``: ``(dx, dgamma, dbeta)``; the last two are float32.  ``mean`` and ``rstd`` are the
+    forward pass's; ``gamma`` may be None."""
+    lib = _lib or load()
+    _need(dy.dim() == 2, "dy is a matrix")
+    rows, cols = dy.shape
+    with _On(dy, stream) as on:
+        f32 = on.torch.float32
+        if dx is None:
+            dx = on.torch.empty((rows, cols), dtype=dy.dtype, device=dy.device)
+        dgamma = on.torch.empty((cols,), dtype=f32, device=dy.device)
+        dbeta = on.torch.empty((cols,), dtype=f32, device=dy.device)
+        _need(mean is not None and rstd is not None, "mean and rstd are required")
+        g, gt = _vector(gamma, cols, dy, "gamma")
+        op = _LayerNorm(rows, cols, _type_code(dy, "dy"), gt, 0.0, 0, _matrix(x, rows, cols, dy, "x"), _NO_MATRIX, g, None,
+                        _vector(mean, rows, dy, "mean", f32)[0], _vector(rstd, rows, dy, "rstd", f32)[0])
+        grads = _LayerNormGrads(_matrix(dy, rows, cols, dy, "dy"), _matrix(dx, rows, cols, dy, "dx"), dgamma.data_ptr(),
+                                dbeta.data_ptr())
+        keep, sp, sn = on.scratch(lib.redist_layer_norm_scratch_bytes(op, grads), scratch, dy)
+        rc = lib.redist_layer_norm_backward(op, grads, sp, sn, on.ptr)
+    if rc:
+        raise RedistError(rc, "redist_layer_norm_backward")
+    return dx, dgamma, dbeta
+
+
+def orthogonalize(x, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale: float = 1.0,
+                  out=None, scratch=None, stream=None):
+    """``redist_orthogonalize``: every matrix of ``x`` -- (rows, cols) or (batch, rows, cols), bfloat16, float16 or
+    float32, rows contiguous -- after ``steps`` Newton-Schulz steps, times ``scale``, in bfloat16.  ``coefficients`` is
+    one triple for all steps, or one triple per step."""
+    lib = _lib or load()
+    _need(x.dim() in (2, 3), "x is a matrix or a stack of matrices")
+    _need(1 <= steps <= 64, "1 to 64 steps")
+    flat = [float(v) for c in coefficients for v in (c if hasattr(c, "__len__") else (c,))]
+    if len(flat) == 3:
+        flat = flat * steps
+    _need(len(flat) == 3 * steps, "coefficients is one triple, or one per step")
+    with _On(x, stream) as on:
+        bf16 = on.torch.bfloat16
+        if out is None:
+            out = on.torch.empty(x.shape, dtype=bf16, device=x.device)
+        _need(out.shape == x.shape and out.dtype == bf16 and out.device == x.device, "out has to be x's shape in bfloat16")
+        if x.numel() == 0:
+            return out
+        batch = x.shape[0] if x.dim() == 3 else 1
+        op = _Orthogonal(batch, x.shape[-2], x.shape[-1], _type_code(x, "x"), steps, eps, scale, 0,
+                         (x.data_ptr(), x.stride(-2), x.stride(-1)), (out.data_ptr(), out.stride(-2), out.stride(-1)),
+                         x.stride(0) if x.dim() == 3 else 0, out.stride(0) if x.dim() == 3 else 0,
+                         ctypes.addressof(coefs := (ctypes.c_float * len(flat))(*flat)))
+        keep, sp, sn = on.scratch(lib.redist_orthogonalize_scratch_bytes(op), scratch, x)
+        rc = lib.redist_orthogonalize(op, sp, sn, on.ptr)
+    if rc:
+        raise RedistError(rc, "redist_orthogonalize")
+    return out
+
+
+def redist_product_timeouts() -> int:
+    """Thread blocks of the matrix products whose bounded wait ran out on the current device (0 in a healthy run)."""
+    return int(load().redist_product_timeouts())

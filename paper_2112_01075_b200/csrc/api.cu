@@ -217,6 +217,14 @@ redist_status run_plan(const Plan &p, const void *const *src_shards, void *const
 
 }  // namespace redist
 
+namespace redist {
+Tuning current_tuning()
+{
+    std::lock_guard<std::mutex> lock(g_mutex);
+    return g_tuning;
+}
+}  // namespace redist
+
 extern "C" {
 
 const char *redist_status_string(redist_status s)

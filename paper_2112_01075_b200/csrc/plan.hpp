@@ -79,6 +79,9 @@ struct Tuning {
     }
 };
 
+// The values in force now (the operators have no plan to copy them into).
+Tuning current_tuning();
+
 enum BufKind { BUF_SRC = 0, BUF_DST = 1, BUF_SCRATCH0 = 2, BUF_SCRATCH1 = 3, BUF_GLOBAL = 4 };
 
 struct Launch {
