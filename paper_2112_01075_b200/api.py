@@ -14,6 +14,7 @@ import contextlib
 import ctypes
 import json
 import os
+import struct
 from typing import List, Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -592,74 +593,106 @@ def shard_global(G, mesh_shape, dtype) -> list:
 # ``stream`` (default: the current one); what a call allocates itself, scratch included, is allocated on
 # that stream, so the caching allocator hands it on in stream order.  Tensors of another stream than their
 # own need the usual care of the caller (wait_stream, record_stream).
+#
+# The smallest calls take less time on the GPU than a few dozen lines of Python: arguments go over as one
+# packed block per call (the layout of the C structures), and scratch is asked for where it is needed.
 
-_TYPE_CODES = None
-_NO_MATRIX = (None, 0, 0)
+_MATRIX = "Pqq"
+_pack_linear = struct.Struct("3q4i" + _MATRIX * 5 + "P").pack
+_pack_linear_grads = struct.Struct(_MATRIX * 3 + "P").pack
+_pack_layer_norm = struct.Struct("2q2ifi" + _MATRIX * 2 + "4P").pack
+_pack_layer_norm_grads = struct.Struct(_MATRIX * 2 + "2P").pack
+_pack_orthogonal = struct.Struct("3q2idfi" + _MATRIX * 2 + "2qP").pack
+_ESCRATCH = 5
+
+_ops = None
 
 
-def _type_code(t, what: str) -> int:
-    global _TYPE_CODES
-    if _TYPE_CODES is None:
+class _Operators:
+    """torch, its type codes, and the entry points with the argument types of a packed block."""
+
+    def __init__(self):
         import torch
-        _TYPE_CODES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-    code = _TYPE_CODES.get(t.dtype)
+
+        lib = load()
+        self.torch, self.empty = torch, torch.empty
+        self.codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+        self.u8, self.f32, self.bf16 = torch.uint8, torch.float32, torch.bfloat16
+        self.current_device = torch.cuda.current_device
+        self.raw_stream = torch._C._cuda_getCurrentRawStream if torch.cuda.is_available() else None
+        vp, sz = ctypes.c_void_p, ctypes.c_size_t
+        for name, blocks, scratch in (("linear_forward", 1, True), ("linear_backward", 2, True), ("layer_norm_forward", 1, False),
+                                      ("layer_norm_backward", 2, True), ("orthogonalize", 1, True)):
+            fn = lib["redist_" + name]                       # an object of its own: the attribute keeps its types
+            fn.argtypes, fn.restype = [vp] * blocks + ([vp, sz] if scratch else []) + [vp], ctypes.c_int32
+            setattr(self, name, fn)
+        for name, blocks in (("linear", 2), ("layer_norm", 2), ("orthogonalize", 1)):
+            fn = lib[f"redist_{name}_scratch_bytes"]
+            fn.argtypes, fn.restype = [vp] * blocks, sz
+            setattr(self, name + "_scratch_bytes", fn)
+
+    def stream(self, device, given):
+        """The stream a call on ``device`` runs on (an address)."""
+        if device.type != "cuda":
+            raise RedistError(1, "CUDA tensors are required")
+        if device.index != self.current_device():
+            raise RedistError(1, "tensors have to be on the current device")
+        return given.cuda_stream if given is not None else self.raw_stream(device.index)
+
+    def scratch(self, need, given, device, what):
+        """(tensor, address, bytes) of the scratch of one call."""
+        if not need:
+            return None, None, 0
+        if given is None:
+            given = self.empty(need, dtype=self.u8, device=device)
+        elif not given.is_cuda or not given.is_contiguous():
+            raise RedistError(1, "scratch has to be a contiguous CUDA tensor")
+        return given, given.data_ptr(), given.numel() * given.element_size()
+
+
+def _operators() -> _Operators:
+    global _ops
+    if _ops is None:
+        _ops = _Operators()
+    return _ops
+
+
+def _allocating(stream):
+    """A context in which torch allocates for ``stream``."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+    return torch.cuda.stream(stream)
+
+
+def _code(o, t, what: str) -> int:
+    code = o.codes.get(t.dtype)
     if code is None:
         raise RedistError(1, f"{what} is bfloat16, float16 or float32, not {t.dtype}")
     return code
 
 
-def _need(condition: bool, what: str) -> None:
-    if not condition:
-        raise RedistError(1, what)
-
-
-def _matrix(t, rows: int, cols: int, like, what: str):
-    """``t`` as a redist_matrix of the given size, of the type and on the device of ``like``."""
+def _matrix(t, shape, dtype, device, what: str):
+    """``t`` as the three fields of a redist_matrix, checked."""
     if t is None:
-        return _NO_MATRIX
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise RedistError(1, f"{what} has to be {rows} x {cols}, not {tuple(t.shape)}")
-    if t.dtype != like.dtype or t.device != like.device:
-        raise RedistError(1, f"{what} has to be of {like.dtype} on {like.device}, not {t.dtype} on {t.device}")
-    return (t.data_ptr(), t.stride(0), t.stride(1))
+        return 0, 0, 0
+    if t.shape != shape:
+        raise RedistError(1, f"{what} has to be {shape[0]} x {shape[1]}, not {tuple(t.shape)}")
+    if t.dtype is not dtype or t.device != device:
+        raise RedistError(1, f"{what} has to be of {dtype} on {device}, not {t.dtype} on {t.device}")
+    a, b = t.stride()
+    return t.data_ptr(), a, b
 
 
-def _vector(t, length: int, like, what: str, dtype=None):
-    """Address and type code of a contiguous vector on the device of ``like``."""
+def _vector(o, t, length: int, device, what: str, dtype=None):
+    """Address and type code of a contiguous vector."""
     if t is None:
-        return None, 0
-    _need(t.dim() == 1 and t.shape[0] == length and t.device == like.device and (length <= 1 or t.stride(0) == 1),
-          f"{what} has to be a contiguous vector of {length} elements on {like.device}")
-    _need(dtype is None or t.dtype == dtype, f"{what} has to be of {dtype}")
-    return t.data_ptr(), _type_code(t, what)
-
-
-class _On:
-    """The stream a call runs on; inside the context torch allocates for that stream."""
-
-    def __init__(self, like, stream):
-        import torch
-        _need(like.is_cuda, "CUDA tensors are required")
-        _need(like.device.index == torch.cuda.current_device(), "tensors have to be on the current device")
-        self.torch, self.given = torch, stream
-        self.context = torch.cuda.stream(stream) if stream is not None else None
-        self.ptr = (stream if stream is not None else torch.cuda.current_stream()).cuda_stream or None
-
-    def __enter__(self):
-        if self.context is not None:
-            self.context.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self.context is not None:
-            self.context.__exit__(*exc)
-
-    def scratch(self, need: int, given, like):
-        if not need:
-            return None, None, 0
-        t = given if given is not None else self.torch.empty(need, dtype=self.torch.uint8, device=like.device)
-        _need(t.is_cuda and t.is_contiguous(), "scratch has to be a contiguous CUDA tensor")
-        return t, t.data_ptr(), t.numel() * t.element_size()
+        return 0, 0
+    if t.shape != (length,) or t.device != device or not t.is_contiguous():
+        raise RedistError(1, f"{what} has to be a contiguous vector of {length} elements on {device}")
+    if dtype is not None and t.dtype is not dtype:
+        raise RedistError(1, f"{what} has to be of {dtype}")
+    return t.data_ptr(), _code(o, t, what)
 
 
 def _activation(name: str) -> int:
@@ -668,25 +701,41 @@ def _activation(name: str) -> int:
     return ACTIVATIONS.index(name)
 
 
+def _matrices(**tensors) -> None:
+    for name, t in tensors.items():
+        if t.dim() != 2:
+            raise RedistError(1, f"{name} has to be a matrix, not of {t.dim()} dimensions")
+
+
 def linear_forward(x, w, bias=None, residual=None, activation: str = "none", out=None, pre=None, scratch=None, stream=None):
     """``redist_linear_forward``: ``activation(x @ w.T + bias) + residual``, in one pass over the products.
 
     ``x`` (rows, in) and ``w`` (out, in), bfloat16 or float16, rows or columns contiguous; ``bias`` (out,) of any
     type; ``residual`` (rows, out); ``pre`` (rows, out), if given, receives ``x @ w.T + bias`` for the backward pass.
     Returns ``out`` (rows, out)."""
-    lib = _lib or load()
-    _need(x.dim() == 2 and w.dim() == 2, "x and w are matrices")
+    if stream is not None:
+        with _allocating(stream):
+            return _linear_forward(x, w, bias, residual, activation, out, pre, scratch, stream)
+    return _linear_forward(x, w, bias, residual, activation, out, pre, scratch, None)
+
+
+def _linear_forward(x, w, bias, residual, activation, out, pre, scratch, stream):
+    o = _ops or _operators()
+    _matrices(x=x, w=w)
     rows, k = x.shape
     n = w.shape[0]
-    with _On(x, stream) as on:
-        if out is None:
-            out = on.torch.empty((rows, n), dtype=x.dtype, device=x.device)
-        b, bt = _vector(bias, n, x, "bias")
-        op = _Linear(rows, k, n, _type_code(x, "x"), bt, _activation(activation), 0, _matrix(x, rows, k, x, "x"),
-                     _matrix(w, n, k, x, "w"), _matrix(residual, rows, n, x, "residual"), _matrix(out, rows, n, x, "out"),
-                     _matrix(pre, rows, n, x, "pre"), b)
-        keep, sp, sn = on.scratch(lib.redist_linear_scratch_bytes(op, None), scratch, x)
-        rc = lib.redist_linear_forward(op, sp, sn, on.ptr)
+    device, dtype, shape = x.device, x.dtype, (rows, n)
+    at = o.stream(device, stream)
+    if out is None:
+        out = o.empty(shape, dtype=dtype, device=device)
+    b, bt = _vector(o, bias, n, device, "bias")
+    op = _pack_linear(rows, k, n, _code(o, x, "x"), bt, _activation(activation), 0, x.data_ptr(), *x.stride(),
+                      *_matrix(w, (n, k), dtype, device, "w"), *_matrix(residual, shape, dtype, device, "residual"),
+                      *_matrix(out, shape, dtype, device, "out"), *_matrix(pre, shape, dtype, device, "pre"), b)
+    rc = o.linear_forward(op, None, 0, at) if scratch is None else _ESCRATCH
+    if rc == _ESCRATCH:                                      # operands off 16-byte boundaries: rare
+        keep, sp, sn = o.scratch(o.linear_scratch_bytes(op, None), scratch, device, "linear")
+        rc = o.linear_forward(op, sp, sn, at)
     if rc:
         raise RedistError(rc, "redist_linear_forward")
     return out
@@ -697,74 +746,101 @@ def linear_backward(dy, x, w, pre=None, activation: str = "none", need=(True, Tr
     """``redist_linear_backward``: ``(dx, dw, dbias)``, the gradients of :func:`linear_forward` (that of ``residual`` is
     ``dy`` itself).  ``need`` says which of the three are wanted; the others are None.  ``pre`` is what the forward pass
     kept (not needed without an activation).  dx and dw have the type of ``dy``, dbias is float32."""
-    lib = _lib or load()
-    _need(dy.dim() == 2 and x.dim() == 2 and w.dim() == 2, "dy, x and w are matrices")
+    if stream is not None:
+        with _allocating(stream):
+            return _linear_backward(dy, x, w, pre, activation, need, dx, dw, dbias, scratch, stream)
+    return _linear_backward(dy, x, w, pre, activation, need, dx, dw, dbias, scratch, None)
+
+
+def _linear_backward(dy, x, w, pre, activation, need, dx, dw, dbias, scratch, stream):
+    o = _ops or _operators()
+    _matrices(dy=dy, x=x, w=w)
     rows, n = dy.shape
     k = x.shape[1]
-    act = _activation(activation)
-    with _On(dy, stream) as on:
-        empty = on.torch.empty
-        if need[0] and dx is None:
-            dx = empty((rows, k), dtype=dy.dtype, device=dy.device)
-        if need[1] and dw is None:
-            dw = empty((n, k), dtype=dy.dtype, device=dy.device)
-        if need[2] and dbias is None:
-            dbias = empty((n,), dtype=on.torch.float32, device=dy.device)
-        op = _Linear(rows, k, n, _type_code(dy, "dy"), 0, act, 0, _matrix(x, rows, k, dy, "x"), _matrix(w, n, k, dy, "w"),
-                     _NO_MATRIX, _NO_MATRIX, _matrix(pre, rows, n, dy, "pre"), None)
-        g = _LinearGrads(_matrix(dy, rows, n, dy, "dy"), _matrix(dx if need[0] else None, rows, k, dy, "dx"),
-                         _matrix(dw if need[1] else None, n, k, dy, "dw"),
-                         _vector(dbias if need[2] else None, n, dy, "dbias", on.torch.float32)[0])
-        keep, sp, sn = on.scratch(lib.redist_linear_scratch_bytes(op, g), scratch, dy)
-        rc = lib.redist_linear_backward(op, g, sp, sn, on.ptr)
+    device, dtype = dy.device, dy.dtype
+    at = o.stream(device, stream)
+    empty, wide, tall, long = o.empty, (rows, n), (rows, k), (n, k)
+    if not need[0]:
+        dx = None
+    elif dx is None:
+        dx = empty(tall, dtype=dtype, device=device)
+    if not need[1]:
+        dw = None
+    elif dw is None:
+        dw = empty(long, dtype=dtype, device=device)
+    if not need[2]:
+        dbias = None
+    elif dbias is None:
+        dbias = empty((n,), dtype=o.f32, device=device)
+    op = _pack_linear(rows, k, n, _code(o, dy, "dy"), 0, _activation(activation), 0, *_matrix(x, tall, dtype, device, "x"),
+                      *_matrix(w, long, dtype, device, "w"), 0, 0, 0, 0, 0, 0, *_matrix(pre, wide, dtype, device, "pre"), 0)
+    g = _pack_linear_grads(dy.data_ptr(), *dy.stride(), *_matrix(dx, tall, dtype, device, "dx"),
+                           *_matrix(dw, long, dtype, device, "dw"), _vector(o, dbias, n, device, "dbias", o.f32)[0])
+    keep, sp, sn = o.scratch(o.linear_scratch_bytes(op, g), scratch, device, "linear")
+    rc = o.linear_backward(op, g, sp, sn, at)
     if rc:
         raise RedistError(rc, "redist_linear_backward")
-    return dx if need[0] else None, dw if need[1] else None, dbias if need[2] else None
+    return dx, dw, dbias
 
 
 def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, out=None, stream=None):
     """``redist_layer_norm_forward``: ``(y, mean, rstd)``.  ``x`` (rows, cols) in bfloat16, float16 or float32 with
     contiguous rows; ``gamma`` and ``beta`` (cols,), both of one type; ``mean`` and ``rstd`` (rows,) in float32 are
     what the backward pass needs."""
-    lib = _lib or load()
-    _need(x.dim() == 2, "x is a matrix")
-    rows, cols = x.shape
-    with _On(x, stream) as on:
-        if out is None:
-            out = on.torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-        stats = on.torch.empty((2, rows), dtype=on.torch.float32, device=x.device)
-        _need(gamma is None or beta is None or gamma.dtype == beta.dtype, "gamma and beta have to be of one type")
-        g, gt = _vector(gamma, cols, x, "gamma")
-        b, bt = _vector(beta, cols, x, "beta")
-        at = stats.data_ptr()
-        op = _LayerNorm(rows, cols, _type_code(x, "x"), gt if g else bt, eps, 0, _matrix(x, rows, cols, x, "x"),
-                        _matrix(out, rows, cols, x, "out"), g, b, at or None, at + 4 * rows if at else None)
-        rc = lib.redist_layer_norm_forward(op, on.ptr)
+    if stream is not None:
+        with _allocating(stream):
+            return _layer_norm_forward(x, gamma, beta, eps, out, stream)
+    return _layer_norm_forward(x, gamma, beta, eps, out, None)
+
+
+def _layer_norm_forward(x, gamma, beta, eps, out, stream):
+    o = _ops or _operators()
+    _matrices(x=x)
+    shape, dtype, device = x.shape, x.dtype, x.device
+    rows, cols = shape
+    at = o.stream(device, stream)
+    if out is None:
+        out = o.empty(shape, dtype=dtype, device=device)
+    mean, rstd = o.empty((2, rows), dtype=o.f32, device=device).unbind()
+    g, gt = _vector(o, gamma, cols, device, "gamma")
+    b, bt = _vector(o, beta, cols, device, "beta")
+    if g and b and gt != bt:
+        raise RedistError(1, "gamma and beta have to be of one type")
+    op = _pack_layer_norm(rows, cols, _code(o, x, "x"), gt if g else bt, eps, 0, x.data_ptr(), *x.stride(),
+                          *_matrix(out, shape, dtype, device, "out"), g, b, mean.data_ptr(), rstd.data_ptr())
+    rc = o.layer_norm_forward(op, at)
     if rc:
         raise RedistError(rc, "redist_layer_norm_forward")
-    return out, stats[0], stats[1]
+    return out, mean, rstd
 
 
 def layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, scratch=None, stream=None):
     """``redist_layer_norm_backward``: ``(dx, dgamma, dbeta)``; the last two are float32.  ``mean`` and ``rstd`` are the
     forward pass's; ``gamma`` may be None."""
-    lib = _lib or load()
-    _need(dy.dim() == 2, "dy is a matrix")
-    rows, cols = dy.shape
-    with _On(dy, stream) as on:
-        f32 = on.torch.float32
-        if dx is None:
-            dx = on.torch.empty((rows, cols), dtype=dy.dtype, device=dy.device)
-        dgamma = on.torch.empty((cols,), dtype=f32, device=dy.device)
-        dbeta = on.torch.empty((cols,), dtype=f32, device=dy.device)
-        _need(mean is not None and rstd is not None, "mean and rstd are required")
-        g, gt = _vector(gamma, cols, dy, "gamma")
-        op = _LayerNorm(rows, cols, _type_code(dy, "dy"), gt, 0.0, 0, _matrix(x, rows, cols, dy, "x"), _NO_MATRIX, g, None,
-                        _vector(mean, rows, dy, "mean", f32)[0], _vector(rstd, rows, dy, "rstd", f32)[0])
-        grads = _LayerNormGrads(_matrix(dy, rows, cols, dy, "dy"), _matrix(dx, rows, cols, dy, "dx"), dgamma.data_ptr(),
-                                dbeta.data_ptr())
-        keep, sp, sn = on.scratch(lib.redist_layer_norm_scratch_bytes(op, grads), scratch, dy)
-        rc = lib.redist_layer_norm_backward(op, grads, sp, sn, on.ptr)
+    if stream is not None:
+        with _allocating(stream):
+            return _layer_norm_backward(dy, x, gamma, mean, rstd, dx, scratch, stream)
+    return _layer_norm_backward(dy, x, gamma, mean, rstd, dx, scratch, None)
+
+
+def _layer_norm_backward(dy, x, gamma, mean, rstd, dx, scratch, stream):
+    o = _ops or _operators()
+    _matrices(dy=dy)
+    shape, dtype, device = dy.shape, dy.dtype, dy.device
+    rows, cols = shape
+    at = o.stream(device, stream)
+    if dx is None:
+        dx = o.empty(shape, dtype=dtype, device=device)
+    dgamma, dbeta = o.empty((2, cols), dtype=o.f32, device=device).unbind()
+    if mean is None or rstd is None:
+        raise RedistError(1, "mean and rstd are required")
+    g, gt = _vector(o, gamma, cols, device, "gamma")
+    op = _pack_layer_norm(rows, cols, _code(o, dy, "dy"), gt, 0.0, 0, *_matrix(x, shape, dtype, device, "x"), 0, 0, 0, g, 0,
+                          _vector(o, mean, rows, device, "mean", o.f32)[0], _vector(o, rstd, rows, device, "rstd", o.f32)[0])
+    grads = _pack_layer_norm_grads(dy.data_ptr(), *dy.stride(), *_matrix(dx, shape, dtype, device, "dx"), dgamma.data_ptr(),
+                                   dbeta.data_ptr())
+    keep, sp, sn = o.scratch(o.layer_norm_scratch_bytes(op, grads), scratch, device, "layer norm")
+    rc = o.layer_norm_backward(op, grads, sp, sn, at)
     if rc:
         raise RedistError(rc, "redist_layer_norm_backward")
     return dx, dgamma, dbeta
@@ -775,27 +851,38 @@ def orthogonalize(x, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps
     """``redist_orthogonalize``: every matrix of ``x`` -- (rows, cols) or (batch, rows, cols), bfloat16, float16 or
     float32, rows contiguous -- after ``steps`` Newton-Schulz steps, times ``scale``, in bfloat16.  ``coefficients`` is
     one triple for all steps, or one triple per step."""
-    lib = _lib or load()
-    _need(x.dim() in (2, 3), "x is a matrix or a stack of matrices")
-    _need(1 <= steps <= 64, "1 to 64 steps")
+    if stream is not None:
+        with _allocating(stream):
+            return _orthogonalize(x, steps, coefficients, eps, scale, out, scratch, stream)
+    return _orthogonalize(x, steps, coefficients, eps, scale, out, scratch, None)
+
+
+def _orthogonalize(x, steps, coefficients, eps, scale, out, scratch, stream):
+    o = _ops or _operators()
+    if x.dim() not in (2, 3):
+        raise RedistError(1, "x is a matrix or a stack of matrices")
+    if not 1 <= steps <= 64:
+        raise RedistError(1, "1 to 64 steps")
     flat = [float(v) for c in coefficients for v in (c if hasattr(c, "__len__") else (c,))]
     if len(flat) == 3:
         flat = flat * steps
-    _need(len(flat) == 3 * steps, "coefficients is one triple, or one per step")
-    with _On(x, stream) as on:
-        bf16 = on.torch.bfloat16
-        if out is None:
-            out = on.torch.empty(x.shape, dtype=bf16, device=x.device)
-        _need(out.shape == x.shape and out.dtype == bf16 and out.device == x.device, "out has to be x's shape in bfloat16")
-        if x.numel() == 0:
-            return out
-        batch = x.shape[0] if x.dim() == 3 else 1
-        op = _Orthogonal(batch, x.shape[-2], x.shape[-1], _type_code(x, "x"), steps, eps, scale, 0,
-                         (x.data_ptr(), x.stride(-2), x.stride(-1)), (out.data_ptr(), out.stride(-2), out.stride(-1)),
-                         x.stride(0) if x.dim() == 3 else 0, out.stride(0) if x.dim() == 3 else 0,
-                         ctypes.addressof(coefs := (ctypes.c_float * len(flat))(*flat)))
-        keep, sp, sn = on.scratch(lib.redist_orthogonalize_scratch_bytes(op), scratch, x)
-        rc = lib.redist_orthogonalize(op, sp, sn, on.ptr)
+    if len(flat) != 3 * steps:
+        raise RedistError(1, "coefficients is one triple, or one per step")
+    shape, device = x.shape, x.device
+    at = o.stream(device, stream)
+    code = _code(o, x, "x")
+    if out is None:
+        out = o.empty(shape, dtype=o.bf16, device=device)
+    elif out.shape != shape or out.dtype is not o.bf16 or out.device != device:
+        raise RedistError(1, "out has to be x's shape in bfloat16")
+    if x.numel() == 0:
+        return out
+    batch, xs, os = (shape[0], x.stride(), out.stride()) if len(shape) == 3 else (1, (0, *x.stride()), (0, *out.stride()))
+    triples = (ctypes.c_float * len(flat))(*flat)
+    op = _pack_orthogonal(batch, shape[-2], shape[-1], code, steps, eps, scale, 0, x.data_ptr(), xs[1], xs[2], out.data_ptr(), os[1],
+                          os[2], xs[0], os[0], ctypes.addressof(triples))
+    keep, sp, sn = o.scratch(o.orthogonalize_scratch_bytes(op), scratch, device, "orthogonalize")
+    rc = o.orthogonalize(op, sp, sn, at)
     if rc:
         raise RedistError(rc, "redist_orthogonalize")
     return out

@@ -26,8 +26,8 @@ OBJ = os.path.join(HERE, "_obj")
 LIB = os.path.join(HERE, "libredist_b200.so")
 LIB_BOUNDS = os.path.join(HERE, "libredist_b200_bounds.so")
 SOURCES = ["api.cu", "kernels.cu", "static_scratch.cu", "planner.cpp", "descriptor.cpp", "describe.cpp", "multi_gpu.cpp",
-           "operators.cu", "product.cu", "rows.cu"]
-HEADERS = ["plan.hpp", "copy_params.h", "kernels.h", "product.h", "rows.h", "elements.cuh"]
+           "operators.cu", "product.cu", "few.cu", "rows.cu"]
+HEADERS = ["plan.hpp", "copy_params.h", "kernels.h", "product.h", "rows.h", "elements.cuh", "activation.cuh"]
 CHECKED = ["kernels.cu"]          # sources that differ in the checked build
 # (source, object name, defines): the kernels compile as three parts side by side (see REDIST_PART in kernels.cu)
 UNITS = [(s, os.path.splitext(s)[0], []) for s in SOURCES if s != "kernels.cu"] + \

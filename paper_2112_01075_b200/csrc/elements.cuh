@@ -63,10 +63,10 @@ __device__ __forceinline__ uint4 load16_any(const void *p, int bytes)
     const uintptr_t at = reinterpret_cast<uintptr_t>(p);
     const uint32_t off = uint32_t(at & 15);
     const uint4 *q = reinterpret_cast<const uint4 *>(at - off);
-    const uint4 a = __ldg(q);
+    const uint4 a = *q;
     if (off == 0) return a;
     uint4 b = make_uint4(0, 0, 0, 0);
-    if (int(off) + bytes > 16) b = __ldg(q + 1);
+    if (int(off) + bytes > 16) b = q[1];
     const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     const uint32_t word = off >> 2, bit = (off & 3) * 8;
     uint32_t r[5];

@@ -208,12 +208,42 @@ redist_status check_backward(const redist_linear &q, const redist_linear_grads &
     return uintptr_t(g.dbias) % 4 ? REDIST_EALIGN : REDIST_OK;
 }
 
+// Scratch of a product whose sum may be split.
+void *parts_of(i64 m, i64 n, i64 k, Pieces &pieces)
+{
+    Product p = {};
+    p.m = m;
+    p.n = n;
+    p.k = k;
+    p.batch = 1;
+    p.kind = EPI_LINEAR;
+    const i64 bytes = product_scratch_bytes(p);
+    return bytes ? pieces.take(bytes) : nullptr;
+}
+
+// A forward call of a few rows reads its operands as they lie and needs no scratch.
+bool few_rows(const redist_linear &q)
+{
+    return q.rows <= kFewRows && row_major(q.x, q.rows, q.in_features) && row_major(q.w, q.out_features, q.in_features);
+}
+
+// Everything another forward call takes from scratch.
+struct Forward {
+    Placed x, w;
+    void *parts;
+    Forward(const redist_linear &q, Pieces &p)
+        : x(q.x, q.rows, q.in_features, p), w(q.w, q.out_features, q.in_features, p), parts(parts_of(q.rows, q.out_features, q.in_features, p))
+    {
+    }
+};
+
 // What a backward call takes from scratch, in the order in which it is laid out.
 struct Backward {
     bool fresh;             // dz is computed (or laid out) into scratch; else dy itself is the operand
     i64 ld_dz = 0;
     void *dz = nullptr;
     float *partials = nullptr;
+    void *parts_dx = nullptr, *parts_dw = nullptr;
     Placed w, x;
     Backward(const redist_linear &q, const redist_linear_grads &g, Pieces &p)
         : fresh((g.dx.data || g.dw.data) && (q.activation != REDIST_ACT_NONE || !operand_fits(g.dy.data, lines_of(g.dy, q.rows, q.out_features).ld, 0, 1))),
@@ -222,6 +252,8 @@ struct Backward {
     {
         ld_dz = fresh ? round_up(q.out_features, 64) : lines_of(g.dy, q.rows, q.out_features).ld;
         if (fresh) dz = p.take(q.rows * ld_dz * 2);
+        if (g.dx.data) parts_dx = parts_of(q.rows, q.in_features, q.out_features, p);
+        if (g.dw.data) parts_dw = parts_of(q.out_features, q.in_features, q.rows, p);
         if (g.dbias) partials = static_cast<float *>(p.take(i64(column_partial_bytes(q.rows, q.out_features))));
     }
 };
@@ -294,8 +326,7 @@ redist_status check_norm_grads(const redist_layer_norm &q, const redist_layer_no
 int sm_count()
 {
     int device = 0, sms = 0;
-    if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) sms = 148;
-    return sms;
+    return current_device(&device, &sms) == cudaSuccess ? sms : 148;
 }
 
 // ---- orthogonalisation ---------------------------------------------------------------------------------------
@@ -387,8 +418,8 @@ size_t redist_linear_scratch_bytes(const redist_linear *op, const redist_linear_
     if (!op) return 0;
     Pieces p{0};
     if (!grads) {
-        if (check_forward(*op) != REDIST_OK || op->rows == 0) return 0;
-        Placed x(op->x, op->rows, op->in_features, p), w(op->w, op->out_features, op->in_features, p);
+        if (check_forward(*op) != REDIST_OK || op->rows == 0 || few_rows(*op)) return 0;
+        Forward f(*op, p);
     } else {
         if (check_backward(*op, *grads) != REDIST_OK || op->rows == 0) return 0;
         Backward b(*op, *grads, p);
@@ -404,9 +435,10 @@ redist_status redist_linear_forward(const redist_linear *op, void *scratch, size
         TRY(check_forward(q));
         if (q.rows == 0) return REDIST_OK;
         const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-        Pieces p{uintptr_t(scratch)};
-        Placed x(q.x, q.rows, q.in_features, p), w(q.w, q.out_features, q.in_features, p);
-        const bool in_place = q.residual.data == q.out.data && lines_of(q.residual, q.rows, q.out_features).ld == lines_of(q.out, q.rows, q.out_features).ld;
+        const bool few = few_rows(q), in_place = q.residual.data == q.out.data &&
+                                                 lines_of(q.residual, q.rows, q.out_features).ld == lines_of(q.out, q.rows, q.out_features).ld;
+        Pieces p{uintptr_t(scratch)}, none{0};
+        const Forward f(q, few ? none : p);
         const Extent outs[3] = {extent(q.out, q.rows, q.out_features, 2), extent(q.pre, q.pre.data ? q.rows : 0, q.out_features, 2), extent(scratch, p.used)};
         const Extent ins[4] = {extent(q.x, q.rows, q.in_features, 2), extent(q.w, q.out_features, q.in_features, 2),
                                extent(q.bias, q.out_features * type_bytes(q.bias_type)),
@@ -414,9 +446,7 @@ redist_status redist_linear_forward(const redist_linear *op, void *scratch, size
         TRY(apart(outs, 3, ins, 4));
         TRY(check_scratch(scratch, scratch_bytes, p.used));
         const LaunchOptions o = options();
-        TRY(cuda(x.lay(q.type, o, stream)));
-        TRY(cuda(w.lay(q.type, o, stream)));
-        Product d = product_of(q.rows, q.out_features, q.in_features, q.type, x.operand(true), w.operand(true), q.out, q.rows, q.out_features);
+        Product d = product_of(q.rows, q.out_features, q.in_features, q.type, f.x.operand(true), f.w.operand(true), q.out, q.rows, q.out_features);
         d.e.bias = q.bias;
         d.e.bias_type = q.bias_type;
         d.e.activation = q.activation;
@@ -424,7 +454,14 @@ redist_status redist_linear_forward(const redist_linear *op, void *scratch, size
         if (q.residual.data) d.e.ld_residual = lines_of(q.residual, q.rows, q.out_features).ld;
         d.e.pre = q.pre.data;
         if (q.pre.data) d.e.ld_pre = lines_of(q.pre, q.rows, q.out_features).ld;
-        return cuda(launch_product(d, o, stream));
+        if (few) {
+            d.a = Operand{f.x.from.data, f.x.from.ld, 0, 0};
+            d.b = Operand{f.w.from.data, f.w.from.ld, 0, 0};
+            return cuda(launch_few_rows(d, o, stream));
+        }
+        TRY(cuda(f.x.lay(q.type, o, stream)));
+        TRY(cuda(f.w.lay(q.type, o, stream)));
+        return cuda(launch_product(d, f.parts, o, stream));
     } catch (...) {
         return REDIST_EINTERNAL;
     }
@@ -477,12 +514,12 @@ redist_status redist_linear_backward(const redist_linear *op, const redist_linea
         if (g.dx.data) {
             TRY(cuda(b.w.lay(q.type, o, stream)));
             TRY(cuda(launch_product(product_of(q.rows, q.in_features, q.out_features, q.type, Operand{dz, b.ld_dz, 0, 0}, b.w.operand(false), g.dx,
-                                               q.rows, q.in_features), o, stream)));
+                                               q.rows, q.in_features), b.parts_dx, o, stream)));
         }
         if (g.dw.data) {
             TRY(cuda(b.x.lay(q.type, o, stream)));
             TRY(cuda(launch_product(product_of(q.out_features, q.in_features, q.rows, q.type, Operand{dz, b.ld_dz, 0, 1}, b.x.operand(false), g.dw,
-                                               q.out_features, q.in_features), o, stream)));
+                                               q.out_features, q.in_features), b.parts_dw, o, stream)));
         }
         return REDIST_OK;
     } catch (...) {
@@ -608,7 +645,7 @@ redist_status redist_orthogonalize(const redist_orthogonal *op, void *scratch, s
             g.e.alpha = float(steps.a[k] * x * x);
             g.e.scale = first ? w.scale : nullptr;
             g.e.alpha_power = 2;
-            TRY(cuda(launch_product(g, o, stream)));
+            TRY(cuda(launch_product(g, nullptr, o, stream)));
             // B = b A + c A A (A alone where c is zero: its factor goes into the update)
             double factor = double(abc[1]) / steps.a[k];
             const void *poly = w.a;
@@ -622,7 +659,7 @@ redist_status redist_orthogonalize(const redist_orthogonal *op, void *scratch, s
                 g.e.ld_add = w.ld_gram;
                 g.e.add_batch = w.gram_plane;
                 g.e.scale = nullptr;
-                TRY(cuda(launch_product(g, o, stream)));
+                TRY(cuda(launch_product(g, nullptr, o, stream)));
                 factor = 1.0 / steps.b[k];
                 poly = w.b;
             }
@@ -648,7 +685,7 @@ redist_status redist_orthogonalize(const redist_orthogonal *op, void *scratch, s
             u.e.beta = float(double(abc[0]) * to * x);
             u.e.scale = first ? w.scale : nullptr;
             u.e.alpha_power = u.e.beta_power = 1;
-            TRY(cuda(launch_product(u, o, stream)));
+            TRY(cuda(launch_product(u, nullptr, o, stream)));
         }
         return REDIST_OK;
     } catch (...) {

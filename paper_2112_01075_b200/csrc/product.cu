@@ -2,7 +2,7 @@
 //
 // One thread block (CG = 1) or a pair of them on two SMs (CG = 2) owns a tile of 128 CG x BN outputs at a time and
 // walks over the sum in steps of 64: one thread brings the 128-byte wide slices of both operands into a ring of
-// shared-memory stages by TMA (128-byte swizzle), one thread issues the tcgen05.mma that consume them, and four
+// shared-memory stages by TMA (128-byte swizzle), one thread issues the tcgen05.mma that consume them, and eight
 // warps turn the finished accumulator of the previous tile into outputs while the next one runs: tensor memory holds
 // two accumulators of BN columns.  Operands may be contiguous along the sum or along their rows (the gradients need
 // both): only the boxes and the shared-memory descriptors differ.  Ragged sizes cost nothing extra: the TMA fills
@@ -15,23 +15,26 @@
 
 #include <cuda.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cstring>
 
+#include "activation.cuh"
 #include "elements.cuh"
+#include "rows.h"
 
 namespace redist {
 
 namespace {
 
 constexpr int kBK = 64;                 // elements of the sum per stage: 128 bytes, one swizzle row
-constexpr int kThreads = 256;           // warp 0 loads, warp 1 multiplies, warp 2 owns tensor memory, warps 4-7 store
+constexpr int kThreads = 384;           // warp 0 loads, warp 1 multiplies, warp 2 owns tensor memory, warps 4-11 store
 constexpr int kRing = 196608;           // bytes of the ring of stages
-constexpr int kPitch = 36;              // words per row of a warp's 32 x 32 transpose buffer: 16-byte accesses of
-                                        // eight lanes, by rows or by row groups, fall into distinct banks
-constexpr int kEpiBytes = 4 * 32 * kPitch * 4;
+constexpr int kPiece = 2048;            // a warp's 32 x 32 piece of 16-bit outputs: rows of 64 bytes, 64-byte swizzle
+constexpr int kEpiBytes = 8 * 2 * kPiece;                   // two pieces per warp: one is filled while one is stored
+constexpr int kBiasBytes = 8 * 32 * 4;
 constexpr int kBarBytes = 256;
-constexpr int kSmem = 1024 + kRing + kEpiBytes + kBarBytes;
+constexpr int kSmem = 1024 + kRing + kEpiBytes + kBiasBytes + kBarBytes;
 constexpr int kMaxStages = 12;
 
 __device__ unsigned int g_product_timeouts = 0;
@@ -39,9 +42,11 @@ __device__ unsigned int g_product_timeouts = 0;
 struct ProductParams {
     int32_t m, n, k_blocks, batch;
     int32_t tiles_m, tiles_n, tiles_per_matrix, tiles;
+    int32_t splits, k_per_split;        // parts of the sum, each a unit of work of its own (EPI_PARTIAL)
     int32_t symmetric, a_along_rows, b_along_rows;
     uint32_t idesc, wait_polls, test_extra_tx;
-    int32_t vector_out;                 // every row of out (and residual, pre) starts on a 16-byte boundary
+    int32_t aligned_out;                // every row of out and pre starts on a 16-byte boundary: pieces go out by TMA
+    int32_t aligned_residual;
     Epilogue e;
 };
 
@@ -54,18 +59,32 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
 
+// True when the phase is over, false when `polls` polls have not seen it end.  The loop is hidden from the compiler: the
+// loading and the multiplying warp stay convergent in its eyes, and the descriptors of what they issue in uniform
+// registers (a k-step took 400 cycles to issue when they did not, more than the tensor cores need for it).
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t polls)
 {
-    for (uint32_t i = 0; i < polls; ++i) {
-        uint32_t done;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.b32 %0, 1, 0, p;\n\t}"
-            : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (done) return true;
-    }
-    return false;
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, %3;\n"
+        "POLL:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "@p bra DONE;\n\t"
+        "sub.u32 n, n, 1;\n\t"
+        "setp.ne.u32 q, n, 0;\n\t"
+        "@q bra POLL;\n"
+        "DONE:\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(done) : "r"(bar), "r"(parity), "r"(polls) : "memory");
+    return done != 0;
+}
+
+// One lane of a convergent warp, always the same.
+__device__ __forceinline__ bool elected()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
@@ -184,7 +203,7 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32])
 // ---- tiles ---------------------------------------------------------------------------------------
 
 struct Tile {
-    int tm, tn, matrix;
+    int tm, tn, matrix, k0, k1;         // k0 ... k1: its steps of the sum
 };
 
 // Tiles of a matrix in groups of eight tile rows, column after column within a group, so that the blocks at work at
@@ -192,6 +211,14 @@ struct Tile {
 __device__ __forceinline__ Tile tile_at(const ProductParams &p, int t)
 {
     Tile r;
+    r.k0 = 0;
+    r.k1 = p.k_blocks;
+    if (p.splits > 1) {
+        const int part = t % p.splits;
+        t /= p.splits;
+        r.k0 = part * p.k_per_split;
+        r.k1 = min(p.k_blocks, r.k0 + p.k_per_split);
+    }
     r.matrix = t / p.tiles_per_matrix;
     int q = t - r.matrix * p.tiles_per_matrix;
     if (p.symmetric) {
@@ -212,33 +239,65 @@ __device__ __forceinline__ Tile tile_at(const ProductParams &p, int t)
 
 // ---- epilogue --------------------------------------------------------------------------------------
 
-__device__ __forceinline__ float activate(float z, int act)
-{
-    if (act == ACT_RELU) return z < 0.0f ? 0.0f : z;                     // NaN stays
-    if (act == ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    if (act == ACT_SILU) return __fdividef(z, 1.0f + __expf(-z));
-    return z;
-}
+// A warp takes its quarter of the lanes (rows) and half of the columns of an accumulator, 32 x 32 values at a time: a
+// lane holds 32 neighbours of one row, computes, rounds and writes them to a piece in shared memory, from where a TMA
+// store takes it (or, where rows are not on 16-byte boundaries, the warp itself, row by row).  Everything 32-bit stays
+// in registers; 12 us for a 256 x 256 tile when the 32-bit accumulators went through shared memory became 3 us.
 
-// `count` (1 to 8) neighbouring elements, from 16 bytes of packed ones.
-__device__ __forceinline__ void store_some(void *p, const uint4 &v, int count)
-{
-    if (count >= 8) {
-        *static_cast<uint4 *>(p) = v;
-        return;
+// Where the 16 bytes of columns 8 j ... 8 j + 7 of row r of a piece lie (the TMA's 64-byte swizzle).
+__device__ __forceinline__ uint32_t piece_at(int r, int j) { return uint32_t(r * 64 + ((j ^ ((r >> 1) & 3)) << 4)); }
+
+// A warp's two pieces, used in turn.
+struct Pieces {
+    uint8_t *smem;
+    uint32_t addr;
+    int turn = 0;
+
+    // the piece to fill next, free of the store that used it last
+    __device__ __forceinline__ uint8_t *next(int lane)
+    {
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
+        return smem + turn * kPiece;
     }
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 7; ++i)
-        if (i < count) static_cast<uint16_t *>(p)[i] = uint16_t(w[i >> 1] >> (16 * (i & 1)));
-}
 
-template <typename T> __device__ __forceinline__ uint4 pack8(const float (&v)[8])
+    // Rows row0 ... and columns col0 ... of the output are in the piece: send them off.
+    __device__ __forceinline__ void store(const CUtensorMap *map, int lane, int row0, int col0, int matrix)
+    {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                         ::"l"(map), "r"(addr + turn * kPiece), "r"(col0), "r"(row0), "r"(matrix) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        turn ^= 1;
+    }
+
+    // The same row by row, two bytes per lane.
+    __device__ __forceinline__ void store_rows(uint16_t *out, int64_t ld, int lane, int row0, int col0, int m, int n)
+    {
+        __syncwarp();
+        const uint8_t *piece = smem + turn * kPiece;
+        uint16_t *to = out + int64_t(row0) * ld + col0 + lane;
+        const bool in = col0 + lane < n;
+#pragma unroll 8
+        for (int r = 0; r < 32; ++r)
+            if (in && row0 + r < m) to[r * ld] = *reinterpret_cast<const uint16_t *>(piece + piece_at(r, lane >> 3) + (lane & 7) * 2);
+        __syncwarp();
+    }
+};
+
+template <typename T> __device__ __forceinline__ void put_row(uint8_t *piece, int lane, const float (&v)[32])
 {
-    return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<uint4 *>(piece + piece_at(lane, j)) =
+            make_uint4(pack2<T>(v[8 * j], v[8 * j + 1]), pack2<T>(v[8 * j + 2], v[8 * j + 3]), pack2<T>(v[8 * j + 4], v[8 * j + 5]),
+                       pack2<T>(v[8 * j + 6], v[8 * j + 7]));
 }
 
-template <typename T> __device__ __forceinline__ void unpack8(const uint4 &u, float (&v)[8])
+template <typename T> __device__ __forceinline__ void unpack8(const uint4 &u, float *v)
 {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -249,128 +308,92 @@ template <typename T> __device__ __forceinline__ void unpack8(const uint4 &u, fl
     }
 }
 
-// One 32 x 32 piece of the linear epilogue.  `buf` holds the accumulators, row by row; (row0, col0) is its place.
+// 32 x 32 values of the linear epilogue; `bias` holds the columns' biases, `ahead` the lane's row of the residual.
 template <typename T>
-__device__ __forceinline__ void linear_piece(const ProductParams &p, float *buf, int lane, int row0, int col0)
+__device__ __forceinline__ void linear_piece(const ProductParams &p, const CUtensorMap *map_out, const CUtensorMap *map_pre, Pieces &pieces,
+                                             float (&v)[32], const float *bias, const uint4 (&ahead)[4], int lane, int row0, int col0)
 {
     const Epilogue &e = p.e;
-    if (p.vector_out) {
-        const int c = col0 + (lane & 3) * 8, count = p.n - c;
-        if (count <= 0) return;
-        float bias[8];
+    if (e.bias) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bias[i] = e.bias && i < count ? load_any(e.bias, e.bias_type, c + i) : 0.0f;
-#pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            const int r = it * 8 + (lane >> 2), row = row0 + r;
-            if (row >= p.m) break;
-            const float4 *s = reinterpret_cast<const float4 *>(buf + r * kPitch + (lane & 3) * 8);
-            const float4 x = s[0], y = s[1];
-            float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += bias[i];
-            if (e.pre) store_some(static_cast<T *>(e.pre) + int64_t(row) * e.ld_pre + c, pack8<T>(v), count);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], e.activation);
-            if (e.residual) {
-                const T *q = static_cast<const T *>(e.residual) + int64_t(row) * e.ld_residual + c;
-                float w[8];
-                if (count >= 8) {
-                    unpack8<T>(*reinterpret_cast<const uint4 *>(q), w);      // may be the output itself
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = i < count ? to_float(q[i]) : 0.0f;
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += w[i];
-            }
-            store_some(static_cast<T *>(e.out) + int64_t(row) * e.ld_out + c, pack8<T>(v), count);
+        for (int j = 0; j < 8; ++j) {
+            const float4 b = *reinterpret_cast<const float4 *>(bias + 4 * j);
+            v[4 * j] += b.x;
+            v[4 * j + 1] += b.y;
+            v[4 * j + 2] += b.z;
+            v[4 * j + 3] += b.w;
         }
-    } else {
-        const int c = col0 + lane;
-        if (c >= p.n) return;
-        const float bias = e.bias ? load_any(e.bias, e.bias_type, c) : 0.0f;
-        for (int r = 0; r < 32 && row0 + r < p.m; ++r) {
-            const int64_t row = row0 + r;
-            float v = buf[r * kPitch + lane] + bias;
-            if (e.pre) static_cast<T *>(e.pre)[row * e.ld_pre + c] = from_float<T>(v);
-            v = activate(v, e.activation);
-            if (e.residual) v += to_float(static_cast<const T *>(e.residual)[row * e.ld_residual + c]);
-            static_cast<T *>(e.out)[row * e.ld_out + c] = from_float<T>(v);
+    }
+    if (e.pre) {
+        put_row<T>(pieces.next(lane), lane, v);
+        if (p.aligned_out) pieces.store(map_pre, lane, row0, col0, 0);
+        else pieces.store_rows(static_cast<uint16_t *>(e.pre), e.ld_pre, lane, row0, col0, p.m, p.n);
+    }
+    activate32(v, e.activation);
+    if (e.residual) {
+        float w[32];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) unpack8<T>(ahead[j], w + 8 * j);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] += w[i];
+    }
+    put_row<T>(pieces.next(lane), lane, v);
+    if (p.aligned_out) pieces.store(map_out, lane, row0, col0, 0);
+    else pieces.store_rows(static_cast<uint16_t *>(e.out), e.ld_out, lane, row0, col0, p.m, p.n);
+}
+
+// 32 x 32 values of the scaled epilogue; `hi` and `lo` hold the lane's row of what is added.  A mirrored piece is
+// written a second time with rows and columns exchanged.
+__device__ __forceinline__ void scaled_piece(const ProductParams &p, const CUtensorMap *map_out, const CUtensorMap *map_lo, Pieces &pieces,
+                                             float (&v)[32], const uint4 (&hi)[4], const uint4 (&lo)[4], int lane, int row0, int col0,
+                                             int matrix, float alpha, float beta, bool mirror)
+{
+    const Epilogue &e = p.e;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] *= alpha;
+    if (e.hi) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float w[8], u[8];
+            unpack8<__half>(hi[j], w);
+            unpack8<__half>(lo[j], u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[8 * j + i] = fmaf(beta, fmaf(u[i], 1.0f / 2048.0f, w[i]), v[8 * j + i]);
         }
+    }
+    uint8_t *piece = pieces.next(lane);
+    if (e.out_type == T_BF16) {
+        put_row<__nv_bfloat16>(piece, lane, v);
+        if (p.aligned_out) pieces.store(map_out, lane, row0, col0, matrix);
+        else pieces.store_rows(static_cast<uint16_t *>(e.out) + int64_t(matrix) * e.out_batch, e.ld_out, lane, row0, col0, p.m, p.n);
+        return;
+    }
+    put_row<__half>(piece, lane, v);
+    pieces.store(map_out, lane, row0, col0, matrix);
+    if (e.out_lo) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = (v[i] - __half2float(__float2half_rn(v[i]))) * 2048.0f;
+        put_row<__half>(pieces.next(lane), lane, v);
+        pieces.store(map_lo, lane, row0, col0, matrix);
+    }
+    if (mirror) {
+        piece = pieces.next(lane);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) *reinterpret_cast<__half *>(piece + piece_at(i, lane >> 3) + (lane & 7) * 2) = __float2half_rn(v[i]);
+        pieces.store(map_out, lane, col0, row0, matrix);
     }
 }
 
-// One piece of the scaled epilogue.  hi, lo and f16 outputs lie in workspaces whose rows start on 16-byte boundaries
-// and are padded to whole 16 bytes; only a bf16 output may be ragged.  f16 results leave their values in `buf`, from
-// where a mirrored tile is stored along its columns.
-__device__ __forceinline__ void scaled_piece(const ProductParams &p, float *buf, int lane, int row0, int col0, int matrix,
-                                             float alpha, float beta, bool mirror)
+// The lane's row of 32 neighbours from column col0 on, 16 bytes at a time; what lies outside n reads as zero (or as
+// the padding of a workspace row: it is not stored).
+template <bool ALIGNED> __device__ __forceinline__ void get_row(const uint16_t *row, bool in, int left, uint4 (&v)[4])
 {
-    const Epilogue &e = p.e;
-    const int c = col0 + (lane & 3) * 8, count = p.n - c;
-    if (count > 0) {
 #pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            const int r = it * 8 + (lane >> 2), row = row0 + r;
-            if (row >= p.m) break;
-            float4 *s = reinterpret_cast<float4 *>(buf + r * kPitch + (lane & 3) * 8);
-            const float4 x = s[0], y = s[1];
-            float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= alpha;
-            const int64_t at = int64_t(matrix) * e.add_batch + int64_t(row) * e.ld_add + c;
-            if (e.hi) {
-                float w[8];
-                unpack8<__half>(*reinterpret_cast<const uint4 *>(static_cast<const __half *>(e.hi) + at), w);
-                if (e.lo) {
-                    float u[8];
-                    unpack8<__half>(*reinterpret_cast<const uint4 *>(static_cast<const __half *>(e.lo) + at), u);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = fmaf(u[i], 1.0f / 2048.0f, w[i]);
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = fmaf(beta, w[i], v[i]);
-            }
-            const int64_t to = int64_t(matrix) * e.out_batch + int64_t(row) * e.ld_out + c;
-            if (e.out_type == T_BF16) {
-                __nv_bfloat16 *q = static_cast<__nv_bfloat16 *>(e.out) + to;
-                if (p.vector_out) {
-                    store_some(q, pack8<__nv_bfloat16>(v), count);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (i < count) q[i] = __float2bfloat16_rn(v[i]);
-                }
-            } else {
-                const uint4 h = pack8<__half>(v);
-                *reinterpret_cast<uint4 *>(static_cast<__half *>(e.out) + to) = h;
-                if (e.out_lo) {
-                    float w[8];
-                    unpack8<__half>(h, w);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = (v[i] - w[i]) * 2048.0f;
-                    *reinterpret_cast<uint4 *>(static_cast<__half *>(e.out_lo) + at) = pack8<__half>(w);
-                }
-                if (mirror) {
-                    s[0] = make_float4(v[0], v[1], v[2], v[3]);
-                    s[1] = make_float4(v[4], v[5], v[6], v[7]);
-                }
-            }
-        }
-    }
-    if (!mirror) return;
-    __syncwarp();
-    if (col0 + lane < p.n) {
-        __half *q = static_cast<__half *>(e.out) + int64_t(matrix) * e.out_batch + int64_t(col0 + lane) * e.ld_out + row0;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            if (row0 + g * 8 >= p.m) break;
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = buf[(g * 8 + i) * kPitch + lane];
-            *reinterpret_cast<uint4 *>(q + g * 8) = pack8<__half>(v);
-        }
+    for (int j = 0; j < 4; ++j) {
+        v[j] = make_uint4(0, 0, 0, 0);
+        if (!in || left <= 8 * j) continue;
+        if (ALIGNED) v[j] = *reinterpret_cast<const uint4 *>(row + 8 * j);
+        else v[j] = load16_any(row + 8 * j, min(left - 8 * j, 8) * 2);
     }
 }
 
@@ -379,27 +402,28 @@ __device__ __forceinline__ void scaled_piece(const ProductParams &p, float *buf,
 template <int CG, int BN, int KIND>
 __global__ void __launch_bounds__(kThreads, 1)
 redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                      const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_more,
                       const __grid_constant__ ProductParams p)
 {
     constexpr int kRowsB = BN / CG;                         // rows of B that this block loads
     constexpr int kStageA = 128 * 128, kStageB = kRowsB * 128, kStage = kStageA + kStageB;
     constexpr int kStages = kRing / kStage < kMaxStages ? kRing / kStage : kMaxStages;
     constexpr uint32_t kColumns = 2 * BN < 32 ? 32 : 2 * BN;
+    constexpr int kShare = BN >= 64 ? BN / 2 : BN;          // columns of an accumulator that one warp stores
+    constexpr int kStorers = 4 * (BN / kShare);
     static_assert((kColumns & (kColumns - 1)) == 0 && kColumns <= 512, "tensor memory is allocated in powers of two");
 
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
     uint8_t *ring = raw + (base - smem_addr(raw));
-    float *epi = reinterpret_cast<float *>(ring + kRing);
-    const uint32_t bars = base + kRing + kEpiBytes;
+    const uint32_t bars = base + kRing + kEpiBytes + kBiasBytes;
     auto full = [&](int s) { return bars + 8 * s; };
     auto empty = [&](int s) { return bars + 8 * (kStages + s); };
     auto acc_full = [&](int b) { return bars + 8 * (2 * kStages + b); };
     auto acc_free = [&](int b) { return bars + 8 * (2 * kStages + 2 + b); };
-    const uint32_t tmem_at = bars + 8 * (2 * kStages + 4), failed_at = tmem_at + 4;
-    volatile uint32_t *tmem_word = reinterpret_cast<volatile uint32_t *>(ring + kRing + kEpiBytes + 8 * (2 * kStages + 4));
+    const uint32_t tmem_at = bars + 8 * (2 * kStages + 4);
+    volatile uint32_t *tmem_word = reinterpret_cast<volatile uint32_t *>(ring + kRing + kEpiBytes + kBiasBytes + 8 * (2 * kStages + 4));
     volatile uint32_t *failed = tmem_word + 1;
-    (void)failed_at;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 1 ? 0 : cluster_rank();
@@ -412,7 +436,7 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         }
         for (int b = 0; b < 2; ++b) {
             bar_init(acc_full(b), 1);
-            bar_init(acc_free(b), 4 * CG);
+            bar_init(acc_free(b), kStorers * CG);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *failed = 0;
@@ -427,34 +451,37 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     wait_for_previous();
 
     bool ok = true;
-    if (warp == 0 && lane == 0) {
-        // loads
+    if (warp == 0) {
+        // Loads.  The whole warp walks along, one lane issues; after a wait that ran out it only counts on to the end.
         int stage = 0;
-        uint32_t phase = 0, rounds = 0;
-        for (int t = first; ok && t < p.tiles; t += step) {
+        uint32_t phase = 0, rounds = 0, polls = p.wait_polls;
+        const uint32_t announced = CG * kStage + p.test_extra_tx;
+        for (int t = first; t < p.tiles; t += step) {
             const Tile at = tile_at(p, t);
             const int row_a = (at.tm * CG + int(rank)) * 128, row_b = at.tn * BN + int(rank) * kRowsB;
-            for (int kb = 0; kb < p.k_blocks; ++kb) {
-                if (!bar_wait(empty(stage), phase ^ 1, p.wait_polls)) {
+            for (int kb = at.k0; kb < at.k1; ++kb) {
+                if (!bar_wait(empty(stage), phase ^ 1, polls)) {
                     ok = false;
-                    break;
+                    polls = 1;
                 }
-                const uint32_t to_a = base + stage * kStage, to_b = to_a + kStageA;
-                const uint32_t bar = CG == 1 ? full(stage) : in_first(full(stage));
-                if (rank == 0) bar_expect(full(stage), CG * kStage + p.test_extra_tx);
-                if (p.a_along_rows) {
+                if (elected() && ok) {
+                    const uint32_t to_a = base + stage * kStage, to_b = to_a + kStageA;
+                    const uint32_t bar = CG == 1 ? full(stage) : in_first(full(stage));
+                    if (rank == 0) bar_expect(full(stage), announced);
+                    if (p.a_along_rows) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) load_box<CG>(to_a + i * kBK * 128, &map_a, bar, row_a + 64 * i, kb * kBK, at.matrix);
-                } else {
-                    load_box<CG>(to_a, &map_a, bar, kb * kBK, row_a, at.matrix);
-                }
-                if (p.b_along_rows) {
+                        for (int i = 0; i < 2; ++i) load_box<CG>(to_a + i * kBK * 128, &map_a, bar, row_a + 64 * i, kb * kBK, at.matrix);
+                    } else {
+                        load_box<CG>(to_a, &map_a, bar, kb * kBK, row_a, at.matrix);
+                    }
+                    if (p.b_along_rows) {
 #pragma unroll
-                    for (int i = 0; i < kRowsB / 64; ++i) load_box<CG>(to_b + i * kBK * 128, &map_b, bar, row_b + 64 * i, kb * kBK, at.matrix);
-                } else {
-                    load_box<CG>(to_b, &map_b, bar, kb * kBK, row_b, at.matrix);
+                        for (int i = 0; i < kRowsB / 64; ++i) load_box<CG>(to_b + i * kBK * 128, &map_b, bar, row_b + 64 * i, kb * kBK, at.matrix);
+                    } else {
+                        load_box<CG>(to_b, &map_b, bar, kb * kBK, row_b, at.matrix);
+                    }
                 }
-                if (++stage == kStages) {
+                if (ok && ++stage == kStages) {
                     stage = 0;
                     phase ^= 1;
                     rounds = 1;
@@ -474,52 +501,53 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         }
         if (!ok && rank != 0)                                             // its copies report to the first block: give
             for (int i = 0; i < 64; ++i) __nanosleep(1 << 15);            // them 2 ms to land in memory it still owns
-    } else if (warp == 1 && lane == 0 && rank == 0) {
-        // products
+    } else if (warp == 1 && rank == 0) {
+        // Products, in the same way.
         int stage = 0;
-        uint32_t phase = 0;
+        uint32_t phase = 0, polls = p.wait_polls;
         int use = 0;
-        for (int t = first; ok && t < p.tiles; t += step, ++use) {
+        const uint64_t desc_a = slice_desc(base, p.a_along_rows), desc_b = slice_desc(base + kStageA, p.b_along_rows);
+        const uint64_t step_a = p.a_along_rows ? 2048 >> 4 : 32 >> 4, step_b = p.b_along_rows ? 2048 >> 4 : 32 >> 4;
+        for (int t = first; t < p.tiles; t += step, ++use) {
             const int buf = use & 1;
-            if (!bar_wait(acc_free(buf), ((use >> 1) & 1) ^ 1, p.wait_polls)) {
+            if (!bar_wait(acc_free(buf), ((use >> 1) & 1) ^ 1, polls)) {
                 ok = false;
-                break;
+                polls = 1;
             }
             fence_after();
             const uint32_t acc = tmem + buf * BN;
-            for (int kb = 0; kb < p.k_blocks; ++kb) {
-                if (!bar_wait(full(stage), phase, p.wait_polls)) {
+            const Tile at = tile_at(p, t);
+            for (int kb = at.k0; kb < at.k1; ++kb) {
+                if (!bar_wait(full(stage), phase, polls)) {
                     ok = false;
-                    break;
+                    polls = 1;
                 }
                 fence_after();
-                const uint32_t at_a = base + stage * kStage, at_b = at_a + kStageA;
-                const uint64_t da = slice_desc(at_a, p.a_along_rows), db = slice_desc(at_b, p.b_along_rows);
-                const uint64_t da_step = p.a_along_rows ? 2048 >> 4 : 32 >> 4, db_step = p.b_along_rows ? 2048 >> 4 : 32 >> 4;
+                if (elected() && ok) {
+                    const uint64_t da = desc_a + uint32_t(stage * (kStage >> 4)), db = desc_b + uint32_t(stage * (kStage >> 4));
 #pragma unroll
-                for (int i = 0; i < kBK / 16; ++i) mma<CG>(acc, da + i * da_step, db + i * db_step, p.idesc, (kb | i) != 0);
-                commit<CG>(empty(stage));
+                    for (int i = 0; i < kBK / 16; ++i) mma<CG>(acc, da + i * step_a, db + i * step_b, p.idesc, kb > at.k0 || i > 0);
+                    commit<CG>(empty(stage));
+                    if (kb + 1 == at.k1) commit<CG>(acc_full(buf));
+                }
                 if (++stage == kStages) {
                     stage = 0;
                     phase ^= 1;
                 }
             }
-            if (ok) commit<CG>(acc_full(buf));
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 4 && warp < 4 + kStorers) {
         // outputs
-        const int quarter = warp & 3;
-        float *buf = epi + quarter * 32 * kPitch;
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        Pieces pieces{ring + kRing + (warp - 4) * 2 * kPiece, base + kRing + (warp - 4) * 2 * kPiece};
+        float *bias = reinterpret_cast<float *>(ring + kRing + kEpiBytes) + (warp - 4) * 32;
         int use = 0;
         for (int t = first; t < p.tiles; t += step, ++use) {
             const int b = use & 1;
-            if (!bar_wait(acc_full(b), (use >> 1) & 1, p.wait_polls)) {
-                ok = false;
-                break;
-            }
-            fence_after();
             const Tile at = tile_at(p, t);
-            const int row0 = (at.tm * CG + int(rank)) * 128 + quarter * 32, col0 = at.tn * BN;
+            const int row0 = (at.tm * CG + int(rank)) * 128 + quarter * 32, col_at = at.tn * BN + half * kShare;
+            const int64_t row = row0 + lane;
+            const bool in = row < p.m;
             float alpha = p.e.alpha, beta = p.e.beta;
             if (KIND == EPI_SCALED && p.e.scale) {
                 const float s = p.e.scale[at.matrix];
@@ -527,21 +555,65 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 for (int i = 0; i < p.e.beta_power; ++i) beta *= s;
             }
             const bool mirror = KIND == EPI_SCALED && p.symmetric && at.tm != at.tn;
-#pragma unroll 1
-            for (int c = 0; c < BN; c += 32) {
-                if (col0 + c >= p.n || row0 >= p.m) break;
-                uint32_t v[32];
-                tmem_load32(tmem + (uint32_t(quarter * 32) << 16) + b * BN + c, v);
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    *reinterpret_cast<uint4 *>(buf + lane * kPitch + 4 * i) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                __syncwarp();
+            // what a piece needs besides its accumulators is fetched before the wait (the first piece) or while the
+            // piece before it is computed
+            uint4 more[4], rest[4];
+            float next_bias = 0.0f;
+            auto fetch = [&](int col0) {
+                const int left = p.n - col0;
                 if constexpr (KIND == EPI_LINEAR) {
-                    if (p.e.out_type == T_BF16) linear_piece<__nv_bfloat16>(p, buf, lane, row0, col0 + c);
-                    else linear_piece<__half>(p, buf, lane, row0, col0 + c);
+                    if (p.e.residual) {
+                        const uint16_t *q = static_cast<const uint16_t *>(p.e.residual) + row * p.e.ld_residual + col0;
+                        if (p.aligned_residual && left >= 32) get_row<true>(q, in, left, more);
+                        else get_row<false>(q, in, left, more);
+                    }
+                    if (p.e.bias) next_bias = lane < left ? load_any(p.e.bias, p.e.bias_type, col0 + lane) : 0.0f;
+                } else if (KIND == EPI_SCALED && p.e.hi) {
+                    const int64_t q = int64_t(at.matrix) * p.e.add_batch + row * p.e.ld_add + col0;
+                    get_row<true>(static_cast<const uint16_t *>(p.e.hi) + q, in, left, more);
+                    if (p.e.lo) get_row<true>(static_cast<const uint16_t *>(p.e.lo) + q, in, left, rest);
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < 4; ++i) more[i] = rest[i] = make_uint4(0, 0, 0, 0);
+            if (col_at < p.n && row0 < p.m) fetch(col_at);
+            if (!bar_wait(acc_full(b), (use >> 1) & 1, p.wait_polls)) {
+                ok = false;
+                break;
+            }
+            fence_after();
+#pragma unroll 1
+            for (int c = 0; c < kShare; c += 32) {
+                const int col0 = col_at + c;
+                if (col0 >= p.n || row0 >= p.m) break;
+                uint32_t u[32];
+                tmem_load32(tmem + (uint32_t(quarter * 32) << 16) + b * BN + half * kShare + c, u);
+                float v[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
+                uint4 now[4], now_rest[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    now[i] = more[i];
+                    now_rest[i] = rest[i];
+                }
+                if (KIND == EPI_LINEAR && p.e.bias) {
+                    __syncwarp();
+                    bias[lane] = next_bias;
+                    __syncwarp();
+                }
+                if (c + 32 < kShare && col0 + 32 < p.n) fetch(col0 + 32);
+                if constexpr (KIND == EPI_PARTIAL) {
+                    if (in) {
+                        float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(p.e.out) + (int64_t(t % p.splits) * p.m + row) * p.e.ld_out + col0);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) q[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    }
+                } else if constexpr (KIND == EPI_LINEAR) {
+                    if (p.e.out_type == T_BF16) linear_piece<__nv_bfloat16>(p, &map_out, &map_more, pieces, v, bias, now, lane, row0, col0);
+                    else linear_piece<__half>(p, &map_out, &map_more, pieces, v, bias, now, lane, row0, col0);
                 } else {
-                    scaled_piece(p, buf, lane, row0, col0 + c, at.matrix, alpha, beta, mirror);
+                    scaled_piece(p, &map_out, &map_more, pieces, v, now, now_rest, lane, row0, col0, at.matrix, alpha, beta, mirror);
                 }
             }
             fence_before();
@@ -553,6 +625,7 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first(acc_free(b))) : "memory");
             }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     if (!ok) *failed = 1;
     __syncwarp();
@@ -602,10 +675,23 @@ bool make_map(CUtensorMap *map, const Operand &op, int64_t rows, int64_t cols, i
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tensor map of a row-major output, stored in pieces of 32 x 32.
+bool make_out_map(CUtensorMap *map, void *data, int64_t ld, int64_t batch_stride, int64_t m, int64_t n, int batch)
+{
+    EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[3] = {cuuint64_t(n), cuuint64_t(m), cuuint64_t(batch)};
+    const int64_t line = m > 1 ? ld : (n + 7) / 8 * 8;
+    const cuuint64_t strides[2] = {cuuint64_t(line) * 2, cuuint64_t(batch > 1 ? batch_stride : line) * 2};
+    const cuuint32_t box[3] = {32, 32, 1}, one[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool on_16(const void *p, int64_t ld) { return p == nullptr || (uintptr_t(p) % 16 == 0 && ld % 8 == 0); }
 
 template <int CG, int BN, int KIND>
-cudaError_t launch(const Product &q, const LaunchOptions &o, int sms, cudaStream_t stream)
+cudaError_t launch(const Product &q, int splits, const LaunchOptions &o, int device, int sms, cudaStream_t stream)
 {
     ProductParams p;
     std::memset(&p, 0, sizeof p);
@@ -616,9 +702,11 @@ cudaError_t launch(const Product &q, const LaunchOptions &o, int sms, cudaStream
     p.tiles_m = int32_t((q.m + 128 * CG - 1) / (128 * CG));
     p.tiles_n = int32_t((q.n + BN - 1) / BN);
     const int64_t per = q.symmetric ? int64_t(p.tiles_m) * (p.tiles_m + 1) / 2 : int64_t(p.tiles_m) * p.tiles_n;
-    if (per * q.batch > INT32_MAX / 2) return cudaErrorInvalidValue;
+    if (per * q.batch * splits > INT32_MAX / 2) return cudaErrorInvalidValue;
     p.tiles_per_matrix = int32_t(per);
-    p.tiles = int32_t(per * q.batch);
+    p.tiles = int32_t(per * q.batch * splits);
+    p.splits = splits;
+    p.k_per_split = (p.k_blocks + splits - 1) / splits;
     p.symmetric = q.symmetric;
     p.a_along_rows = q.a.along_rows;
     p.b_along_rows = q.b.along_rows;
@@ -630,13 +718,26 @@ cudaError_t launch(const Product &q, const LaunchOptions &o, int sms, cudaStream
     p.test_extra_tx = o.test_extra_tx;
     p.e = q.e;
     const Epilogue &e = q.e;
-    p.vector_out = on_16(e.out, e.ld_out) && (q.batch == 1 || e.out_batch % 8 == 0) && on_16(e.residual, e.ld_residual) && on_16(e.pre, e.ld_pre);
-    CUtensorMap ma, mb;
+    p.aligned_out = KIND != EPI_PARTIAL && on_16(e.out, e.ld_out) && (q.batch == 1 || e.out_batch % 8 == 0) && on_16(e.pre, e.ld_pre);
+    p.aligned_residual = on_16(e.residual, e.ld_residual);
+    CUtensorMap ma, mb, mo, mm;
     if (!make_map(&ma, q.a, q.m, q.k, q.batch, 128) || !make_map(&mb, q.b, q.n, q.k, q.batch, BN / CG)) return cudaErrorInvalidValue;
+    std::memset(&mo, 0, sizeof mo);
+    std::memset(&mm, 0, sizeof mm);
+    if (p.aligned_out) {
+        void *more = KIND == EPI_LINEAR ? e.pre : e.out_lo;
+        if (!make_out_map(&mo, e.out, e.ld_out, e.out_batch, q.m, q.n, q.batch)) return cudaErrorInvalidValue;
+        if (more && !make_out_map(&mm, more, KIND == EPI_LINEAR ? e.ld_pre : e.ld_add, KIND == EPI_LINEAR ? 0 : e.add_batch, q.m, q.n, q.batch))
+            return cudaErrorInvalidValue;
+    }
 
     auto *kernel = redist_product_kernel<CG, BN, KIND>;
-    cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    if (ce != cudaSuccess) return ce;
+    static std::atomic<uint64_t> ready{0};                  // devices on which this kernel may use its shared memory
+    if (device >= 64 || !(ready.load(std::memory_order_relaxed) >> device & 1)) {
+        const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (ce != cudaSuccess) return ce;
+        if (device < 64) ready.fetch_or(uint64_t(1) << device, std::memory_order_relaxed);
+    }
     cudaLaunchConfig_t cfg = {};
     const int groups = sms / CG;
     cfg.gridDim = dim3(unsigned((p.tiles < groups ? p.tiles : groups) * CG));
@@ -659,26 +760,118 @@ cudaError_t launch(const Product &q, const LaunchOptions &o, int sms, cudaStream
     }
     cfg.attrs = at;
     cfg.numAttrs = unsigned(n_at);
-    return cudaLaunchKernelEx(&cfg, kernel, ma, mb, p);
+    return cudaLaunchKernelEx(&cfg, kernel, ma, mb, mo, mm, p);
 }
 
 }  // namespace
+
+cudaError_t current_device(int *device, int *sms)
+{
+    static std::atomic<int> known[64];
+    cudaError_t ce = cudaGetDevice(device);
+    if (ce != cudaSuccess) return ce;
+    *sms = *device < 64 ? known[*device].load(std::memory_order_relaxed) : 0;
+    if (*sms) return cudaSuccess;
+    ce = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *device);
+    if (ce == cudaSuccess && *device < 64) known[*device].store(*sms, std::memory_order_relaxed);
+    return ce;
+}
 
 bool operand_fits(const void *data, int64_t ld, int64_t batch_stride, int batch)
 {
     return uintptr_t(data) % 16 == 0 && ld % 8 == 0 && (batch == 1 || batch_stride % 8 == 0);
 }
 
-cudaError_t launch_product(const Product &p, const LaunchOptions &o, cudaStream_t stream)
+namespace {
+
+// The tile shapes, and how long they take: microseconds per 64 steps of the sum, and per launch besides (start, the last
+// accumulator's epilogue), fitted to timings of some twenty sizes from 64 x 64 x 1000 to 4096 x 4096 x 4096.  A pair of
+// SMs on 256 x 256 reads half the operand bytes per product of one SM on 128 x 256, but fills the GPU from 74 tiles on;
+// small tiles are bound by the 0.2 us in which one thread can issue a step's copies and products, whatever their size.
+enum Shape { kPair256, kPair128, kOne256, kOne128, kOne64 };
+struct ShapeCost {
+    int rows, cols, per_unit;
+    double step, launch;
+};
+constexpr ShapeCost kCosts[] = {{256, 256, 2, 0.30, 6.0}, {256, 128, 2, 0.245, 4.5}, {128, 256, 1, 0.33, 5.5}, {128, 128, 1, 0.255, 4.5}, {128, 64, 1, 0.22, 3.7}};
+
+struct Choice {
+    Shape shape;
+    int splits;
+};
+
+// The shape, and into how many parts the sum is split, with the least time by these figures.  Parts are summed by a second
+// kernel (3 us and the traffic of the 32-bit parts), so splitting is for results of few tiles and long sums:
+// 256 x 256 results of 16384 steps took 80 us unsplit.
+Choice choose(const Product &p, int sms, bool may_split)
+{
+    Choice best{kPair256, 1};
+    double least = 1e30;
+    const int steps = int((p.k + kBK - 1) / kBK);
+    for (int s = 0; s < 5; ++s) {
+        const ShapeCost &c = kCosts[s];
+        if (p.symmetric && c.rows != c.cols) continue;
+        const int64_t tm = (p.m + c.rows - 1) / c.rows, tn = (p.n + c.cols - 1) / c.cols;
+        const int64_t tiles = (p.symmetric ? tm * (tm + 1) / 2 : tm * tn) * p.batch, units = sms / c.per_unit;
+        const int most = may_split && tiles < units ? int(std::min<int64_t>(units / tiles, steps / 4)) : 1;
+        for (int k = 1; k <= std::max(most, 1); ++k) {
+            const int per = (steps + k - 1) / k, parts = (steps + per - 1) / per;
+            if (parts != k) continue;
+            const int64_t waves = (tiles * k + units - 1) / units;
+            double t = double(waves) * per * c.step + c.launch;
+            if (k > 1) t += 3.0 + double(p.m) * double(p.n) * k * 8e-6 / 4.0;
+            if (t < least) {
+                least = t;
+                best = Choice{Shape(s), k};
+            }
+        }
+    }
+    return best;
+}
+
+template <int KIND> cudaError_t launch_shape(const Product &p, const Choice &c, const LaunchOptions &o, int device, int sms, cudaStream_t stream)
+{
+    switch (c.shape) {
+    case kPair256: return launch<2, 256, KIND>(p, c.splits, o, device, sms, stream);
+    case kOne128: return launch<1, 128, KIND>(p, c.splits, o, device, sms, stream);
+    default: break;
+    }
+    if constexpr (KIND == EPI_SCALED)
+        if (p.symmetric) return cudaErrorInvalidValue;
+    switch (c.shape) {
+    case kPair128: return launch<2, 128, KIND>(p, c.splits, o, device, sms, stream);
+    case kOne256: return launch<1, 256, KIND>(p, c.splits, o, device, sms, stream);
+    default: return launch<1, 64, KIND>(p, c.splits, o, device, sms, stream);
+    }
+}
+
+int64_t part_pitch(int64_t n) { return (n + 31) / 32 * 32; }
+
+}  // namespace
+
+int64_t product_scratch_bytes(const Product &p)
+{
+    int device = 0, sms = 0;
+    if (p.kind != EPI_LINEAR || p.m == 0 || p.n == 0 || current_device(&device, &sms) != cudaSuccess) return 0;
+    const Choice c = choose(p, sms, true);
+    return c.splits > 1 ? c.splits * p.m * part_pitch(p.n) * 4 : 0;
+}
+
+cudaError_t launch_product(const Product &p, void *scratch, const LaunchOptions &o, cudaStream_t stream)
 {
     if (p.m == 0 || p.n == 0 || p.batch == 0) return cudaSuccess;
     int device = 0, sms = 0;
-    cudaError_t ce = cudaGetDevice(&device);
-    if (ce == cudaSuccess) ce = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    const cudaError_t ce = current_device(&device, &sms);
     if (ce != cudaSuccess) return ce;
-    if (p.kind == EPI_LINEAR) return launch<1, 256, EPI_LINEAR>(p, o, sms, stream);
-    if (p.symmetric) return launch<1, 128, EPI_SCALED>(p, o, sms, stream);
-    return launch<1, 256, EPI_SCALED>(p, o, sms, stream);
+    if (p.kind == EPI_SCALED) return launch_shape<EPI_SCALED>(p, choose(p, sms, false), o, device, sms, stream);
+    const Choice c = choose(p, sms, true);
+    if (c.splits == 1) return launch_shape<EPI_LINEAR>(p, c, o, device, sms, stream);
+    Product q = p;
+    q.e = Epilogue{};
+    q.e.out = scratch;
+    q.e.ld_out = part_pitch(p.n);
+    const cudaError_t parts = launch_shape<EPI_PARTIAL>(q, c, o, device, sms, stream);
+    return parts != cudaSuccess ? parts : launch_join(p, static_cast<const float *>(scratch), q.e.ld_out, c.splits, o, stream);
 }
 
 cudaError_t read_product_timeouts(unsigned int *out) { return cudaMemcpyFromSymbol(out, g_product_timeouts, sizeof *out); }

@@ -23,8 +23,9 @@ struct Operand {
 
 // How an accumulator becomes an output.  LINEAR: z = acc + bias[n]; pre = z; out = act(z) + residual.
 // SCALED: v = alpha * acc + beta * (hi + lo / 2048), alpha and beta multiplied by powers of a device scalar
-// per matrix; out = v as f16 (with out_lo = the rest, times 2048) or as bf16.
-enum EpilogueKind { EPI_LINEAR = 0, EPI_SCALED = 1 };
+// per matrix; out = v as f16 (with out_lo = the rest, times 2048) or as bf16.  PARTIAL (inside launch_product only): the
+// 32-bit accumulators of each part of a split sum, out[part][row][ld_out].
+enum EpilogueKind { EPI_LINEAR = 0, EPI_SCALED = 1, EPI_PARTIAL = 2 };
 
 struct Epilogue {
     void *out;
@@ -66,8 +67,18 @@ struct LaunchOptions {
 // Whether an operand may be read as it lies (16-byte boundaries), or has to be laid out anew first.
 bool operand_fits(const void *data, int64_t ld, int64_t batch_stride, int batch);
 
+// The current device and its number of SMs (asked for once per device).
+cudaError_t current_device(int *device, int *sms);
+
+// Scratch that launch_product needs: the 32-bit parts of a sum that is split (only sizes are read).
+int64_t product_scratch_bytes(const Product &p);
+
 // Asynchronous on `stream`; allocates nothing.
-cudaError_t launch_product(const Product &p, const LaunchOptions &o, cudaStream_t stream);
+cudaError_t launch_product(const Product &p, void *scratch, const LaunchOptions &o, cudaStream_t stream);
+
+// The linear epilogue on up to kFewRows rows, both operands contiguous along the sum, at any alignment; no scratch.
+constexpr int kFewRows = 16;
+cudaError_t launch_few_rows(const Product &p, const LaunchOptions &o, cudaStream_t stream);
 
 // Thread blocks of the product kernels whose bounded wait ran out on the current device.  Synchronizes the device.
 cudaError_t read_product_timeouts(unsigned int *out);

@@ -3,6 +3,7 @@
 
 #include <algorithm>
 
+#include "activation.cuh"
 #include "elements.cuh"
 
 namespace redist {
@@ -579,6 +580,57 @@ __global__ void __launch_bounds__(256) redist_scaled_kernel(const Scaled s, int 
     }
 }
 
+// ---- joining the parts of a split product --------------------------------------------------------------------
+
+// A thread takes eight neighbours of a row.
+template <typename T>
+__global__ void __launch_bounds__(256) redist_join_kernel(const Epilogue e, const float *parts, int64_t ld, int splits, int64_t m, int64_t n)
+{
+    let_next_start();
+    wait_for_previous();
+    const int64_t per_row = ld / 8, q = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t row = q / per_row, c = (q - row * per_row) * 8;
+    if (row >= m || c >= n) return;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+        const float4 *at = reinterpret_cast<const float4 *>(parts + (int64_t(s) * m + row) * ld + c);
+        const float4 a = at[0], b = at[1];
+        v[0] += a.x;
+        v[1] += a.y;
+        v[2] += a.z;
+        v[3] += a.w;
+        v[4] += b.x;
+        v[5] += b.y;
+        v[6] += b.z;
+        v[7] += b.w;
+    }
+    const int count = int(min(n - c, int64_t(8)));
+    auto put = [&](void *base, int64_t pitch) {
+        T *to = static_cast<T *>(base) + row * pitch + c;
+        if (count == 8 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
+            *reinterpret_cast<uint4 *>(to) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) to[i] = from_float<T>(v[i]);
+        }
+    };
+    if (e.bias)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) v[i] += load_any(e.bias, e.bias_type, c + i);
+    if (e.pre) put(e.pre, e.ld_pre);
+    activate8(v, e.activation);
+    if (e.residual) {
+        float w[8];
+        split8<T>(load16_any(static_cast<const T *>(e.residual) + row * e.ld_residual + c, count * 2), w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += w[i];
+    }
+    put(e.out, e.ld_out);
+}
+
 // ---- host ---------------------------------------------------------------------------------------------------
 
 template <typename... P, typename... A>
@@ -599,8 +651,7 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, int block, const LaunchOptio
 cudaError_t sm_count(int *sms)
 {
     int device = 0;
-    cudaError_t ce = cudaGetDevice(&device);
-    return ce != cudaSuccess ? ce : cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, device);
+    return current_device(&device, sms);
 }
 
 bool on_16(const void *p, int64_t ld, int64_t element) { return p == nullptr || (uintptr_t(p) % 16 == 0 && ld * element % 16 == 0); }
@@ -711,6 +762,13 @@ cudaError_t launch_lay(const Lay &l, const LaunchOptions &o, cudaStream_t stream
     if (ce != cudaSuccess || !l.sums) return ce;
     return launch(redist_column_sum_kernel, dim3(unsigned((l.cols + 31) / 32), 1), 256, o, stream, static_cast<const float *>(l.partials),
                   int(parts), l.cols, l.cols, l.sums, static_cast<float *>(nullptr));
+}
+
+cudaError_t launch_join(const Product &p, const float *parts, int64_t ld, int splits, const LaunchOptions &o, cudaStream_t stream)
+{
+    const dim3 grid(unsigned((p.m * (ld / 8) + 255) / 256));
+    return p.type == T_BF16 ? launch(redist_join_kernel<__nv_bfloat16>, grid, 256, o, stream, p.e, parts, ld, splits, p.m, p.n)
+                            : launch(redist_join_kernel<__half>, grid, 256, o, stream, p.e, parts, ld, splits, p.m, p.n);
 }
 
 cudaError_t launch_scaled(const Scaled &s, const LaunchOptions &o, cudaStream_t stream)

@@ -64,4 +64,7 @@ struct Scaled {
 constexpr int kNormParts = 128;
 cudaError_t launch_scaled(const Scaled &s, const LaunchOptions &o, cudaStream_t stream);
 
+// The linear epilogue of product `p` on the sum of `splits` parts, parts[s][row][ld], added in this order.
+cudaError_t launch_join(const Product &p, const float *parts, int64_t ld, int splits, const LaunchOptions &o, cudaStream_t stream);
+
 }  // namespace redist
