@@ -5,6 +5,7 @@
 
 #include <cstdint>
 
+#include "elements.cuh"
 #include "product.h"
 
 namespace redist {
@@ -21,26 +22,6 @@ __device__ __forceinline__ float exp2_fast(float v)
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
-}
-
-// Two values at a time: one instruction for both where the operation is an addition or a product.
-struct Pair {
-    uint64_t both;
-    __device__ __forceinline__ Pair(uint64_t v) : both(v) {}
-    __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(both) : "f"(a), "f"(b)); }
-    __device__ __forceinline__ void get(float &a, float &b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(both)); }
-};
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a.both), "l"(b.both), "l"(c.both));
-    return Pair(r);
-}
-__device__ __forceinline__ Pair mul2(Pair a, Pair b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a.both), "l"(b.both));
-    return Pair(r);
 }
 
 // z Phi(z) with Phi(z) = 1/2 + z Q(z^2), Q a polynomial of degree 13 in (z^2 - c/2) / (c/2) on z^2 <= c = 5.2^2, fitted

@@ -47,6 +47,39 @@ template <> __device__ __forceinline__ float2 unpack2<__half>(uint32_t v)
     return __half22float2(*reinterpret_cast<const __half2 *>(&v));
 }
 
+// Two values at a time: one instruction for both where the operation is an addition or a product.
+struct Pair {
+    uint64_t both;
+    __device__ __forceinline__ Pair(uint64_t v) : both(v) {}
+    __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(both) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ void get(float &a, float &b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(both)); }
+    __device__ __forceinline__ float sum() const
+    {
+        float a, b;
+        get(a, b);
+        return a + b;
+    }
+};
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a.both), "l"(b.both), "l"(c.both));
+    return Pair(r);
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a.both), "l"(b.both));
+    return Pair(r);
+}
+
+__device__ __forceinline__ Pair add2(Pair a, Pair b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a.both), "l"(b.both));
+    return Pair(r);
+}
+
 // Element `i` of an array whose type is only known at run time.
 __device__ __forceinline__ float load_any(const void *p, int type, int64_t i)
 {

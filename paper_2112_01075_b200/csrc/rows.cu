@@ -2,6 +2,7 @@
 #include "rows.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "activation.cuh"
 #include "elements.cuh"
@@ -12,84 +13,190 @@ namespace {
 
 // ---- helpers -----------------------------------------------------------------------------------------
 
-// VEC neighbours of a row as they lie in memory.
-template <typename T, int VEC> struct Raw {
-    uint4 u;
-    __device__ __forceinline__ void load(const T *p) { u = __ldg(reinterpret_cast<const uint4 *>(p)); }
-    __device__ __forceinline__ void clear() { u = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void get(float (&v)[VEC]) const
+template <typename T> constexpr int kVec = 16 / int(sizeof(T));          // neighbours in 16 bytes
+
+template <typename T> __device__ __forceinline__ void unpack16(const uint4 &u, float *v)
+{
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack2<T>(w[i]);
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+    }
+}
+
+template <typename T> __device__ __forceinline__ uint4 pack16(const float *v)
+{
+    if constexpr (sizeof(T) == 4)
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    else
+        return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+}
+
+// 16 bytes of shared memory from any even address on.
+__device__ __forceinline__ uint4 read16_any(const uint8_t *p)
+{
+    const uint32_t half = uint32_t(reinterpret_cast<uintptr_t>(p) & 2);
+    const uint32_t *q = reinterpret_cast<const uint32_t *>(p - half);
+    const uint4 u = make_uint4(q[0], q[1], q[2], q[3]);
+    if (!half) return u;
+    return make_uint4(__funnelshift_r(u.x, u.y, 16), __funnelshift_r(u.y, u.z, 16), __funnelshift_r(u.z, u.w, 16), __funnelshift_r(u.w, q[4], 16));
+}
+
+// L threads share a row; a thread holds NV pieces of 16 bytes of it.  The threads of a row that share a warp form a
+// segment, which has NV x kSegment consecutive pieces; piece j of a thread is its segment's (j kSegment + at)-th.
+template <typename T, int L, int NV> struct RowShape {
+    static constexpr int VEC = kVec<T>;
+    static constexpr int kThreads = L < 256 ? 256 : L;
+    static constexpr int kRows = kThreads / L;              // rows a block holds at a time
+    static constexpr int kSegment = L < 32 ? L : 32;
+    static __device__ __forceinline__ int column(int j)     // where a thread's piece begins
     {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-        if constexpr (sizeof(T) == 4) {
+        const int t = int(threadIdx.x) % L;
+        return ((t / kSegment * NV + j) * kSegment + t % kSegment) * VEC;
+    }
+};
+
+// Rows on their way to the registers: every thread copies its own pieces of the next rows into shared memory
+// (cp.async: no registers, no barrier) and takes them out again in turn.  SHIFT: rows start anywhere.  Then a thread copies
+// the aligned blocks in which its pieces begin, the last one of a segment (or of the row) the block after that too, and
+// pieces are read from shared memory at their own offset.  A slot that was taken also serves to shift a row of outputs.
+template <typename T, int L, int NV, int TENSORS, bool SHIFT> struct Stream {
+    using S = RowShape<T, L, NV>;
+    static constexpr int VEC = S::VEC, SEGMENT = S::kSegment;
+    static constexpr int kBlocks = S::kThreads / SEGMENT * (NV * SEGMENT + (SHIFT ? 1 : 0));     // of one row of one tensor
+    // three rows ahead, or as many as leave room for two blocks per SM (one at least)
+    static constexpr int kFit = 100 * 1024 / (TENSORS * kBlocks * 16), kSlots = kFit >= 4 ? 4 : kFit >= 3 ? 3 : 2, kAhead = kSlots - 1;
+    static constexpr int kSmem = kSlots * TENSORS * kBlocks * 16;
+    uint8_t *mine;                  // this thread's first block in the first slot
+    int put = 0, got = 0;
+    bool last;
+
+    __device__ __forceinline__ Stream(uint8_t *smem)
+    {
+        const int segment = int(threadIdx.x) / SEGMENT, at = int(threadIdx.x) % SEGMENT;
+        mine = smem + (segment * (NV * SEGMENT + (SHIFT ? 1 : 0)) + at) * 16;
+        last = at == SEGMENT - 1;
+    }
+    __device__ __forceinline__ uint8_t *place(int slot, int tensor, int piece) const
+    {
+        return mine + ((slot * TENSORS + tensor) * kBlocks + piece * SEGMENT) * 16;
+    }
+
+    // base[i]: this thread's first piece in tensor i's row; in == false: no such row
+    __device__ __forceinline__ void send(const T *const (&base)[TENSORS], bool in, const int (&count)[NV])
+    {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
-        } else {
+        for (int i = 0; i < TENSORS; ++i) {
+            const uint32_t off = SHIFT ? uint32_t(reinterpret_cast<uintptr_t>(base[i]) & 15) : 0;
+            const char *block = reinterpret_cast<const char *>(base[i]) - off;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = unpack2<T>(w[i]);
-                v[2 * i] = f.x;
-                v[2 * i + 1] = f.y;
+            for (int j = 0; j < NV; ++j) {
+                if (!in || count[j] <= 0) continue;
+                const uint32_t to = uint32_t(__cvta_generic_to_shared(place(put, i, j)));
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(block + j * SEGMENT * 16) : "memory");
+                if constexpr (SHIFT)        // the next block, if this piece reaches into it and nobody else brings it
+                    if (((j == NV - 1 && last) || count[j] <= VEC) && off + uint32_t(min(count[j], VEC)) * uint32_t(sizeof(T)) > 16)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 16), "l"(block + j * SEGMENT * 16 + 16) : "memory");
             }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        put = put + 1 == kSlots ? 0 : put + 1;
     }
-    static __device__ __forceinline__ void put(T *p, const float (&v)[VEC], int count)
+
+    // The oldest row sent for (kAhead more are under way); zero beyond the row's end.
+    __device__ __forceinline__ void take(const T *const (&base)[TENSORS], const int (&count)[NV], float (&v)[TENSORS][NV][VEC])
     {
-        if (count >= VEC) {
-            uint4 u;
-            if constexpr (sizeof(T) == 4)
-                u = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-            else
-                u = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
-            *reinterpret_cast<uint4 *>(p) = u;
-        } else {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+        if constexpr (SHIFT) __syncwarp();
 #pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                if (i < count) p[i] = from_float<T>(v[i]);
+        for (int i = 0; i < TENSORS; ++i)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const uint8_t *at = place(got, i, j);
+                if constexpr (SHIFT) unpack16<T>(read16_any(at + (reinterpret_cast<uintptr_t>(base[i]) & 15)), v[i][j]);
+                else unpack16<T>(*reinterpret_cast<const uint4 *>(at), v[i][j]);
+                if (count[j] < VEC)
+#pragma unroll
+                    for (int q = 0; q < VEC; ++q)
+                        if (q >= count[j]) v[i][j][q] = 0.0f;
+            }
+        if constexpr (SHIFT) __syncwarp();                  // the slot may be written again
+        got = got + 1 == kSlots ? 0 : got + 1;
+    }
+
+    // Stores a row of outputs; `to`: this thread's first piece.  SHIFT: the pieces go through the slot just taken, from
+    // which a thread reads the aligned block that ends in its piece, its beginning from the thread before; what no whole
+    // block of a segment covers goes out one by one.
+    __device__ __forceinline__ void store(T *to, bool in, const int (&count)[NV], const float (&v)[NV][VEC])
+    {
+        const int q = SHIFT ? int(reinterpret_cast<uintptr_t>(to) & 15) / int(sizeof(T)) : 0;
+        const int slot = got == 0 ? kSlots - 1 : got - 1;
+        if constexpr (SHIFT) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) *reinterpret_cast<uint4 *>(place(slot, 0, j)) = pack16<T>(v[j]);
+            __syncwarp();
         }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            T *p = to + j * SEGMENT * VEC;
+            if constexpr (!SHIFT) {
+                if (!in) continue;
+                if (count[j] >= VEC) {
+                    *reinterpret_cast<uint4 *>(p) = pack16<T>(v[j]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i)
+                        if (i < count[j]) p[i] = from_float<T>(v[j][i]);
+                }
+            } else {
+                const bool head = j == 0 && int(threadIdx.x) % SEGMENT == 0, tail = j == NV - 1 && last;
+                const uint8_t *at = place(slot, 0, j);
+                const bool whole = in && (!head || q == 0) && count[j] >= VEC - q;
+                if (whole) *reinterpret_cast<uint4 *>(p - q) = read16_any(at - q * int(sizeof(T)));
+                // one by one: my first VEC - q where there is no whole block, my last q where the next piece has none
+                const uint32_t front = (1u << (VEC - q)) - 1, all = (1u << VEC) - 1;
+                uint32_t rest = 0;
+                if (in && count[j] > 0) {
+                    rest = (whole ? 0 : front) | (tail || count[j] - VEC < VEC - q ? all & ~front : 0);
+                    if (count[j] < VEC) rest &= (1u << count[j]) - 1;
+                }
+                if (rest) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i)
+                        if (rest >> i & 1) p[i] = reinterpret_cast<const T *>(at)[i];
+                }
+            }
+        }
+        if constexpr (SHIFT) __syncwarp();
     }
 };
-template <typename T> struct Raw<T, 1> {
-    T u;
-    __device__ __forceinline__ void load(const T *p) { u = __ldg(p); }
-    __device__ __forceinline__ void clear() { u = from_float<T>(0.0f); }
-    __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = to_float(u); }
-    static __device__ __forceinline__ void put(T *p, const float (&v)[1], int) { *p = from_float<T>(v[0]); }
-};
 
-__device__ __forceinline__ float warp_sum(float v)
+// Sums over the L threads that share a row; every thread gets them.  L > 32: `slot` has two entries per warp of the block
+// and may be written again after one more barrier of the row's threads.
+template <int L> __device__ __forceinline__ float2 row_sums(float a, float b, float2 *slot)
 {
 #pragma unroll
-    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    return v;
-}
-
-// Sum over the W warps that share a row; every thread gets it.  W > 1: the whole block calls it, `slot` alternates.
-template <int W> __device__ __forceinline__ float row_sum(float v, float *slot)
-{
-    v = warp_sum(v);
-    if constexpr (W > 1) {
-        if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = 0.0f;
-#pragma unroll
-        for (int i = 0; i < W; ++i) v += slot[i];
+    for (int d = (L < 32 ? L : 32) / 2; d; d >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, d);
+        b += __shfl_xor_sync(0xffffffffu, b, d);
     }
-    return v;
-}
-
-// The same for two sums at once.
-template <int W> __device__ __forceinline__ float2 row_sum2(float a, float b, float2 *slot)
-{
-    a = warp_sum(a);
-    b = warp_sum(b);
-    if constexpr (W > 1) {
-        if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = make_float2(a, b);
-        __syncthreads();
+    if constexpr (L > 32) {
+        const int warp = int(threadIdx.x) >> 5, first = warp & ~(L / 32 - 1);
+        if ((threadIdx.x & 31) == 0) slot[warp] = make_float2(a, b);
+        if constexpr (L < 256) asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / (L / 32)), "n"(L) : "memory");
+        else __syncthreads();
         a = b = 0.0f;
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            a += slot[i].x;
-            b += slot[i].y;
+        for (int i = 0; i < L / 32; ++i) {
+            a += slot[first + i].x;
+            b += slot[first + i].y;
         }
     }
     return make_float2(a, b);
@@ -97,97 +204,128 @@ template <int W> __device__ __forceinline__ float2 row_sum2(float a, float b, fl
 
 // ---- layer norm, forward -------------------------------------------------------------------------------
 
-constexpr int kNormWarps = 8;           // warps of a block whose rows belong to one warp each
-
-// W warps hold a row in registers, NV pieces of VEC neighbours per lane.  Mean first, then the differences d from it,
-// sum of d^2 and sum of d: the latter is what rounding left in the mean, and corrects both (var = mean d^2 - (mean d)^2),
-// so a mean far larger than the spread costs no digits.
-template <typename T, int VEC, int W, int NV>
-__global__ void __launch_bounds__(W == 1 ? 32 * kNormWarps : 32 * W) redist_layer_norm_kernel(const LayerNorm l)
+// Mean first, then the differences d from it, sum of d^2 and sum of d: the latter is what rounding left in the mean, and
+// corrects both (var = mean d^2 - (mean d)^2), so a mean far larger than the spread costs no digits.
+template <typename T, int L, int NV, bool SHIFT>
+__global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_norm_kernel(const LayerNorm l)
 {
-    constexpr int kRows = W == 1 ? kNormWarps : 1;
-    __shared__ float slots[32];
-    __shared__ float2 slots2[32];
-    const int t = W == 1 ? threadIdx.x & 31 : threadIdx.x;
-    const int group = W == 1 ? threadIdx.x >> 5 : 0;
+    using S = RowShape<T, L, NV>;
+    constexpr int VEC = S::VEC;
+    __shared__ float2 slots[2][32];
+    extern __shared__ __align__(16) uint8_t ring[];
+    const int t = int(threadIdx.x) % L, group = int(threadIdx.x) / L, cols = int(l.cols);
     let_next_start();
     wait_for_previous();
+    int count[NV];
     float gamma[NV][VEC], beta[NV][VEC];
+    Stream<T, L, NV, 1, SHIFT> rows(ring);
+    const int64_t step = int64_t(gridDim.x) * S::kRows;
+    const int64_t start = int64_t(blockIdx.x) * S::kRows + group;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) count[j] = cols - S::column(j);
+    auto at = [&](int64_t row) { return static_cast<const T *>(l.x) + row * l.ld_x + S::column(0); };
+#pragma unroll
+    for (int i = 0; i < rows.kAhead; ++i) {
+        const T *const base[1] = {at(start + i * step)};
+        rows.send(base, start + i * step < l.rows, count);
+    }
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const int64_t c = int64_t(j * W * 32 + t) * VEC + i;
-            gamma[j][i] = l.gamma && c < l.cols ? load_any(l.gamma, l.weight_type, c) : 1.0f;
-            beta[j][i] = l.beta && c < l.cols ? load_any(l.beta, l.weight_type, c) : 0.0f;
+            const int c = S::column(j) + i;
+            gamma[j][i] = l.gamma && c < cols ? load_any(l.gamma, l.weight_type, c) : 1.0f;
+            beta[j][i] = l.beta && c < cols ? load_any(l.beta, l.weight_type, c) : 0.0f;
         }
-    const float over = 1.0f / float(l.cols);
-    const int64_t step = int64_t(gridDim.x) * kRows;
-    Raw<T, VEC> next[NV];
-    auto fetch = [&](int64_t row) {
+    const float over = 1.0f / float(cols);
+    const int64_t turns = (l.rows - int64_t(blockIdx.x) * S::kRows + step - 1) / step;       // the same for all rows of the block
+    int64_t row = start;
+    for (int64_t turn = 0; turn < turns; ++turn, row += step) {
+        const T *const ahead[1] = {at(row + rows.kAhead * step)};
+        rows.send(ahead, row + rows.kAhead * step < l.rows, count);
+        const T *const base[1] = {at(row)};
+        float all[1][NV][VEC];
+        rows.take(base, count, all);
+        float (&v)[NV][VEC] = all[0];
+        Pair sums(0.0f, 0.0f), rests(0.0f, 0.0f), squares(0.0f, 0.0f);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; i += 2) sums = add2(sums, Pair(v[j][i], v[j][i + 1]));
+        const float mean = row_sums<L>(sums.sum(), 0.0f, slots[0]).x * over;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int64_t c = int64_t(j * W * 32 + t) * VEC;
-            if (row < l.rows && c < l.cols) next[j].load(static_cast<const T *>(l.x) + row * l.ld_x + c);
-            else next[j].clear();
+#pragma unroll
+            for (int i = 0; i < VEC; i += 2) add2(Pair(v[j][i], v[j][i + 1]), Pair(-mean, -mean)).get(v[j][i], v[j][i + 1]);
+            if (count[j] < VEC)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (i >= count[j]) v[j][i] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VEC; i += 2) {
+                const Pair d(v[j][i], v[j][i + 1]);
+                rests = add2(rests, d);
+                squares = fma2(d, d, squares);
+            }
         }
-    };
-    int64_t row = int64_t(blockIdx.x) * kRows + group;
-    fetch(row);
-    for (; row < l.rows; row += step) {
-        float v[NV][VEC];
-#pragma unroll
-        for (int j = 0; j < NV; ++j) next[j].get(v[j]);
-        fetch(row + step);
-        float sum = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const int64_t c = int64_t(j * W * 32 + t) * VEC + i;
-                if (c < l.cols) sum += v[j][i];
-            }
-        float mean = row_sum<W>(sum, slots) * over;
-        float rest = 0.0f, square = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const int64_t c = int64_t(j * W * 32 + t) * VEC + i;
-                v[j][i] -= mean;
-                if (c < l.cols) {
-                    rest += v[j][i];
-                    square = fmaf(v[j][i], v[j][i], square);
-                }
-            }
-        const float2 both = row_sum2<W>(rest, square, slots2);
-        rest = both.x * over;
-        mean += rest;
+        const float2 both = row_sums<L>(rests.sum(), squares.sum(), slots[1]);
+        const float rest = both.x * over;
         float var = both.y * over - rest * rest;
-        if (var < 0.0f) var = 0.0f;                     // by rounding alone; NaN stays
+        if (var < 0.0f) var = 0.0f;                         // by rounding alone; NaN stays
         const float rstd = 1.0f / sqrtf(var + l.eps);
+        const bool in = row < l.rows;
+        const float less = -rest * rstd;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int64_t c = int64_t(j * W * 32 + t) * VEC;
-            if (c >= l.cols) continue;
-            float y[VEC];
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) y[i] = fmaf((v[j][i] - rest) * rstd, gamma[j][i], beta[j][i]);
-            Raw<T, VEC>::put(static_cast<T *>(l.y) + row * l.ld_y + c, y, int(min(l.cols - c, int64_t(VEC))));
-        }
-        if (t == 0) {
-            if (l.mean) l.mean[row] = mean;
+            for (int i = 0; i < VEC; i += 2)
+                fma2(fma2(Pair(v[j][i], v[j][i + 1]), Pair(rstd, rstd), Pair(less, less)), Pair(gamma[j][i], gamma[j][i + 1]),
+                     Pair(beta[j][i], beta[j][i + 1]))
+                    .get(v[j][i], v[j][i + 1]);
+        rows.store(static_cast<T *>(l.y) + row * l.ld_y + S::column(0), in, count, v);
+        if (t == 0 && in) {
+            if (l.mean) l.mean[row] = mean + rest;
             if (l.rstd) l.rstd[row] = rstd;
         }
     }
 }
 
-// Rows that do not fit into the registers of a block: three passes over a row, which its first pass left in L2.
-template <typename T>
-__global__ void __launch_bounds__(1024) redist_layer_norm_long_kernel(const LayerNorm l)
+// Eight neighbours at any alignment from global memory; what is not wanted reads as zero.
+template <typename T> __device__ __forceinline__ void load8(const T *p, int count, float (&v)[8])
 {
-    __shared__ float slots[32];
-    __shared__ float2 slots2[32];
+    if constexpr (sizeof(T) == 2) {
+        unpack16<T>(load16_any(p, min(count, 8) * 2), v);
+    } else {
+        unpack16<T>(load16_any(p, min(count, 4) * 4), v);
+        uint4 b = make_uint4(0, 0, 0, 0);
+        if (count > 4) b = load16_any(p + 4, (min(count, 8) - 4) * 4);
+        unpack16<T>(b, v + 4);
+    }
+    if (count < 8)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i >= count) v[i] = 0.0f;
+}
+
+template <typename T> __device__ __forceinline__ void store8(T *p, const float (&v)[8], int count)
+{
+    if (count >= 8 && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+#pragma unroll
+        for (int i = 0; i < 8; i += kVec<T>) *reinterpret_cast<uint4 *>(p + i) = pack16<T>(v + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) p[i] = from_float<T>(v[i]);
+    }
+}
+
+// Rows that do not fit into the registers of a block: three passes over a row, which its first pass left in L2.
+constexpr int kLong = 512;
+
+template <typename T>
+__global__ void __launch_bounds__(kLong) redist_layer_norm_long_kernel(const LayerNorm l)
+{
+    __shared__ float2 slots[2][32];
     let_next_start();
     wait_for_previous();
     const float over = 1.0f / float(l.cols);
@@ -195,22 +333,43 @@ __global__ void __launch_bounds__(1024) redist_layer_norm_long_kernel(const Laye
         const T *x = static_cast<const T *>(l.x) + row * l.ld_x;
         T *y = static_cast<T *>(l.y) + row * l.ld_y;
         float sum = 0.0f, rest = 0.0f, square = 0.0f;
-        for (int64_t c = threadIdx.x; c < l.cols; c += 1024) sum += to_float(x[c]);
-        float mean = row_sum<32>(sum, slots) * over;
-        for (int64_t c = threadIdx.x; c < l.cols; c += 1024) {
-            const float d = to_float(x[c]) - mean;
-            rest += d;
-            square = fmaf(d, d, square);
+#pragma unroll 2
+        for (int64_t c = int64_t(threadIdx.x) * 8; c < l.cols; c += kLong * 8) {
+            float v[8];
+            load8<T>(x + c, int(min(l.cols - c, int64_t(8))), v);
+            sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         }
-        const float2 both = row_sum2<32>(rest, square, slots2);
+        const float mean = row_sums<kLong>(sum, 0.0f, slots[0]).x * over;
+#pragma unroll 2
+        for (int64_t c = int64_t(threadIdx.x) * 8; c < l.cols; c += kLong * 8) {
+            float v[8];
+            const int count = int(min(l.cols - c, int64_t(8)));
+            load8<T>(x + c, count, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) {
+                    const float d = v[i] - mean;
+                    rest += d;
+                    square = fmaf(d, d, square);
+                }
+        }
+        const float2 both = row_sums<kLong>(rest, square, slots[1]);
         rest = both.x * over;
         float var = both.y * over - rest * rest;
-        if (var < 0.0f) var = 0.0f;                     // by rounding alone; NaN stays
+        if (var < 0.0f) var = 0.0f;
         const float rstd = 1.0f / sqrtf(var + l.eps);
-        for (int64_t c = threadIdx.x; c < l.cols; c += 1024) {
-            const float g = l.gamma ? load_any(l.gamma, l.weight_type, c) : 1.0f;
-            const float b = l.beta ? load_any(l.beta, l.weight_type, c) : 0.0f;
-            y[c] = from_float<T>(fmaf((to_float(x[c]) - mean - rest) * rstd, g, b));
+#pragma unroll 2
+        for (int64_t c = int64_t(threadIdx.x) * 8; c < l.cols; c += kLong * 8) {
+            float v[8];
+            const int count = int(min(l.cols - c, int64_t(8)));
+            load8<T>(x + c, count, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float g = l.gamma && i < count ? load_any(l.gamma, l.weight_type, c + i) : 1.0f;
+                const float b = l.beta && i < count ? load_any(l.beta, l.weight_type, c + i) : 0.0f;
+                v[i] = fmaf((v[i] - mean - rest) * rstd, g, b);
+            }
+            store8<T>(y + c, v, count);
         }
         if (threadIdx.x == 0) {
             if (l.mean) l.mean[row] = mean + rest;
@@ -223,114 +382,109 @@ __global__ void __launch_bounds__(1024) redist_layer_norm_long_kernel(const Laye
 
 // With c = dy gamma and xh = (x - mean) rstd: dx = rstd (c - mean(c) - xh mean(c xh)).  A block walks over its rows
 // and keeps the column sums of dy xh and dy in registers; partials holds them per block, gamma's before beta's.
-template <typename T, int VEC, int W, int NV>
-__global__ void __launch_bounds__(W == 1 ? 32 * kNormWarps : 32 * W) redist_layer_norm_grad_kernel(const LayerNorm l, float *partials)
+template <typename T, int L, int NV, bool SHIFT>
+__global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_norm_grad_kernel(const LayerNorm l, float *partials)
 {
-    constexpr int kRows = W == 1 ? kNormWarps : 1;
-    __shared__ float slots[2][32];
-    const int t = W == 1 ? threadIdx.x & 31 : threadIdx.x;
-    const int group = W == 1 ? threadIdx.x >> 5 : 0;
+    using S = RowShape<T, L, NV>;
+    constexpr int VEC = S::VEC;
+    __shared__ float2 slots[2][32];
+    extern __shared__ __align__(16) uint8_t ring[];
+    const int t = int(threadIdx.x) % L, group = int(threadIdx.x) / L, cols = int(l.cols);
     let_next_start();
     wait_for_previous();
+    int count[NV];
     float gamma[NV][VEC], dgamma[NV][VEC], dbeta[NV][VEC];
+    Stream<T, L, NV, 2, SHIFT> rows(ring);
+    const int64_t step = int64_t(gridDim.x) * S::kRows;
+    const int64_t start = int64_t(blockIdx.x) * S::kRows + group;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) count[j] = cols - S::column(j);
+    auto at_x = [&](int64_t row) { return static_cast<const T *>(l.x) + row * l.ld_x + S::column(0); };
+    auto at_dy = [&](int64_t row) { return static_cast<const T *>(l.dy) + row * l.ld_dy + S::column(0); };
+#pragma unroll
+    for (int i = 0; i < rows.kAhead; ++i) {
+        const T *const base[2] = {at_x(start + i * step), at_dy(start + i * step)};
+        rows.send(base, start + i * step < l.rows, count);
+    }
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const int64_t c = int64_t(j * W * 32 + t) * VEC + i;
-            gamma[j][i] = l.gamma && c < l.cols ? load_any(l.gamma, l.weight_type, c) : 1.0f;
+            const int c = S::column(j) + i;
+            gamma[j][i] = l.gamma && c < cols ? load_any(l.gamma, l.weight_type, c) : 1.0f;
             dgamma[j][i] = dbeta[j][i] = 0.0f;
         }
-    const float over = 1.0f / float(l.cols);
-    const int64_t step = int64_t(gridDim.x) * kRows;
-    Raw<T, VEC> next_x[NV], next_dy[NV];
-    auto fetch = [&](int64_t row) {
+    const float over = 1.0f / float(cols);
+    const int64_t turns = (l.rows - int64_t(blockIdx.x) * S::kRows + step - 1) / step;
+    int64_t row = start;
+    float next_mean = row < l.rows ? l.mean[row] : 0.0f, next_rstd = row < l.rows ? l.rstd[row] : 0.0f;
+    for (int64_t turn = 0; turn < turns; ++turn, row += step) {
+        const T *const ahead[2] = {at_x(row + rows.kAhead * step), at_dy(row + rows.kAhead * step)};
+        rows.send(ahead, row + rows.kAhead * step < l.rows, count);
+        const bool in = row < l.rows;
+        const float mean = next_mean, rstd = next_rstd;
+        next_mean = next_rstd = 0.0f;
+        if (row + step < l.rows) {
+            next_mean = l.mean[row + step];
+            next_rstd = l.rstd[row + step];
+        }
+        const T *const base[2] = {at_x(row), at_dy(row)};
+        float both[2][NV][VEC];
+        rows.take(base, count, both);
+        float (&xh)[NV][VEC] = both[0], (&c1)[NV][VEC] = both[1];
+        // (beyond the row's end dy is zero, and with it all that is summed; so it is in rows that are not there)
+        const float by = in ? rstd : 0.0f;
+        Pair s1(0.0f, 0.0f), s2(0.0f, 0.0f);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int64_t c = int64_t(j * W * 32 + t) * VEC;
-            if (row < l.rows && c < l.cols) {
-                next_x[j].load(static_cast<const T *>(l.x) + row * l.ld_x + c);
-                next_dy[j].load(static_cast<const T *>(l.dy) + row * l.ld_dy + c);
-            } else {
-                next_x[j].clear();
-                next_dy[j].clear();
+            if (!in)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) xh[j][i] = c1[j][i] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VEC; i += 2) {
+                const Pair dy(c1[j][i], c1[j][i + 1]);
+                const Pair h = mul2(add2(Pair(xh[j][i], xh[j][i + 1]), Pair(-mean, -mean)), Pair(by, by));
+                fma2(dy, h, Pair(dgamma[j][i], dgamma[j][i + 1])).get(dgamma[j][i], dgamma[j][i + 1]);
+                add2(dy, Pair(dbeta[j][i], dbeta[j][i + 1])).get(dbeta[j][i], dbeta[j][i + 1]);
+                const Pair c = mul2(dy, Pair(gamma[j][i], gamma[j][i + 1]));
+                s1 = add2(s1, c);
+                s2 = fma2(c, h, s2);
+                h.get(xh[j][i], xh[j][i + 1]);
+                c.get(c1[j][i], c1[j][i + 1]);
             }
         }
-    };
-    int64_t row = int64_t(blockIdx.x) * kRows + group;
-    fetch(row);
-    int turn = 0;
-    for (; row < l.rows; row += step, turn ^= 1) {
-        const float mean = l.mean[row], rstd = l.rstd[row];
-        float xh[NV][VEC], c1[NV][VEC];
-        float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            next_x[j].get(xh[j]);
-            next_dy[j].get(c1[j]);
-        }
-        fetch(row + step);
+        const float2 sums = row_sums<L>(s1.sum(), s2.sum(), slots[turn & 1]);
+        const float m1 = -sums.x * over, m2 = -sums.y * over;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const int64_t c = int64_t(j * W * 32 + t) * VEC + i;
-                const bool in = VEC == 1 || c < l.cols;     // VEC == 1: what lies outside was fetched as zero
-                const float dy = in ? c1[j][i] : 0.0f;
-                const float h = c < l.cols ? (xh[j][i] - mean) * rstd : 0.0f;
-                dgamma[j][i] = fmaf(dy, h, dgamma[j][i]);
-                dbeta[j][i] += dy;
-                c1[j][i] = dy * gamma[j][i];
-                xh[j][i] = h;
-                s1 += c1[j][i];
-                s2 = fmaf(c1[j][i], h, s2);
-            }
-        s1 = warp_sum(s1);
-        s2 = warp_sum(s2);
-        if constexpr (W > 1) {
-            if ((threadIdx.x & 31) == 0) {
-                slots[turn][2 * (threadIdx.x >> 5) % 32] = s1;
-                slots[turn][(2 * (threadIdx.x >> 5) + 1) % 32] = s2;
-            }
-            __syncthreads();
-            s1 = s2 = 0.0f;
-#pragma unroll
-            for (int i = 0; i < W; ++i) {
-                s1 += slots[turn][2 * i];
-                s2 += slots[turn][2 * i + 1];
-            }
-        }
-        s1 *= over;
-        s2 *= over;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int64_t c = int64_t(j * W * 32 + t) * VEC;
-            if (c >= l.cols) continue;
-            float d[VEC];
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) d[i] = (c1[j][i] - s1 - xh[j][i] * s2) * rstd;
-            Raw<T, VEC>::put(static_cast<T *>(l.dx) + row * l.ld_dx + c, d, int(min(l.cols - c, int64_t(VEC))));
-        }
+            for (int i = 0; i < VEC; i += 2)
+                mul2(add2(fma2(Pair(xh[j][i], xh[j][i + 1]), Pair(m2, m2), Pair(c1[j][i], c1[j][i + 1])), Pair(m1, m1)), Pair(by, by))
+                    .get(c1[j][i], c1[j][i + 1]);
+        rows.store(static_cast<T *>(l.dx) + row * l.ld_dx + S::column(0), in, count, c1);
     }
     if (!partials) return;
     float *out = partials + int64_t(blockIdx.x) * 2 * l.cols;
-    if constexpr (W == 1) {
-        // the block's eight warps hold sums of the same columns
-        __shared__ float all[kNormWarps][32 * VEC];
+    if constexpr (S::kRows > 1) {
+        // the block's groups hold sums of the same columns: added in the order of the groups
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        float *all = reinterpret_cast<float *>(ring);       // [group][column of this piece]
+        static_assert(Stream<T, L, NV, 2, SHIFT>::kSmem >= 256 * VEC * 4, "the ring holds one piece of every thread");
 #pragma unroll
         for (int which = 0; which < 2; ++which)
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 __syncthreads();
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) all[group][t * VEC + i] = which ? dbeta[j][i] : dgamma[j][i];
+                for (int i = 0; i < VEC; ++i) all[(group * VEC + i) * L + t] = which ? dbeta[j][i] : dgamma[j][i];
                 __syncthreads();
-                for (int q = threadIdx.x; q < 32 * VEC; q += 32 * kNormWarps) {
+                for (int q = int(threadIdx.x); q < L * VEC; q += S::kThreads) {
+                    const int i = q / L, from = q % L;
                     float s = 0.0f;
-#pragma unroll
-                    for (int w = 0; w < kNormWarps; ++w) s += all[w][q];
-                    const int64_t c = int64_t(j) * 32 * VEC + q;
-                    if (c < l.cols) out[which * l.cols + c] = s;
+#pragma unroll 8
+                    for (int g = 0; g < S::kRows; ++g) s += all[(g * VEC + i) * L + from];
+                    const int c = ((from / S::kSegment * NV + j) * S::kSegment + from % S::kSegment) * VEC + i;
+                    if (c < cols) out[which * l.cols + c] = s;
                 }
             }
     } else {
@@ -338,8 +492,8 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kNormWarps : 32 * W) redist_laye
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const int64_t c = int64_t(j * W * 32 + t) * VEC + i;
-                if (c < l.cols) {
+                const int c = S::column(j) + i;
+                if (c < cols) {
                     out[c] = dgamma[j][i];
                     out[l.cols + c] = dbeta[j][i];
                 }
@@ -349,51 +503,88 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kNormWarps : 32 * W) redist_laye
 
 // Long rows: dx alone, with a second pass over a row that the first left in L2 ...
 template <typename T>
-__global__ void __launch_bounds__(1024) redist_layer_norm_grad_long_kernel(const LayerNorm l)
+__global__ void __launch_bounds__(kLong) redist_layer_norm_grad_long_kernel(const LayerNorm l)
 {
-    __shared__ float slots[2][32];
+    __shared__ float2 slots[2][32];
     let_next_start();
     wait_for_previous();
     const float over = 1.0f / float(l.cols);
-    for (int64_t row = blockIdx.x; row < l.rows; row += gridDim.x) {
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < l.rows; row += gridDim.x, turn ^= 1) {
         const T *x = static_cast<const T *>(l.x) + row * l.ld_x, *dy = static_cast<const T *>(l.dy) + row * l.ld_dy;
         T *dx = static_cast<T *>(l.dx) + row * l.ld_dx;
         const float mean = l.mean[row], rstd = l.rstd[row];
         float s1 = 0.0f, s2 = 0.0f;
-        for (int64_t c = threadIdx.x; c < l.cols; c += 1024) {
-            const float g = to_float(dy[c]) * (l.gamma ? load_any(l.gamma, l.weight_type, c) : 1.0f);
-            s1 += g;
-            s2 = fmaf(g, (to_float(x[c]) - mean) * rstd, s2);
+        for (int64_t c = int64_t(threadIdx.x) * 8; c < l.cols; c += kLong * 8) {
+            float v[8], d[8];
+            const int count = int(min(l.cols - c, int64_t(8)));
+            load8<T>(x + c, count, v);
+            load8<T>(dy + c, count, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) {
+                    const float g = d[i] * (l.gamma ? load_any(l.gamma, l.weight_type, c + i) : 1.0f);
+                    s1 += g;
+                    s2 = fmaf(g, (v[i] - mean) * rstd, s2);
+                }
         }
-        s1 = row_sum<32>(s1, slots[0]) * over;
-        s2 = row_sum<32>(s2, slots[1]) * over;
-        for (int64_t c = threadIdx.x; c < l.cols; c += 1024) {
-            const float g = to_float(dy[c]) * (l.gamma ? load_any(l.gamma, l.weight_type, c) : 1.0f);
-            dx[c] = from_float<T>((g - s1 - (to_float(x[c]) - mean) * rstd * s2) * rstd);
+        const float2 sums = row_sums<kLong>(s1, s2, slots[turn]);
+        s1 = sums.x * over;
+        s2 = sums.y * over;
+        for (int64_t c = int64_t(threadIdx.x) * 8; c < l.cols; c += kLong * 8) {
+            float v[8], d[8];
+            const int count = int(min(l.cols - c, int64_t(8)));
+            load8<T>(x + c, count, v);
+            load8<T>(dy + c, count, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) v[i] = (d[i] * (l.gamma ? load_any(l.gamma, l.weight_type, c + i) : 1.0f) - s1 - (v[i] - mean) * rstd * s2) * rstd;
+            store8<T>(dx + c, v, count);
         }
-        __syncthreads();
     }
 }
 
-// ... and the column sums on their own: a thread per column, a slice of the rows per block row.
+// ... and the column sums on their own: a lane has eight columns, a warp every eighth row of the block's slice.
 template <typename T>
 __global__ void __launch_bounds__(256) redist_layer_norm_columns_kernel(const LayerNorm l, float *partials)
 {
+    __shared__ float all[2][8][256];
     let_next_start();
     wait_for_previous();
-    const int64_t c = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (c >= l.cols) return;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int64_t c = int64_t(blockIdx.x) * 256 + lane * 8;
+    const int count = int(min(l.cols - c, int64_t(8)));
     const int64_t per = (l.rows + gridDim.y - 1) / gridDim.y, lo = per * blockIdx.y, hi = min(l.rows, lo + per);
-    float g = 0.0f, b = 0.0f;
-    for (int64_t row = lo; row < hi; ++row) {
-        const float dy = to_float(static_cast<const T *>(l.dy)[row * l.ld_dy + c]);
-        const float x = to_float(static_cast<const T *>(l.x)[row * l.ld_x + c]);
-        g = fmaf(dy, (x - l.mean[row]) * l.rstd[row], g);
-        b += dy;
+    float g[8] = {}, b[8] = {};
+    if (count > 0)
+#pragma unroll 2
+        for (int64_t row = lo + w; row < hi; row += 8) {
+            float v[8], d[8];
+            load8<T>(static_cast<const T *>(l.x) + row * l.ld_x + c, count, v);
+            load8<T>(static_cast<const T *>(l.dy) + row * l.ld_dy + c, count, d);
+            const float mean = l.mean[row], rstd = l.rstd[row];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                g[i] = fmaf(d[i], (v[i] - mean) * rstd, g[i]);
+                b[i] += d[i];
+            }
+        }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        all[0][w][lane * 8 + i] = g[i];
+        all[1][w][lane * 8 + i] = b[i];
     }
+    __syncthreads();
+    const int64_t cc = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (cc >= l.cols) return;
     float *out = partials + int64_t(blockIdx.y) * 2 * l.cols;
-    out[c] = g;
-    out[l.cols + c] = b;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += all[which][i][threadIdx.x];
+        out[which * l.cols + cc] = s;
+    }
 }
 
 // out[c] = sum over the parts of partials[part][c], in the same order every time.
@@ -439,17 +630,6 @@ constexpr int kLayCols = 256;
 // Rows of a block: 64, or more where the grid would grow beyond its limit.
 int64_t lay_rows(int64_t rows) { return 64 * ((rows + 64 * 32768 - 1) / (64 * 32768)); }
 
-template <typename T> __device__ __forceinline__ void split8(const uint4 &u, float (&v)[8])
-{
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = unpack2<T>(w[i]);
-        v[2 * i] = f.x;
-        v[2 * i + 1] = f.y;
-    }
-}
-
 // A block takes rows_per_block rows by 256 columns, a warp every eighth row, a lane eight neighbours.
 template <typename T>
 __global__ void __launch_bounds__(256) redist_lay_kernel(const Lay l, int64_t rows_per_block)
@@ -468,10 +648,10 @@ __global__ void __launch_bounds__(256) redist_lay_kernel(const Lay l, int64_t ro
             uint4 u = load16_any(static_cast<const T *>(l.src) + row * l.ld_src + c, count * 2);
             if (l.z || l.sums) {
                 float v[8];
-                split8<T>(u, v);
+                unpack16<T>(u, v);
                 if (l.z) {
                     float z[8];
-                    split8<T>(load16_any(static_cast<const T *>(l.z) + row * l.ld_z + c, count * 2), z);
+                    unpack16<T>(load16_any(static_cast<const T *>(l.z) + row * l.ld_z + c, count * 2), z);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[i] *= slope(z[i], l.activation);
                     u = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
@@ -495,24 +675,6 @@ __global__ void __launch_bounds__(256) redist_lay_kernel(const Lay l, int64_t ro
 }
 
 // ---- the input of the orthogonalisation --------------------------------------------------------------------
-
-template <typename T> struct Eight {     // eight neighbours at any alignment; what is not wanted reads as zero
-    static __device__ __forceinline__ void load(const T *p, int count, float (&v)[8])
-    {
-        if constexpr (sizeof(T) == 2) {
-            split8<T>(load16_any(p, count * 2), v);
-        } else {
-            const uint4 a = load16_any(p, min(count, 4) * 4);
-            uint4 b = make_uint4(0, 0, 0, 0);
-            if (count > 4) b = load16_any(p + 4, (count - 4) * 4);
-            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < count ? v[i] : 0.0f;
-    }
-};
 
 __device__ __forceinline__ double block_sum(double v, double *slots)
 {
@@ -539,7 +701,7 @@ __global__ void __launch_bounds__(256) redist_norm_parts_kernel(const Scaled s)
     for (int64_t q = int64_t(blockIdx.x) * 256 + threadIdx.x; q < all; q += step) {
         const int64_t row = q / per_row, c = (q - row * per_row) * 8;
         float v[8];
-        Eight<T>::load(x + row * s.ld_x + c, int(min(s.cols - c, int64_t(8))), v);
+        load8<T>(x + row * s.ld_x + c, int(min(s.cols - c, int64_t(8))), v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fma(double(v[i]), double(v[i]), sum);
     }
@@ -565,13 +727,13 @@ __global__ void __launch_bounds__(256) redist_scaled_kernel(const Scaled s, int 
     for (int64_t q = int64_t(blockIdx.x) * 256 + threadIdx.x; q < all; q += step) {
         const int64_t row = q / per_row, c = (q - row * per_row) * 8;
         float v[8], h[8];
-        Eight<T>::load(x + row * s.ld_x + c, int(min(s.cols - c, int64_t(8))), v);
+        load8<T>(x + row * s.ld_x + c, int(min(s.cols - c, int64_t(8))), v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= power;
         const uint4 u = make_uint4(pack2<__half>(v[0], v[1]), pack2<__half>(v[2], v[3]), pack2<__half>(v[4], v[5]), pack2<__half>(v[6], v[7]));
         *reinterpret_cast<uint4 *>(hi + row * s.ld + c) = u;
         if (lo) {
-            split8<__half>(u, h);
+            unpack16<__half>(u, h);
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[i] = (v[i] - h[i]) * 2048.0f;
             *reinterpret_cast<uint4 *>(lo + row * s.ld + c) =
@@ -624,7 +786,7 @@ __global__ void __launch_bounds__(256) redist_join_kernel(const Epilogue e, cons
     activate8(v, e.activation);
     if (e.residual) {
         float w[8];
-        split8<T>(load16_any(static_cast<const T *>(e.residual) + row * e.ld_residual + c, count * 2), w);
+        unpack16<T>(load16_any(static_cast<const T *>(e.residual) + row * e.ld_residual + c, count * 2), w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += w[i];
     }
@@ -634,9 +796,14 @@ __global__ void __launch_bounds__(256) redist_join_kernel(const Epilogue e, cons
 // ---- host ---------------------------------------------------------------------------------------------------
 
 template <typename... P, typename... A>
-cudaError_t launch(void (*kernel)(P...), dim3 grid, int block, const LaunchOptions &o, cudaStream_t stream, A... args)
+cudaError_t launch_with(int smem, void (*kernel)(P...), dim3 grid, int block, const LaunchOptions &o, cudaStream_t stream, A... args)
 {
     cudaLaunchConfig_t cfg = {};
+    if (smem > 48 * 1024) {
+        const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (ce != cudaSuccess) return ce;
+    }
+    cfg.dynamicSmemBytes = size_t(smem);
     cfg.gridDim = grid;
     cfg.blockDim = dim3(unsigned(block));
     cfg.stream = stream;
@@ -648,6 +815,12 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, int block, const LaunchOptio
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, int block, const LaunchOptions &o, cudaStream_t stream, A... args)
+{
+    return launch_with(0, kernel, grid, block, o, stream, args...);
+}
+
 cudaError_t sm_count(int *sms)
 {
     int device = 0;
@@ -656,42 +829,69 @@ cudaError_t sm_count(int *sms)
 
 bool on_16(const void *p, int64_t ld, int64_t element) { return p == nullptr || (uintptr_t(p) % 16 == 0 && ld * element % 16 == 0); }
 
-template <typename T, int VEC> cudaError_t forward_as(const LayerNorm &l, int sms, const LaunchOptions &o, cudaStream_t stream)
+// Threads per row and pieces per thread by the row's length: up to 16 neighbours per thread (more would cost the registers
+// that hold gamma and beta), within that the fewest threads; rows of fewer than 32 pieces share warps.
+template <typename T, typename F> bool by_pieces(int64_t pieces, F f)
 {
-    const int64_t pieces = (l.cols + VEC - 1) / VEC;
-    auto grid = [&](int rows_per_block, int blocks_per_sm) {
-        return dim3(unsigned(std::min<int64_t>((l.rows + rows_per_block - 1) / rows_per_block, int64_t(sms) * blocks_per_sm)));
-    };
-    if (pieces <= 32) return launch(redist_layer_norm_kernel<T, VEC, 1, 1>, grid(kNormWarps, 8), 32 * kNormWarps, o, stream, l);
-    if (pieces <= 64) return launch(redist_layer_norm_kernel<T, VEC, 1, 2>, grid(kNormWarps, 6), 32 * kNormWarps, o, stream, l);
-    if (pieces <= 256) return launch(redist_layer_norm_kernel<T, VEC, 8, 1>, grid(1, 8), 256, o, stream, l);
-    if (pieces <= 512) return launch(redist_layer_norm_kernel<T, VEC, 8, 2>, grid(1, 6), 256, o, stream, l);
-    if (pieces <= 1024) return launch(redist_layer_norm_kernel<T, VEC, 16, 2>, grid(1, 3), 512, o, stream, l);
-    if (pieces <= 2048) return launch(redist_layer_norm_kernel<T, VEC, 32, 2>, grid(1, 1), 1024, o, stream, l);
-    return launch(redist_layer_norm_long_kernel<T>, grid(1, 2), 1024, o, stream, l);
+    using std::integral_constant;
+    constexpr int MOST = 16 / kVec<T>;
+#define TAKE(THREADS, NV)                                                                       \
+    if (pieces <= THREADS * NV) {                                                               \
+        f(integral_constant<int, THREADS>(), integral_constant<int, NV>());                     \
+        return true;                                                                            \
+    }
+    TAKE(8, 1)
+    TAKE(16, 1)
+    TAKE(32, 1)
+    TAKE(32, 2)
+    TAKE(32, MOST)
+    TAKE(64, MOST)
+    TAKE(128, MOST)
+    TAKE(256, MOST)
+    TAKE(512, MOST)
+#undef TAKE
+    return false;
 }
 
-// Parts of the column sums and, through `run`, the launches of the backward pass: one place that knows both.
+unsigned row_blocks(const LayerNorm &l, int rows_per_block, int threads, int smem, int registers, int sms)
+{
+    const int64_t resident = std::max<int64_t>(1, std::min<int64_t>({2048 / threads, 65536 / (threads * registers), 220 * 1024 / std::max(smem + 1024, 1)}));
+    return unsigned(std::min<int64_t>((l.rows + rows_per_block - 1) / rows_per_block, sms * resident));
+}
+
+template <typename T, bool SHIFT> cudaError_t forward_as(const LayerNorm &l, int sms, const LaunchOptions &o, cudaStream_t stream)
+{
+    cudaError_t ce = cudaSuccess;
+    const bool held = by_pieces<T>((l.cols + kVec<T> - 1) / kVec<T>, [&](auto threads, auto pieces) {
+        constexpr int L = decltype(threads)::value, NV = decltype(pieces)::value;
+        using S = RowShape<T, L, NV>;
+        constexpr int smem = Stream<T, L, NV, 1, SHIFT>::kSmem;
+        ce = launch_with(smem, redist_layer_norm_kernel<T, L, NV, SHIFT>, dim3(row_blocks(l, S::kRows, S::kThreads, smem, NV == 1 ? 56 : 80, sms)), S::kThreads, o, stream, l);
+    });
+    if (held) return ce;
+    return launch(redist_layer_norm_long_kernel<T>, dim3(unsigned(std::min<int64_t>(l.rows, sms * 4))), kLong, o, stream, l);
+}
+
+// Blocks of the backward pass per SM at most, and slices of the rows for long rows' column sums: what the parts of the
+// column sums need of scratch follows from these.
 constexpr int kGradPerSm = 2, kLongParts = 64;
 
-template <typename T, int VEC>
+template <typename T, bool SHIFT>
 cudaError_t backward_as(const LayerNorm &l, float *partials, int sms, const LaunchOptions &o, cudaStream_t stream)
 {
-    const int64_t pieces = (l.cols + VEC - 1) / VEC;
-    auto grid = [&](int rows_per_block, int blocks_per_sm) {
-        return int(std::min<int64_t>((l.rows + rows_per_block - 1) / rows_per_block, int64_t(sms) * blocks_per_sm));
-    };
     int parts = 0;
-    cudaError_t ce;
-    if (pieces <= 32) ce = launch(redist_layer_norm_grad_kernel<T, VEC, 1, 1>, dim3(parts = grid(kNormWarps, 2)), 32 * kNormWarps, o, stream, l, partials);
-    else if (pieces <= 64) ce = launch(redist_layer_norm_grad_kernel<T, VEC, 1, 2>, dim3(parts = grid(kNormWarps, 2)), 32 * kNormWarps, o, stream, l, partials);
-    else if (pieces <= 256) ce = launch(redist_layer_norm_grad_kernel<T, VEC, 8, 1>, dim3(parts = grid(1, 2)), 256, o, stream, l, partials);
-    else if (pieces <= 512) ce = launch(redist_layer_norm_grad_kernel<T, VEC, 8, 2>, dim3(parts = grid(1, 2)), 256, o, stream, l, partials);
-    else if (pieces <= 1024) ce = launch(redist_layer_norm_grad_kernel<T, VEC, 16, 2>, dim3(parts = grid(1, 1)), 512, o, stream, l, partials);
-    else {
-        ce = launch(redist_layer_norm_grad_long_kernel<T>, dim3(grid(1, 2)), 1024, o, stream, l);
+    cudaError_t ce = cudaSuccess;
+    const bool held = by_pieces<T>((l.cols + kVec<T> - 1) / kVec<T>, [&](auto threads, auto pieces) {
+        constexpr int L = decltype(threads)::value, NV = decltype(pieces)::value;
+        using S = RowShape<T, L, NV>;
+        constexpr int smem = Stream<T, L, NV, 2, SHIFT>::kSmem;
+        parts = int(std::min<unsigned>(row_blocks(l, S::kRows, S::kThreads, smem, 128, sms), unsigned(sms * kGradPerSm)));
+        ce = launch_with(smem, redist_layer_norm_grad_kernel<T, L, NV, SHIFT>, dim3(unsigned(parts)), S::kThreads, o, stream, l, partials);
+    });
+    if (!held) {
+        ce = launch(redist_layer_norm_grad_long_kernel<T>, dim3(unsigned(std::min<int64_t>(l.rows, sms * 4))), kLong, o, stream, l);
         if (ce != cudaSuccess || !partials) return ce;
-        parts = int(std::min<int64_t>(l.rows, kLongParts));
+        parts = int(std::min<int64_t>((l.rows + 7) / 8, kLongParts));
         ce = launch(redist_layer_norm_columns_kernel<T>, dim3(unsigned((l.cols + 255) / 256), unsigned(parts)), 256, o, stream, l, partials);
     }
     if (ce != cudaSuccess || !partials) return ce;
@@ -721,9 +921,8 @@ cudaError_t launch_layer_norm_forward(const LayerNorm &l, const LaunchOptions &o
     if (ce != cudaSuccess || l.rows == 0) return ce;
     return by_type(l.type, [&](auto t) {
         using T = decltype(t);
-        constexpr int VEC = 16 / sizeof(T);
-        if (on_16(l.x, l.ld_x, sizeof(T)) && on_16(l.y, l.ld_y, sizeof(T))) return forward_as<T, VEC>(l, sms, o, stream);
-        return forward_as<T, 1>(l, sms, o, stream);
+        if (on_16(l.x, l.ld_x, sizeof(T)) && on_16(l.y, l.ld_y, sizeof(T))) return forward_as<T, false>(l, sms, o, stream);
+        return forward_as<T, true>(l, sms, o, stream);
     });
 }
 
@@ -740,10 +939,9 @@ cudaError_t launch_layer_norm_backward(const LayerNorm &l, void *workspace, cons
     float *partials = l.dgamma || l.dbeta ? static_cast<float *>(workspace) : nullptr;
     return by_type(l.type, [&](auto t) {
         using T = decltype(t);
-        constexpr int VEC = 16 / sizeof(T);
         if (on_16(l.x, l.ld_x, sizeof(T)) && on_16(l.dy, l.ld_dy, sizeof(T)) && on_16(l.dx, l.ld_dx, sizeof(T)))
-            return backward_as<T, VEC>(l, partials, sms, o, stream);
-        return backward_as<T, 1>(l, partials, sms, o, stream);
+            return backward_as<T, false>(l, partials, sms, o, stream);
+        return backward_as<T, true>(l, partials, sms, o, stream);
     });
 }
 
