@@ -29,7 +29,7 @@ __device__ __forceinline__ float exp2_fast(float v)
 // rounding of 32-bit Horner 2.3e-7).  Beyond, z Q(c) passes 1/2 and saturation makes Phi exactly 0 or 1.  Ten
 // instructions a value, no special functions, where erff takes thirty and branches; accurate to 2.3e-7 |z|.
 // Eight values are interleaved, so that the chain of one hides behind the others'.
-__device__ __forceinline__ void gelu8(float *z)
+__device__ __forceinline__ void phi8(const float *z, float *phi)
 {
     const float top = 5.2f * 5.2f;
     constexpr float kQ[14] = {-4.813592823e-04f, 1.268577063e-03f, -1.221270184e-03f, 1.799950609e-03f, -4.789268132e-03f,
@@ -52,8 +52,36 @@ __device__ __forceinline__ void gelu8(float *z)
     for (int k = 0; k < 4; ++k) {
         float q0, q1;
         Pair(q[k]).get(q0, q1);
-        z[2 * k] *= __saturatef(fmaf(z[2 * k], q0, 0.5f));
-        z[2 * k + 1] *= __saturatef(fmaf(z[2 * k + 1], q1, 0.5f));
+        phi[2 * k] = __saturatef(fmaf(z[2 * k], q0, 0.5f));
+        phi[2 * k + 1] = __saturatef(fmaf(z[2 * k + 1], q1, 0.5f));
+    }
+}
+
+__device__ __forceinline__ void gelu8(float *z)
+{
+    float phi[8];
+    phi8(z, phi);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] *= phi[i];
+}
+
+// v times the activation's slope at z.
+__device__ __forceinline__ void times_slope8(float (&v)[8], const float (&z)[8], int act)
+{
+    if (act == ACT_GELU) {                                  // Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi)
+        float phi[8];
+        phi8(z, phi);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= fmaf(z[i] * 0.39894228f, exp2_fast(z[i] * z[i] * -0.72134752f), phi[i]);
+    } else if (act == ACT_SILU) {                           // with s = 1 / (1 + exp(-z)): s + z s (1 - s)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float s = reciprocal(1.0f + exp2_fast(z[i] * -1.44269504f));
+            v[i] *= fmaf(z[i] * s, 1.0f - s, s);
+        }
+    } else if (act == ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = z[i] > 0.0f ? v[i] : v[i] * 0.0f;
     }
 }
 

@@ -150,9 +150,10 @@ struct Placed {
         ld = fits ? from.ld : round_up(from.line, 64);
         if (!fits) copy = pieces.take(from.lines * ld * 2);
     }
-    cudaError_t lay(int type, const LaunchOptions &o, cudaStream_t stream) const
+    // Adds what lays it anew to a list of such.
+    void lay(int type, Lay *list, int &count) const
     {
-        if (fits) return cudaSuccess;
+        if (fits) return;
         Lay l = {};
         l.rows = from.lines;
         l.cols = from.line;
@@ -161,7 +162,7 @@ struct Placed {
         l.ld_src = from.ld;
         l.dst = copy;
         l.ld_dst = ld;
-        return launch_lay(l, o, stream);
+        list[count++] = l;
     }
     // `rows_survive`: the product sums over this matrix's columns (else over its rows)
     Operand operand(bool rows_survive) const { return Operand{fits ? from.data : copy, ld, 0, from.by_rows == rows_survive ? 0 : 1}; }
@@ -459,8 +460,11 @@ redist_status redist_linear_forward(const redist_linear *op, void *scratch, size
             d.b = Operand{f.w.from.data, f.w.from.ld, 0, 0};
             return cuda(launch_few_rows(d, o, stream));
         }
-        TRY(cuda(f.x.lay(q.type, o, stream)));
-        TRY(cuda(f.w.lay(q.type, o, stream)));
+        Lay list[2];
+        int lays = 0;
+        f.x.lay(q.type, list, lays);
+        f.w.lay(q.type, list, lays);
+        TRY(cuda(launch_lay(list, lays, o, stream)));
         return cuda(launch_product(d, f.parts, o, stream));
     } catch (...) {
         return REDIST_EINTERNAL;
@@ -492,6 +496,8 @@ redist_status redist_linear_backward(const redist_linear *op, const redist_linea
         TRY(check_scratch(scratch, scratch_bytes, p.used));
         const LaunchOptions o = options();
         const Lines dy = lines_of(g.dy, q.rows, q.out_features);
+        Lay list[3];
+        int lays = 0;
         if (b.fresh || g.dbias) {
             Lay l = {};
             l.rows = q.rows;
@@ -508,16 +514,17 @@ redist_status redist_linear_backward(const redist_linear *op, const redist_linea
             l.ld_dst = b.ld_dz;
             l.sums = g.dbias;
             l.partials = b.partials;
-            TRY(cuda(launch_lay(l, o, stream)));
+            list[lays++] = l;
         }
+        if (g.dx.data) b.w.lay(q.type, list, lays);
+        if (g.dw.data) b.x.lay(q.type, list, lays);
+        TRY(cuda(launch_lay(list, lays, o, stream)));
         const void *dz = b.fresh ? b.dz : g.dy.data;
         if (g.dx.data) {
-            TRY(cuda(b.w.lay(q.type, o, stream)));
             TRY(cuda(launch_product(product_of(q.rows, q.in_features, q.out_features, q.type, Operand{dz, b.ld_dz, 0, 0}, b.w.operand(false), g.dx,
                                                q.rows, q.in_features), b.parts_dx, o, stream)));
         }
         if (g.dw.data) {
-            TRY(cuda(b.x.lay(q.type, o, stream)));
             TRY(cuda(launch_product(product_of(q.out_features, q.in_features, q.rows, q.type, Operand{dz, b.ld_dz, 0, 1}, b.x.operand(false), g.dw,
                                                q.out_features, q.in_features), b.parts_dw, o, stream)));
         }

@@ -1,7 +1,7 @@
 // D = epilogue(A B^T): 16-bit operands, 32-bit accumulation on the tensor cores (tcgen05).
 //
 // One thread block (CG = 1) or a pair of them on two SMs (CG = 2) owns a tile of 128 CG x BN outputs at a time and
-// walks over the sum in steps of 64: one thread brings the 128-byte wide slices of both operands into a ring of
+// walks over the sum in steps of 64 KB: two threads bring the 128-byte wide slices of the two operands into a ring of
 // shared-memory stages by TMA (128-byte swizzle), one thread issues the tcgen05.mma that consume them, and eight
 // warps turn the finished accumulator of the previous tile into outputs while the next one runs: tensor memory holds
 // two accumulators of BN columns.  Operands may be contiguous along the sum or along their rows (the gradients need
@@ -28,7 +28,7 @@ namespace redist {
 namespace {
 
 constexpr int kBK = 64;                 // elements of the sum per stage: 128 bytes, one swizzle row
-constexpr int kThreads = 384;           // warp 0 loads, warp 1 multiplies, warp 2 owns tensor memory, warps 4-11 store
+constexpr int kThreads = 384;           // warps 0 and 3 load, warp 1 multiplies, warp 2 owns tensor memory, warps 4-11 store
 constexpr int kRing = 196608;           // bytes of the ring of stages
 constexpr int kPiece = 2048;            // a warp's 32 x 32 piece of 16-bit outputs: rows of 64 bytes, 64-byte swizzle
 constexpr int kEpiBytes = 8 * 2 * kPiece;                   // two pieces per warp: one is filled while one is stored
@@ -207,8 +207,9 @@ struct Tile {
 };
 
 // Tiles of a matrix in groups of eight tile rows, column after column within a group, so that the blocks at work at
-// one time share slices of both operands in L2.  Symmetric: the lower triangle, row after row.
-__device__ __forceinline__ Tile tile_at(const ProductParams &p, int t)
+// one time share slices of both operands in L2.  Symmetric: those that reach the lower triangle, row after row; R is a
+// tile's height over its width (a whole number there), so that tile row i has R (i + 1) of them.
+template <int R> __device__ __forceinline__ Tile tile_at(const ProductParams &p, int t)
 {
     Tile r;
     r.k0 = 0;
@@ -222,11 +223,11 @@ __device__ __forceinline__ Tile tile_at(const ProductParams &p, int t)
     r.matrix = t / p.tiles_per_matrix;
     int q = t - r.matrix * p.tiles_per_matrix;
     if (p.symmetric) {
-        int i = int((sqrtf(8.0f * float(q) + 1.0f) - 1.0f) * 0.5f);
-        while (i * (i + 1) / 2 > q) --i;
-        while ((i + 1) * (i + 2) / 2 <= q) ++i;
+        int i = int((sqrtf(8.0f / R * float(q) + 1.0f) - 1.0f) * 0.5f);
+        while (R * (i * (i + 1) / 2) > q) --i;
+        while (R * ((i + 1) * (i + 2) / 2) <= q) ++i;
         r.tm = i;
-        r.tn = q - i * (i + 1) / 2;
+        r.tn = q - R * (i * (i + 1) / 2);
     } else {
         const int per_group = 8 * p.tiles_n, group = q / per_group;
         const int rows = min(8, p.tiles_m - group * 8);
@@ -399,14 +400,14 @@ template <bool ALIGNED> __device__ __forceinline__ void get_row(const uint16_t *
 
 // ---- the kernel ------------------------------------------------------------------------------------
 
-template <int CG, int BN, int KIND>
+template <int CG, int BN, int KB, int KIND>
 __global__ void __launch_bounds__(kThreads, 1)
 redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                       const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_more,
                       const __grid_constant__ ProductParams p)
 {
     constexpr int kRowsB = BN / CG;                         // rows of B that this block loads
-    constexpr int kStageA = 128 * 128, kStageB = kRowsB * 128, kStage = kStageA + kStageB;
+    constexpr int kSliceA = 128 * 128, kSliceB = kRowsB * 128, kStageA = KB * kSliceA, kStageB = KB * kSliceB, kStage = kStageA + kStageB;
     constexpr int kStages = kRing / kStage < kMaxStages ? kRing / kStage : kMaxStages;
     constexpr uint32_t kColumns = 2 * BN < 32 ? 32 : 2 * BN;
     constexpr int kShare = BN >= 64 ? BN / 2 : BN;          // columns of an accumulator that one warp stores
@@ -431,7 +432,7 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            bar_init(full(s), 1);
+            bar_init(full(s), 2);                           // both operands' bytes are announced
             bar_init(empty(s), 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -451,34 +452,37 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     wait_for_previous();
 
     bool ok = true;
-    if (warp == 0) {
-        // Loads.  The whole warp walks along, one lane issues; after a wait that ran out it only counts on to the end.
+    if (warp == 0 || warp == 3) {
+        // Loads: warp 0 those of A, warp 3 those of B.  The whole warp walks along, one lane issues; after a wait that ran
+        // out it only counts on to the end.
+        const bool second = warp == 3;
         int stage = 0;
         uint32_t phase = 0, rounds = 0, polls = p.wait_polls;
-        const uint32_t announced = CG * kStage + p.test_extra_tx;
+        const CUtensorMap *map = second ? &map_b : &map_a;
+        const int along_rows = second ? p.b_along_rows : p.a_along_rows;
+        const uint32_t announced = CG * (second ? kStageB : kStageA + p.test_extra_tx);
         for (int t = first; t < p.tiles; t += step) {
-            const Tile at = tile_at(p, t);
-            const int row_a = (at.tm * CG + int(rank)) * 128, row_b = at.tn * BN + int(rank) * kRowsB;
+            const Tile at = tile_at<CG * 128 / BN>(p, t);
+            const int row = second ? at.tn * BN + int(rank) * kRowsB : (at.tm * CG + int(rank)) * 128;
             for (int kb = at.k0; kb < at.k1; ++kb) {
                 if (!bar_wait(empty(stage), phase ^ 1, polls)) {
                     ok = false;
                     polls = 1;
                 }
                 if (elected() && ok) {
-                    const uint32_t to_a = base + stage * kStage, to_b = to_a + kStageA;
+                    const uint32_t to = base + stage * kStage + (second ? kStageA : 0);
                     const uint32_t bar = CG == 1 ? full(stage) : in_first(full(stage));
                     if (rank == 0) bar_expect(full(stage), announced);
-                    if (p.a_along_rows) {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) load_box<CG>(to_a + i * kBK * 128, &map_a, bar, row_a + 64 * i, kb * kBK, at.matrix);
-                    } else {
-                        load_box<CG>(to_a, &map_a, bar, kb * kBK, row_a, at.matrix);
-                    }
-                    if (p.b_along_rows) {
-#pragma unroll
-                        for (int i = 0; i < kRowsB / 64; ++i) load_box<CG>(to_b + i * kBK * 128, &map_b, bar, row_b + 64 * i, kb * kBK, at.matrix);
-                    } else {
-                        load_box<CG>(to_b, &map_b, bar, kb * kBK, row_b, at.matrix);
+                    for (int k = 0; k < KB; ++k) {
+                        const int x = (kb * KB + k) * kBK;
+                        const uint32_t slice = to + k * (second ? kSliceB : kSliceA);
+                        if (!along_rows) {
+                            load_box<CG>(slice, map, bar, x, row, at.matrix);
+                        } else {
+                            const int boxes = second ? kRowsB / 64 : 2;
+                            for (int i = 0; i < boxes; ++i) load_box<CG>(slice + i * kBK * 128, map, bar, row + 64 * i, x, at.matrix);
+                        }
                     }
                 }
                 if (ok && ++stage == kStages) {
@@ -516,7 +520,7 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             }
             fence_after();
             const uint32_t acc = tmem + buf * BN;
-            const Tile at = tile_at(p, t);
+            const Tile at = tile_at<CG * 128 / BN>(p, t);
             for (int kb = at.k0; kb < at.k1; ++kb) {
                 if (!bar_wait(full(stage), phase, polls)) {
                     ok = false;
@@ -526,7 +530,10 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 if (elected() && ok) {
                     const uint64_t da = desc_a + uint32_t(stage * (kStage >> 4)), db = desc_b + uint32_t(stage * (kStage >> 4));
 #pragma unroll
-                    for (int i = 0; i < kBK / 16; ++i) mma<CG>(acc, da + i * step_a, db + i * step_b, p.idesc, kb > at.k0 || i > 0);
+                    for (int k = 0; k < KB; ++k)
+#pragma unroll
+                        for (int i = 0; i < kBK / 16; ++i)
+                            mma<CG>(acc, da + k * (kSliceA >> 4) + i * step_a, db + k * (kSliceB >> 4) + i * step_b, p.idesc, kb > at.k0 || k + i > 0);
                     commit<CG>(empty(stage));
                     if (kb + 1 == at.k1) commit<CG>(acc_full(buf));
                 }
@@ -544,7 +551,7 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         int use = 0;
         for (int t = first; t < p.tiles; t += step, ++use) {
             const int b = use & 1;
-            const Tile at = tile_at(p, t);
+            const Tile at = tile_at<CG * 128 / BN>(p, t);
             const int row0 = (at.tm * CG + int(rank)) * 128 + quarter * 32, col_at = at.tn * BN + half * kShare;
             const int64_t row = row0 + lane;
             const bool in = row < p.m;
@@ -554,7 +561,6 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 for (int i = 0; i < p.e.alpha_power; ++i) alpha *= s;
                 for (int i = 0; i < p.e.beta_power; ++i) beta *= s;
             }
-            const bool mirror = KIND == EPI_SCALED && p.symmetric && at.tm != at.tn;
             // what a piece needs besides its accumulators is fetched before the wait (the first piece) or while the
             // piece before it is computed
             uint4 more[4], rest[4];
@@ -613,6 +619,8 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     if (p.e.out_type == T_BF16) linear_piece<__nv_bfloat16>(p, &map_out, &map_more, pieces, v, bias, now, lane, row0, col0);
                     else linear_piece<__half>(p, &map_out, &map_more, pieces, v, bias, now, lane, row0, col0);
                 } else {
+                    // above the diagonal only what no tile computes
+                    const bool mirror = p.symmetric && row0 / BN > col0 / (128 * CG) * (128 * CG / BN) + (128 * CG / BN - 1);
                     scaled_piece(p, &map_out, &map_more, pieces, v, now, now_rest, lane, row0, col0, at.matrix, alpha, beta, mirror);
                 }
             }
@@ -688,20 +696,26 @@ bool make_out_map(CUtensorMap *map, void *data, int64_t ld, int64_t batch_stride
                   CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tiles that reach the lower triangle: ratio (i + 1) in tile row i, but no more than there are columns.
+int64_t symmetric_tiles(int64_t tiles_m, int64_t tiles_n, int64_t ratio)
+{
+    return ratio * (tiles_m * (tiles_m - 1) / 2) + std::min(tiles_n, ratio * tiles_m);
+}
+
 bool on_16(const void *p, int64_t ld) { return p == nullptr || (uintptr_t(p) % 16 == 0 && ld % 8 == 0); }
 
-template <int CG, int BN, int KIND>
+template <int CG, int BN, int KB, int KIND>
 cudaError_t launch(const Product &q, int splits, const LaunchOptions &o, int device, int sms, cudaStream_t stream)
 {
     ProductParams p;
     std::memset(&p, 0, sizeof p);
     p.m = int32_t(q.m);
     p.n = int32_t(q.n);
-    p.k_blocks = int32_t((q.k + kBK - 1) / kBK);
+    p.k_blocks = int32_t((q.k + KB * kBK - 1) / (KB * kBK));
     p.batch = q.batch;
     p.tiles_m = int32_t((q.m + 128 * CG - 1) / (128 * CG));
     p.tiles_n = int32_t((q.n + BN - 1) / BN);
-    const int64_t per = q.symmetric ? int64_t(p.tiles_m) * (p.tiles_m + 1) / 2 : int64_t(p.tiles_m) * p.tiles_n;
+    const int64_t per = q.symmetric ? symmetric_tiles(p.tiles_m, p.tiles_n, 128 * CG / BN) : int64_t(p.tiles_m) * p.tiles_n;
     if (per * q.batch * splits > INT32_MAX / 2) return cudaErrorInvalidValue;
     p.tiles_per_matrix = int32_t(per);
     p.tiles = int32_t(per * q.batch * splits);
@@ -731,7 +745,7 @@ cudaError_t launch(const Product &q, int splits, const LaunchOptions &o, int dev
             return cudaErrorInvalidValue;
     }
 
-    auto *kernel = redist_product_kernel<CG, BN, KIND>;
+    auto *kernel = redist_product_kernel<CG, BN, KB, KIND>;
     static std::atomic<uint64_t> ready{0};                  // devices on which this kernel may use its shared memory
     if (device >= 64 || !(ready.load(std::memory_order_relaxed) >> device & 1)) {
         const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
@@ -784,16 +798,19 @@ bool operand_fits(const void *data, int64_t ld, int64_t batch_stride, int batch)
 
 namespace {
 
-// The tile shapes, and how long they take: microseconds per 64 steps of the sum, and per launch besides (start, the last
-// accumulator's epilogue), fitted to timings of some twenty sizes from 64 x 64 x 1000 to 4096 x 4096 x 4096.  A pair of
-// SMs on 256 x 256 reads half the operand bytes per product of one SM on 128 x 256, but fills the GPU from 74 tiles on;
-// small tiles are bound by the 0.2 us in which one thread can issue a step's copies and products, whatever their size.
+// The tile shapes, and how long they take: microseconds per 64 steps of the sum, where the tiles fit on the GPU at once
+// and where they take several rounds, and per launch besides (start, the last accumulator's epilogue); fitted to timings
+// of some twenty sizes from 64 x 64 x 1000 to 4096 x 4096 x 4096.  A pair of SMs on 256 x 256 reads half the operand
+// bytes per product of one SM on 128 x 256, but fills the GPU from 74 tiles on; small tiles are bound by the 0.15 us in
+// which the warps can issue 64 steps' copies and products, whatever their size (with two slices of 64 per stage; with
+// one it was 0.22).
 enum Shape { kPair256, kPair128, kOne256, kOne128, kOne64 };
 struct ShapeCost {
-    int rows, cols, per_unit;
-    double step, launch;
+    int rows, cols, per_unit, slices;       // slices: steps of 64 per stage
+    double step, step_rounds, launch;
 };
-constexpr ShapeCost kCosts[] = {{256, 256, 2, 0.30, 6.0}, {256, 128, 2, 0.245, 4.5}, {128, 256, 1, 0.33, 5.5}, {128, 128, 1, 0.255, 4.5}, {128, 64, 1, 0.22, 3.7}};
+constexpr ShapeCost kCosts[] = {{256, 256, 2, 1, 0.32, 0.33, 5.5}, {256, 128, 2, 2, 0.166, 0.23, 4.5}, {128, 256, 1, 1, 0.34, 0.39, 4.0},
+                                {128, 128, 1, 2, 0.21, 0.28, 4.2}, {128, 64, 1, 2, 0.15, 0.20, 3.6}};
 
 struct Choice {
     Shape shape;
@@ -807,18 +824,18 @@ Choice choose(const Product &p, int sms, bool may_split)
 {
     Choice best{kPair256, 1};
     double least = 1e30;
-    const int steps = int((p.k + kBK - 1) / kBK);
     for (int s = 0; s < 5; ++s) {
         const ShapeCost &c = kCosts[s];
-        if (p.symmetric && c.rows != c.cols) continue;
+        const int steps = int((p.k + kBK * c.slices - 1) / (kBK * c.slices));
+        if (p.symmetric && c.rows < c.cols) continue;
         const int64_t tm = (p.m + c.rows - 1) / c.rows, tn = (p.n + c.cols - 1) / c.cols;
-        const int64_t tiles = (p.symmetric ? tm * (tm + 1) / 2 : tm * tn) * p.batch, units = sms / c.per_unit;
-        const int most = may_split && tiles < units ? int(std::min<int64_t>(units / tiles, steps / 4)) : 1;
+        const int64_t tiles = (p.symmetric ? symmetric_tiles(tm, tn, c.rows / c.cols) : tm * tn) * p.batch, units = sms / c.per_unit;
+        const int most = may_split && tiles < units ? int(std::min<int64_t>(units / tiles, steps * c.slices / 4)) : 1;
         for (int k = 1; k <= std::max(most, 1); ++k) {
             const int per = (steps + k - 1) / k, parts = (steps + per - 1) / per;
             if (parts != k) continue;
             const int64_t waves = (tiles * k + units - 1) / units;
-            double t = double(waves) * per * c.step + c.launch;
+            double t = double(waves) * per * c.slices * (waves > 1 ? c.step_rounds : c.step) + c.launch;
             if (k > 1) t += 3.0 + double(p.m) * double(p.n) * k * 8e-6 / 4.0;
             if (t < least) {
                 least = t;
@@ -832,16 +849,11 @@ Choice choose(const Product &p, int sms, bool may_split)
 template <int KIND> cudaError_t launch_shape(const Product &p, const Choice &c, const LaunchOptions &o, int device, int sms, cudaStream_t stream)
 {
     switch (c.shape) {
-    case kPair256: return launch<2, 256, KIND>(p, c.splits, o, device, sms, stream);
-    case kOne128: return launch<1, 128, KIND>(p, c.splits, o, device, sms, stream);
-    default: break;
-    }
-    if constexpr (KIND == EPI_SCALED)
-        if (p.symmetric) return cudaErrorInvalidValue;
-    switch (c.shape) {
-    case kPair128: return launch<2, 128, KIND>(p, c.splits, o, device, sms, stream);
-    case kOne256: return launch<1, 256, KIND>(p, c.splits, o, device, sms, stream);
-    default: return launch<1, 64, KIND>(p, c.splits, o, device, sms, stream);
+    case kPair256: return launch<2, 256, 1, KIND>(p, c.splits, o, device, sms, stream);
+    case kPair128: return launch<2, 128, 2, KIND>(p, c.splits, o, device, sms, stream);
+    case kOne256: return launch<1, 256, 1, KIND>(p, c.splits, o, device, sms, stream);
+    case kOne128: return launch<1, 128, 2, KIND>(p, c.splits, o, device, sms, stream);
+    default: return launch<1, 64, 2, KIND>(p, c.splits, o, device, sms, stream);
     }
 }
 

@@ -613,53 +613,75 @@ __global__ void __launch_bounds__(256) redist_column_sum_kernel(const float *par
 
 // ---- operands of a product -------------------------------------------------------------------------------
 
-__device__ __forceinline__ float slope(float z, int act)
-{
-    if (act == ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if (act == ACT_GELU)
-        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
-    if (act == ACT_SILU) {
-        const float s = 1.0f / (1.0f + __expf(-z));
-        return s * (1.0f + z * (1.0f - s));
-    }
-    return 1.0f;
-}
-
 constexpr int kLayCols = 256;
 
-// Rows of a block: 64, or more where the grid would grow beyond its limit.
-int64_t lay_rows(int64_t rows) { return 64 * ((rows + 64 * 32768 - 1) / (64 * 32768)); }
+// Rows of a block: 128, fewer where that leaves SMs without work, more where the grid would grow beyond its limit.
+int64_t lay_rows(int64_t rows, int64_t cols)
+{
+    int64_t per = 128 * ((rows + 128 * 32768 - 1) / (128 * 32768));
+    while (per > 8 && ((rows + per - 1) / per) * ((cols + kLayCols - 1) / kLayCols) < 4 * 148) per /= 2;
+    return per;
+}
 
-// A block takes rows_per_block rows by 256 columns, a warp every eighth row, a lane eight neighbours.
-template <typename T>
-__global__ void __launch_bounds__(256) redist_lay_kernel(const Lay l, int64_t rows_per_block)
+struct Lays {
+    Lay l[3];
+    int64_t rows_per_block[3];
+};
+
+// Up to three matrices in one launch.  A block takes rows_per_block rows by 256 columns, a warp every eighth row, a lane
+// eight neighbours.
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(256) redist_lay_kernel(const __grid_constant__ Lays lays)
 {
     __shared__ float all[8][kLayCols];
     let_next_start();
     wait_for_previous();
+    const Lay &l = lays.l[blockIdx.z];
+    const int64_t rows_per_block = lays.rows_per_block[blockIdx.z];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int64_t c = int64_t(blockIdx.x) * kLayCols + lane * 8;
+    const int64_t lo = int64_t(blockIdx.y) * rows_per_block, hi = min(l.rows, lo + rows_per_block);
+    if (lo >= l.rows || int64_t(blockIdx.x) * kLayCols >= l.cols) return;
     const int count = int(min(l.cols - c, int64_t(8)));
     float sums[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    const int64_t lo = int64_t(blockIdx.y) * rows_per_block, hi = min(l.rows, lo + rows_per_block);
+    // four rows' loads are under way at a time: one after the other they leave half of the memory's time unused
+    constexpr int kBatch = 4;
     if (count > 0)
-#pragma unroll 4
-        for (int64_t row = lo + w; row < hi; row += 8) {
-            uint4 u = load16_any(static_cast<const T *>(l.src) + row * l.ld_src + c, count * 2);
-            if (l.z || l.sums) {
-                float v[8];
-                unpack16<T>(u, v);
-                if (l.z) {
-                    float z[8];
-                    unpack16<T>(load16_any(static_cast<const T *>(l.z) + row * l.ld_z + c, count * 2), z);
+        for (int64_t row = lo + w; row < hi; row += 8 * kBatch) {
+            uint4 u[kBatch], y[kBatch];
+            const T *src = static_cast<const T *>(l.src) + row * l.ld_src + c, *z = static_cast<const T *>(l.z) + row * l.ld_z + c;
+            if (ALIGNED && count >= 8) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] *= slope(z[i], l.activation);
-                    u = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
-                }
+                for (int k = 0; k < kBatch; ++k)
+                    if (row + 8 * k < hi) {
+                        u[k] = *reinterpret_cast<const uint4 *>(src + 8 * k * l.ld_src);
+                        if (l.z) y[k] = *reinterpret_cast<const uint4 *>(z + 8 * k * l.ld_z);
+                    }
+            } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sums[i] += v[i];
+                for (int k = 0; k < kBatch; ++k)
+                    if (row + 8 * k < hi) {
+                        u[k] = load16_any(src + 8 * k * l.ld_src, count * 2);
+                        if (l.z) y[k] = load16_any(z + 8 * k * l.ld_z, count * 2);
+                    }
             }
-            if (l.dst) *reinterpret_cast<uint4 *>(static_cast<T *>(l.dst) + row * l.ld_dst + c) = u;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (row + 8 * k >= hi) break;
+                if (l.z || l.sums) {
+                    float v[8];
+                    unpack16<T>(u[k], v);
+                    if (l.z) {
+                        float at[8];
+                        unpack16<T>(y[k], at);
+                        times_slope8(v, at, l.activation);
+                        u[k] = pack16<T>(v);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sums[i] += v[i];
+                }
+                if (l.dst) *reinterpret_cast<uint4 *>(static_cast<T *>(l.dst) + (row + 8 * k) * l.ld_dst + c) = u[k];
+            }
         }
     if (!l.sums) return;
 #pragma unroll
@@ -947,19 +969,37 @@ cudaError_t launch_layer_norm_backward(const LayerNorm &l, void *workspace, cons
 
 size_t column_partial_bytes(int64_t rows, int64_t cols)
 {
-    return rows > 0 ? size_t((rows + lay_rows(rows) - 1) / lay_rows(rows) * cols * 4) : 0;
+    if (rows == 0) return 0;
+    const int64_t per = lay_rows(rows, cols);
+    return size_t((rows + per - 1) / per * cols * 4);
 }
 
-cudaError_t launch_lay(const Lay &l, const LaunchOptions &o, cudaStream_t stream)
+cudaError_t launch_lay(const Lay *l, int count, const LaunchOptions &o, cudaStream_t stream)
 {
-    if (l.rows == 0) return l.sums ? cudaMemsetAsync(l.sums, 0, size_t(l.cols) * 4, stream) : cudaSuccess;
-    const int64_t per = lay_rows(l.rows), parts = (l.rows + per - 1) / per;
-    const dim3 grid(unsigned((l.cols + kLayCols - 1) / kLayCols), unsigned(parts));
-    cudaError_t ce = l.type == T_BF16 ? launch(redist_lay_kernel<__nv_bfloat16>, grid, 256, o, stream, l, per)
-                                      : launch(redist_lay_kernel<__half>, grid, 256, o, stream, l, per);
-    if (ce != cudaSuccess || !l.sums) return ce;
-    return launch(redist_column_sum_kernel, dim3(unsigned((l.cols + 31) / 32), 1), 256, o, stream, static_cast<const float *>(l.partials),
-                  int(parts), l.cols, l.cols, l.sums, static_cast<float *>(nullptr));
+    Lays lays = {};
+    int64_t x = 0, y = 0;
+    for (int i = 0; i < count; ++i) {
+        lays.l[i] = l[i];
+        lays.rows_per_block[i] = lay_rows(l[i].rows, l[i].cols);
+        x = std::max(x, (l[i].cols + kLayCols - 1) / kLayCols);
+        y = std::max(y, (l[i].rows + lays.rows_per_block[i] - 1) / lays.rows_per_block[i]);
+    }
+    if (count == 0 || x == 0 || y == 0) return cudaSuccess;
+    const dim3 grid{unsigned(x), unsigned(y), unsigned(count)};
+    bool aligned = true;
+    for (int i = 0; i < count; ++i) aligned = aligned && on_16(l[i].src, l[i].ld_src, 2) && on_16(l[i].z, l[i].ld_z, 2);
+    cudaError_t ce;
+    if (l[0].type == T_BF16)
+        ce = aligned ? launch(redist_lay_kernel<__nv_bfloat16, true>, grid, 256, o, stream, lays) : launch(redist_lay_kernel<__nv_bfloat16, false>, grid, 256, o, stream, lays);
+    else
+        ce = aligned ? launch(redist_lay_kernel<__half, true>, grid, 256, o, stream, lays) : launch(redist_lay_kernel<__half, false>, grid, 256, o, stream, lays);
+    for (int i = 0; i < count && ce == cudaSuccess; ++i)
+        if (l[i].sums) {
+            const int64_t per = lays.rows_per_block[i];
+            ce = launch(redist_column_sum_kernel, dim3(unsigned((l[i].cols + 31) / 32), 1), 256, o, stream, static_cast<const float *>(l[i].partials),
+                        int((l[i].rows + per - 1) / per), l[i].cols, l[i].cols, l[i].sums, static_cast<float *>(nullptr));
+        }
+    return ce;
 }
 
 cudaError_t launch_join(const Product &p, const float *parts, int64_t ld, int splits, const LaunchOptions &o, cudaStream_t stream)

@@ -46,7 +46,8 @@ struct Lay {
     float *partials;
 };
 size_t column_partial_bytes(int64_t rows, int64_t cols);
-cudaError_t launch_lay(const Lay &l, const LaunchOptions &o, cudaStream_t stream);
+// Up to three of them in one launch (all of one type).
+cudaError_t launch_lay(const Lay *l, int count, const LaunchOptions &o, cudaStream_t stream);
 
 // The input of the orthogonalisation: |X|_F of every matrix, and X times a power of two that brings the norm to
 // [2^13, 2^14), as f16 (hi) and, for 32-bit inputs, the rest times 2048 (lo).  scale[matrix] = 1 / (norm times that).
