@@ -275,16 +275,86 @@ struct Pieces {
         turn ^= 1;
     }
 
-    // The same row by row, two bytes per lane.
-    __device__ __forceinline__ void store_rows(uint16_t *out, int64_t ld, int lane, int row0, int col0, int m, int n)
+    // ---- rows that start anywhere: the piece to fill, and what sends it off
+
+    __device__ __forceinline__ uint8_t *plain() const { return smem; }
+
+    // Stores `cnt` (up to 32) columns of up to `rows` rows from the piece, `to` the first of them.  A row's aligned blocks
+    // of 16 bytes go out whole, four per row; what the last of them lacks of a piece waits in `carry` (0: out, 1: pre) for
+    // the piece to its right.  Only a row's ends go out two bytes at a time.
+    __device__ __forceinline__ void store_any(uint16_t *to, int64_t ld, int lane, int rows, int cnt, bool first, bool last, int carry) const
+    {
+        uint8_t *kept = smem + 3072 + carry * 512;
+        auto word = [&](int r, int w) -> uint32_t {
+            return *reinterpret_cast<const uint32_t *>(w >= 0 ? smem + piece_at(r, w >> 2) + (w & 3) * 4 : kept + r * 16 + (w + 4) * 4);
+        };
+        auto element = [&](int r, int e) -> uint16_t {
+            return *reinterpret_cast<const uint16_t *>(e >= 0 ? smem + piece_at(r, e >> 3) + (e & 7) * 2 : kept + r * 16 + (e + 8) * 2);
+        };
+        __syncwarp();
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const int r = it * 8 + (lane >> 2);
+            uint16_t *row = to + r * ld;
+            const int s = 8 * (lane & 3) - int(reinterpret_cast<uintptr_t>(row) & 15) / 2;
+            if (r < rows && (s >= 0 || !first) && s + 8 <= cnt) {
+                const int w = s >> 1;                       // rounds down, below zero too
+                uint4 u = make_uint4(word(r, w), word(r, w + 1), word(r, w + 2), word(r, w + 3));
+                if (s & 1) {
+                    const uint32_t end = word(r, w + 4);
+                    u = make_uint4(__funnelshift_r(u.x, u.y, 16), __funnelshift_r(u.y, u.z, 16), __funnelshift_r(u.z, u.w, 16), __funnelshift_r(u.w, end, 16));
+                }
+                *reinterpret_cast<uint4 *>(row + s) = u;
+            }
+        }
+        if ((first || last) && lane < rows) {
+            uint16_t *row = to + lane * ld;
+            const int p = int(reinterpret_cast<uintptr_t>(row) & 15) / 2, head = p ? 8 - p : 0;
+            if (first)
+                for (int e = 0; e < min(head, cnt); ++e) row[e] = element(lane, e);
+            if (last) {
+                const int whole = ((cnt + p) >> 3) * 8 - p;
+                for (int e = first ? max(whole, head) : whole; e < cnt; ++e) row[e] = element(lane, e);
+            }
+        }
+        __syncwarp();
+        if (!last) *reinterpret_cast<uint4 *>(kept + lane * 16) = *reinterpret_cast<const uint4 *>(smem + piece_at(lane, 3));
+        __syncwarp();
+    }
+
+    // Rows of a matrix whose rows start anywhere, 32 columns of 32 rows: `ask` loads the aligned blocks that hold them, lanes
+    // along the rows; `take` hands every lane its row.
+    static __device__ __forceinline__ void ask(const uint16_t *from, int64_t ld, int lane, int rows, int cnt, uint4 (&blocks)[4], uint4 &end)
+    {
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const int r = it * 8 + (lane >> 2), b = lane & 3;
+            const uintptr_t at = reinterpret_cast<uintptr_t>(from + r * ld);
+            blocks[it] = make_uint4(0, 0, 0, 0);
+            if (r < rows && 16 * b < int(at & 15) + 2 * cnt) blocks[it] = *reinterpret_cast<const uint4 *>((at & ~uintptr_t(15)) + 16 * b);
+        }
+        const uintptr_t at = reinterpret_cast<uintptr_t>(from + lane * ld);
+        end = make_uint4(0, 0, 0, 0);
+        if (lane < rows && 64 < int(at & 15) + 2 * cnt) end = *reinterpret_cast<const uint4 *>((at & ~uintptr_t(15)) + 64);
+    }
+    __device__ __forceinline__ void take(const uint16_t *from, int64_t ld, int lane, uint4 (&blocks)[4], const uint4 &end) const
     {
         __syncwarp();
-        const uint8_t *piece = smem + turn * kPiece;
-        uint16_t *to = out + int64_t(row0) * ld + col0 + lane;
-        const bool in = col0 + lane < n;
-#pragma unroll 8
-        for (int r = 0; r < 32; ++r)
-            if (in && row0 + r < m) to[r * ld] = *reinterpret_cast<const uint16_t *>(piece + piece_at(r, lane >> 3) + (lane & 7) * 2);
+#pragma unroll
+        for (int it = 0; it < 4; ++it) *reinterpret_cast<uint4 *>(smem + (it * 8 + (lane >> 2)) * 80 + (lane & 3) * 16) = blocks[it];
+        *reinterpret_cast<uint4 *>(smem + lane * 80 + 64) = end;
+        __syncwarp();
+        const int off = int(reinterpret_cast<uintptr_t>(from + lane * ld) & 15);
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(smem + lane * 80 + (off & ~3));
+        uint32_t v[17];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = w[i];
+        v[16] = off & 2 ? w[16] : 0;
+        if (off & 2)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = __funnelshift_r(v[i], v[i + 1], 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) blocks[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
         __syncwarp();
     }
 };
@@ -312,7 +382,8 @@ template <typename T> __device__ __forceinline__ void unpack8(const uint4 &u, fl
 // 32 x 32 values of the linear epilogue; `bias` holds the columns' biases, `ahead` the lane's row of the residual.
 template <typename T>
 __device__ __forceinline__ void linear_piece(const ProductParams &p, const CUtensorMap *map_out, const CUtensorMap *map_pre, Pieces &pieces,
-                                             float (&v)[32], const float *bias, const uint4 (&ahead)[4], int lane, int row0, int col0)
+                                             float (&v)[32], const float *bias, const uint4 (&ahead)[4], int lane, int row0, int col0,
+                                             bool first, bool last)
 {
     const Epilogue &e = p.e;
     if (e.bias) {
@@ -326,9 +397,13 @@ __device__ __forceinline__ void linear_piece(const ProductParams &p, const CUten
         }
     }
     if (e.pre) {
-        put_row<T>(pieces.next(lane), lane, v);
-        if (p.aligned_out) pieces.store(map_pre, lane, row0, col0, 0);
-        else pieces.store_rows(static_cast<uint16_t *>(e.pre), e.ld_pre, lane, row0, col0, p.m, p.n);
+        if (p.aligned_out) {
+            put_row<T>(pieces.next(lane), lane, v);
+            pieces.store(map_pre, lane, row0, col0, 0);
+        } else {
+            put_row<T>(pieces.plain(), lane, v);
+            pieces.store_any(static_cast<uint16_t *>(e.pre) + int64_t(row0) * e.ld_pre + col0, e.ld_pre, lane, p.m - row0, min(32, p.n - col0), first, last, 1);
+        }
     }
     activate32(v, e.activation);
     if (e.residual) {
@@ -338,16 +413,20 @@ __device__ __forceinline__ void linear_piece(const ProductParams &p, const CUten
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] += w[i];
     }
-    put_row<T>(pieces.next(lane), lane, v);
-    if (p.aligned_out) pieces.store(map_out, lane, row0, col0, 0);
-    else pieces.store_rows(static_cast<uint16_t *>(e.out), e.ld_out, lane, row0, col0, p.m, p.n);
+    if (p.aligned_out) {
+        put_row<T>(pieces.next(lane), lane, v);
+        pieces.store(map_out, lane, row0, col0, 0);
+    } else {
+        put_row<T>(pieces.plain(), lane, v);
+        pieces.store_any(static_cast<uint16_t *>(e.out) + int64_t(row0) * e.ld_out + col0, e.ld_out, lane, p.m - row0, min(32, p.n - col0), first, last, 0);
+    }
 }
 
 // 32 x 32 values of the scaled epilogue; `hi` and `lo` hold the lane's row of what is added.  A mirrored piece is
 // written a second time with rows and columns exchanged.
 __device__ __forceinline__ void scaled_piece(const ProductParams &p, const CUtensorMap *map_out, const CUtensorMap *map_lo, Pieces &pieces,
                                              float (&v)[32], const uint4 (&hi)[4], const uint4 (&lo)[4], int lane, int row0, int col0,
-                                             int matrix, float alpha, float beta, bool mirror)
+                                             int matrix, float alpha, float beta, bool mirror, bool first, bool last)
 {
     const Epilogue &e = p.e;
 #pragma unroll
@@ -362,11 +441,16 @@ __device__ __forceinline__ void scaled_piece(const ProductParams &p, const CUten
             for (int i = 0; i < 8; ++i) v[8 * j + i] = fmaf(beta, fmaf(u[i], 1.0f / 2048.0f, w[i]), v[8 * j + i]);
         }
     }
+    if (e.out_type == T_BF16 && !p.aligned_out) {
+        put_row<__nv_bfloat16>(pieces.plain(), lane, v);
+        pieces.store_any(static_cast<uint16_t *>(e.out) + int64_t(matrix) * e.out_batch + int64_t(row0) * e.ld_out + col0, e.ld_out, lane, p.m - row0,
+                         min(32, p.n - col0), first, last, 0);
+        return;
+    }
     uint8_t *piece = pieces.next(lane);
     if (e.out_type == T_BF16) {
         put_row<__nv_bfloat16>(piece, lane, v);
-        if (p.aligned_out) pieces.store(map_out, lane, row0, col0, matrix);
-        else pieces.store_rows(static_cast<uint16_t *>(e.out) + int64_t(matrix) * e.out_batch, e.ld_out, lane, row0, col0, p.m, p.n);
+        pieces.store(map_out, lane, row0, col0, matrix);
         return;
     }
     put_row<__half>(piece, lane, v);
@@ -385,16 +469,14 @@ __device__ __forceinline__ void scaled_piece(const ProductParams &p, const CUten
     }
 }
 
-// The lane's row of 32 neighbours from column col0 on, 16 bytes at a time; what lies outside n reads as zero (or as
-// the padding of a workspace row: it is not stored).
-template <bool ALIGNED> __device__ __forceinline__ void get_row(const uint16_t *row, bool in, int left, uint4 (&v)[4])
+// The lane's row of 32 neighbours, 16 bytes at a time; what lies outside the matrix reads as zero (or as the padding of a
+// workspace row: it is not stored).
+__device__ __forceinline__ void get_row(const uint16_t *row, bool in, int left, uint4 (&v)[4])
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         v[j] = make_uint4(0, 0, 0, 0);
-        if (!in || left <= 8 * j) continue;
-        if (ALIGNED) v[j] = *reinterpret_cast<const uint4 *>(row + 8 * j);
-        else v[j] = load16_any(row + 8 * j, min(left - 8 * j, 8) * 2);
+        if (in && left > 8 * j) v[j] = *reinterpret_cast<const uint4 *>(row + 8 * j);
     }
 }
 
@@ -569,15 +651,15 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 const int left = p.n - col0;
                 if constexpr (KIND == EPI_LINEAR) {
                     if (p.e.residual) {
-                        const uint16_t *q = static_cast<const uint16_t *>(p.e.residual) + row * p.e.ld_residual + col0;
-                        if (p.aligned_residual && left >= 32) get_row<true>(q, in, left, more);
-                        else get_row<false>(q, in, left, more);
+                        const uint16_t *q = static_cast<const uint16_t *>(p.e.residual) + int64_t(row0) * p.e.ld_residual + col0;
+                        if (p.aligned_residual) get_row(q + lane * p.e.ld_residual, in, left, more);
+                        else Pieces::ask(q, p.e.ld_residual, lane, p.m - row0, min(32, left), more, rest[0]);
                     }
                     if (p.e.bias) next_bias = lane < left ? load_any(p.e.bias, p.e.bias_type, col0 + lane) : 0.0f;
                 } else if (KIND == EPI_SCALED && p.e.hi) {
                     const int64_t q = int64_t(at.matrix) * p.e.add_batch + row * p.e.ld_add + col0;
-                    get_row<true>(static_cast<const uint16_t *>(p.e.hi) + q, in, left, more);
-                    if (p.e.lo) get_row<true>(static_cast<const uint16_t *>(p.e.lo) + q, in, left, rest);
+                    get_row(static_cast<const uint16_t *>(p.e.hi) + q, in, left, more);
+                    if (p.e.lo) get_row(static_cast<const uint16_t *>(p.e.lo) + q, in, left, rest);
                 }
             };
 #pragma unroll
@@ -608,7 +690,10 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     bias[lane] = next_bias;
                     __syncwarp();
                 }
-                if (c + 32 < kShare && col0 + 32 < p.n) fetch(col0 + 32);
+                const bool begins = c == 0, ends = c + 32 >= kShare || col0 + 32 >= p.n;
+                if (!ends) fetch(col0 + 32);
+                if (KIND == EPI_LINEAR && p.e.residual && !p.aligned_residual)
+                    pieces.take(static_cast<const uint16_t *>(p.e.residual) + int64_t(row0) * p.e.ld_residual + col0, p.e.ld_residual, lane, now, now_rest[0]);
                 if constexpr (KIND == EPI_PARTIAL) {
                     if (in) {
                         float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(p.e.out) + (int64_t(t % p.splits) * p.m + row) * p.e.ld_out + col0);
@@ -616,12 +701,12 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                         for (int i = 0; i < 8; ++i) q[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                     }
                 } else if constexpr (KIND == EPI_LINEAR) {
-                    if (p.e.out_type == T_BF16) linear_piece<__nv_bfloat16>(p, &map_out, &map_more, pieces, v, bias, now, lane, row0, col0);
-                    else linear_piece<__half>(p, &map_out, &map_more, pieces, v, bias, now, lane, row0, col0);
+                    if (p.e.out_type == T_BF16) linear_piece<__nv_bfloat16>(p, &map_out, &map_more, pieces, v, bias, now, lane, row0, col0, begins, ends);
+                    else linear_piece<__half>(p, &map_out, &map_more, pieces, v, bias, now, lane, row0, col0, begins, ends);
                 } else {
                     // above the diagonal only what no tile computes
                     const bool mirror = p.symmetric && row0 / BN > col0 / (128 * CG) * (128 * CG / BN) + (128 * CG / BN - 1);
-                    scaled_piece(p, &map_out, &map_more, pieces, v, now, now_rest, lane, row0, col0, at.matrix, alpha, beta, mirror);
+                    scaled_piece(p, &map_out, &map_more, pieces, v, now, now_rest, lane, row0, col0, at.matrix, alpha, beta, mirror, begins, ends);
                 }
             }
             fence_before();
@@ -734,6 +819,7 @@ cudaError_t launch(const Product &q, int splits, const LaunchOptions &o, int dev
     const Epilogue &e = q.e;
     p.aligned_out = KIND != EPI_PARTIAL && on_16(e.out, e.ld_out) && (q.batch == 1 || e.out_batch % 8 == 0) && on_16(e.pre, e.ld_pre);
     p.aligned_residual = on_16(e.residual, e.ld_residual);
+    p.aligned_out = p.aligned_out && p.aligned_residual;    // one way of using the pieces' memory per launch
     CUtensorMap ma, mb, mo, mm;
     if (!make_map(&ma, q.a, q.m, q.k, q.batch, 128) || !make_map(&mb, q.b, q.n, q.k, q.batch, BN / CG)) return cudaErrorInvalidValue;
     std::memset(&mo, 0, sizeof mo);
