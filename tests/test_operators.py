@@ -539,20 +539,20 @@ def test_scratch_is_enough_and_nothing_else_is_written():
         assert e.value.status == 5
 
     own = api._operators()
-    real = own.empty
+    real = own.strided
     sizes = []
     try:
         def empty(*a, **k):                                              # what the binding allocates for itself
             if k.get("dtype") == torch.uint8:
-                sizes.append(a[0])
+                sizes.append(a[0][0])
             return real(*a, **k)
-        own.empty = empty
+        own.strided = empty
         api.linear_forward(x, w)
         api.linear_backward(dy, x, w, pre, "silu")
         api.layer_norm_backward(x, x, None, torch.zeros(77, device="cuda"), torch.ones(77, device="cuda"))
         api.orthogonalize(m)
     finally:
-        own.empty = real
+        own.strided = real
     assert len(sizes) == 4
     run(lambda s: api.linear_forward(x, w, scratch=s), sizes[0])
     run(lambda s: api.linear_backward(dy, x, w, pre, "silu", scratch=s), sizes[1])
@@ -561,11 +561,13 @@ def test_scratch_is_enough_and_nothing_else_is_written():
 
 
 @pytest.mark.gpu
-def test_a_wait_that_runs_out_is_counted_and_returns():
+@pytest.mark.parametrize("rows,k,n", [(700, 640, 600), (2048, 1024, 2304), (300, 4096, 200)])
+def test_a_wait_that_runs_out_is_counted_and_returns(rows, k, n):
     """test_extra_tx announces bytes that never come: every stage's wait runs out, the call returns, the counter says
-    so, and the next call works.  (The copies themselves all land, so nothing is left in flight.)"""
+    so, and the next call works.  (The copies themselves all land, so nothing is left in flight.)  Single SMs, pairs, and a
+    split sum."""
     g = gen(11)
-    x, w = rand(g, 700, 640, dtype=BF16), rand(g, 600, 640, dtype=BF16)
+    x, w = rand(g, rows, k, dtype=BF16), rand(g, n, k, dtype=BF16)
     want = api.linear_forward(x, w)
     before = api.redist_product_timeouts()
     with api.tuning(test_extra_tx=16, wait_polls=64):
