@@ -202,28 +202,67 @@ template <int L> __device__ __forceinline__ float2 row_sums(float a, float b, fl
     return make_float2(a, b);
 }
 
+// Rows too long for a block are shared by a cluster of CL blocks, each with its own columns: the blocks' sums meet in every
+// block's shared memory and are added in the order of the blocks.  `meet` has CL entries per use and may be used again
+// after one more such meeting.
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <int L, int CL> __device__ __forceinline__ float2 row_sums(float a, float b, float2 *slot, float2 *meet, uint32_t rank)
+{
+    const float2 mine = row_sums<L>(a, b, slot);
+    if constexpr (CL == 1) return mine;
+    if (threadIdx.x < CL) {
+        const uint32_t here = uint32_t(__cvta_generic_to_shared(meet + rank));
+        uint32_t there;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here), "r"(threadIdx.x));
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(mine.x), "f"(mine.y) : "memory");
+    }
+    __syncwarp();
+    cluster_sync();
+    float2 all = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < CL; ++i) {
+        all.x += meet[i].x;
+        all.y += meet[i].y;
+    }
+    return all;
+}
+
 // ---- layer norm, forward -------------------------------------------------------------------------------
 
 // Mean first, then the differences d from it, sum of d^2 and sum of d: the latter is what rounding left in the mean, and
 // corrects both (var = mean d^2 - (mean d)^2), so a mean far larger than the spread costs no digits.
-template <typename T, int L, int NV, bool SHIFT>
-__global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_norm_kernel(const LayerNorm l)
+template <typename T, int L, int NV, bool SHIFT, int CL>
+__global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads, L >= 512 ? 2 : 3) redist_layer_norm_kernel(const LayerNorm l)
 {
     using S = RowShape<T, L, NV>;
     constexpr int VEC = S::VEC;
-    __shared__ float2 slots[2][32];
+    __shared__ float2 slots[2][32], meet[2][CL];
     extern __shared__ __align__(16) uint8_t ring[];
-    const int t = int(threadIdx.x) % L, group = int(threadIdx.x) / L, cols = int(l.cols);
+    const uint32_t rank = CL > 1 ? cluster_rank() : 0;
+    const int from = int(rank) * L * NV * VEC;              // this block's first column
+    const int t = int(threadIdx.x) % L, group = int(threadIdx.x) / L, cols = int(l.cols) - from;
     let_next_start();
     wait_for_previous();
     int count[NV];
     float gamma[NV][VEC], beta[NV][VEC];
     Stream<T, L, NV, 1, SHIFT> rows(ring);
-    const int64_t step = int64_t(gridDim.x) * S::kRows;
-    const int64_t start = int64_t(blockIdx.x) * S::kRows + group;
+    const int64_t step = int64_t(gridDim.x / CL) * S::kRows;
+    const int64_t start = int64_t(blockIdx.x / CL) * S::kRows + group;
 #pragma unroll
     for (int j = 0; j < NV; ++j) count[j] = cols - S::column(j);
-    auto at = [&](int64_t row) { return static_cast<const T *>(l.x) + row * l.ld_x + S::column(0); };
+    auto at = [&](int64_t row) { return static_cast<const T *>(l.x) + row * l.ld_x + from + S::column(0); };
 #pragma unroll
     for (int i = 0; i < rows.kAhead; ++i) {
         const T *const base[1] = {at(start + i * step)};
@@ -234,11 +273,11 @@ __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_nor
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             const int c = S::column(j) + i;
-            gamma[j][i] = l.gamma && c < cols ? load_any(l.gamma, l.weight_type, c) : 1.0f;
-            beta[j][i] = l.beta && c < cols ? load_any(l.beta, l.weight_type, c) : 0.0f;
+            gamma[j][i] = l.gamma && c < cols ? load_any(l.gamma, l.weight_type, from + c) : 1.0f;
+            beta[j][i] = l.beta && c < cols ? load_any(l.beta, l.weight_type, from + c) : 0.0f;
         }
-    const float over = 1.0f / float(cols);
-    const int64_t turns = (l.rows - int64_t(blockIdx.x) * S::kRows + step - 1) / step;       // the same for all rows of the block
+    const float over = 1.0f / float(l.cols);
+    const int64_t turns = (l.rows - int64_t(blockIdx.x / CL) * S::kRows + step - 1) / step;       // the same for all rows of the block
     int64_t row = start;
     for (int64_t turn = 0; turn < turns; ++turn, row += step) {
         const T *const ahead[1] = {at(row + rows.kAhead * step)};
@@ -252,7 +291,7 @@ __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_nor
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < VEC; i += 2) sums = add2(sums, Pair(v[j][i], v[j][i + 1]));
-        const float mean = row_sums<L>(sums.sum(), 0.0f, slots[0]).x * over;
+        const float mean = row_sums<L, CL>(sums.sum(), 0.0f, slots[0], meet[0], rank).x * over;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
 #pragma unroll
@@ -268,7 +307,7 @@ __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_nor
                 squares = fma2(d, d, squares);
             }
         }
-        const float2 both = row_sums<L>(rests.sum(), squares.sum(), slots[1]);
+        const float2 both = row_sums<L, CL>(rests.sum(), squares.sum(), slots[1], meet[1], rank);
         const float rest = both.x * over;
         float var = both.y * over - rest * rest;
         if (var < 0.0f) var = 0.0f;                         // by rounding alone; NaN stays
@@ -282,12 +321,13 @@ __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_nor
                 fma2(fma2(Pair(v[j][i], v[j][i + 1]), Pair(rstd, rstd), Pair(less, less)), Pair(gamma[j][i], gamma[j][i + 1]),
                      Pair(beta[j][i], beta[j][i + 1]))
                     .get(v[j][i], v[j][i + 1]);
-        rows.store(static_cast<T *>(l.y) + row * l.ld_y + S::column(0), in, count, v);
-        if (t == 0 && in) {
+        rows.store(static_cast<T *>(l.y) + row * l.ld_y + from + S::column(0), in, count, v);
+        if (t == 0 && in && rank == 0) {
             if (l.mean) l.mean[row] = mean + rest;
             if (l.rstd) l.rstd[row] = rstd;
         }
     }
+    if constexpr (CL > 1) cluster_sync();                   // the others write into this block's shared memory
 }
 
 // Eight neighbours at any alignment from global memory; what is not wanted reads as zero.
@@ -382,25 +422,27 @@ __global__ void __launch_bounds__(kLong) redist_layer_norm_long_kernel(const Lay
 
 // With c = dy gamma and xh = (x - mean) rstd: dx = rstd (c - mean(c) - xh mean(c xh)).  A block walks over its rows
 // and keeps the column sums of dy xh and dy in registers; partials holds them per block, gamma's before beta's.
-template <typename T, int L, int NV, bool SHIFT>
+template <typename T, int L, int NV, bool SHIFT, int CL>
 __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_norm_grad_kernel(const LayerNorm l, float *partials)
 {
     using S = RowShape<T, L, NV>;
     constexpr int VEC = S::VEC;
-    __shared__ float2 slots[2][32];
+    __shared__ float2 slots[2][32], meet[2][CL];
     extern __shared__ __align__(16) uint8_t ring[];
-    const int t = int(threadIdx.x) % L, group = int(threadIdx.x) / L, cols = int(l.cols);
+    const uint32_t rank = CL > 1 ? cluster_rank() : 0;
+    const int from = int(rank) * L * NV * VEC;              // this block's first column
+    const int t = int(threadIdx.x) % L, group = int(threadIdx.x) / L, cols = int(l.cols) - from;
     let_next_start();
     wait_for_previous();
     int count[NV];
     float gamma[NV][VEC], dgamma[NV][VEC], dbeta[NV][VEC];
     Stream<T, L, NV, 2, SHIFT> rows(ring);
-    const int64_t step = int64_t(gridDim.x) * S::kRows;
-    const int64_t start = int64_t(blockIdx.x) * S::kRows + group;
+    const int64_t step = int64_t(gridDim.x / CL) * S::kRows;
+    const int64_t start = int64_t(blockIdx.x / CL) * S::kRows + group;
 #pragma unroll
     for (int j = 0; j < NV; ++j) count[j] = cols - S::column(j);
-    auto at_x = [&](int64_t row) { return static_cast<const T *>(l.x) + row * l.ld_x + S::column(0); };
-    auto at_dy = [&](int64_t row) { return static_cast<const T *>(l.dy) + row * l.ld_dy + S::column(0); };
+    auto at_x = [&](int64_t row) { return static_cast<const T *>(l.x) + row * l.ld_x + from + S::column(0); };
+    auto at_dy = [&](int64_t row) { return static_cast<const T *>(l.dy) + row * l.ld_dy + from + S::column(0); };
 #pragma unroll
     for (int i = 0; i < rows.kAhead; ++i) {
         const T *const base[2] = {at_x(start + i * step), at_dy(start + i * step)};
@@ -411,11 +453,11 @@ __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_nor
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             const int c = S::column(j) + i;
-            gamma[j][i] = l.gamma && c < cols ? load_any(l.gamma, l.weight_type, c) : 1.0f;
+            gamma[j][i] = l.gamma && c < cols ? load_any(l.gamma, l.weight_type, from + c) : 1.0f;
             dgamma[j][i] = dbeta[j][i] = 0.0f;
         }
-    const float over = 1.0f / float(cols);
-    const int64_t turns = (l.rows - int64_t(blockIdx.x) * S::kRows + step - 1) / step;
+    const float over = 1.0f / float(l.cols);
+    const int64_t turns = (l.rows - int64_t(blockIdx.x / CL) * S::kRows + step - 1) / step;
     int64_t row = start;
     float next_mean = row < l.rows ? l.mean[row] : 0.0f, next_rstd = row < l.rows ? l.rstd[row] : 0.0f;
     for (int64_t turn = 0; turn < turns; ++turn, row += step) {
@@ -453,7 +495,7 @@ __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_nor
                 c.get(c1[j][i], c1[j][i + 1]);
             }
         }
-        const float2 sums = row_sums<L>(s1.sum(), s2.sum(), slots[turn & 1]);
+        const float2 sums = row_sums<L, CL>(s1.sum(), s2.sum(), slots[turn & 1], meet[turn & 1], rank);
         const float m1 = -sums.x * over, m2 = -sums.y * over;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
@@ -461,10 +503,11 @@ __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_nor
             for (int i = 0; i < VEC; i += 2)
                 mul2(add2(fma2(Pair(xh[j][i], xh[j][i + 1]), Pair(m2, m2), Pair(c1[j][i], c1[j][i + 1])), Pair(m1, m1)), Pair(by, by))
                     .get(c1[j][i], c1[j][i + 1]);
-        rows.store(static_cast<T *>(l.dx) + row * l.ld_dx + S::column(0), in, count, c1);
+        rows.store(static_cast<T *>(l.dx) + row * l.ld_dx + from + S::column(0), in, count, c1);
     }
+    if constexpr (CL > 1) cluster_sync();
     if (!partials) return;
-    float *out = partials + int64_t(blockIdx.x) * 2 * l.cols;
+    float *out = partials + int64_t(blockIdx.x / CL) * 2 * l.cols + from;
     if constexpr (S::kRows > 1) {
         // the block's groups hold sums of the same columns: added in the order of the groups
         asm volatile("cp.async.wait_all;" ::: "memory");
@@ -711,27 +754,61 @@ __device__ __forceinline__ double block_sum(double v, double *slots)
 }
 
 // Squares are summed in 64 bits: their range (2^-298 to 2^256) does not fit into 32, and the kernel stays bound by memory.
-template <typename T>
+// Warps take rows (or pieces of 1024 columns of them) in turn, four loads under way per lane.
+template <typename T, bool ALIGNED, typename F> __device__ __forceinline__ void along_rows(const Scaled &s, F f)
+{
+    constexpr int kRaw = int(sizeof(T)) / 2;                // 16-byte blocks in eight neighbours
+    const T *x = static_cast<const T *>(s.x) + int64_t(blockIdx.y) * s.x_batch;
+    const int lane = threadIdx.x & 31, cols = int(s.cols), per_row = (cols + 1023) / 1024;
+    const int64_t warps = int64_t(gridDim.x) * 8, all = s.rows * per_row;
+    for (int64_t q = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5); q < all; q += warps) {
+        const int64_t row = per_row == 1 ? q : q / per_row;
+        const int c0 = int(q - row * per_row) * 1024 + lane * 8;
+        const T *p = x + row * s.ld_x + c0;
+        if (ALIGNED && c0 + 776 <= cols) {                  // all four pieces are whole
+            uint4 u[4][kRaw];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < kRaw; ++i) u[k][i] = __ldg(reinterpret_cast<const uint4 *>(p + k * 256) + i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < kRaw; ++i) unpack16<T>(u[k][i], v + i * kVec<T>);
+                f(row, c0 + k * 256, v);
+            }
+        } else {
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
+                if (c0 + k * 256 >= cols) break;
+                float v[8];
+                load8<T>(p + k * 256, min(cols - c0 - k * 256, 8), v);
+                f(row, c0 + k * 256, v);
+            }
+        }
+    }
+}
+
+template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(256) redist_norm_parts_kernel(const Scaled s)
 {
     __shared__ double slots[8];
     let_next_start();
     wait_for_previous();
-    const T *x = static_cast<const T *>(s.x) + int64_t(blockIdx.y) * s.x_batch;
-    const int64_t per_row = (s.cols + 7) / 8, all = s.rows * per_row, step = int64_t(gridDim.x) * 256;
-    double sum = 0.0;
-    for (int64_t q = int64_t(blockIdx.x) * 256 + threadIdx.x; q < all; q += step) {
-        const int64_t row = q / per_row, c = (q - row * per_row) * 8;
-        float v[8];
-        load8<T>(x + row * s.ld_x + c, int(min(s.cols - c, int64_t(8))), v);
+    double sum = 0.0, more = 0.0;
+    along_rows<T, ALIGNED>(s, [&](int64_t, int, const float (&v)[8]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fma(double(v[i]), double(v[i]), sum);
-    }
-    sum = block_sum(sum, slots);
+        for (int i = 0; i < 8; i += 2) {
+            sum = fma(double(v[i]), double(v[i]), sum);
+            more = fma(double(v[i + 1]), double(v[i + 1]), more);
+        }
+    });
+    sum = block_sum(sum + more, slots);
     if (threadIdx.x == 0) s.partials[int64_t(blockIdx.y) * kNormParts + blockIdx.x] = sum;
 }
 
-template <typename T>
+template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(256) redist_scaled_kernel(const Scaled s, int parts)
 {
     __shared__ double slots[8];
@@ -743,25 +820,20 @@ __global__ void __launch_bounds__(256) redist_scaled_kernel(const Scaled s, int 
     const bool finite = norm - norm == 0.0;
     const float power = finite ? ldexpf(1.0f, 14 - exponent) : __int_as_float(0x7fffffff);
     if (blockIdx.x == 0 && threadIdx.x == 0) s.scale[blockIdx.y] = finite ? float(1.0 / ldexp(fraction, 14)) : 1.0f;
-    const T *x = static_cast<const T *>(s.x) + int64_t(blockIdx.y) * s.x_batch;
     __half *hi = static_cast<__half *>(s.hi) + int64_t(blockIdx.y) * s.plane, *lo = s.lo ? static_cast<__half *>(s.lo) + int64_t(blockIdx.y) * s.plane : nullptr;
-    const int64_t per_row = (s.cols + 7) / 8, all = s.rows * per_row, step = int64_t(gridDim.x) * 256;
-    for (int64_t q = int64_t(blockIdx.x) * 256 + threadIdx.x; q < all; q += step) {
-        const int64_t row = q / per_row, c = (q - row * per_row) * 8;
-        float v[8], h[8];
-        load8<T>(x + row * s.ld_x + c, int(min(s.cols - c, int64_t(8))), v);
+    along_rows<T, ALIGNED>(s, [&](int64_t row, int c, float (&v)[8]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= power;
-        const uint4 u = make_uint4(pack2<__half>(v[0], v[1]), pack2<__half>(v[2], v[3]), pack2<__half>(v[4], v[5]), pack2<__half>(v[6], v[7]));
+        const uint4 u = pack16<__half>(v);
         *reinterpret_cast<uint4 *>(hi + row * s.ld + c) = u;
         if (lo) {
+            float h[8];
             unpack16<__half>(u, h);
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[i] = (v[i] - h[i]) * 2048.0f;
-            *reinterpret_cast<uint4 *>(lo + row * s.ld + c) =
-                make_uint4(pack2<__half>(h[0], h[1]), pack2<__half>(h[2], h[3]), pack2<__half>(h[4], h[5]), pack2<__half>(h[6], h[7]));
+            *reinterpret_cast<uint4 *>(lo + row * s.ld + c) = pack16<__half>(h);
         }
-    }
+    });
 }
 
 // ---- joining the parts of a split product --------------------------------------------------------------------
@@ -818,7 +890,7 @@ __global__ void __launch_bounds__(256) redist_join_kernel(const Epilogue e, cons
 // ---- host ---------------------------------------------------------------------------------------------------
 
 template <typename... P, typename... A>
-cudaError_t launch_with(int smem, void (*kernel)(P...), dim3 grid, int block, const LaunchOptions &o, cudaStream_t stream, A... args)
+cudaError_t launch_with(int smem, int cluster, void (*kernel)(P...), dim3 grid, int block, const LaunchOptions &o, cudaStream_t stream, A... args)
 {
     cudaLaunchConfig_t cfg = {};
     if (smem > 48 * 1024) {
@@ -829,18 +901,29 @@ cudaError_t launch_with(int smem, void (*kernel)(P...), dim3 grid, int block, co
     cfg.gridDim = grid;
     cfg.blockDim = dim3(unsigned(block));
     cfg.stream = stream;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute at[2];
+    int n_at = 0;
+    if (o.pdl) {
+        at[n_at].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[n_at].val.programmaticStreamSerializationAllowed = 1;
+        ++n_at;
+    }
+    if (cluster > 1) {
+        at[n_at].id = cudaLaunchAttributeClusterDimension;
+        at[n_at].val.clusterDim.x = unsigned(cluster);
+        at[n_at].val.clusterDim.y = 1;
+        at[n_at].val.clusterDim.z = 1;
+        ++n_at;
+    }
     cfg.attrs = at;
-    cfg.numAttrs = o.pdl ? 1 : 0;
+    cfg.numAttrs = unsigned(n_at);
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
 template <typename... P, typename... A>
 cudaError_t launch(void (*kernel)(P...), dim3 grid, int block, const LaunchOptions &o, cudaStream_t stream, A... args)
 {
-    return launch_with(0, kernel, grid, block, o, stream, args...);
+    return launch_with(0, 1, kernel, grid, block, o, stream, args...);
 }
 
 cudaError_t sm_count(int *sms)
@@ -852,25 +935,29 @@ cudaError_t sm_count(int *sms)
 bool on_16(const void *p, int64_t ld, int64_t element) { return p == nullptr || (uintptr_t(p) % 16 == 0 && ld * element % 16 == 0); }
 
 // Threads per row and pieces per thread by the row's length: up to 16 neighbours per thread (more would cost the registers
-// that hold gamma and beta), within that the fewest threads; rows of fewer than 32 pieces share warps.
+// that hold gamma and beta), within that the fewest threads; rows of fewer than 32 pieces share warps, rows of more than a
+// block's 8192 (16-bit) or 4096 (32-bit) columns are shared by a cluster.
 template <typename T, typename F> bool by_pieces(int64_t pieces, F f)
 {
     using std::integral_constant;
     constexpr int MOST = 16 / kVec<T>;
-#define TAKE(THREADS, NV)                                                                       \
-    if (pieces <= THREADS * NV) {                                                               \
-        f(integral_constant<int, THREADS>(), integral_constant<int, NV>());                     \
+#define TAKE(THREADS, NV, CL)                                                                   \
+    if (pieces <= THREADS * NV * CL) {                                                          \
+        f(integral_constant<int, THREADS>(), integral_constant<int, NV>(), integral_constant<int, CL>()); \
         return true;                                                                            \
     }
-    TAKE(8, 1)
-    TAKE(16, 1)
-    TAKE(32, 1)
-    TAKE(32, 2)
-    TAKE(32, MOST)
-    TAKE(64, MOST)
-    TAKE(128, MOST)
-    TAKE(256, MOST)
-    TAKE(512, MOST)
+    TAKE(8, 1, 1)
+    TAKE(16, 1, 1)
+    TAKE(32, 1, 1)
+    TAKE(32, 2, 1)
+    TAKE(32, MOST, 1)
+    TAKE(64, MOST, 1)
+    TAKE(128, MOST, 1)
+    TAKE(256, MOST, 1)
+    TAKE(512, MOST, 1)
+    TAKE(512, MOST, 2)
+    TAKE(512, MOST, 4)
+    TAKE(512, MOST, 8)
 #undef TAKE
     return false;
 }
@@ -884,11 +971,12 @@ unsigned row_blocks(const LayerNorm &l, int rows_per_block, int threads, int sme
 template <typename T, bool SHIFT> cudaError_t forward_as(const LayerNorm &l, int sms, const LaunchOptions &o, cudaStream_t stream)
 {
     cudaError_t ce = cudaSuccess;
-    const bool held = by_pieces<T>((l.cols + kVec<T> - 1) / kVec<T>, [&](auto threads, auto pieces) {
-        constexpr int L = decltype(threads)::value, NV = decltype(pieces)::value;
+    const bool held = by_pieces<T>((l.cols + kVec<T> - 1) / kVec<T>, [&](auto threads, auto pieces, auto cluster) {
+        constexpr int L = decltype(threads)::value, NV = decltype(pieces)::value, CL = decltype(cluster)::value;
         using S = RowShape<T, L, NV>;
         constexpr int smem = Stream<T, L, NV, 1, SHIFT>::kSmem;
-        ce = launch_with(smem, redist_layer_norm_kernel<T, L, NV, SHIFT>, dim3(row_blocks(l, S::kRows, S::kThreads, smem, NV == 1 ? 56 : 80, sms)), S::kThreads, o, stream, l);
+        ce = launch_with(smem, CL, redist_layer_norm_kernel<T, L, NV, SHIFT, CL>, dim3(row_blocks(l, S::kRows, S::kThreads, smem, L >= 512 ? 64 : NV == 1 ? 56 : 80, sms / CL) * CL),
+                         S::kThreads, o, stream, l);
     });
     if (held) return ce;
     return launch(redist_layer_norm_long_kernel<T>, dim3(unsigned(std::min<int64_t>(l.rows, sms * 4))), kLong, o, stream, l);
@@ -903,12 +991,12 @@ cudaError_t backward_as(const LayerNorm &l, float *partials, int sms, const Laun
 {
     int parts = 0;
     cudaError_t ce = cudaSuccess;
-    const bool held = by_pieces<T>((l.cols + kVec<T> - 1) / kVec<T>, [&](auto threads, auto pieces) {
-        constexpr int L = decltype(threads)::value, NV = decltype(pieces)::value;
+    const bool held = by_pieces<T>((l.cols + kVec<T> - 1) / kVec<T>, [&](auto threads, auto pieces, auto cluster) {
+        constexpr int L = decltype(threads)::value, NV = decltype(pieces)::value, CL = decltype(cluster)::value;
         using S = RowShape<T, L, NV>;
         constexpr int smem = Stream<T, L, NV, 2, SHIFT>::kSmem;
-        parts = int(std::min<unsigned>(row_blocks(l, S::kRows, S::kThreads, smem, 128, sms), unsigned(sms * kGradPerSm)));
-        ce = launch_with(smem, redist_layer_norm_grad_kernel<T, L, NV, SHIFT>, dim3(unsigned(parts)), S::kThreads, o, stream, l, partials);
+        parts = int(std::min<unsigned>(row_blocks(l, S::kRows, S::kThreads, smem, 128, sms / CL), unsigned(sms * kGradPerSm)));
+        ce = launch_with(smem, CL, redist_layer_norm_grad_kernel<T, L, NV, SHIFT, CL>, dim3(unsigned(parts * CL)), S::kThreads, o, stream, l, partials);
     });
     if (!held) {
         ce = launch(redist_layer_norm_grad_long_kernel<T>, dim3(unsigned(std::min<int64_t>(l.rows, sms * 4))), kLong, o, stream, l);
@@ -1011,14 +1099,16 @@ cudaError_t launch_join(const Product &p, const float *parts, int64_t ld, int sp
 
 cudaError_t launch_scaled(const Scaled &s, const LaunchOptions &o, cudaStream_t stream)
 {
-    const int64_t pieces = s.rows * ((s.cols + 7) / 8);
-    const int parts = int(std::min<int64_t>(kNormParts, (pieces + 1023) / 1024));
-    const int blocks = int(std::min<int64_t>(1024, (pieces + 511) / 512));
+    const int64_t turns = s.rows * ((s.cols + 1023) / 1024);               // of a warp
+    const int parts = int(std::min<int64_t>(kNormParts, (turns + 7) / 8));
+    const int blocks = int(std::min<int64_t>(1024, (turns + 7) / 8));
     return by_type(s.type, [&](auto t) {
         using T = decltype(t);
-        cudaError_t ce = launch(redist_norm_parts_kernel<T>, dim3(unsigned(parts), unsigned(s.batch)), 256, o, stream, s);
+        const bool aligned = on_16(s.x, s.ld_x, sizeof(T)) && s.x_batch * int64_t(sizeof(T)) % 16 == 0;
+        const dim3 first{unsigned(parts), unsigned(s.batch)}, second{unsigned(blocks), unsigned(s.batch)};
+        cudaError_t ce = aligned ? launch(redist_norm_parts_kernel<T, true>, first, 256, o, stream, s) : launch(redist_norm_parts_kernel<T, false>, first, 256, o, stream, s);
         if (ce != cudaSuccess) return ce;
-        return launch(redist_scaled_kernel<T>, dim3(unsigned(blocks), unsigned(s.batch)), 256, o, stream, s, parts);
+        return aligned ? launch(redist_scaled_kernel<T, true>, second, 256, o, stream, s, parts) : launch(redist_scaled_kernel<T, false>, second, 256, o, stream, s, parts);
     });
 }
 
