@@ -180,6 +180,12 @@ template <typename T, int L, int NV, int TENSORS, bool SHIFT> struct Stream {
 
 // Sums over the L threads that share a row; every thread gets them.  L > 32: `slot` has two entries per warp of the block
 // and may be written again after one more barrier of the row's threads.
+template <int L> __device__ __forceinline__ void row_barrier()
+{
+    if constexpr (L < 256) asm volatile("bar.sync %0, %1;" ::"r"(1 + (int(threadIdx.x) >> 5) / (L / 32)), "n"(L) : "memory");
+    else __syncthreads();
+}
+
 template <int L> __device__ __forceinline__ float2 row_sums(float a, float b, float2 *slot)
 {
 #pragma unroll
@@ -190,16 +196,36 @@ template <int L> __device__ __forceinline__ float2 row_sums(float a, float b, fl
     if constexpr (L > 32) {
         const int warp = int(threadIdx.x) >> 5, first = warp & ~(L / 32 - 1);
         if ((threadIdx.x & 31) == 0) slot[warp] = make_float2(a, b);
-        if constexpr (L < 256) asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / (L / 32)), "n"(L) : "memory");
-        else __syncthreads();
-        a = b = 0.0f;
+        row_barrier<L>();
+        Pair sum(0.0f, 0.0f);
 #pragma unroll
-        for (int i = 0; i < L / 32; ++i) {
-            a += slot[first + i].x;
-            b += slot[first + i].y;
+        for (int i = 0; i < L / 32; i += 2) {
+            const float4 two = *reinterpret_cast<const float4 *>(slot + first + i);
+            sum = add2(add2(sum, Pair(two.x, two.y)), Pair(two.z, two.w));
         }
+        sum.get(a, b);
     }
     return make_float2(a, b);
+}
+
+// One sum only.
+template <int L> __device__ __forceinline__ float row_sum(float a, float2 *slot)
+{
+#pragma unroll
+    for (int d = (L < 32 ? L : 32) / 2; d; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
+    if constexpr (L > 32) {
+        float *one = reinterpret_cast<float *>(slot);
+        const int warp = int(threadIdx.x) >> 5, first = warp & ~(L / 32 - 1);
+        if ((threadIdx.x & 31) == 0) one[warp] = a;
+        row_barrier<L>();
+        a = 0.0f;
+#pragma unroll
+        for (int i = 0; i < L / 32; i += 2) {
+            const float2 two = *reinterpret_cast<const float2 *>(one + first + i);
+            a += two.x + two.y;
+        }
+    }
+    return a;
 }
 
 // Rows too long for a block are shared by a cluster of CL blocks, each with its own columns: the blocks' sums meet in every
@@ -248,7 +274,7 @@ __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads, L >= 512 ? 2 : 3
 {
     using S = RowShape<T, L, NV>;
     constexpr int VEC = S::VEC;
-    __shared__ float2 slots[2][32], meet[2][CL];
+    __shared__ __align__(16) float2 slots[2][32], meet[2][CL];
     extern __shared__ __align__(16) uint8_t ring[];
     const uint32_t rank = CL > 1 ? cluster_rank() : 0;
     const int from = int(rank) * L * NV * VEC;              // this block's first column
@@ -291,7 +317,7 @@ __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads, L >= 512 ? 2 : 3
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < VEC; i += 2) sums = add2(sums, Pair(v[j][i], v[j][i + 1]));
-        const float mean = row_sums<L, CL>(sums.sum(), 0.0f, slots[0], meet[0], rank).x * over;
+        const float mean = (CL == 1 ? row_sum<L>(sums.sum(), slots[0]) : row_sums<L, CL>(sums.sum(), 0.0f, slots[0], meet[0], rank).x) * over;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
 #pragma unroll
@@ -365,7 +391,7 @@ constexpr int kLong = 512;
 template <typename T>
 __global__ void __launch_bounds__(kLong) redist_layer_norm_long_kernel(const LayerNorm l)
 {
-    __shared__ float2 slots[2][32];
+    __shared__ __align__(16) float2 slots[2][32];
     let_next_start();
     wait_for_previous();
     const float over = 1.0f / float(l.cols);
@@ -379,7 +405,7 @@ __global__ void __launch_bounds__(kLong) redist_layer_norm_long_kernel(const Lay
             load8<T>(x + c, int(min(l.cols - c, int64_t(8))), v);
             sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         }
-        const float mean = row_sums<kLong>(sum, 0.0f, slots[0]).x * over;
+        const float mean = row_sum<kLong>(sum, slots[0]) * over;
 #pragma unroll 2
         for (int64_t c = int64_t(threadIdx.x) * 8; c < l.cols; c += kLong * 8) {
             float v[8];
@@ -423,11 +449,11 @@ __global__ void __launch_bounds__(kLong) redist_layer_norm_long_kernel(const Lay
 // With c = dy gamma and xh = (x - mean) rstd: dx = rstd (c - mean(c) - xh mean(c xh)).  A block walks over its rows
 // and keeps the column sums of dy xh and dy in registers; partials holds them per block, gamma's before beta's.
 template <typename T, int L, int NV, bool SHIFT, int CL>
-__global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_norm_grad_kernel(const LayerNorm l, float *partials)
+__global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads, L <= 32 && NV == 1 ? 4 : L <= 256 ? 2 : 1) redist_layer_norm_grad_kernel(const LayerNorm l, float *partials)
 {
     using S = RowShape<T, L, NV>;
     constexpr int VEC = S::VEC;
-    __shared__ float2 slots[2][32], meet[2][CL];
+    __shared__ __align__(16) float2 slots[2][32], meet[2][CL];
     extern __shared__ __align__(16) uint8_t ring[];
     const uint32_t rank = CL > 1 ? cluster_rank() : 0;
     const int from = int(rank) * L * NV * VEC;              // this block's first column
@@ -548,7 +574,7 @@ __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads) redist_layer_nor
 template <typename T>
 __global__ void __launch_bounds__(kLong) redist_layer_norm_grad_long_kernel(const LayerNorm l)
 {
-    __shared__ float2 slots[2][32];
+    __shared__ __align__(16) float2 slots[2][32];
     let_next_start();
     wait_for_previous();
     const float over = 1.0f / float(l.cols);
@@ -982,9 +1008,10 @@ template <typename T, bool SHIFT> cudaError_t forward_as(const LayerNorm &l, int
     return launch(redist_layer_norm_long_kernel<T>, dim3(unsigned(std::min<int64_t>(l.rows, sms * 4))), kLong, o, stream, l);
 }
 
-// Blocks of the backward pass per SM at most, and slices of the rows for long rows' column sums: what the parts of the
+// Slices of the rows for long rows' column sums, and blocks of the backward pass per SM at most: what the parts of the
 // column sums need of scratch follows from these.
-constexpr int kGradPerSm = 2, kLongParts = 64;
+constexpr int kLongParts = 64;
+constexpr int grad_per_sm(int64_t pieces) { return pieces <= 32 ? 4 : 2; }       // by the registers that hold the sums
 
 template <typename T, bool SHIFT>
 cudaError_t backward_as(const LayerNorm &l, float *partials, int sms, const LaunchOptions &o, cudaStream_t stream)
@@ -995,7 +1022,8 @@ cudaError_t backward_as(const LayerNorm &l, float *partials, int sms, const Laun
         constexpr int L = decltype(threads)::value, NV = decltype(pieces)::value, CL = decltype(cluster)::value;
         using S = RowShape<T, L, NV>;
         constexpr int smem = Stream<T, L, NV, 2, SHIFT>::kSmem;
-        parts = int(std::min<unsigned>(row_blocks(l, S::kRows, S::kThreads, smem, 128, sms / CL), unsigned(sms * kGradPerSm)));
+        parts = int(std::min<unsigned>(row_blocks(l, S::kRows, S::kThreads, smem, L <= 32 && NV == 1 ? 64 : 128, sms / CL),
+                                       unsigned(sms * grad_per_sm((l.cols + kVec<T> - 1) / kVec<T>))));
         ce = launch_with(smem, CL, redist_layer_norm_grad_kernel<T, L, NV, SHIFT, CL>, dim3(unsigned(parts * CL)), S::kThreads, o, stream, l, partials);
     });
     if (!held) {
@@ -1018,9 +1046,10 @@ template <typename F> cudaError_t by_type(int type, F f)
 
 }  // namespace
 
-size_t layer_norm_backward_bytes(int64_t rows, int64_t cols, int, int sms)
+size_t layer_norm_backward_bytes(int64_t rows, int64_t cols, int type, int sms)
 {
-    const int64_t parts = std::min<int64_t>(rows, std::max(int64_t(sms) * kGradPerSm, int64_t(kLongParts)));
+    const int64_t vec = 16 / type_bytes(type);
+    const int64_t parts = std::min<int64_t>(rows, std::max(int64_t(sms) * grad_per_sm((cols + vec - 1) / vec), int64_t(kLongParts)));
     return size_t(parts * 2 * cols * 4);
 }
 
