@@ -657,10 +657,13 @@ __global__ void __launch_bounds__(256) redist_layer_norm_columns_kernel(const La
 }
 
 // out[c] = sum over the parts of partials[part][c], in the same order every time.
-__global__ void __launch_bounds__(256) redist_column_sum_kernel(const float *partials, int parts, int64_t stride, int64_t cols,
-                                                               float *first, float *second)
+// A warp per 32nd of the parts: the loads of one thread are few and independent.
+constexpr int kSumThreads = 1024;
+
+__global__ void __launch_bounds__(kSumThreads) redist_column_sum_kernel(const float *partials, int parts, int64_t stride, int64_t cols,
+                                                                       float *first, float *second)
 {
-    __shared__ float all[8][33];
+    __shared__ float all[kSumThreads / 32][33];
     let_next_start();
     wait_for_previous();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
@@ -669,15 +672,15 @@ __global__ void __launch_bounds__(256) redist_column_sum_kernel(const float *par
     float *out = blockIdx.y ? second : first;
     float s = 0.0f;
     if (out && c < cols)
-        for (int q = w; q < parts; q += 8) s += p[q * stride + c];
+#pragma unroll 8
+        for (int q = w; q < parts; q += kSumThreads / 32) s += __ldg(p + q * stride + c);
     all[w][lane] = s;
     __syncthreads();
-    if (w == 0 && out && c < cols) {
-        s = 0.0f;
+    // the warps' sums of column `w` of the block
+    s = all[lane][w];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s += all[i][lane];
-        out[c] = s;
-    }
+    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    if (lane == 0 && out && int64_t(blockIdx.x) * 32 + w < cols) out[int64_t(blockIdx.x) * 32 + w] = s;
 }
 
 // ---- operands of a product -------------------------------------------------------------------------------
@@ -1033,7 +1036,7 @@ cudaError_t backward_as(const LayerNorm &l, float *partials, int sms, const Laun
         ce = launch(redist_layer_norm_columns_kernel<T>, dim3(unsigned((l.cols + 255) / 256), unsigned(parts)), 256, o, stream, l, partials);
     }
     if (ce != cudaSuccess || !partials) return ce;
-    return launch(redist_column_sum_kernel, dim3(unsigned((l.cols + 31) / 32), 2), 256, o, stream, static_cast<const float *>(partials), parts,
+    return launch(redist_column_sum_kernel, dim3(unsigned((l.cols + 31) / 32), 2), kSumThreads, o, stream, static_cast<const float *>(partials), parts,
                   int64_t(2) * l.cols, l.cols, l.dgamma, l.dbeta);
 }
 
@@ -1113,7 +1116,7 @@ cudaError_t launch_lay(const Lay *l, int count, const LaunchOptions &o, cudaStre
     for (int i = 0; i < count && ce == cudaSuccess; ++i)
         if (l[i].sums) {
             const int64_t per = lays.rows_per_block[i];
-            ce = launch(redist_column_sum_kernel, dim3(unsigned((l[i].cols + 31) / 32), 1), 256, o, stream, static_cast<const float *>(l[i].partials),
+            ce = launch(redist_column_sum_kernel, dim3(unsigned((l[i].cols + 31) / 32), 1), kSumThreads, o, stream, static_cast<const float *>(l[i].partials),
                         int((l[i].rows + per - 1) / per), l[i].cols, l[i].cols, l[i].sums, static_cast<float *>(nullptr));
         }
     return ce;
