@@ -88,31 +88,45 @@ __device__ __forceinline__ float load_any(const void *p, int type, int64_t i)
     return to_float(static_cast<const __half *>(p)[i]);
 }
 
-// 16 bytes that start at any multiple of the element size: the one or two aligned 16-byte blocks that hold them,
-// shifted together.  `bytes` of the 16 are wanted (1 to 16); a block that holds none of those is not touched, so
-// nothing is read outside the 16-byte blocks of the array's own bytes.
+// 16 bytes that start at any multiple of the element size: the one or two aligned 16-byte blocks that hold them, to be
+// shifted together.  `bytes` of the 16 are wanted (1 to 16); a block that holds none of those is not touched, so nothing is
+// read outside the 16-byte blocks of the array's own bytes.  Loading and shifting are two steps, so that several loads can be
+// under way before the first is looked at.
+struct Blocks {
+    uint4 a, b;
+    __device__ __forceinline__ void load(const void *p, int bytes)
+    {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        const uint32_t off = uint32_t(at & 15);
+        const uint4 *q = reinterpret_cast<const uint4 *>(at - off);
+        a = q[0];
+        b = make_uint4(0, 0, 0, 0);
+        if (int(off) + bytes > 16) b = q[1];
+    }
+    __device__ __forceinline__ uint4 get(const void *p) const
+    {
+        const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p) & 15);
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        const uint32_t word = off >> 2, bit = (off & 3) * 8;
+        uint32_t r[5];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            uint32_t v = w[i];
+            if (word == 1) v = w[i + 1];
+            if (word == 2) v = w[i + 2];
+            if (word == 3) v = i + 3 < 8 ? w[i + 3] : 0;
+            r[i] = v;
+        }
+        return make_uint4(__funnelshift_r(r[0], r[1], bit), __funnelshift_r(r[1], r[2], bit), __funnelshift_r(r[2], r[3], bit),
+                          __funnelshift_r(r[3], r[4], bit));
+    }
+};
+
 __device__ __forceinline__ uint4 load16_any(const void *p, int bytes)
 {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-    const uint32_t off = uint32_t(at & 15);
-    const uint4 *q = reinterpret_cast<const uint4 *>(at - off);
-    const uint4 a = *q;
-    if (off == 0) return a;
-    uint4 b = make_uint4(0, 0, 0, 0);
-    if (int(off) + bytes > 16) b = q[1];
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    const uint32_t word = off >> 2, bit = (off & 3) * 8;
-    uint32_t r[5];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {
-        uint32_t v = w[i];
-        if (word == 1) v = w[i + 1];
-        if (word == 2) v = w[i + 2];
-        if (word == 3) v = i + 3 < 8 ? w[i + 3] : 0;
-        r[i] = v;
-    }
-    return make_uint4(__funnelshift_r(r[0], r[1], bit), __funnelshift_r(r[1], r[2], bit),
-                      __funnelshift_r(r[2], r[3], bit), __funnelshift_r(r[3], r[4], bit));
+    Blocks v;
+    v.load(p, bytes);
+    return v.get(p);
 }
 
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

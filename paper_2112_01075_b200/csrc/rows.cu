@@ -716,44 +716,35 @@ __global__ void __launch_bounds__(256) redist_lay_kernel(const __grid_constant__
     if (lo >= l.rows || int64_t(blockIdx.x) * kLayCols >= l.cols) return;
     const int count = int(min(l.cols - c, int64_t(8)));
     float sums[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    // four rows' loads are under way at a time: one after the other they leave half of the memory's time unused
-    constexpr int kBatch = 4;
+    // One row at a time and many warps: two or four rows' loads under way per warp cost registers, thus warps, and were
+    // slower (4096 x 16384 with GELU: 80 us, with four 91; at odd strides 120 and 203).
     if (count > 0)
-        for (int64_t row = lo + w; row < hi; row += 8 * kBatch) {
-            uint4 u[kBatch], y[kBatch];
+        for (int64_t row = lo + w; row < hi; row += 8) {
             const T *src = static_cast<const T *>(l.src) + row * l.ld_src + c, *z = static_cast<const T *>(l.z) + row * l.ld_z + c;
+            uint4 u, y;
             if (ALIGNED && count >= 8) {
-#pragma unroll
-                for (int k = 0; k < kBatch; ++k)
-                    if (row + 8 * k < hi) {
-                        u[k] = *reinterpret_cast<const uint4 *>(src + 8 * k * l.ld_src);
-                        if (l.z) y[k] = *reinterpret_cast<const uint4 *>(z + 8 * k * l.ld_z);
-                    }
+                u = *reinterpret_cast<const uint4 *>(src);
+                if (l.z) y = *reinterpret_cast<const uint4 *>(z);
             } else {
-#pragma unroll
-                for (int k = 0; k < kBatch; ++k)
-                    if (row + 8 * k < hi) {
-                        u[k] = load16_any(src + 8 * k * l.ld_src, count * 2);
-                        if (l.z) y[k] = load16_any(z + 8 * k * l.ld_z, count * 2);
-                    }
+                Blocks a, b = {};
+                a.load(src, count * 2);
+                if (l.z) b.load(z, count * 2);
+                u = a.get(src);
+                y = b.get(z);
             }
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                if (row + 8 * k >= hi) break;
-                if (l.z || l.sums) {
-                    float v[8];
-                    unpack16<T>(u[k], v);
-                    if (l.z) {
-                        float at[8];
-                        unpack16<T>(y[k], at);
-                        times_slope8(v, at, l.activation);
-                        u[k] = pack16<T>(v);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) sums[i] += v[i];
+            if (l.z || l.sums) {
+                float v[8];
+                unpack16<T>(u, v);
+                if (l.z) {
+                    float at[8];
+                    unpack16<T>(y, at);
+                    times_slope8(v, at, l.activation);
+                    u = pack16<T>(v);
                 }
-                if (l.dst) *reinterpret_cast<uint4 *>(static_cast<T *>(l.dst) + (row + 8 * k) * l.ld_dst + c) = u[k];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sums[i] += v[i];
             }
+            if (l.dst) *reinterpret_cast<uint4 *>(static_cast<T *>(l.dst) + row * l.ld_dst + c) = u;
         }
     if (!l.sums) return;
 #pragma unroll
@@ -808,11 +799,25 @@ template <typename T, bool ALIGNED, typename F> __device__ __forceinline__ void 
                 f(row, c0 + k * 256, v);
             }
         } else {
-#pragma unroll 1
+            Blocks u[4][kRaw];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < kRaw; ++i) {
+                    const int left = cols - c0 - k * 256 - i * kVec<T>;
+                    if (left > 0) u[k][i].load(p + k * 256 + i * kVec<T>, min(left, kVec<T>) * int(sizeof(T)));
+                }
+#pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (c0 + k * 256 >= cols) break;
+                const int left = cols - c0 - k * 256;
+                if (left <= 0) break;
                 float v[8];
-                load8<T>(p + k * 256, min(cols - c0 - k * 256, 8), v);
+#pragma unroll
+                for (int i = 0; i < kRaw; ++i) unpack16<T>(u[k][i].get(p + k * 256 + i * kVec<T>), v + i * kVec<T>);
+                if (left < 8)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i >= left) v[i] = 0.0f;
                 f(row, c0 + k * 256, v);
             }
         }
