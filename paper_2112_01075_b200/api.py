@@ -618,8 +618,10 @@ class _Operators:
         self.torch, self.empty, self.strided = torch, torch.empty, torch.empty_strided
         self.codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
         self.u8, self.f32, self.bf16 = torch.uint8, torch.float32, torch.bfloat16
-        self.current_device = torch.cuda.current_device
-        self.raw_stream = torch._C._cuda_getCurrentRawStream if torch.cuda.is_available() else None
+        self.current_device = self.raw_stream = None
+        if torch.cuda.is_available():
+            torch.cuda.init()
+            self.current_device, self.raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
         vp, sz = ctypes.c_void_p, ctypes.c_size_t
         for name, blocks, scratch in (("linear_forward", 1, True), ("linear_backward", 2, True), ("layer_norm_forward", 1, False),
                                       ("layer_norm_backward", 2, True), ("orthogonalize", 1, True)):
@@ -633,11 +635,12 @@ class _Operators:
 
     def stream(self, device, given):
         """The stream a call on ``device`` runs on (an address)."""
-        if device.type != "cuda":
+        if device.type != "cuda" or self.current_device is None:
             raise RedistError(1, "CUDA tensors are required")
-        if device.index != self.current_device():
+        index = device.index
+        if index != self.current_device():
             raise RedistError(1, "tensors have to be on the current device")
-        return given.cuda_stream if given is not None else self.raw_stream(device.index)
+        return given.cuda_stream if given is not None else self.raw_stream(index)
 
     def matrix(self, rows, cols, dtype, device):
         """An uninitialised row-major matrix (half the time of torch.empty)."""
@@ -692,20 +695,25 @@ def _vector(o, t, length: int, device, what: str, dtype=None):
     """Address and type code of a contiguous vector."""
     if t is None:
         return 0, 0
-    if t.shape != (length,) or t.device != device or not t.is_contiguous():
+    if t.dim() != 1 or t.shape[0] != length or t.device != device or not t.is_contiguous():
         raise RedistError(1, f"{what} has to be a contiguous vector of {length} elements on {device}")
     if dtype is not None and t.dtype is not dtype:
         raise RedistError(1, f"{what} has to be of {dtype}")
-    return t.data_ptr(), _code(o, t, what)
+    code = o.codes.get(t.dtype)
+    return t.data_ptr(), code if code is not None else _code(o, t, what)
+
+
+_ACTIVATION_CODES = {name: code for code, name in enumerate(ACTIVATIONS)}
 
 
 def _activation(name: str) -> int:
-    if name not in ACTIVATIONS:
+    code = _ACTIVATION_CODES.get(name)
+    if code is None:
         raise RedistError(1, f"activation is one of {ACTIVATIONS}, not {name!r}")
-    return ACTIVATIONS.index(name)
+    return code
 
 
-def _matrices(**tensors) -> None:
+def _not_matrices(**tensors) -> None:
     for name, t in tensors.items():
         if t.dim() != 2:
             raise RedistError(1, f"{name} has to be a matrix, not of {t.dim()} dimensions")
@@ -725,7 +733,8 @@ def linear_forward(x, w, bias=None, residual=None, activation: str = "none", out
 
 def _linear_forward(x, w, bias, residual, activation, out, pre, scratch, stream):
     o = _ops or _operators()
-    _matrices(x=x, w=w)
+    if x.dim() != 2 or w.dim() != 2:
+        _not_matrices(x=x, w=w)
     rows, k = x.shape
     n = w.shape[0]
     device, dtype, shape = x.device, x.dtype, (rows, n)
@@ -758,7 +767,8 @@ def linear_backward(dy, x, w, pre=None, activation: str = "none", need=(True, Tr
 
 def _linear_backward(dy, x, w, pre, activation, need, dx, dw, dbias, scratch, stream):
     o = _ops or _operators()
-    _matrices(dy=dy, x=x, w=w)
+    if dy.dim() != 2 or x.dim() != 2 or w.dim() != 2:
+        _not_matrices(dy=dy, x=x, w=w)
     rows, n = dy.shape
     k = x.shape[1]
     device, dtype = dy.device, dy.dtype
@@ -799,7 +809,8 @@ def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, out=None, st
 
 def _layer_norm_forward(x, gamma, beta, eps, out, stream):
     o = _ops or _operators()
-    _matrices(x=x)
+    if x.dim() != 2:
+        _not_matrices(x=x)
     shape, dtype, device = x.shape, x.dtype, x.device
     rows, cols = shape
     at = o.stream(device, stream)
@@ -829,7 +840,8 @@ def layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, scratch=None, stream=
 
 def _layer_norm_backward(dy, x, gamma, mean, rstd, dx, scratch, stream):
     o = _ops or _operators()
-    _matrices(dy=dy)
+    if dy.dim() != 2:
+        _not_matrices(dy=dy)
     shape, dtype, device = dy.shape, dy.dtype, dy.device
     rows, cols = shape
     at = o.stream(device, stream)
