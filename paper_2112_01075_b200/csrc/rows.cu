@@ -39,14 +39,40 @@ template <typename T> __device__ __forceinline__ uint4 pack16(const float *v)
         return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
 }
 
-// 16 bytes of shared memory from any even address on.
-__device__ __forceinline__ uint4 read16_any(const uint8_t *p)
+// Bytes 4 WORD (+ 2 with `half`) ... of two consecutive 16-byte blocks, 16 of them.
+template <int WORD> __device__ __forceinline__ uint4 join16(const uint4 &a, const uint4 &b, bool half)
 {
-    const uint32_t half = uint32_t(reinterpret_cast<uintptr_t>(p) & 2);
-    const uint32_t *q = reinterpret_cast<const uint32_t *>(p - half);
-    const uint4 u = make_uint4(q[0], q[1], q[2], q[3]);
-    if (!half) return u;
-    return make_uint4(__funnelshift_r(u.x, u.y, 16), __funnelshift_r(u.y, u.z, 16), __funnelshift_r(u.z, u.w, 16), __funnelshift_r(u.w, q[4], 16));
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (!half) return make_uint4(w[WORD], w[WORD + 1], w[WORD + 2], w[WORD + 3]);
+    return make_uint4(__funnelshift_r(w[WORD], w[WORD + 1], 16), __funnelshift_r(w[WORD + 1], w[WORD + 2], 16),
+                      __funnelshift_r(w[WORD + 2], w[WORD + 3], 16), __funnelshift_r(w[WORD + 3], w[WORD + 4], 16));
+}
+
+// NV pieces of 16 bytes of shared memory, `pitch` bytes apart, each from byte `off` (even, below 16) on.  All threads of a
+// row have the same offset: the branches hardly ever diverge, and whole blocks are read, where single words would meet in
+// the same banks.
+template <int NV> __device__ __forceinline__ void read_any(const uint8_t *p, int pitch, uint32_t off, uint4 (&u)[NV])
+{
+    const bool half = off & 2;
+    auto all = [&](auto word) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const uint4 *q = reinterpret_cast<const uint4 *>(p + j * pitch);
+            u[j] = join16<decltype(word)::value>(q[0], q[1], half);
+        }
+    };
+    if (off == 0) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) u[j] = *reinterpret_cast<const uint4 *>(p + j * pitch);
+    } else if (off < 4) {
+        all(std::integral_constant<int, 0>());
+    } else if (off < 8) {
+        all(std::integral_constant<int, 1>());
+    } else if (off < 12) {
+        all(std::integral_constant<int, 2>());
+    } else {
+        all(std::integral_constant<int, 3>());
+    }
 }
 
 // L threads share a row; a thread holds NV pieces of 16 bytes of it.  The threads of a row that share a warp form a
@@ -73,7 +99,8 @@ template <typename T, int L, int NV, int TENSORS, bool SHIFT> struct Stream {
     static constexpr int kBlocks = S::kThreads / SEGMENT * (NV * SEGMENT + (SHIFT ? 1 : 0));     // of one row of one tensor
     // three rows ahead, or as many as leave room for two blocks per SM (one at least)
     static constexpr int kFit = 100 * 1024 / (TENSORS * kBlocks * 16), kSlots = kFit >= 4 ? 4 : kFit >= 3 ? 3 : 2, kAhead = kSlots - 1;
-    static constexpr int kSmem = kSlots * TENSORS * kBlocks * 16;
+    static constexpr int kPad = SHIFT ? 128 : 0;            // the block before the first is read, though not used
+    static constexpr int kSmem = kPad + kSlots * TENSORS * kBlocks * 16;
     uint8_t *mine;                  // this thread's first block in the first slot
     int put = 0, got = 0;
     bool last;
@@ -81,7 +108,7 @@ template <typename T, int L, int NV, int TENSORS, bool SHIFT> struct Stream {
     __device__ __forceinline__ Stream(uint8_t *smem)
     {
         const int segment = int(threadIdx.x) / SEGMENT, at = int(threadIdx.x) % SEGMENT;
-        mine = smem + (segment * (NV * SEGMENT + (SHIFT ? 1 : 0)) + at) * 16;
+        mine = smem + kPad + (segment * (NV * SEGMENT + (SHIFT ? 1 : 0)) + at) * 16;
         last = at == SEGMENT - 1;
     }
     __device__ __forceinline__ uint8_t *place(int slot, int tensor, int piece) const
@@ -116,17 +143,18 @@ template <typename T, int L, int NV, int TENSORS, bool SHIFT> struct Stream {
         asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
         if constexpr (SHIFT) __syncwarp();
 #pragma unroll
-        for (int i = 0; i < TENSORS; ++i)
+        for (int i = 0; i < TENSORS; ++i) {
+            uint4 u[NV];
+            read_any<NV>(place(got, i, 0), SEGMENT * 16, SHIFT ? uint32_t(reinterpret_cast<uintptr_t>(base[i]) & 15) : 0, u);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const uint8_t *at = place(got, i, j);
-                if constexpr (SHIFT) unpack16<T>(read16_any(at + (reinterpret_cast<uintptr_t>(base[i]) & 15)), v[i][j]);
-                else unpack16<T>(*reinterpret_cast<const uint4 *>(at), v[i][j]);
+                unpack16<T>(u[j], v[i][j]);
                 if (count[j] < VEC)
 #pragma unroll
                     for (int q = 0; q < VEC; ++q)
                         if (q >= count[j]) v[i][j][q] = 0.0f;
             }
+        }
         if constexpr (SHIFT) __syncwarp();                  // the slot may be written again
         got = got + 1 == kSlots ? 0 : got + 1;
     }
@@ -138,10 +166,13 @@ template <typename T, int L, int NV, int TENSORS, bool SHIFT> struct Stream {
     {
         const int q = SHIFT ? int(reinterpret_cast<uintptr_t>(to) & 15) / int(sizeof(T)) : 0;
         const int slot = got == 0 ? kSlots - 1 : got - 1;
+        uint4 blocks[NV];
         if constexpr (SHIFT) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) *reinterpret_cast<uint4 *>(place(slot, 0, j)) = pack16<T>(v[j]);
             __syncwarp();
+            // (what a segment's first piece reads before itself it does not use)
+            read_any<NV>(place(slot, 0, 0) - (q ? 16 : 0), SEGMENT * 16, q ? uint32_t(16 - q * int(sizeof(T))) : 0, blocks);
         }
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -159,7 +190,7 @@ template <typename T, int L, int NV, int TENSORS, bool SHIFT> struct Stream {
                 const bool head = j == 0 && int(threadIdx.x) % SEGMENT == 0, tail = j == NV - 1 && last;
                 const uint8_t *at = place(slot, 0, j);
                 const bool whole = in && (!head || q == 0) && count[j] >= VEC - q;
-                if (whole) *reinterpret_cast<uint4 *>(p - q) = read16_any(at - q * int(sizeof(T)));
+                if (whole) *reinterpret_cast<uint4 *>(p - q) = blocks[j];
                 // one by one: my first VEC - q where there is no whole block, my last q where the next piece has none
                 const uint32_t front = (1u << (VEC - q)) - 1, all = (1u << VEC) - 1;
                 uint32_t rest = 0;
