@@ -8,6 +8,13 @@
 // both): only the boxes and the shared-memory descriptors differ.  Ragged sizes cost nothing extra: the TMA fills
 // what lies outside an operand with zeros, and the epilogue stores what lies inside the result.
 //
+// What bounds it: large products the tensor cores and, in long runs, the power they may draw -- 8192 x 4096 -> 8192 with
+// GELU keeps their pipe busy 96 % of the cycles at 1.44 GHz; 16384 x 4096 -> 16384 takes 1510-1560 us (1410-1450
+// TFLOP/s; 1370 is what a library product sustains, 1649 its best), 1575-1660 with bias and GELU, back to back.  Small
+// products: the 2 us of a launch, 1 us to the first operands, 0.1-0.15 us per 64 steps of the sum, 1-3 us for the last
+// epilogue (512^3: 4.4 us, 1024^3: 6.0).  Rows of outputs or residuals off 16-byte boundaries cost about 20 us per
+// 4096 x 4096 outputs in the epilogue's stores.
+//
 // Every wait on an mbarrier is bounded.  A role whose wait runs out leaves its loop, so the others' waits run out too;
 // the block waits (bounded) for its own copies in flight, counts itself in g_product_timeouts, frees its tensor
 // memory and returns without storing the tile.
@@ -243,7 +250,8 @@ template <int R> __device__ __forceinline__ Tile tile_at(const ProductParams &p,
 // A warp takes its quarter of the lanes (rows) and half of the columns of an accumulator, 32 x 32 values at a time: a
 // lane holds 32 neighbours of one row, computes, rounds and writes them to a piece in shared memory, from where a TMA
 // store takes it (or, where rows are not on 16-byte boundaries, the warp itself, row by row).  Everything 32-bit stays
-// in registers; 12 us for a 256 x 256 tile when the 32-bit accumulators went through shared memory became 3 us.
+// in registers: a 256 x 256 tile takes 2 us (GELU: 2.4 more, bias 0.7, residual 1, pre-activation 0.9), 12 when the
+// 32-bit accumulators went through shared memory.  It hides behind the next tile's sum from about 1000 steps on.
 
 // Where the 16 bytes of columns 8 j ... 8 j + 7 of row r of a piece lie (the TMA's 64-byte swizzle).
 __device__ __forceinline__ uint32_t piece_at(int r, int j) { return uint32_t(r * 64 + ((j ^ ((r >> 1) & 3)) << 4)); }
@@ -904,7 +912,7 @@ struct Choice {
 };
 
 // The shape, and into how many parts the sum is split, with the least time by these figures.  Parts are summed by a second
-// kernel (3 us and the traffic of the 32-bit parts), so splitting is for results of few tiles and long sums:
+// kernel (3 us, a chain of loads and the traffic of the 32-bit parts), so splitting is for results of few tiles and long sums:
 // 256 x 256 results of 16384 steps took 80 us unsplit.
 Choice choose(const Product &p, int sms, bool may_split)
 {
@@ -916,13 +924,13 @@ Choice choose(const Product &p, int sms, bool may_split)
         if (p.symmetric && c.rows < c.cols) continue;
         const int64_t tm = (p.m + c.rows - 1) / c.rows, tn = (p.n + c.cols - 1) / c.cols;
         const int64_t tiles = (p.symmetric ? symmetric_tiles(tm, tn, c.rows / c.cols) : tm * tn) * p.batch, units = sms / c.per_unit;
-        const int most = may_split && tiles < units ? int(std::min<int64_t>(units / tiles, steps * c.slices / 4)) : 1;
+        const int most = may_split && tiles < units ? int(std::min<int64_t>({units / tiles, steps * c.slices / 4, 16})) : 1;
         for (int k = 1; k <= std::max(most, 1); ++k) {
             const int per = (steps + k - 1) / k, parts = (steps + per - 1) / per;
             if (parts != k) continue;
             const int64_t waves = (tiles * k + units - 1) / units;
             double t = double(waves) * per * c.slices * (waves > 1 ? c.step_rounds : c.step) + c.launch;
-            if (k > 1) t += 3.0 + double(p.m) * double(p.n) * k * 8e-6 / 4.0;
+            if (k > 1) t += 3.0 + 0.2 * k + double(p.m) * double(p.n) * k * 8e-6 / 4.0;
             if (t < least) {
                 least = t;
                 best = Choice{Shape(s), k};

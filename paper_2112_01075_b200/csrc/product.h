@@ -77,7 +77,7 @@ int64_t product_scratch_bytes(const Product &p);
 cudaError_t launch_product(const Product &p, void *scratch, const LaunchOptions &o, cudaStream_t stream);
 
 // The linear epilogue on up to kFewRows rows, both operands contiguous along the sum, at any alignment; no scratch.
-constexpr int kFewRows = 16;
+constexpr int kFewRows = 32;
 cudaError_t launch_few_rows(const Product &p, const LaunchOptions &o, cudaStream_t stream);
 
 // Thread blocks of the product kernels whose bounded wait ran out on the current device.  Synchronizes the device.

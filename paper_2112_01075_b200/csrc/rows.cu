@@ -298,6 +298,10 @@ template <int L, int CL> __device__ __forceinline__ float2 row_sums(float a, flo
 
 // ---- layer norm, forward -------------------------------------------------------------------------------
 
+// A row is read once and written once: 16384 x 4096 bf16 41 us at the measured copy rate, 53 here (f32: 82 and 98); what is
+// missing is spent on instructions and on the two barriers per row (issue slots 64 % used, three blocks of 256 threads per
+// SM).  Two barriers because the sum of squares waits for the mean: one pass with a shifted sum would save one, and lose
+// digits where the shift is far from the mean.
 // Mean first, then the differences d from it, sum of d^2 and sum of d: the latter is what rounding left in the mean, and
 // corrects both (var = mean d^2 - (mean d)^2), so a mean far larger than the spread costs no digits.
 template <typename T, int L, int NV, bool SHIFT, int CL>
@@ -478,7 +482,10 @@ __global__ void __launch_bounds__(kLong) redist_layer_norm_long_kernel(const Lay
 // ---- layer norm, backward ------------------------------------------------------------------------------
 
 // With c = dy gamma and xh = (x - mean) rstd: dx = rstd (c - mean(c) - xh mean(c xh)).  A block walks over its rows
-// and keeps the column sums of dy xh and dy in registers; partials holds them per block, gamma's before beta's.
+// and keeps the column sums of dy xh and dy in registers; partials holds them per block, gamma's before beta's, and a
+// second kernel adds the blocks' in a fixed order (atomics would not).  16384 x 4096 bf16: 61 us at the measured copy rate,
+// 78 here (with the second kernel's 4); 262144 x 256: 84.  The sums' registers allow two blocks per SM; what they have under way
+// of the next rows lies in shared memory instead.
 template <typename T, int L, int NV, bool SHIFT, int CL>
 __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads, L <= 32 && NV == 1 ? 4 : L <= 256 ? 2 : 1) redist_layer_norm_grad_kernel(const LayerNorm l, float *partials)
 {
