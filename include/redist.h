@@ -186,7 +186,9 @@ void redist_plan_cache_clear(void);
  *   "step_latency"       >= 0   elements added to the cost of every collective while searching: small
  *                               transfers are bound by per-step latency, not by bytes (Section 8, the
  *                               third research question); 0 (default) is the paper's cost model
- *   "wait_polls"         >= 1   mbarrier polls before a bulk-copy block gives up (default 2^18)
+ *   "wait_polls"         >= 1   mbarrier polls before a bulk-copy block gives up (default 2^18); the operators'
+ *                               matrix products take it from the values in force at the call, as they do "pdl" and
+ *                               "test_extra_tx"
  *   "test_extra_tx"      >= 0   test only: makes every bounded wait run out (see redist_bulk_timeouts)
  *   "test_shrink_tiles"  >= 0   test only: the checked build takes every tile to be that many bytes shorter
  *                               (see redist_debug_bounds_report); no effect on the normal build
