@@ -289,7 +289,7 @@ struct Pieces {
 
     // Stores `cnt` (up to 32) columns of up to `rows` rows from the piece, `to` the first of them.  A row's aligned blocks
     // of 16 bytes go out whole, four per row; what the last of them lacks of a piece waits in `carry` (0: out, 1: pre) for
-    // the piece to its right.  Only a row's ends go out two bytes at a time.
+    // the piece to its right.  Only a row's ends go out in smaller stores.
     __device__ __forceinline__ void store_any(uint16_t *to, int64_t ld, int lane, int rows, int cnt, bool first, bool last, int carry) const
     {
         uint8_t *kept = smem + 3072 + carry * 512;
@@ -299,6 +299,7 @@ struct Pieces {
         auto element = [&](int r, int e) -> uint16_t {
             return *reinterpret_cast<const uint16_t *>(e >= 0 ? smem + piece_at(r, e >> 3) + (e & 7) * 2 : kept + r * 16 + (e + 8) * 2);
         };
+        auto two = [&](int r, int e) -> uint32_t { return element(r, e) | uint32_t(element(r, e + 1)) << 16; };
         __syncwarp();
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
@@ -318,11 +319,36 @@ struct Pieces {
         if ((first || last) && lane < rows) {
             uint16_t *row = to + lane * ld;
             const int p = int(reinterpret_cast<uintptr_t>(row) & 15) / 2, head = p ? 8 - p : 0;
-            if (first)
-                for (int e = 0; e < min(head, cnt); ++e) row[e] = element(lane, e);
+            // in stores of two, four and eight bytes: a row's end begins (its beginning ends) on a 16-byte boundary
+            if (first && cnt < head) {
+                for (int e = 0; e < cnt; ++e) row[e] = element(lane, e);
+            } else if (first) {
+                int e = 0;
+                if (head & 1) {
+                    row[e] = element(lane, e);
+                    e += 1;
+                }
+                if (head & 2) {
+                    *reinterpret_cast<uint32_t *>(row + e) = two(lane, e);
+                    e += 2;
+                }
+                if (head & 4) *reinterpret_cast<uint2 *>(row + e) = make_uint2(two(lane, e), two(lane, e + 2));
+            }
             if (last) {
                 const int whole = ((cnt + p) >> 3) * 8 - p;
-                for (int e = first ? max(whole, head) : whole; e < cnt; ++e) row[e] = element(lane, e);
+                int e = first ? max(whole, head) : whole;
+                const int left = cnt - e;
+                if (left > 0) {
+                    if (left & 4) {
+                        *reinterpret_cast<uint2 *>(row + e) = make_uint2(two(lane, e), two(lane, e + 2));
+                        e += 4;
+                    }
+                    if (left & 2) {
+                        *reinterpret_cast<uint32_t *>(row + e) = two(lane, e);
+                        e += 2;
+                    }
+                    if (left & 1) row[e] = element(lane, e);
+                }
             }
         }
         __syncwarp();

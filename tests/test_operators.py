@@ -477,6 +477,53 @@ def test_orthogonalize_scale_of_the_input_and_special_values():
     assert bool(torch.isnan(got[2]).all()) and bool(torch.isnan(got[3]).all())
 
 
+# ---- offsets beyond 32 bits -------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("stride", [(1 << 26) + 8, (1 << 26) + 1])
+def test_rows_far_apart(stride):
+    """40 rows 2^26 elements apart: offsets pass 2^31 elements and 2^32 bytes, on 16-byte boundaries and off them."""
+    g = gen(30)
+    buffer = torch.zeros(40 * stride, dtype=BF16, device="cuda")
+    far = lambda t: buffer.as_strided(t.shape, (stride, 1)).copy_(t)                       # noqa: E731
+    x, w, r = rand(g, 40, 72, dtype=BF16), rand(g, 56, 72, dtype=BF16), rand(g, 40, 56, dtype=BF16)
+    for rows in (12, 40):                                                                  # both kernels
+        assert torch.equal(api.linear_forward(far(x)[:rows], w), api.linear_forward(x[:rows].contiguous(), w))
+    want = api.linear_forward(x, w, residual=r)
+    assert torch.equal(api.linear_forward(x, w, residual=far(r)), want)
+    assert torch.equal(api.linear_forward(x, w, residual=r, out=buffer.as_strided((40, 56), (stride, 1))), want)
+    assert torch.equal(api.linear_forward(w, far(x)), api.linear_forward(w, x))
+    got = api.linear_backward(far(r), x, w)
+    assert all(torch.equal(a, b) for a, b in zip(got, api.linear_backward(r, x, w)))
+    got = api.linear_backward(r, far(x), w, r, "relu", dx=torch.empty_like(x))
+    assert all(torch.equal(a, b) for a, b in zip(got, api.linear_backward(r, x, w, r, "relu")))
+    y, mean, rstd = api.layer_norm_forward(x)
+    near = dict(rtol=2.0 ** -7, atol=1e-5)
+    assert torch.allclose(api.layer_norm_forward(far(x))[0], y, **near)
+    assert torch.allclose(api.layer_norm_forward(x, out=buffer.as_strided((40, 72), (stride, 1)))[0], y, **near)
+    dx, dg, db = api.layer_norm_backward(y, x, None, mean, rstd)
+    for got in (api.layer_norm_backward(far(y), x, None, mean, rstd), api.layer_norm_backward(y, far(x), None, mean, rstd),
+                api.layer_norm_backward(y, x, None, mean, rstd, dx=buffer.as_strided((40, 72), (stride, 1)))):
+        assert torch.allclose(got[0], dx, rtol=2.0 ** -7, atol=1e-4) and torch.allclose(got[1], dg, rtol=1e-5, atol=1e-4)
+    assert torch.equal(api.orthogonalize(far(x)), api.orthogonalize(x))
+    assert torch.equal(api.orthogonalize(x, out=buffer.as_strided((40, 72), (stride, 1))), api.orthogonalize(x))
+
+
+@pytest.mark.gpu
+def test_more_than_two_to_the_31_outputs():
+    """140000 x 16000 outputs and as many elements in a layer norm; rows from the beginning, the middle and the end."""
+    g = gen(31)
+    x, w = rand(g, 140000, 64, dtype=BF16), rand(g, 16000, 64, scale=0.1, dtype=BF16)
+    y = api.linear_forward(x, w, activation="relu")
+    n, mean, rstd = api.layer_norm_forward(y)
+    for at in (0, 70000, 134215, 139900):                                                  # 134218 x 16000 is 2^31
+        part = slice(at, at + 100)
+        z, slack = products(x[part], w)
+        within(y[part], act64(z, "relu"), slack, BF16)
+        m64, r64, xh = norm64(y[part], 1e-5)
+        assert torch.allclose(n[part].double(), xh, rtol=2.0 ** -8, atol=1e-4) and torch.allclose(rstd[part].double(), r64, rtol=1e-5)
+
+
 # ---- streams, graphs, scratch, waits ------------------------------------------------------------------------------
 
 @pytest.mark.gpu
