@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads, L >= 512 ? 2 : 3
         const float rest = both.x * over;
         float var = both.y * over - rest * rest;
         if (var < 0.0f) var = 0.0f;                         // by rounding alone; NaN stays
-        const float rstd = 1.0f / sqrtf(var + l.eps);
+        const float rstd = rsqrtf(var + l.eps);
         const bool in = row < l.rows;
         const float less = -rest * rstd;
 #pragma unroll
@@ -458,7 +458,7 @@ __global__ void __launch_bounds__(kLong) redist_layer_norm_long_kernel(const Lay
         rest = both.x * over;
         float var = both.y * over - rest * rest;
         if (var < 0.0f) var = 0.0f;
-        const float rstd = 1.0f / sqrtf(var + l.eps);
+        const float rstd = rsqrtf(var + l.eps);
 #pragma unroll 2
         for (int64_t c = int64_t(threadIdx.x) * 8; c < l.cols; c += kLong * 8) {
             float v[8];
