@@ -298,14 +298,14 @@ template <int L, int CL> __device__ __forceinline__ float2 row_sums(float a, flo
 
 // ---- layer norm, forward -------------------------------------------------------------------------------
 
-// A row is read once and written once: 16384 x 4096 bf16 41 us at the measured copy rate, 53 here (f32: 82 and 98); what is
+// A row is read once and written once: 16384 x 4096 bf16 41 us at the measured copy rate, 49 here (f32: 82 and 87); what is
 // missing is spent on instructions and on the two barriers per row (issue slots 64 % used, three blocks of 256 threads per
-// SM).  Two barriers because the sum of squares waits for the mean: one pass with a shifted sum would save one, and lose
+// SM; four where aligned 32-bit rows of 2049 to 4096 columns leave registers for them: 97 -> 87 us, but 48 -> 57 at 2048).  Two barriers because the sum of squares waits for the mean: one pass with a shifted sum would save one, and lose
 // digits where the shift is far from the mean.
 // Mean first, then the differences d from it, sum of d^2 and sum of d: the latter is what rounding left in the mean, and
 // corrects both (var = mean d^2 - (mean d)^2), so a mean far larger than the spread costs no digits.
 template <typename T, int L, int NV, bool SHIFT, int CL>
-__global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads, L >= 512 ? 2 : 3) redist_layer_norm_kernel(const LayerNorm l)
+__global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads, L >= 512 ? 2 : sizeof(T) == 4 && !SHIFT && L == 256 ? 4 : 3) redist_layer_norm_kernel(const LayerNorm l)
 {
     using S = RowShape<T, L, NV>;
     constexpr int VEC = S::VEC;
@@ -1047,7 +1047,7 @@ template <typename T, bool SHIFT> cudaError_t forward_as(const LayerNorm &l, int
         constexpr int L = decltype(threads)::value, NV = decltype(pieces)::value, CL = decltype(cluster)::value;
         using S = RowShape<T, L, NV>;
         constexpr int smem = Stream<T, L, NV, 1, SHIFT>::kSmem;
-        ce = launch_with(smem, CL, redist_layer_norm_kernel<T, L, NV, SHIFT, CL>, dim3(row_blocks(l, S::kRows, S::kThreads, smem, L >= 512 ? 64 : NV == 1 ? 56 : 80, sms / CL) * CL),
+        ce = launch_with(smem, CL, redist_layer_norm_kernel<T, L, NV, SHIFT, CL>, dim3(row_blocks(l, S::kRows, S::kThreads, smem, L >= 512 || (sizeof(T) == 4 && !SHIFT && L == 256) ? 64 : NV == 1 ? 56 : 80, sms / CL) * CL),
                          S::kThreads, o, stream, l);
     });
     if (held) return ce;
