@@ -460,7 +460,7 @@ __device__ __forceinline__ void linear_piece(const ProductParams &p, const CUten
 // written a second time with rows and columns exchanged.
 __device__ __forceinline__ void scaled_piece(const ProductParams &p, const CUtensorMap *map_out, const CUtensorMap *map_lo, Pieces &pieces,
                                              float (&v)[32], const uint4 (&hi)[4], const uint4 (&lo)[4], int lane, int row0, int col0,
-                                             int matrix, float alpha, float beta, bool mirror, bool first, bool last)
+                                             int matrix, float alpha, float beta, float center, bool mirror, bool first, bool last)
 {
     const Epilogue &e = p.e;
 #pragma unroll
@@ -474,6 +474,11 @@ __device__ __forceinline__ void scaled_piece(const ProductParams &p, const CUten
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[8 * j + i] = fmaf(beta, fmaf(u[i], 1.0f / 2048.0f, w[i]), v[8 * j + i]);
         }
+    }
+    if (e.diagonal && row0 == col0) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i == lane) v[i] = fmaf(-center, e.on_diagonal, v[i]);
     }
     if (e.out_type == T_BF16 && !p.aligned_out) {
         put_row<__nv_bfloat16>(pieces.plain(), lane, v);
@@ -664,7 +669,8 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         Pieces pieces{ring + kRing + (warp - 4) * 2 * kPiece, base + kRing + (warp - 4) * 2 * kPiece};
         float *bias = reinterpret_cast<float *>(ring + kRing + kEpiBytes) + (warp - 4) * 32;
-        int use = 0;
+        int use = 0, centred = -1;
+        float center = 0.0f;
         for (int t = first; t < p.tiles; t += step, ++use) {
             const int b = use & 1;
             const Tile at = tile_at<CG * 128 / BN>(p, t);
@@ -672,6 +678,20 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             const int64_t row = row0 + lane;
             const bool in = row < p.m;
             float alpha = p.e.alpha, beta = p.e.beta;
+            if (KIND == EPI_SCALED && p.e.diagonal) {
+                if (at.matrix != centred) {             // every warp for itself, all in the same order
+                    const __half *d = static_cast<const __half *>(p.e.diagonal) + int64_t(at.matrix) * p.e.diagonal_batch;
+                    float t = 0.0f;
+#pragma unroll 4
+                    for (int i = lane; i < p.e.diagonal_n; i += 32) t += __half2float(d[i * p.e.diagonal_step]);
+#pragma unroll
+                    for (int i = 16; i; i >>= 1) t += __shfl_xor_sync(0xffffffffu, t, i);
+                    t *= p.e.mean_scale;
+                    center = t >= 0.25f ? t * fmaf(t, p.e.center_2, p.e.center_1) : 0.0f;
+                    centred = at.matrix;
+                }
+                beta = fmaf(center, p.e.to_beta, beta);
+            }
             if (KIND == EPI_SCALED && p.e.scale) {
                 const float s = p.e.scale[at.matrix];
                 for (int i = 0; i < p.e.alpha_power; ++i) alpha *= s;
@@ -740,7 +760,7 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 } else {
                     // above the diagonal only what no tile computes
                     const bool mirror = p.symmetric && row0 / BN > col0 / (128 * CG) * (128 * CG / BN) + (128 * CG / BN - 1);
-                    scaled_piece(p, &map_out, &map_more, pieces, v, now, now_rest, lane, row0, col0, at.matrix, alpha, beta, mirror, begins, ends);
+                    scaled_piece(p, &map_out, &map_more, pieces, v, now, now_rest, lane, row0, col0, at.matrix, alpha, beta, center, mirror, begins, ends);
                 }
             }
             fence_before();

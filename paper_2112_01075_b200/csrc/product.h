@@ -45,6 +45,13 @@ struct Epilogue {
     float alpha, beta;
     int32_t alpha_power, beta_power;// how often scale[matrix] multiplies alpha / beta
     int32_t out_type;
+    // SCALED, centred: t = mean_scale * the sum of diagonal_n f16 elements, diagonal_step apart from diagonal + i *
+    // diagonal_batch on (a sample of the diagonal of matrix i); c = t (center_1 + t center_2) where t is at least 1/4, else 0.
+    // on_diagonal * c is subtracted from the result's diagonal, to_beta * c (scaled as beta is) added to beta.  Null: neither.
+    const void *diagonal;
+    int64_t diagonal_step, diagonal_batch;
+    int32_t diagonal_n;
+    float mean_scale, center_1, center_2, on_diagonal, to_beta;
 };
 
 struct Product {
