@@ -292,7 +292,7 @@ struct Pieces {
     // the piece to its right.  Only a row's ends go out in smaller stores.
     __device__ __forceinline__ void store_any(uint16_t *to, int64_t ld, int lane, int rows, int cnt, bool first, bool last, int carry) const
     {
-        uint8_t *kept = smem + 3072 + carry * 512;
+        uint8_t *kept = smem + 2 * kPiece - (2 - carry) * 512;
         auto word = [&](int r, int w) -> uint32_t {
             return *reinterpret_cast<const uint32_t *>(w >= 0 ? smem + piece_at(r, w >> 2) + (w & 3) * 4 : kept + r * 16 + (w + 4) * 4);
         };
