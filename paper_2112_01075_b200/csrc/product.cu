@@ -15,9 +15,10 @@
 // epilogue (512^3: 4.4 us, 1024^3: 6.0).  Rows of outputs or residuals off 16-byte boundaries cost about 20 us per
 // 4096 x 4096 outputs in the epilogue's stores.
 //
-// Every wait on an mbarrier is bounded.  A role whose wait runs out leaves its loop, so the others' waits run out too;
-// the block waits (bounded) for its own copies in flight, counts itself in g_product_timeouts, frees its tensor
-// memory and returns without storing the tile.
+// Every wait on an mbarrier is bounded.  A role whose wait runs out leaves its
+// loop, so the others' waits run out too; products already issued are awaited, as they are in a healthy run, and so are
+// copies in flight (both with limits of their own, which wait_polls does not shorten); then the block counts itself in
+// g_product_timeouts, frees its tensor memory and returns without storing the tile.
 #include "product.h"
 
 #include <cuda.h>
@@ -43,6 +44,9 @@ constexpr int kBiasBytes = 8 * 32 * 4;
 constexpr int kBarBytes = 256;
 constexpr int kSmem = 1024 + kRing + kEpiBytes + kBiasBytes + kBarBytes;
 constexpr int kMaxStages = 12;
+// (a poll holds a thread for up to 4 us)
+constexpr uint32_t kDrainPolls = 1 << 16;       // for products already issued, which always end
+constexpr uint32_t kCopyPolls = 1 << 10;        // for a stage's copies once a wait has run out: 4 ms
 
 __device__ unsigned int g_product_timeouts = 0;
 
@@ -66,9 +70,10 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
 
-// True when the phase is over, false when `polls` polls have not seen it end.  The loop is hidden from the compiler: the
-// loading and the multiplying warp stay convergent in its eyes, and the descriptors of what they issue in uniform
-// registers (a k-step took 400 cycles to issue when they did not, more than the tensor cores need for it).
+// True when the phase is over, false when this lane's `polls` polls have not seen it end.  (The roles that act through one
+// lane ask that lane; the storing warps ask all.)  The loop is hidden from the compiler: the loading and the multiplying
+// warp stay convergent in its eyes, and the descriptors of what they issue in uniform registers (a k-step took 400 cycles to
+// issue when they did not, more than the tensor cores need for it).
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t polls)
 {
     uint32_t done;
@@ -533,6 +538,7 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     constexpr uint32_t kColumns = 2 * BN < 32 ? 32 : 2 * BN;
     constexpr int kShare = BN >= 64 ? BN / 2 : BN;          // columns of an accumulator that one warp stores
     constexpr int kStorers = 4 * (BN / kShare);
+    static_assert(8 * (2 * kStages + 5) + 8 <= kBarBytes, "barriers, tensor memory's address and the flag");
     static_assert((kColumns & (kColumns - 1)) == 0 && kColumns <= 512, "tensor memory is allocated in powers of two");
 
     extern __shared__ uint8_t raw[];
@@ -543,8 +549,9 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     auto empty = [&](int s) { return bars + 8 * (kStages + s); };
     auto acc_full = [&](int b) { return bars + 8 * (2 * kStages + b); };
     auto acc_free = [&](int b) { return bars + 8 * (2 * kStages + 2 + b); };
-    const uint32_t tmem_at = bars + 8 * (2 * kStages + 4);
-    volatile uint32_t *tmem_word = reinterpret_cast<volatile uint32_t *>(ring + kRing + kEpiBytes + kBiasBytes + 8 * (2 * kStages + 4));
+    const uint32_t drained = bars + 8 * (2 * kStages + 4);
+    const uint32_t tmem_at = bars + 8 * (2 * kStages + 5);
+    volatile uint32_t *tmem_word = reinterpret_cast<volatile uint32_t *>(ring + kRing + kEpiBytes + kBiasBytes + 8 * (2 * kStages + 5));
     volatile uint32_t *failed = tmem_word + 1;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -560,6 +567,7 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             bar_init(acc_full(b), 1);
             bar_init(acc_free(b), kStorers * CG);
         }
+        bar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *failed = 0;
     }
@@ -615,17 +623,13 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         }
         // every stage's last use has to be over before this block may end: its products read, its copies landed
         const int used = rounds ? kStages : stage;
-        for (int i = 0; i < used; ++i) {
-            const int s = rounds ? (stage + i) % kStages : i;
-            const uint32_t last = s < stage ? phase : phase ^ 1;          // the phase of the stage's last use
-            if (ok) {
-                ok = bar_wait(empty(s), last, p.wait_polls);
-            } else if (rank == 0) {
-                bar_wait(full(s), last, p.wait_polls);
-            }
-        }
+        auto use = [&](int i) { return rounds ? (stage + i) % kStages : i; };
+        auto last = [&](int s) { return s < stage ? phase : phase ^ 1; };   // the phase of the stage's last use
+        for (int i = 0; i < used && ok; ++i) ok = bar_wait(empty(use(i)), last(use(i)), p.wait_polls);
+        if (!ok && rank == 0)
+            for (int i = 0; i < used; ++i) bar_wait(full(use(i)), last(use(i)), kCopyPolls);
         if (!ok && rank != 0)                                             // its copies report to the first block: give
-            for (int i = 0; i < 64; ++i) __nanosleep(1 << 15);            // them 2 ms to land in memory it still owns
+            for (int i = 0; i < 128; ++i) __nanosleep(1 << 15);           // them 4 ms to land in memory it still owns
     } else if (warp == 1 && rank == 0) {
         // Products, in the same way.
         int stage = 0;
@@ -664,6 +668,11 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 }
             }
         }
+        // whatever became of the waits: what was issued reads the stages and writes tensor memory, of both blocks of a pair
+        if (elected()) commit<CG>(drained);
+        ok = bar_wait(drained, 0, kDrainPolls) && ok;
+    } else if (warp == 1) {
+        ok = bar_wait(drained, 0, kDrainPolls);                           // reported by the first block
     } else if (warp >= 4 && warp < 4 + kStorers) {
         // outputs
         const int quarter = warp & 3, half = (warp - 4) >> 2;
@@ -719,7 +728,8 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
 #pragma unroll
             for (int i = 0; i < 4; ++i) more[i] = rest[i] = make_uint4(0, 0, 0, 0);
             if (col_at < p.n && row0 < p.m) fetch(col_at);
-            if (!bar_wait(acc_full(b), (use >> 1) & 1, p.wait_polls)) {
+            // one answer for the warp: what follows is for all of its lanes
+            if (!__all_sync(0xffffffffu, bar_wait(acc_full(b), (use >> 1) & 1, p.wait_polls))) {
                 ok = false;
                 break;
             }

@@ -626,6 +626,28 @@ def test_a_wait_that_runs_out_is_counted_and_returns(rows, k, n):
     assert api.redist_product_timeouts() == after
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,k,n,long", [(700, 640, 600, False), (8192, 1024, 4096, True), (300, 4096, 200, False), (64, 200000, 64, True)])
+def test_a_healthy_call_that_runs_out_of_polls_ends_in_order(rows, k, n, long):
+    """With a handful of polls a wait runs out while copies and products are on their way, at least where a tile's sum
+    takes longer than a poll (the hardware may hold a thread for microseconds in one): on the pairs that 512 full
+    tiles take, and in a split sum of 200000.  The call returns; it has been counted, or its result is right; and what it
+    left behind (barriers, tensor memory) does not reach the next call."""
+    g = gen(13)
+    x, w = rand(g, rows, k, dtype=BF16), rand(g, n, k, dtype=BF16)
+    want = api.linear_forward(x, w)
+    before = first = api.redist_product_timeouts()
+    for polls in (1, 1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 64):
+        with api.tuning(wait_polls=polls):
+            got = api.linear_forward(x, w)
+        after = api.redist_product_timeouts()
+        assert after > before or torch.equal(got, want), polls
+        assert torch.equal(api.linear_forward(x, w), want), polls
+        assert api.redist_product_timeouts() == after, polls
+        before = after
+    assert after > first or not long                         # some of them did run out
+
+
 # ---- refusals (no GPU) ----------------------------------------------------------------------------------------------
 
 def linear_op(**kw):
