@@ -188,7 +188,7 @@ void redist_plan_cache_clear(void);
  *                               third research question); 0 (default) is the paper's cost model
  *   "wait_polls"         >= 1   mbarrier polls before a bulk-copy block gives up (default 2^18); the operators'
  *                               matrix products take it from the values in force at the call, as they do "pdl" and
- *                               "test_extra_tx"
+ *                               "test_extra_tx" (the wait for a whole sum gets it again for every 512 stages)
  *   "test_extra_tx"      >= 0   test only: makes every bounded wait run out (see redist_bulk_timeouts)
  *   "test_shrink_tiles"  >= 0   test only: the checked build takes every tile to be that many bytes shorter
  *                               (see redist_debug_bounds_report); no effect on the normal build
@@ -520,7 +520,8 @@ redist_status redist_orthogonalize(const redist_orthogonal *op, void *scratch, s
 /*
  * redist_product_timeouts -- health counter of the matrix products, as redist_bulk_timeouts is of the bulk
  * copies: thread blocks whose bounded wait ("wait_polls") ran out on the current device.  Such a block
- * leaves its tiles unwritten and returns.  0 in a healthy run; -1 on a CUDA error.  Synchronizes the device.
+ * leaves its tiles unwritten and returns, although the call has returned REDIST_OK.  0 in a healthy run; -1 on a CUDA error.
+ * Synchronizes the device.
  */
 int64_t redist_product_timeouts(void);
 

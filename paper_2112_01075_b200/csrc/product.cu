@@ -15,8 +15,8 @@
 // epilogue (512^3: 4.4 us, 1024^3: 6.0).  Rows of outputs or residuals off 16-byte boundaries cost about 20 us per
 // 4096 x 4096 outputs in the epilogue's stores.
 //
-// Every wait on an mbarrier is bounded.  A role whose wait runs out leaves its
-// loop, so the others' waits run out too; products already issued are awaited, as they are in a healthy run, and so are
+// Every wait on an mbarrier is bounded, the storing warps' by polls that grow with a tile's sum.  A role whose wait runs out
+// leaves its loop, so the others' waits run out too; products already issued are awaited, as they are in a healthy run, and so are
 // copies in flight (both with limits of their own, which wait_polls does not shorten); then the block counts itself in
 // g_product_timeouts, frees its tensor memory and returns without storing the tile.
 #include "product.h"
@@ -116,6 +116,14 @@ __device__ __forceinline__ uint32_t in_first(uint32_t addr)
 {
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+
+// ... in the block of rank 1.
+__device__ __forceinline__ uint32_t in_second(uint32_t addr)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(r) : "r"(addr));
     return r;
 }
 
@@ -668,6 +676,11 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 }
             }
         }
+        if (!ok) {
+            *failed = 1;
+            if constexpr (CG == 2)
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_second(tmem_at + 4)), "r"(1u) : "memory");
+        }
         // whatever became of the waits: what was issued reads the stages and writes tensor memory, of both blocks of a pair
         if (elected()) commit<CG>(drained);
         ok = bar_wait(drained, 0, kDrainPolls) && ok;
@@ -728,8 +741,14 @@ redist_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
 #pragma unroll
             for (int i = 0; i < 4; ++i) more[i] = rest[i] = make_uint4(0, 0, 0, 0);
             if (col_at < p.n && row0 < p.m) fetch(col_at);
-            // one answer for the warp: what follows is for all of its lanes
-            if (!__all_sync(0xffffffffu, bar_wait(acc_full(b), (use >> 1) & 1, p.wait_polls))) {
+            // This wait is for a whole tile's sum: the polls again for every 512 stages of it (0.4 ms at most), unless the
+            // multiplying warp has given up.  One answer for the warp: what follows is for all of its lanes.
+            bool ready = false;
+            for (int turns = 1 + (at.k1 - at.k0) / 512; turns > 0 && !ready; --turns) {
+                ready = __all_sync(0xffffffffu, bar_wait(acc_full(b), (use >> 1) & 1, p.wait_polls));
+                if (!ready && __any_sync(0xffffffffu, *failed)) break;
+            }
+            if (!ready) {
                 ok = false;
                 break;
             }

@@ -648,6 +648,29 @@ def test_a_healthy_call_that_runs_out_of_polls_ends_in_order(rows, k, n, long):
     assert after > first or not long                         # some of them did run out
 
 
+@pytest.mark.gpu
+def test_the_wait_for_a_long_sum_grows_with_it():
+    """Sums of 2^22 take longer (10 ms in one piece, 0.6 ms in each of sixteen) than the polls given (1 ms, 1/4 ms), which are
+    plenty for everything that does not grow with the sum."""
+    g = gen(14)
+    k = 1 << 22
+    x = rand(g, 8, k, dtype=BF16)
+    want = api.orthogonalize(x, steps=1)
+    exact = orthogonalize64(x, steps=1)
+    assert float((want.double() - exact).norm() / exact.norm()) < ORTHOGONAL
+    before = api.redist_product_timeouts()
+    with api.tuning(wait_polls=256):
+        got = api.orthogonalize(x, steps=1)
+    assert api.redist_product_timeouts() == before and torch.equal(got, want)
+    x = rand(g, 40, k, dtype=BF16)
+    want = api.linear_forward(x, x[:8])
+    z, slack = products(x, x[:8])
+    within(want, z, slack, BF16)
+    with api.tuning(wait_polls=64):
+        got = api.linear_forward(x, x[:8])
+    assert api.redist_product_timeouts() == before and torch.equal(got, want)
+
+
 # ---- refusals (no GPU) ----------------------------------------------------------------------------------------------
 
 def linear_op(**kw):
