@@ -658,10 +658,15 @@ redist_status redist_orthogonalize(const redist_orthogonal *op, void *scratch, s
             TRY(cuda(launch_product(g, nullptr, o, stream)));
             // B = b A + c A A - z (A alone where c is zero: its factor goes into the update), and a + z for a below.  z = b t +
             // c t^2, with t the mean of (128 samples of) A's diagonal, is about the mean of B's, and the larger part of B
-            // where A is near a multiple of one; what is left rounds to less: 1.8e-3 to 2.2e-3 from the exact result on
-            // Gaussian input of 32 x 64 to 2048 x 2048, of which 1.7e-3 are the output's own rounding, where 2.3e-3 to
-            // 3.0e-3 were.  Only for t >= 1/4, when most directions have grown: before that z X would bring the rounding of
-            // the strong directions into the weak ones, which have yet to grow (8 x 8, one direction: 7e-3).
+            // where A is near a multiple of one; what is left rounds to less.  But z X brings the rounding of X's strong
+            // directions, which B alone would have kept out, into those that have yet to grow, and every later step
+            // multiplies it by its a.  So only where the later steps grow by no more than 4 in all (the last two steps of the
+            // Muon coefficients), and for t >= 1/4.  The error there, on Gaussian input, against none and against centring
+            // wherever t >= 1/4: 128 x 128 2.0e-3 (2.4e-3, 1.9e-3), 32 x 64 2.6e-3 (3.0e-3, 2.1e-3); with half of the
+            // directions strong over a noise of 1e-3, 128 x 256: 2.2e-3 (2.2e-3, 5.7e-3); 1.7e-3 of each is the output's rounding.
+            double later = 1;
+            for (int j = k + 1; j < q.steps; ++j) later *= std::max(1.0, std::fabs(double(q.coefficients[3 * j])));
+            const bool centred = square && later <= 4;
             auto centre = [&](Epilogue &e) {
                 const i64 samples = std::min<i64>(w.small, 128), apart = w.small / samples;
                 e.diagonal = w.a;
@@ -684,8 +689,10 @@ redist_status redist_orthogonalize(const redist_orthogonal *op, void *scratch, s
                 g.e.ld_add = w.ld_gram;
                 g.e.add_batch = w.gram_plane;
                 g.e.scale = nullptr;
-                centre(g.e);
-                g.e.on_diagonal = float(steps.b[k]);
+                if (centred) {
+                    centre(g.e);
+                    g.e.on_diagonal = float(steps.b[k]);
+                }
                 TRY(cuda(launch_product(g, nullptr, o, stream)));
                 factor = 1.0 / steps.b[k];
                 poly = w.b;
@@ -712,7 +719,7 @@ redist_status redist_orthogonalize(const redist_orthogonal *op, void *scratch, s
             u.e.beta = float(double(abc[0]) * to * x);
             u.e.scale = first ? w.scale : nullptr;
             u.e.alpha_power = u.e.beta_power = 1;
-            if (square) {
+            if (centred) {
                 centre(u.e);
                 u.e.to_beta = float(to * x);
             }

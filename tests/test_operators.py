@@ -439,6 +439,29 @@ def test_orthogonalize(batch, m, n, kind, dtype):
     assert torch.equal(got[0], api.orthogonalize(x[0]))
 
 
+# Part of the directions strong and equal, the rest noise.  f16 rounds the operands to 2e-4 of themselves (2^-10 / sqrt(12) over
+# the mean of a binade); A's error passes into X with |b + 2 c A| = 1.2, B's and X's with |B| = 2.8: 8e-4 of the norm a step
+# where the strong directions have settled, passed on by each later step with the polynomial's slope there, about 1.4, all of them
+# alike here: 8e-4 sqrt(1 + 2 + 4 + 8) = 3.2e-3; with the output's 1.7e-3 3.6e-3.  A tenth more is allowed.
+ORTHOGONAL_PARTIAL = 4e-3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n", [(64, 128), (128, 128), (128, 256), (256, 128), (256, 256), (512, 512)])
+@pytest.mark.parametrize("part", [0.25, 0.5, 0.75])
+@pytest.mark.parametrize("noise", [1e-2, 1e-3])
+def test_orthogonalize_part_of_the_directions_strong(m, n, part, noise):
+    g = gen(m + n)
+    small, rank = min(m, n), round(part * min(m, n))
+    u, _ = torch.linalg.qr(rand(g, 2, m, small))
+    v, _ = torch.linalg.qr(rand(g, 2, n, small))
+    x = (u[..., :rank] @ v[..., :rank].mT + noise * max(m, n) ** -0.5 * rand(g, 2, m, n)).to(BF16)
+    got, want = api.orthogonalize(x), orthogonalize64(x)
+    for i in range(2):
+        off = float((got[i].double() - want[i]).norm() / want[i].norm())
+        assert off < ORTHOGONAL_PARTIAL, off
+
+
 @pytest.mark.gpu
 def test_orthogonalize_options_and_strides():
     g = gen(6)
