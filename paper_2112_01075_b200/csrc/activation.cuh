@@ -24,55 +24,55 @@ __device__ __forceinline__ float exp2_fast(float v)
     return r;
 }
 
-// z Phi(z) with Phi(z) = 1/2 + z Q(z^2), Q a polynomial of degree 13 in (z^2 - c/2) / (c/2) on z^2 <= c = 5.2^2, fitted
-// to the normal distribution function by iterated least squares (least maximum of |z| times the error: 6.4e-8; with the
-// rounding of 32-bit Horner 2.3e-7).  Beyond, z Q(c) passes 1/2 and saturation makes Phi exactly 0 or 1.  Ten
-// instructions a value, no special functions, where erff takes thirty and branches; accurate to 2.3e-7 |z|.
-// Eight values are interleaved, so that the chain of one hides behind the others'.
-__device__ __forceinline__ void phi8(const float *z, float *phi)
+// Phi, the normal distribution function, below zero, where its relative accuracy counts: Phi(-x) = exp(-x^2 / 2) R(x) for x =
+// |z|, with R falling slowly, from 1/2 like 1 / (x sqrt(2 pi)).  In v = 1 / (x + 5/2) R is v times a polynomial of degree 7,
+// fitted on 0 <= x <= 13.3 by iterated least squares (relative error 9e-8 up to x = 4, 1.7e-6 at most beyond).  So the lower
+// tail of GELU and of its slope is as accurate as 32-bit numbers reach: 5e-7 + 1.5 z^2 2^-24 of Phi (the latter from the
+// exponent's rounding), where 1 + erf loses all digits towards z = -5.5.  Above zero Phi is 1 - Phi(-z).
+// below[i] = Phi(-|z|), e[i] = 8 exp(-z^2 / 2) (eight times, so that what z e takes out of the subnormal numbers has not been
+// flushed to zero).  Eight values are interleaved, so that the chain of one hides behind the others'.
+__device__ __forceinline__ void phi8(const float *z, float *below, float *e)
 {
-    const float top = 5.2f * 5.2f;
-    constexpr float kQ[14] = {-4.813592823e-04f, 1.268577063e-03f, -1.221270184e-03f, 1.799950609e-03f, -4.789268132e-03f,
-                              8.560134098e-03f, -1.250501070e-02f, 1.795471460e-02f, -2.472365461e-02f, 3.198997304e-02f,
-                              -3.992981836e-02f, 5.002452061e-02f, -6.774366647e-02f, 1.359499991e-01f};
-    uint64_t s[4], q[4];
+    constexpr float kR[8] = {-7.040148735e+00f, 1.433973980e+01f, -1.063558006e+01f, 2.726462602e+00f,
+                             2.835668437e-02f, 2.950876057e-01f, 1.230796501e-01f, 4.989921674e-02f};        // of R / 8
+    uint64_t v[4], q[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        float u0, u1;
         const Pair both(z[2 * k], z[2 * k + 1]);
-        mul2(both, both).get(u0, u1);
-        s[k] = fma2(Pair(fminf(u0, top), fminf(u1, top)), Pair(2.0f / top, 2.0f / top), Pair(-1.0f, -1.0f)).both;
-        q[k] = Pair(kQ[0], kQ[0]).both;
+        fma2(mul2(both, both), Pair(-0.72134752f, -0.72134752f), Pair(3.0f, 3.0f)).get(e[2 * k], e[2 * k + 1]);
+        e[2 * k] = exp2_fast(e[2 * k]);
+        e[2 * k + 1] = exp2_fast(e[2 * k + 1]);
+        v[k] = Pair(reciprocal(fabsf(z[2 * k]) + 2.5f), reciprocal(fabsf(z[2 * k + 1]) + 2.5f)).both;
+        q[k] = Pair(kR[0], kR[0]).both;
     }
 #pragma unroll
-    for (int i = 1; i < 14; ++i)
+    for (int i = 1; i < 8; ++i)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) q[k] = fma2(Pair(q[k]), Pair(s[k]), Pair(kQ[i], kQ[i])).both;
+        for (int k = 0; k < 4; ++k) q[k] = fma2(Pair(q[k]), Pair(v[k]), Pair(kR[i], kR[i])).both;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        float q0, q1;
-        Pair(q[k]).get(q0, q1);
-        phi[2 * k] = __saturatef(fmaf(z[2 * k], q0, 0.5f));
-        phi[2 * k + 1] = __saturatef(fmaf(z[2 * k + 1], q1, 0.5f));
-    }
+    for (int k = 0; k < 4; ++k)
+        mul2(mul2(Pair(q[k]), Pair(v[k])), Pair(e[2 * k], e[2 * k + 1])).get(below[2 * k], below[2 * k + 1]);
 }
 
 __device__ __forceinline__ void gelu8(float *z)
 {
-    float phi[8];
-    phi8(z, phi);
+    float below[8], e[8];
+    phi8(z, below, e);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] *= phi[i];
+    for (int i = 0; i < 8; ++i) z[i] *= z[i] < 0.0f ? below[i] : 1.0f - below[i];
 }
 
 // v times the activation's slope at z.
 __device__ __forceinline__ void times_slope8(float (&v)[8], const float (&z)[8], int act)
 {
     if (act == ACT_GELU) {                                  // Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi)
-        float phi[8];
-        phi8(z, phi);
+        float below[8], e[8];
+        phi8(z, below, e);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= fmaf(z[i] * 0.39894228f, exp2_fast(z[i] * z[i] * -0.72134752f), phi[i]);
+        for (int i = 0; i < 8; ++i) {
+            const float s = fmaf(fabsf(z[i]) * (-0.39894228f / 8), e[i], below[i]);         // of -|z|; that of |z| is 1 - s
+            v[i] *= z[i] < 0.0f ? s : 1.0f - s;
+        }
     } else if (act == ACT_SILU) {                           // with s = 1 / (1 + exp(-z)): s + z s (1 - s)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {

@@ -741,7 +741,7 @@ struct Lays {
 // Up to three matrices in one launch.  A block takes rows_per_block rows by 256 columns, a warp every eighth row, a lane
 // eight neighbours.
 template <typename T, bool ALIGNED>
-__global__ void __launch_bounds__(256) redist_lay_kernel(const __grid_constant__ Lays lays)
+__global__ void __launch_bounds__(256, 4) redist_lay_kernel(const __grid_constant__ Lays lays)
 {
     __shared__ float all[8][kLayCols];
     let_next_start();

@@ -125,6 +125,27 @@ def test_activations_over_their_whole_range(activation):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_gelu_keeps_its_relative_accuracy_below_zero(dtype):
+    """Every number of the type between -14 and 14, forward and slope.  Computed in 32 bits: Phi(z) for z < 0 is exp(-z^2 / 2)
+    times a factor of size 1 / |z|; that factor, the reciprocal in it and the power of two are off by a few 2^-23, together by
+    at most 2^-20 of the value, and the exponent, the rounded product of z, z and a constant, by 3 2^-24 of itself, z^2 / 2:
+    1.5 z^2 2^-24 of the value.  32-bit results below 2^-126 may be flushed to zero."""
+    z = torch.arange(0, 1 << 16, dtype=torch.int32).to(torch.int16).view(dtype).cuda()
+    z = z[z.abs() <= 14].reshape(-1, 1).contiguous()
+    one, z64 = torch.ones((1, 1), dtype=dtype, device="cuda"), z.double()
+    of_itself = 2.0 ** -20 + 1.5 * z64 ** 2 * 2.0 ** -24
+    phi = torch.exp(torch.special.log_ndtr(z64))
+    want = z64 * phi
+    within(api.linear_forward(z, one, activation="gelu"), want, want.abs() * of_itself + 2.0 ** -126, dtype)
+    few = api.linear_forward(one, z, activation="gelu")                     # one row: the other kernel
+    within(few.T, want, want.abs() * of_itself + 2.0 ** -126, dtype)
+    slope, second = slope64(z64, "gelu"), z64 * torch.exp(-z64 * z64 / 2) / math.sqrt(2 * math.pi)
+    _, _, db = api.linear_backward(one.expand(1, z.shape[0]).contiguous(), one, z, z.T.contiguous(), "gelu", need=(False, False, True))
+    within(db, slope[:, 0], ((phi + second.abs()) * of_itself)[:, 0] + 2.0 ** -126, F32)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,k,n", [(40, 96, 72), (300, 136, 520), (1, 256, 64), (6, 520, 90)])
 def test_linear_strides_and_orders(rows, k, n):
     """Column-major operands, padded rows, bases off 16 bytes, outputs and residuals inside wider matrices."""
