@@ -390,8 +390,8 @@ redist_status redist_debug_bounds_report(int64_t out[5]);
  * its contents are undefined before and after.  Sums, means and norms are held in 32 bits or more.
  * Errors of all of them: EINVAL (null pointer, size, type, stride), EALIGN (a pointer off its element
  * size, scratch off 256 bytes), EOVERLAP (an output overlaps an input, scratch or another output, except
- * where said), ESCRATCH, EUNSUPPORTED (2^31 rows, columns or stacked matrices; 65536 for the latter),
- * ECUDA.
+ * where said), ESCRATCH, EUNSUPPORTED (more than 2^31 - 512 rows or columns; in the orthogonalisation more than 2^22, or
+ * more than 65535 matrices), ECUDA.
  */
 typedef enum redist_dtype { REDIST_BF16 = 0, REDIST_F16 = 1, REDIST_F32 = 2 } redist_dtype;
 
@@ -420,8 +420,8 @@ typedef struct redist_matrix {
  *   residual        rows x out_features, row-major, or absent; may be `out` itself
  *   out             rows x out_features, row-major
  *   pre             rows x out_features, row-major, or absent: receives z = x w^T + bias for the backward pass
- * Products are accumulated and the epilogue computed in 32 bits; each output is rounded once.  Operands
- * whose lines do not start on 16-byte boundaries are laid out anew in scratch first.
+ * Products are accumulated (16 at a time, every sum cut off to 24 bits) and the epilogue computed in 32 bits; each
+ * output is rounded once.  Operands whose lines do not start on 16-byte boundaries are laid out anew in scratch first.
  *
  * redist_linear_backward -- the gradients.  With dz = dy activation'(pre):
  *   dx = dz w  (rows x in_features)     dw = dz^T x  (out_features x in_features)     dbias = sum of dz's rows
@@ -503,7 +503,8 @@ redist_status redist_layer_norm_backward(const redist_layer_norm *op, const redi
  *     Gaussian; low rank; one direction     0.7       0.45   0.3        0.25    0.22
  *     a part or all of the singular
  *     values equal, the rest noise          0.9       0.75   0.5        0.35    0.3
- * (equal singular values pass the same errors on, where others average).
+ * (equal singular values pass the same errors on, where others average), with sums of up to 2^18.  Longer ones lose more
+ * in their 32-bit accumulation: 2^19 0.4, 2^20 0.6, 2^22 2.3.
  * Intermediates are scaled by powers of two found on the host from the coefficients; coefficients under
  * which a singular value could leave [0, 256] are refused (EINVAL).  A matrix with an infinity or NaN
  * gives NaN throughout, a zero matrix zeros.

@@ -484,6 +484,24 @@ def test_orthogonalize_part_of_the_directions_strong(m, n, part, noise):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("m,n", [(8, 1 << 20), (3 << 18, 16)])
+def test_orthogonalize_long_rows(m, n):
+    """The tensor cores add 16 products at a time and cut each sum off to 24 bits: at most 2^-23 of a sum that is half of the
+    last on average, so A is small by up to k 2^-28; b A + 2 c A A, about 1.4 of that, goes into X, and the steps pass it on."""
+    x = rand(gen(n), m, n, dtype=BF16)
+    got, want = api.orthogonalize(x), orthogonalize64(x)
+    off = float((got.double() - want).norm() / want.norm())
+    assert off < ORTHOGONAL + 2 * max(m, n) * 2.0 ** -28, off
+
+
+@pytest.mark.parametrize("rows,cols", [(1, (1 << 31) - 600), ((1 << 31) - 600, 1), (1, (1 << 22) + 1), ((1 << 22) + 1, 8)])
+def test_orthogonalize_refuses_sums_that_32_bits_do_not_hold(rows, cols):
+    abc = (ctypes.c_float * 3)(*MUON)
+    op = api._Orthogonal(1, rows, cols, 0, 1, 1e-7, 1.0, 0, (0x10000, cols, 1), (0x900000000, cols, 1), 0, 0, ctypes.addressof(abc))
+    assert api.load().redist_orthogonalize(op, None, 0, None) == 10 and api.load().redist_orthogonalize_scratch_bytes(op) == 0
+
+
+@pytest.mark.gpu
 def test_orthogonalize_options_and_strides():
     g = gen(6)
     x = rand(g, 3, 70, 90, dtype=BF16)
