@@ -652,8 +652,8 @@ class _Operators:
             return None, None, 0
         if given is None:
             given = self.strided((need,), (1,), dtype=self.u8, device=device)
-        elif not given.is_cuda or not given.is_contiguous():
-            raise RedistError(1, "scratch has to be a contiguous CUDA tensor")
+        elif given.device != device or not given.is_contiguous():
+            raise RedistError(1, f"scratch has to be a contiguous tensor on {device}")
         return given, given.data_ptr(), given.numel() * given.element_size()
 
 

@@ -830,6 +830,31 @@ def test_the_binding_refuses_before_the_foreign_call():
         assert e.value.status == 1
 
 
+class ScratchElsewhere:
+    """A scratch tensor on another device than the operands, as far as the binding looks at one."""
+    is_cuda, device = True, torch.device("cuda", 1)
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 0x1000000
+
+    def numel(self):
+        return 1 << 20
+
+    def element_size(self):
+        return 1
+
+
+def test_scratch_on_another_device_is_refused():
+    o = api._operators()
+    assert o.scratch(256, ScratchElsewhere(), torch.device("cuda", 1))[1:] == (0x1000000, 1 << 20)
+    with pytest.raises(api.RedistError) as e:
+        o.scratch(256, ScratchElsewhere(), torch.device("cuda", 0))
+    assert e.value.status == 1
+
+
 @pytest.mark.gpu
 def test_the_binding_refuses_mismatched_tensors():
     z = lambda *s, dtype=BF16: torch.zeros(s, dtype=dtype, device="cuda")               # noqa: E731
