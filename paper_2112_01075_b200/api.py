@@ -594,6 +594,11 @@ def shard_global(G, mesh_shape, dtype) -> list:
 # that stream, so the caching allocator hands it on in stream order.  Tensors of another stream than their
 # own need the usual care of the caller (wait_stream, record_stream).
 #
+# Autograd does not see the operators: results require no gradient, whatever the arguments do, and the gradients are
+# calls of their own (:func:`linear_backward`, :func:`layer_norm_backward`), to be put into a
+# ``torch.autograd.Function`` where a graph is wanted.  Tensors of the caller that a call writes get a new version, so that a
+# graph which kept their old contents refuses to go on with the new ones.
+#
 # The smallest calls take less time on the GPU than a few dozen lines of Python: arguments go over as one
 # packed block per call (the layout of the C structures), and scratch is asked for where it is needed.
 
@@ -616,6 +621,7 @@ class _Operators:
 
         lib = load()
         self.torch, self.empty, self.strided = torch, torch.empty, torch.empty_strided
+        self.written = torch.autograd.graph.increment_version
         self.codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
         self.u8, self.f32, self.bf16 = torch.uint8, torch.float32, torch.bfloat16
         self.current_device = self.raw_stream = None
@@ -739,7 +745,8 @@ def _linear_forward(x, w, bias, residual, activation, out, pre, scratch, stream)
     n = w.shape[0]
     device, dtype, shape = x.device, x.dtype, (rows, n)
     at = o.stream(device, stream)
-    if out is None:
+    given = out is not None
+    if not given:
         out = o.matrix(rows, n, dtype, device)
     b, bt = _vector(o, bias, n, device, "bias")
     op = _pack_linear(rows, k, n, _code(o, x, "x"), bt, _activation(activation), 0, x.data_ptr(), *x.stride(),
@@ -751,6 +758,8 @@ def _linear_forward(x, w, bias, residual, activation, out, pre, scratch, stream)
         rc = o.linear_forward(op, sp, sn, at)
     if rc:
         raise RedistError(rc, "redist_linear_forward")
+    if pre is not None or given:
+        o.written([t for t in (pre, out) if t is not None])
     return out
 
 
@@ -774,6 +783,7 @@ def _linear_backward(dy, x, w, pre, activation, need, dx, dw, dbias, scratch, st
     device, dtype = dy.device, dy.dtype
     at = o.stream(device, stream)
     wide, tall, long = (rows, n), (rows, k), (n, k)
+    given = [t for t, wanted in zip((dx, dw, dbias), need) if wanted and t is not None]
     if not need[0]:
         dx = None
     elif dx is None:
@@ -794,6 +804,8 @@ def _linear_backward(dy, x, w, pre, activation, need, dx, dw, dbias, scratch, st
     rc = o.linear_backward(op, g, sp, sn, at)
     if rc:
         raise RedistError(rc, "redist_linear_backward")
+    if given:
+        o.written(given)
     return dx, dw, dbias
 
 
@@ -814,7 +826,8 @@ def _layer_norm_forward(x, gamma, beta, eps, out, stream):
     shape, dtype, device = x.shape, x.dtype, x.device
     rows, cols = shape
     at = o.stream(device, stream)
-    if out is None:
+    given = out is not None
+    if not given:
         out = o.matrix(rows, cols, dtype, device)
     mean, rstd = o.matrix(2, rows, o.f32, device).unbind()
     g, gt = _vector(o, gamma, cols, device, "gamma")
@@ -826,6 +839,8 @@ def _layer_norm_forward(x, gamma, beta, eps, out, stream):
     rc = o.layer_norm_forward(op, at)
     if rc:
         raise RedistError(rc, "redist_layer_norm_forward")
+    if given:
+        o.written(out)
     return out, mean, rstd
 
 
@@ -845,7 +860,8 @@ def _layer_norm_backward(dy, x, gamma, mean, rstd, dx, scratch, stream):
     shape, dtype, device = dy.shape, dy.dtype, dy.device
     rows, cols = shape
     at = o.stream(device, stream)
-    if dx is None:
+    given = dx is not None
+    if not given:
         dx = o.matrix(rows, cols, dtype, device)
     dgamma, dbeta = o.matrix(2, cols, o.f32, device).unbind()
     if mean is None or rstd is None:
@@ -859,6 +875,8 @@ def _layer_norm_backward(dy, x, gamma, mean, rstd, dx, scratch, stream):
     rc = o.layer_norm_backward(op, grads, sp, sn, at)
     if rc:
         raise RedistError(rc, "redist_layer_norm_backward")
+    if given:
+        o.written(dx)
     return dx, dgamma, dbeta
 
 
@@ -887,7 +905,8 @@ def _orthogonalize(x, steps, coefficients, eps, scale, out, scratch, stream):
     shape, device = x.shape, x.device
     at = o.stream(device, stream)
     code = _code(o, x, "x")
-    if out is None:
+    given = out is not None
+    if not given:
         out = o.empty(shape, dtype=o.bf16, device=device)
     elif out.shape != shape or out.dtype is not o.bf16 or out.device != device:
         raise RedistError(1, "out has to be x's shape in bfloat16")
@@ -901,6 +920,8 @@ def _orthogonalize(x, steps, coefficients, eps, scale, out, scratch, stream):
     rc = o.orthogonalize(op, sp, sn, at)
     if rc:
         raise RedistError(rc, "redist_orthogonalize")
+    if given:
+        o.written(out)
     return out
 
 

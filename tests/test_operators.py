@@ -733,6 +733,37 @@ def test_the_wait_for_a_long_sum_grows_with_it():
     assert api.redist_product_timeouts() == before and torch.equal(got, want)
 
 
+@pytest.mark.gpu
+def test_autograd_sees_what_is_written_and_nothing_else():
+    """Results are not part of a graph; a tensor that is written has another version, so that a graph which kept its old
+    contents says so instead of using the new ones."""
+    g = gen(15)
+    z = lambda *s, dtype=BF16: torch.zeros(s, dtype=dtype, device="cuda")               # noqa: E731
+    x, w = rand(g, 40, 64, dtype=BF16).requires_grad_(), rand(g, 72, 64, dtype=BF16).requires_grad_()
+    y, pre, out = api.linear_forward(x, w), z(40, 72), z(40, 72)
+    assert not y.requires_grad and x._version == 0 and w._version == 0
+    wide = z(40, 144)
+    dx, dw, db, norm, dn, orth = z(40, 64), z(72, 64), z(72, dtype=F32), z(40, 64), z(40, 64), z(40, 64)
+    xd, wd = x.detach(), w.detach()
+    for call, written in ((lambda: api.linear_forward(xd, wd, out=out, pre=pre), (out, pre)),
+                          (lambda: api.linear_forward(xd, wd, out=wide[:, 72:]), (wide,)),
+                          (lambda: api.linear_backward(y, xd, wd, dx=dx, dw=dw, dbias=db), (dx, dw, db)),
+                          (lambda: api.layer_norm_forward(xd, out=norm), (norm,)),
+                          (lambda: api.layer_norm_backward(xd, xd, None, z(40, dtype=F32), z(40, dtype=F32), dx=dn), (dn,)),
+                          (lambda: api.orthogonalize(xd, out=orth), (orth,))):
+        before = [t._version for t in written]
+        call()
+        assert all(t._version > b for t, b in zip(written, before))
+        assert xd._version == 0 and wd._version == 0
+    leaf = torch.ones_like(out).requires_grad_()
+    loss = (leaf * out).sum()                                            # keeps `out`
+    api.linear_forward(xd, wd, out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():
+        api.linear_forward(xd, wd, out=torch.empty_like(out))
+
+
 # ---- refusals (no GPU) ----------------------------------------------------------------------------------------------
 
 def linear_op(**kw):
