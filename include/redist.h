@@ -192,6 +192,11 @@ void redist_plan_cache_clear(void);
  *   "test_extra_tx"      >= 0   test only: makes every bounded wait run out (see redist_bulk_timeouts)
  *   "test_shrink_tiles"  >= 0   test only: the checked build takes every tile to be that many bytes shorter
  *                               (see redist_debug_bounds_report); no effect on the normal build
+ *   "test_product_shape" 0..5   test only: the tile on which every matrix product of the operators runs, whatever its
+ *                               size: 256 x 256 or 256 x 128 on a pair of SMs, 128 x 256, 128 x 128 or 128 x 64 on
+ *                               one; 0 (default): chosen by size.  128 x 256 is not used where the result is symmetric
+ *   "test_product_parts" 0..16  test only, with the former: into how many parts the sums are split (the
+ *                               orthogonalisation's never are); 0 (default): one
  * Errors: EINVAL for an unknown name or a value out of range.
  */
 redist_status redist_tuning_set(const char *name, int64_t value);

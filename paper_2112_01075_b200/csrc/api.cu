@@ -86,6 +86,8 @@ const TuningName kTuningNames[] = {
     {"wait_polls", &Tuning::wait_polls, 1, int64_t(1) << 30},
     {"test_extra_tx", &Tuning::test_extra_tx, 0, 1 << 20},
     {"test_shrink_tiles", &Tuning::test_shrink_tiles, 0, 1 << 20},
+    {"test_product_shape", &Tuning::test_product_shape, 0, 5},
+    {"test_product_parts", &Tuning::test_product_parts, 0, 16},
 };
 
 constexpr size_t kCacheEntries = 256;

@@ -35,7 +35,7 @@ redist_status cuda(cudaError_t ce)
 LaunchOptions options()
 {
     const Tuning t = current_tuning();
-    return LaunchOptions{int32_t(t.pdl), uint32_t(t.wait_polls), uint32_t(t.test_extra_tx)};
+    return LaunchOptions{int32_t(t.pdl), uint32_t(t.wait_polls), uint32_t(t.test_extra_tx), int32_t(t.test_product_shape), int32_t(t.test_product_parts)};
 }
 
 i64 round_up(i64 v, i64 to) { return (v + to - 1) / to * to; }
@@ -210,7 +210,7 @@ redist_status check_backward(const redist_linear &q, const redist_linear_grads &
 }
 
 // Scratch of a product whose sum may be split.
-void *parts_of(i64 m, i64 n, i64 k, Pieces &pieces)
+void *parts_of(i64 m, i64 n, i64 k, const LaunchOptions &o, Pieces &pieces)
 {
     Product p = {};
     p.m = m;
@@ -218,7 +218,7 @@ void *parts_of(i64 m, i64 n, i64 k, Pieces &pieces)
     p.k = k;
     p.batch = 1;
     p.kind = EPI_LINEAR;
-    const i64 bytes = product_scratch_bytes(p);
+    const i64 bytes = product_scratch_bytes(p, o);
     return bytes ? pieces.take(bytes) : nullptr;
 }
 
@@ -226,17 +226,17 @@ void *parts_of(i64 m, i64 n, i64 k, Pieces &pieces)
 // at any size; from 17 on x's fragments take registers from the loads of w, and only a small w (whose call is over before
 // the other kernel has set up its tensor memory) is read faster: 24 rows through 1024 -> 1024 4.3 us against 5.9, 4096 ->
 // 130 4.2 against 8.2, but 4096 -> 4096 18 against 12, 16384 -> 1000 19 against 14 and 4096 -> 16384 41 against 27.
-bool few_rows(const redist_linear &q)
+bool few_rows(const redist_linear &q, const LaunchOptions &o)
 {
-    return q.rows <= kFewRows && (q.rows <= 16 || q.in_features * q.out_features <= (i64(1) << 22)) && row_major(q.x, q.rows, q.in_features) && row_major(q.w, q.out_features, q.in_features);
+    return !o.test_shape && q.rows <= kFewRows && (q.rows <= 16 || q.in_features * q.out_features <= (i64(1) << 22)) && row_major(q.x, q.rows, q.in_features) && row_major(q.w, q.out_features, q.in_features);
 }
 
 // Everything another forward call takes from scratch.
 struct Forward {
     Placed x, w;
     void *parts;
-    Forward(const redist_linear &q, Pieces &p)
-        : x(q.x, q.rows, q.in_features, p), w(q.w, q.out_features, q.in_features, p), parts(parts_of(q.rows, q.out_features, q.in_features, p))
+    Forward(const redist_linear &q, const LaunchOptions &o, Pieces &p)
+        : x(q.x, q.rows, q.in_features, p), w(q.w, q.out_features, q.in_features, p), parts(parts_of(q.rows, q.out_features, q.in_features, o, p))
     {
     }
 };
@@ -249,15 +249,15 @@ struct Backward {
     float *partials = nullptr;
     void *parts_dx = nullptr, *parts_dw = nullptr;
     Placed w, x;
-    Backward(const redist_linear &q, const redist_linear_grads &g, Pieces &p)
+    Backward(const redist_linear &q, const redist_linear_grads &g, const LaunchOptions &o, Pieces &p)
         : fresh((g.dx.data || g.dw.data) && (q.activation != REDIST_ACT_NONE || !operand_fits(g.dy.data, lines_of(g.dy, q.rows, q.out_features).ld, 0, 1))),
           w(g.dx.data ? q.w : redist_matrix{nullptr, 1, 1}, g.dx.data ? q.out_features : 0, g.dx.data ? q.in_features : 0, p),
           x(g.dw.data ? q.x : redist_matrix{nullptr, 1, 1}, g.dw.data ? q.rows : 0, g.dw.data ? q.in_features : 0, p)
     {
         ld_dz = fresh ? round_up(q.out_features, 64) : lines_of(g.dy, q.rows, q.out_features).ld;
         if (fresh) dz = p.take(q.rows * ld_dz * 2);
-        if (g.dx.data) parts_dx = parts_of(q.rows, q.in_features, q.out_features, p);
-        if (g.dw.data) parts_dw = parts_of(q.out_features, q.in_features, q.rows, p);
+        if (g.dx.data) parts_dx = parts_of(q.rows, q.in_features, q.out_features, o, p);
+        if (g.dw.data) parts_dw = parts_of(q.out_features, q.in_features, q.rows, o, p);
         if (g.dbias) partials = static_cast<float *>(p.take(i64(column_partial_bytes(q.rows, q.out_features))));
     }
 };
@@ -425,12 +425,13 @@ size_t redist_linear_scratch_bytes(const redist_linear *op, const redist_linear_
 {
     if (!op) return 0;
     Pieces p{0};
+    const LaunchOptions o = options();
     if (!grads) {
-        if (check_forward(*op) != REDIST_OK || op->rows == 0 || few_rows(*op)) return 0;
-        Forward f(*op, p);
+        if (check_forward(*op) != REDIST_OK || op->rows == 0 || few_rows(*op, o)) return 0;
+        Forward f(*op, o, p);
     } else {
         if (check_backward(*op, *grads) != REDIST_OK || op->rows == 0) return 0;
-        Backward b(*op, *grads, p);
+        Backward b(*op, *grads, o, p);
     }
     return size_t(p.used);
 }
@@ -443,17 +444,17 @@ redist_status redist_linear_forward(const redist_linear *op, void *scratch, size
         TRY(check_forward(q));
         if (q.rows == 0) return REDIST_OK;
         const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-        const bool few = few_rows(q), in_place = q.residual.data == q.out.data &&
+        const LaunchOptions o = options();
+        const bool few = few_rows(q, o), in_place = q.residual.data == q.out.data &&
                                                  lines_of(q.residual, q.rows, q.out_features).ld == lines_of(q.out, q.rows, q.out_features).ld;
         Pieces p{uintptr_t(scratch)}, none{0};
-        const Forward f(q, few ? none : p);
+        const Forward f(q, o, few ? none : p);
         const Extent outs[3] = {extent(q.out, q.rows, q.out_features, 2), extent(q.pre, q.pre.data ? q.rows : 0, q.out_features, 2), extent(scratch, p.used)};
         const Extent ins[4] = {extent(q.x, q.rows, q.in_features, 2), extent(q.w, q.out_features, q.in_features, 2),
                                extent(q.bias, q.out_features * type_bytes(q.bias_type)),
                                extent(q.residual, q.residual.data && !in_place ? q.rows : 0, q.out_features, 2)};
         TRY(apart(outs, 3, ins, 4));
         TRY(check_scratch(scratch, scratch_bytes, p.used));
-        const LaunchOptions o = options();
         Product d = product_of(q.rows, q.out_features, q.in_features, q.type, f.x.operand(true), f.w.operand(true), q.out, q.rows, q.out_features);
         d.e.bias = q.bias;
         d.e.bias_type = q.bias_type;
@@ -493,15 +494,15 @@ redist_status redist_linear_backward(const redist_linear *op, const redist_linea
                                            size_t(q.out_features), stream)));
             return g.dbias ? cuda(cudaMemsetAsync(g.dbias, 0, size_t(q.out_features) * 4, stream)) : REDIST_OK;
         }
+        const LaunchOptions o = options();
         Pieces p{uintptr_t(scratch)};
-        Backward b(q, g, p);
+        Backward b(q, g, o, p);
         const Extent outs[4] = {extent(g.dx, g.dx.data ? q.rows : 0, q.in_features, 2), extent(g.dw, g.dw.data ? q.out_features : 0, q.in_features, 2),
                                 extent(g.dbias, q.out_features * 4), extent(scratch, p.used)};
         const Extent ins[4] = {extent(g.dy, q.rows, q.out_features, 2), extent(q.pre, q.activation != REDIST_ACT_NONE ? q.rows : 0, q.out_features, 2),
                                extent(q.w, g.dx.data ? q.out_features : 0, q.in_features, 2), extent(q.x, g.dw.data ? q.rows : 0, q.in_features, 2)};
         TRY(apart(outs, 4, ins, 4));
         TRY(check_scratch(scratch, scratch_bytes, p.used));
-        const LaunchOptions o = options();
         const Lines dy = lines_of(g.dy, q.rows, q.out_features);
         Lay list[3];
         int lays = 0;

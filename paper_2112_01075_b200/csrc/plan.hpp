@@ -70,12 +70,14 @@ struct Tuning {
     int64_t wait_polls = 1 << 18;     // mbarrier polls before a bulk-copy block gives up
     int64_t test_extra_tx = 0;        // test only, see CopyGeometry::test_extra_tx
     int64_t test_shrink_tiles = 0;    // test only: bytes by which the checked build believes every tile to be shorter
+    int64_t test_product_shape = 0;   // test only: tile shape of the operators' products, see LaunchOptions::test_shape
+    int64_t test_product_parts = 0;   // test only: parts of their sums
     bool operator==(const Tuning &o) const
     {
         return bulk == o.bulk && gather == o.gather && zip == o.zip && box == o.box && box_width == o.box_width && zip_walks == o.zip_walks &&
                zip_by_range_slots == o.zip_by_range_slots && item_kb == o.item_kb && l2_hint == o.l2_hint && piece == o.piece && pdl == o.pdl && nvtx == o.nvtx &&
                step_latency == o.step_latency && wait_polls == o.wait_polls && test_extra_tx == o.test_extra_tx &&
-               test_shrink_tiles == o.test_shrink_tiles;
+               test_shrink_tiles == o.test_shrink_tiles && test_product_shape == o.test_product_shape && test_product_parts == o.test_product_parts;
     }
 };
 

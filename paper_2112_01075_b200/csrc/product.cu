@@ -989,8 +989,13 @@ struct Choice {
 // The shape, and into how many parts the sum is split, with the least time by these figures.  Parts are summed by a second
 // kernel (3 us, a chain of loads and the traffic of the 32-bit parts), so splitting is for results of few tiles and long sums:
 // 256 x 256 results of 16384 steps took 80 us unsplit.
-Choice choose(const Product &p, int sms, bool may_split)
+Choice choose(const Product &p, int sms, bool may_split, const LaunchOptions &o)
 {
+    if (o.test_shape && !(p.symmetric && kCosts[o.test_shape - 1].rows < kCosts[o.test_shape - 1].cols)) {
+        const int stage = kBK * kCosts[o.test_shape - 1].slices, steps = int((p.k + stage - 1) / stage);
+        const int k = may_split && o.test_parts ? std::min(o.test_parts, steps) : 1, per = (steps + k - 1) / k;
+        return Choice{Shape(o.test_shape - 1), (steps + per - 1) / per};
+    }
     Choice best{kPair256, 1};
     double least = 1e30;
     for (int s = 0; s < 5; ++s) {
@@ -1030,11 +1035,11 @@ int64_t part_pitch(int64_t n) { return (n + 31) / 32 * 32; }
 
 }  // namespace
 
-int64_t product_scratch_bytes(const Product &p)
+int64_t product_scratch_bytes(const Product &p, const LaunchOptions &o)
 {
     int device = 0, sms = 0;
     if (p.kind != EPI_LINEAR || p.m == 0 || p.n == 0 || current_device(&device, &sms) != cudaSuccess) return 0;
-    const Choice c = choose(p, sms, true);
+    const Choice c = choose(p, sms, true, o);
     return c.splits > 1 ? c.splits * p.m * part_pitch(p.n) * 4 : 0;
 }
 
@@ -1044,8 +1049,8 @@ cudaError_t launch_product(const Product &p, void *scratch, const LaunchOptions 
     int device = 0, sms = 0;
     const cudaError_t ce = current_device(&device, &sms);
     if (ce != cudaSuccess) return ce;
-    if (p.kind == EPI_SCALED) return launch_shape<EPI_SCALED>(p, choose(p, sms, false), o, device, sms, stream);
-    const Choice c = choose(p, sms, true);
+    if (p.kind == EPI_SCALED) return launch_shape<EPI_SCALED>(p, choose(p, sms, false, o), o, device, sms, stream);
+    const Choice c = choose(p, sms, true, o);
     if (c.splits == 1) return launch_shape<EPI_LINEAR>(p, c, o, device, sms, stream);
     Product q = p;
     q.e = Epilogue{};

@@ -69,6 +69,7 @@ struct LaunchOptions {
     int32_t pdl;
     uint32_t wait_polls;
     uint32_t test_extra_tx;
+    int32_t test_shape, test_parts;     // test only: 1 + the Shape, and the parts of a sum, that every product takes; 0: chosen
 };
 
 // Whether an operand may be read as it lies (16-byte boundaries), or has to be laid out anew first.
@@ -77,8 +78,8 @@ bool operand_fits(const void *data, int64_t ld, int64_t batch_stride, int batch)
 // The current device and its number of SMs (asked for once per device).
 cudaError_t current_device(int *device, int *sms);
 
-// Scratch that launch_product needs: the 32-bit parts of a sum that is split (only sizes are read).
-int64_t product_scratch_bytes(const Product &p);
+// Scratch that launch_product needs with the same options: the 32-bit parts of a sum that is split (only sizes are read).
+int64_t product_scratch_bytes(const Product &p, const LaunchOptions &o);
 
 // Asynchronous on `stream`; allocates nothing.
 cudaError_t launch_product(const Product &p, void *scratch, const LaunchOptions &o, cudaStream_t stream);
