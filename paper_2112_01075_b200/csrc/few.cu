@@ -4,11 +4,13 @@
 // two rows of w at a time straight into the fragments of mma.m16n8k16 -- w's rows are the fragment's m, x's rows its n.
 // The order of a sum is free, so eight neighbours serve as columns (2t, 2t+1, 2t+8, 2t+9) of two products, and x is
 // read in the same order.  Four lanes so read 128 bytes of a row with one instruction; with 16 bytes a lane the memory
-// gave a sixth less (1 x 4096 -> 16384: 27.4 against 23.9 us; 16 rows 25.7; 134 MB take 20.5 us at the measured copy
-// rate).  1 x 4096 -> 4096 takes 7.5 us (5.1), of which two are the launch.  Latency of memory bounds it: what counts is
-// the number of loads under way, thus few registers (four blocks per SM) and x fetched only while w is.  The eight warps of a block take turns along the sum (up to 256 bytes of every row each), and where w has few rows a cluster of blocks
-// splits it further; the parts meet in (distributed) shared memory and are added in a fixed order.  One launch, no
-// tensor memory, no tensor maps: what those take to set up is more than the small calls need altogether.
+// gave a sixth less (1 x 4096 -> 16384: 27.4 against 23.9 us with the same weight again, part of which L2 keeps; 16 rows
+// 25.7).  With nothing in L2 that takes 26 us (134 MB take 20.5 at the measured copy rate), 1 x 4096 -> 4096 8.6 (5.1), of
+// which two are the launch.  Latency of memory bounds it: what counts is the number of loads under way, thus few
+// registers (four blocks per SM) and x fetched only while w is.  The eight warps of a block take turns along the sum (up to
+// 256 bytes of every row each), and where w has few rows a cluster of blocks splits it further; the parts meet in
+// (distributed) shared memory and are added in a fixed order.  One launch, no tensor memory, no tensor maps: what those
+// take to set up is more than the small calls need altogether.
 #include "product.h"
 
 #include <algorithm>

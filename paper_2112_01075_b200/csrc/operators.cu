@@ -225,10 +225,12 @@ void *parts_of(i64 m, i64 n, i64 k, const LaunchOptions &o, Pieces &pieces)
 // A forward call of a few rows reads its operands as they lie and needs no scratch.  Up to 16 rows that is the faster way
 // at any size; from 17 on x's fragments take registers from the loads of w, and only a small w (whose call is over before
 // the other kernel has set up its tensor memory) is read faster: 24 rows through 1024 -> 1024 4.3 us against 5.9, 4096 ->
-// 130 4.2 against 8.2, but 4096 -> 4096 18 against 12, 16384 -> 1000 19 against 14 and 4096 -> 16384 41 against 27.
+// 130 4.2 against 8.2, but 4096 -> 4096 18 against 12, 16384 -> 1000 19 against 14 and 4096 -> 16384 41 against 27 (the same
+// weight again and again, so that L2 has what fits).
 bool few_rows(const redist_linear &q, const LaunchOptions &o)
 {
-    return !o.test_shape && q.rows <= kFewRows && (q.rows <= 16 || q.in_features * q.out_features <= (i64(1) << 22)) && row_major(q.x, q.rows, q.in_features) && row_major(q.w, q.out_features, q.in_features);
+    return !o.test_shape && q.rows <= kFewRows && (q.rows <= 16 || q.in_features * q.out_features <= (i64(1) << 22)) &&
+           row_major(q.x, q.rows, q.in_features) && row_major(q.w, q.out_features, q.in_features);
 }
 
 // Everything another forward call takes from scratch.

@@ -9,16 +9,17 @@
 // what lies outside an operand with zeros, and the epilogue stores what lies inside the result.
 //
 // What bounds it: large products the tensor cores and, in long runs, the power they may draw -- 8192 x 4096 -> 8192 with
-// GELU keeps their pipe busy 96 % of the cycles at 1.44 GHz; 16384 x 4096 -> 16384 takes 1510-1560 us (1410-1450
-// TFLOP/s; 1370 is what a library product sustains, 1649 its best), 1575-1660 with bias and GELU, back to back.  Small
+// GELU keeps their pipe busy 96 % of the cycles at 1.43 GHz; 16384 x 4096 -> 16384 takes 1370 us in a run of 50 ms and 1600
+// in one of two seconds (1605 and 1372 TFLOP/s; a library product 1649 at its best and 1372 sustained), with bias and GELU
+// 1385 and 1615.  A stack of 2048 x 2048 squares keeps the pipe busy 64-70 %: 32 stages of sum do not hide the last epilogue.  Small
 // products: the 2 us of a launch, 1 us to the first operands, 0.1-0.15 us per 64 steps of the sum, 1-3 us for the last
 // epilogue (512^3: 4.4 us, 1024^3: 6.0).  Rows of outputs or residuals off 16-byte boundaries cost about 20 us per
 // 4096 x 4096 outputs in the epilogue's stores.
 //
-// Every wait on an mbarrier is bounded, the storing warps' by polls that grow with a tile's sum.  A role whose wait runs out
-// leaves its loop, so the others' waits run out too; products already issued are awaited, as they are in a healthy run, and so are
-// copies in flight (both with limits of their own, which wait_polls does not shorten); then the block counts itself in
-// g_product_timeouts, frees its tensor memory and returns without storing the tile.
+// Every wait on an mbarrier is bounded, the storing warps' by polls that grow with a tile's sum.  A role whose wait runs
+// out leaves its loop, so the others' waits run out too; products already issued are awaited, as they are in a healthy
+// run, and so are copies in flight (both with limits of their own, which wait_polls does not shorten); then the block
+// counts itself in g_product_timeouts, frees its tensor memory and returns without storing the tile.
 #include "product.h"
 
 #include <cuda.h>
@@ -263,7 +264,7 @@ template <int R> __device__ __forceinline__ Tile tile_at(const ProductParams &p,
 // A warp takes its quarter of the lanes (rows) and half of the columns of an accumulator, 32 x 32 values at a time: a
 // lane holds 32 neighbours of one row, computes, rounds and writes them to a piece in shared memory, from where a TMA
 // store takes it (or, where rows are not on 16-byte boundaries, the warp itself, row by row).  Everything 32-bit stays
-// in registers: a 256 x 256 tile takes 2 us (GELU: 2.4 more, bias 0.7, residual 1, pre-activation 0.9), 12 when the
+// in registers: a 256 x 256 tile takes 2 us (GELU 2.3 more, SiLU 2, bias 0.8, residual 2.2, pre-activation 1), 12 when the
 // 32-bit accumulators went through shared memory.  It hides behind the next tile's sum from about 1000 steps on.
 
 // Where the 16 bytes of columns 8 j ... 8 j + 7 of row r of a piece lie (the TMA's 64-byte swizzle).

@@ -298,10 +298,11 @@ template <int L, int CL> __device__ __forceinline__ float2 row_sums(float a, flo
 
 // ---- layer norm, forward -------------------------------------------------------------------------------
 
-// A row is read once and written once: 16384 x 4096 bf16 41 us at the measured copy rate, 49 here (f32: 82 and 87); what is
+// A row is read once and written once: 16384 x 4096 bf16 41 us at the measured copy rate, 50 here (f32: 82 and 88); what is
 // missing is spent on instructions and on the two barriers per row (issue slots 64 % used, three blocks of 256 threads per
-// SM; four where aligned 32-bit rows of 2049 to 4096 columns leave registers for them: 97 -> 87 us, but 48 -> 57 at 2048).  Two barriers because the sum of squares waits for the mean: one pass with a shifted sum would save one, and lose
-// digits where the shift is far from the mean.
+// SM; four where aligned 32-bit rows of 2049 to 4096 columns leave registers for them: 97 -> 87 us, but 48 -> 57 at 2048).
+// Two barriers because the sum of squares waits for the mean: one pass with a shifted sum would save one, and lose digits
+// where the shift is far from the mean.
 // Mean first, then the differences d from it, sum of d^2 and sum of d: the latter is what rounding left in the mean, and
 // corrects both (var = mean d^2 - (mean d)^2), so a mean far larger than the spread costs no digits.
 template <typename T, int L, int NV, bool SHIFT, int CL>
@@ -484,8 +485,8 @@ __global__ void __launch_bounds__(kLong) redist_layer_norm_long_kernel(const Lay
 // With c = dy gamma and xh = (x - mean) rstd: dx = rstd (c - mean(c) - xh mean(c xh)).  A block walks over its rows
 // and keeps the column sums of dy xh and dy in registers; partials holds them per block, gamma's before beta's, and a
 // second kernel adds the blocks' in a fixed order (atomics would not).  16384 x 4096 bf16: 61 us at the measured copy rate,
-// 78 here (with the second kernel's 4); 262144 x 256: 84.  The sums' registers allow two blocks per SM; what they have under way
-// of the next rows lies in shared memory instead.
+// 79 here (with the second kernel's 4); 262144 x 256: 80.  The sums' registers allow two blocks per SM; what they have
+// under way of the next rows lies in shared memory instead.
 template <typename T, int L, int NV, bool SHIFT, int CL>
 __global__ void __launch_bounds__(RowShape<T, L, NV>::kThreads, L <= 32 && NV == 1 ? 4 : L <= 256 ? 2 : 1) redist_layer_norm_grad_kernel(const LayerNorm l, float *partials)
 {
@@ -725,7 +726,8 @@ __global__ void __launch_bounds__(kSumThreads) redist_column_sum_kernel(const fl
 
 constexpr int kLayCols = 256;
 
-// Rows of a block: 128, fewer where that leaves SMs without work, more where the grid would grow beyond its limit.
+// Rows of a block: 128, fewer where that leaves SMs without work (148 of them at four blocks each, written here because
+// scratch is asked for by sizes alone), more where the grid would grow beyond its limit.
 int64_t lay_rows(int64_t rows, int64_t cols)
 {
     int64_t per = 128 * ((rows + 128 * 32768 - 1) / (128 * 32768));
@@ -754,8 +756,9 @@ __global__ void __launch_bounds__(256, 4) redist_lay_kernel(const __grid_constan
     if (lo >= l.rows || int64_t(blockIdx.x) * kLayCols >= l.cols) return;
     const int count = int(min(l.cols - c, int64_t(8)));
     float sums[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    // One row at a time and many warps: two or four rows' loads under way per warp cost registers, thus warps, and were
-    // slower (4096 x 16384 with GELU: 80 us, with four 91; at odd strides 120 and 203).
+    // One row at a time and many warps (four blocks per SM, for which GELU has to do with 64 registers): two or four rows'
+    // loads under way per warp cost registers, thus warps, and were slower (4096 x 16384 with GELU: 80 us, with four 91; at
+    // odd strides 120 and 203).  61 us at the measured copy rate without dz, which adds 20 of them.
     if (count > 0)
         for (int64_t row = lo + w; row < hi; row += 8) {
             const T *src = static_cast<const T *>(l.src) + row * l.ld_src + c, *z = static_cast<const T *>(l.z) + row * l.ld_z + c;
@@ -777,6 +780,9 @@ __global__ void __launch_bounds__(256, 4) redist_lay_kernel(const __grid_constan
                     float at[8];
                     unpack16<T>(y, at);
                     times_slope8(v, at, l.activation);
+                    // dz becomes an operand of two products: 16 bits, as the tensor cores take them with the other operand.
+                    // (bf16 gradients are 2.3e-3 off with it, 1.7e-3 by their own rounding alone; dz in two halves would cost
+                    // both products once more.)  The column sums below take the 32-bit values.
                     u = pack16<T>(v);
                 }
 #pragma unroll
