@@ -91,7 +91,7 @@ template <int N> __device__ __forceinline__ void activate_all(float *v, int act)
     if (act == ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < N; i += 8) gelu8(v + i);
-    } else if (act == ACT_SILU) {
+    } else if (act == ACT_SILU) {                           // (0 below z = -87.3, where it is above -1.1e-36: the reciprocal is flushed)
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] *= reciprocal(1.0f + exp2_fast(v[i] * -1.44269504f));
     } else if (act == ACT_RELU) {
