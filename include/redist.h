@@ -503,9 +503,9 @@ redist_status redist_layer_norm_backward(const redist_layer_norm *op, const redi
  * The products run on 16-bit floats with 32-bit accumulation; X itself is carried from step to step in 22
  * bits, because small singular values grow by a factor of a per step and with them every error made in X.
  * How far results are off the exact iteration, in per cent of the norm (0.17 of it is the rounding of out), for the
- * coefficients of the Muon optimiser (3.4445, -4.7750, 2.0315) and five steps, most seen in 64 matrices each:
- *     min(rows, cols)                       2 to 4    8      16 to 32   64      128 and more
- *     Gaussian; low rank; one direction     0.7       0.45   0.3        0.25    0.22
+ * coefficients of the Muon optimiser (3.4445, -4.7750, 2.0315) and five steps, the most seen in 64 matrices each (8 and 2 of the largest):
+ *     min(rows, cols)                       1 to 4    8      16 to 32   64      128 and more
+ *     Gaussian; low rank; one direction     0.7       0.45   0.32       0.26    0.22
  *     a part or all of the singular
  *     values equal, the rest noise          0.9       0.75   0.5        0.35    0.3
  * (equal singular values pass the same errors on, where others average), with sums of up to 2^18.  Longer ones lose more
