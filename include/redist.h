@@ -528,6 +528,147 @@ typedef struct redist_orthogonal {
 size_t redist_orthogonalize_scratch_bytes(const redist_orthogonal *op);
 redist_status redist_orthogonalize(const redist_orthogonal *op, void *scratch, size_t scratch_bytes, void *cuda_stream);
 
+/* ---- a block of experts, and the bound on a step's gradients ------------------------------------ */
+
+/*
+ * A feed-forward layer whose weights are a set of experts of which every token uses a few: the router's choice and the order of
+ * the rows, tokens moved to their experts' rows and back, and the linear layer with a weight per range of rows.  All sizes
+ * are static (tokens * chosen rows, whatever the choice), only `offsets` and `position` depend on data and stay on the
+ * device, so plans can move every array between shardings.  Rules and errors as above.
+ *
+ * redist_route_forward -- for every row of logits the `chosen` experts with the largest logits, in that order: equal ones by
+ * the lower index, NaN before everything, minus infinity never (a row has empty places then; one of minus infinities only
+ * goes nowhere).
+ *
+ *   tokens >= 0, 1 <= experts <= 1024, 1 <= chosen <= min(experts, 32), tokens * chosen < 2^31
+ *   type            of logits (and dlogits): REDIST_BF16, REDIST_F16 or REDIST_F32
+ *   logits          tokens x experts, row-major
+ *   normalize       0: weights are softmax(logits) at the chosen experts; 1: softmax over the chosen ones only
+ *   weights         tokens x chosen 32-bit floats, contiguous; 0 in empty places
+ *   choice          tokens x chosen 32-bit integers: the expert; -1 in empty places
+ *   position        tokens x chosen 32-bit integers: the row that this place gets when the rows are ordered by expert, within an
+ *                   expert by token; -1 in empty places
+ *   offsets         experts + 1 32-bit integers: rows offsets[e] ... offsets[e + 1] - 1 belong to expert e
+ *
+ * redist_route_backward -- the gradient of weights: with p = the softmax (0 outside the chosen with normalize) and s = sum over
+ * the chosen of weight * dweight:  dlogits = p (dweight at chosen experts, 0 elsewhere, minus s).  What stands in dweights
+ * at empty places does not count.  Of `op` the sizes, logits (unless normalize), weights and choice are read.
+ */
+typedef struct redist_route {
+    int64_t tokens;
+    int32_t experts, chosen, type, normalize;
+    redist_matrix logits;
+    float *weights;
+    int32_t *choice, *position, *offsets;
+} redist_route;
+
+size_t redist_route_scratch_bytes(const redist_route *op);
+redist_status redist_route_forward(const redist_route *op, void *scratch, size_t scratch_bytes, void *cuda_stream);
+redist_status redist_route_backward(const redist_route *op, const float *dweights, const redist_matrix *dlogits, void *cuda_stream);
+
+/*
+ * redist_dispatch_forward, redist_combine_forward -- tokens to rows, and rows back to tokens:
+ *   dispatch:  row[position[t, j]] = token[t]               combine:  token[t] = residual[t] + sum over j of weights[t, j] row[position[t, j]]
+ * and their gradients:
+ *   redist_dispatch_backward:  token[t] = sum over j of row[position[t, j]]   (row: the rows' gradient; token receives the tokens')
+ *   redist_combine_backward:   drow[position[t, j]] = weights[t, j] token[t],  dweights[t, j] = <token[t], row[position[t, j]]>
+ *                              (token: the output's gradient; that of residual is the same)
+ *
+ *   tokens, rows >= 0, cols >= 1, 1 <= chosen <= 32
+ *   type            of all matrices: REDIST_BF16, REDIST_F16 or REDIST_F32
+ *   token, residual tokens x cols, row-major; residual may be absent, or `token` itself
+ *   row, drow       rows x cols, row-major
+ *   position        tokens x chosen 32-bit integers; a place outside 0 ... rows - 1 (as -1) is empty.  No row may be named twice
+ *                   where rows are written (one of the two would win); rows that nobody names are left as they were
+ *   weights         tokens x chosen 32-bit floats (dispatch: not read); dweights the same, 0 in empty places.  NULL in
+ *                   redist_combine_forward: all 1
+ * Sums are in 32 bits in the order of the places, each output is rounded once; dweights' sums have a fixed order.
+ */
+typedef struct redist_move {
+    int64_t tokens, rows, cols;
+    int32_t type, chosen;
+    redist_matrix token, row, residual, drow;
+    const int32_t *position;
+    const float *weights;
+    float *dweights;
+} redist_move;
+
+redist_status redist_dispatch_forward(const redist_move *op, void *cuda_stream);
+redist_status redist_dispatch_backward(const redist_move *op, void *cuda_stream);
+redist_status redist_combine_forward(const redist_move *op, void *cuda_stream);
+redist_status redist_combine_backward(const redist_move *op, void *cuda_stream);
+
+/*
+ * redist_experts_forward -- the linear layer with a weight per range of rows: for offsets[e] <= r < offsets[e + 1]
+ *   out[r] = activation(x[r] w[e]^T + bias[e])
+ * Rows before offsets[0] and from offsets[experts] on are neither read for nor written to any output.
+ *
+ *   rows >= 0, in_features >= 1, out_features >= 1, 1 <= experts <= 65535
+ *   type            REDIST_BF16 or REDIST_F16: x, w, out and pre
+ *   x               rows x in_features, row-major
+ *   w               experts matrices out_features x in_features, all row-major or all column-major, w_stride elements apart
+ *   bias            experts vectors of out_features elements of bias_type (any), bias_stride elements apart, or NULL
+ *   out, pre        rows x out_features, row-major; pre may be absent: receives z = x w^T + bias for the backward pass
+ *   offsets         device; experts + 1 32-bit integers, not decreasing, 0 ... rows.  Others are taken as the nearest that are, so
+ *                   that nothing outside the arrays is touched
+ *
+ * redist_experts_backward -- the gradients.  With dz = dy activation'(pre), over the rows of expert e:
+ *   dx[r] = dz[r] w[e]     dw[e] = sum of dz[r]^T x[r]     dbias[e] = sum of dz[r]
+ *   dy, dx row-major, dw a stack as w (row-major, dw_stride apart), all of `type`; dbias experts x out_features 32-bit floats,
+ *   contiguous; dx, dw and dbias may each be absent.  Experts without rows get zeros in dw and dbias.  Of `op` the
+ *   sizes, types, activation and offsets, x (unless dw is absent), w (unless dx is absent) and pre (unless the activation is NONE)
+ *   are read.  Accumulation and roundings as in the linear layer; dbias sums the unrounded values in a fixed order.
+ */
+typedef struct redist_experts {
+    int64_t rows, in_features, out_features;
+    int32_t experts, type, bias_type, activation;
+    redist_matrix x, w, out, pre;
+    int64_t w_stride, bias_stride;
+    const void *bias;
+    const int32_t *offsets;
+} redist_experts;
+
+typedef struct redist_experts_grads {
+    redist_matrix dy, dx, dw;
+    int64_t dw_stride;
+    float *dbias;
+} redist_experts_grads;
+
+size_t redist_experts_scratch_bytes(const redist_experts *op, const redist_experts_grads *grads); /* NULL: forward */
+redist_status redist_experts_forward(const redist_experts *op, void *scratch, size_t scratch_bytes, void *cuda_stream);
+redist_status redist_experts_backward(const redist_experts *op, const redist_experts_grads *grads, void *scratch,
+                                      size_t scratch_bytes, void *cuda_stream);
+
+/*
+ * redist_clip -- the norm over all elements of a list of tensors, |g| = sqrt(sum of g^2), and the tensors times
+ * min(1, max_norm / (|g| + eps)).
+ *
+ *   tensors         host; count entries, read during the call: data (contiguous, of type, at any element boundary) and out, which
+ *                   receives the product (NULL or data itself: in place; tensors then stay untouched where the factor is 1).
+ *                   Empty tensors are allowed
+ *   max_norm        >= 0, or negative: the norm only (out is not written)
+ *   eps             >= 0 (1e-6 is usual)
+ *   norm            device; one 32-bit float, or NULL
+ * Squares are summed in a fixed order and without overflow or underflow for every finite input (64 bits where 32 would not
+ * hold them).  The factor follows the formula for all inputs: an infinite norm gives 0 (and NaN where an element is
+ * infinite), a NaN gives NaN throughout.  Errors: also EUNSUPPORTED for more than 2^40 elements in a tensor.
+ */
+typedef struct redist_tensor {
+    void *data, *out;
+    int64_t elements;
+    int32_t type, reserved;                           /* reserved: 0 */
+} redist_tensor;
+
+typedef struct redist_clip_op {
+    const redist_tensor *tensors;
+    int64_t count;
+    float max_norm, eps;
+    float *norm;
+} redist_clip_op;
+
+size_t redist_clip_scratch_bytes(const redist_clip_op *op);
+redist_status redist_clip(const redist_clip_op *op, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
 /*
  * redist_product_timeouts -- health counter of the matrix products, as redist_bulk_timeouts is of the bulk
  * copies: thread blocks whose bounded wait ("wait_polls") ran out on the current device.  Such a block

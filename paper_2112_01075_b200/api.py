@@ -44,6 +44,10 @@ EXPORTS = (
     "redist_linear_scratch_bytes", "redist_linear_forward", "redist_linear_backward",
     "redist_layer_norm_forward", "redist_layer_norm_scratch_bytes", "redist_layer_norm_backward",
     "redist_orthogonalize_scratch_bytes", "redist_orthogonalize", "redist_product_timeouts",
+    "redist_route_scratch_bytes", "redist_route_forward", "redist_route_backward",
+    "redist_dispatch_forward", "redist_dispatch_backward", "redist_combine_forward", "redist_combine_backward",
+    "redist_experts_scratch_bytes", "redist_experts_forward", "redist_experts_backward",
+    "redist_clip_scratch_bytes", "redist_clip",
 )
 
 ACTIVATIONS = ("none", "relu", "gelu", "silu")
@@ -107,6 +111,43 @@ class _Orthogonal(ctypes.Structure):
                 ("scale", ctypes.c_float), ("reserved", ctypes.c_int32), ("x", _Matrix), ("out", _Matrix),
                 ("x_batch_stride", ctypes.c_int64), ("out_batch_stride", ctypes.c_int64),
                 ("coefficients", ctypes.c_void_p)]
+
+
+class _Route(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("experts", ctypes.c_int32), ("chosen", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("normalize", ctypes.c_int32), ("logits", _Matrix),
+                ("weights", ctypes.c_void_p), ("choice", ctypes.c_void_p), ("position", ctypes.c_void_p),
+                ("offsets", ctypes.c_void_p)]
+
+
+class _Move(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("chosen", ctypes.c_int32), ("token", _Matrix), ("row", _Matrix),
+                ("residual", _Matrix), ("drow", _Matrix), ("position", ctypes.c_void_p),
+                ("weights", ctypes.c_void_p), ("dweights", ctypes.c_void_p)]
+
+
+class _Experts(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("in_features", ctypes.c_int64), ("out_features", ctypes.c_int64),
+                ("experts", ctypes.c_int32), ("type", ctypes.c_int32), ("bias_type", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("x", _Matrix), ("w", _Matrix), ("out", _Matrix), ("pre", _Matrix),
+                ("w_stride", ctypes.c_int64), ("bias_stride", ctypes.c_int64), ("bias", ctypes.c_void_p),
+                ("offsets", ctypes.c_void_p)]
+
+
+class _ExpertsGrads(ctypes.Structure):
+    _fields_ = [("dy", _Matrix), ("dx", _Matrix), ("dw", _Matrix), ("dw_stride", ctypes.c_int64),
+                ("dbias", ctypes.c_void_p)]
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("elements", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class _Clip(ctypes.Structure):
+    _fields_ = [("tensors", ctypes.POINTER(_Tensor)), ("count", ctypes.c_int64), ("max_norm", ctypes.c_float),
+                ("eps", ctypes.c_float), ("norm", ctypes.c_void_p)]
 
 
 _lib = None
@@ -193,6 +234,17 @@ def load() -> ctypes.CDLL:
     lib.redist_orthogonalize_scratch_bytes.restype = sz
     lib.redist_orthogonalize.argtypes = [ctypes.POINTER(_Orthogonal), vp, sz, vp]
     lib.redist_orthogonalize.restype = i32
+    for name, blocks, scratch in (("route_forward", (_Route,), True), ("experts_forward", (_Experts,), True),
+                                  ("experts_backward", (_Experts, _ExpertsGrads), True), ("clip", (_Clip,), True),
+                                  ("dispatch_forward", (_Move,), False), ("dispatch_backward", (_Move,), False),
+                                  ("combine_forward", (_Move,), False), ("combine_backward", (_Move,), False)):
+        fn = getattr(lib, "redist_" + name)
+        fn.argtypes, fn.restype = [ctypes.POINTER(b) for b in blocks] + ([vp, sz] if scratch else []) + [vp], i32
+    lib.redist_route_backward.argtypes = [ctypes.POINTER(_Route), vp, ctypes.POINTER(_Matrix), vp]
+    lib.redist_route_backward.restype = i32
+    for name, blocks in (("route", (_Route,)), ("experts", (_Experts, _ExpertsGrads)), ("clip", (_Clip,))):
+        fn = getattr(lib, f"redist_{name}_scratch_bytes")
+        fn.argtypes, fn.restype = [ctypes.POINTER(b) for b in blocks], sz
     lib.redist_product_timeouts.argtypes = []
     lib.redist_product_timeouts.restype = i64
     lib.redist_debug_bounds_report.argtypes = [ctypes.POINTER(i64)]
@@ -608,6 +660,13 @@ _pack_linear_grads = struct.Struct(_MATRIX * 3 + "P").pack
 _pack_layer_norm = struct.Struct("2q2ifi" + _MATRIX * 2 + "4P").pack
 _pack_layer_norm_grads = struct.Struct(_MATRIX * 2 + "2P").pack
 _pack_orthogonal = struct.Struct("3q2idfi" + _MATRIX * 2 + "2qP").pack
+_pack_route = struct.Struct("q4i" + _MATRIX + "4P").pack
+_pack_matrix = struct.Struct(_MATRIX).pack
+_pack_move = struct.Struct("3q2i" + _MATRIX * 4 + "3P").pack
+_pack_experts = struct.Struct("3q4i" + _MATRIX * 4 + "2q2P").pack
+_pack_experts_grads = struct.Struct(_MATRIX * 3 + "qP").pack
+_pack_tensor = struct.Struct("2Pq2i").pack
+_pack_clip = struct.Struct("Pq2fP").pack
 _ESCRATCH = 5
 
 _ops = None
@@ -623,18 +682,21 @@ class _Operators:
         self.torch, self.empty, self.strided = torch, torch.empty, torch.empty_strided
         self.written = torch.autograd.graph.increment_version
         self.codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-        self.u8, self.f32, self.bf16 = torch.uint8, torch.float32, torch.bfloat16
+        self.u8, self.f32, self.bf16, self.i32 = torch.uint8, torch.float32, torch.bfloat16, torch.int32
         self.current_device = self.raw_stream = None
         if torch.cuda.is_available():
             torch.cuda.init()
             self.current_device, self.raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
         vp, sz = ctypes.c_void_p, ctypes.c_size_t
         for name, blocks, scratch in (("linear_forward", 1, True), ("linear_backward", 2, True), ("layer_norm_forward", 1, False),
-                                      ("layer_norm_backward", 2, True), ("orthogonalize", 1, True)):
+                                      ("layer_norm_backward", 2, True), ("orthogonalize", 1, True), ("route_forward", 1, True),
+                                      ("route_backward", 3, False), ("dispatch_forward", 1, False), ("dispatch_backward", 1, False),
+                                      ("combine_forward", 1, False), ("combine_backward", 1, False), ("experts_forward", 1, True),
+                                      ("experts_backward", 2, True), ("clip", 1, True)):
             fn = lib["redist_" + name]                       # an object of its own: the attribute keeps its types
             fn.argtypes, fn.restype = [vp] * blocks + ([vp, sz] if scratch else []) + [vp], ctypes.c_int32
             setattr(self, name, fn)
-        for name, blocks in (("linear", 2), ("layer_norm", 2), ("orthogonalize", 1)):
+        for name, blocks in (("linear", 2), ("layer_norm", 2), ("orthogonalize", 1), ("route", 1), ("experts", 2), ("clip", 1)):
             fn = lib[f"redist_{name}_scratch_bytes"]
             fn.argtypes, fn.restype = [vp] * blocks, sz
             setattr(self, name + "_scratch_bytes", fn)
@@ -923,6 +985,375 @@ def _orthogonalize(x, steps, coefficients, eps, scale, out, scratch, stream):
     if given:
         o.written(out)
     return out
+
+
+# ---- a block of experts -------------------------------------------------------------------------------
+#
+# Nothing here asks the device for a size: a token has ``k`` places whatever the choice, ``tokens * k`` rows hold them in the
+# order of the experts, and where an expert's rows begin (``offsets``) stays on the device.
+
+
+def _table(o, t, shape, dtype, device, what: str) -> int:
+    """Address of a contiguous tensor."""
+    if t is None:
+        raise RedistError(1, f"{what} is required")
+    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
+        raise RedistError(1, f"{what} has to be a contiguous tensor of {tuple(shape)}, {dtype}, on {device}")
+    return t.data_ptr()
+
+
+def route_forward(logits, k: int, normalize: bool = True, scratch=None, stream=None):
+    """``redist_route_forward``: ``(weights, choice, position, offsets)`` for the ``k`` experts of each token with the largest
+    ``logits`` (tokens, experts) -- ties to the lower index, minus infinity never.
+
+    ``weights`` (tokens, k) float32: softmax over the chosen experts, or, without ``normalize``, over all of them;
+    ``choice`` (tokens, k) int32: the experts, -1 in places that stay empty; ``position`` (tokens, k) int32: the places'
+    rows in the order of the experts (-1); ``offsets`` (experts + 1,) int32: where each expert's rows begin."""
+    if stream is not None:
+        with _allocating(stream):
+            return _route_forward(logits, k, normalize, scratch, stream)
+    return _route_forward(logits, k, normalize, scratch, None)
+
+
+def _route_forward(logits, k, normalize, scratch, stream):
+    o = _ops or _operators()
+    if logits.dim() != 2:
+        _not_matrices(logits=logits)
+    tokens, experts = logits.shape
+    if not 1 <= k <= experts:
+        raise RedistError(1, f"1 to {experts} experts can be chosen, not {k}")
+    device = logits.device
+    at = o.stream(device, stream)
+    weights = o.matrix(tokens, k, o.f32, device)
+    choice, position = o.strided((2, tokens, k), (tokens * k, k, 1), dtype=o.i32, device=device).unbind()
+    offsets = o.strided((experts + 1,), (1,), dtype=o.i32, device=device)
+    op = _pack_route(tokens, experts, k, _code(o, logits, "logits"), 1 if normalize else 0, logits.data_ptr(), *logits.stride(),
+                     weights.data_ptr(), choice.data_ptr(), position.data_ptr(), offsets.data_ptr())
+    keep, sp, sn = o.scratch(o.route_scratch_bytes(op), scratch, device)
+    rc = o.route_forward(op, sp, sn, at)
+    if rc:
+        raise RedistError(rc, "redist_route_forward")
+    return weights, choice, position, offsets
+
+
+def route_backward(dweights, logits, weights, choice, normalize: bool = True, dlogits=None, stream=None):
+    """``redist_route_backward``: ``dlogits`` (tokens, experts), of the type of ``logits``, from the gradient ``dweights``
+    (tokens, k) float32 of the forward pass's ``weights``."""
+    if stream is not None:
+        with _allocating(stream):
+            return _route_backward(dweights, logits, weights, choice, normalize, dlogits, stream)
+    return _route_backward(dweights, logits, weights, choice, normalize, dlogits, None)
+
+
+def _route_backward(dweights, logits, weights, choice, normalize, dlogits, stream):
+    o = _ops or _operators()
+    if logits.dim() != 2 or choice.dim() != 2:
+        _not_matrices(logits=logits, choice=choice)
+    shape, dtype, device = logits.shape, logits.dtype, logits.device
+    tokens, experts = shape
+    k = choice.shape[1]
+    if not 1 <= k <= experts:
+        raise RedistError(1, f"1 to {experts} experts can be chosen, not {k}")
+    at = o.stream(device, stream)
+    given = dlogits is not None
+    if not given:
+        dlogits = o.matrix(tokens, experts, dtype, device)
+    places = (tokens, k)
+    op = _pack_route(tokens, experts, k, _code(o, logits, "logits"), 1 if normalize else 0, logits.data_ptr(), *logits.stride(),
+                     _table(o, weights, places, o.f32, device, "weights"), _table(o, choice, places, o.i32, device, "choice"), 0, 0)
+    rc = o.route_backward(op, _table(o, dweights, places, o.f32, device, "dweights"), _pack_matrix(*_matrix(dlogits, shape, dtype, device, "dlogits")), at)
+    if rc:
+        raise RedistError(rc, "redist_route_backward")
+    if given:
+        o.written(dlogits)
+    return dlogits
+
+
+def _move(o, token, row, position, residual=None, drow=None, weights=None, dweights=None):
+    """The packed block of the four moves."""
+    if token.dim() != 2 or row.dim() != 2 or position.dim() != 2:
+        _not_matrices(tokens=token, rows=row, position=position)
+    (tokens, cols), dtype, device = token.shape, token.dtype, token.device
+    rows, k = row.shape[0], position.shape[1]
+    places, wide = (tokens, k), (rows, cols)
+    return _pack_move(tokens, rows, cols, _code(o, token, "tokens"), k, token.data_ptr(), *token.stride(), *_matrix(row, wide, dtype, device, "rows"),
+                      *_matrix(residual, (tokens, cols), dtype, device, "residual"), *_matrix(drow, wide, dtype, device, "drows"),
+                      _table(o, position, places, o.i32, device, "position"),
+                      0 if weights is None else _table(o, weights, places, o.f32, device, "weights"),
+                      0 if dweights is None else _table(o, dweights, places, o.f32, device, "dweights"))
+
+
+def dispatch_forward(x, position, out=None, stream=None):
+    """``redist_dispatch_forward``: every token of ``x`` (tokens, cols) in the rows that ``position`` (tokens, k) int32 names for
+    it.  Returns ``out``, by default (tokens * k, cols); rows that nobody names are left as they were (in a new tensor: undefined).
+    Row-major matrices in bfloat16, float16 or float32."""
+    if stream is not None:
+        with _allocating(stream):
+            return _dispatch_forward(x, position, out, stream)
+    return _dispatch_forward(x, position, out, None)
+
+
+def _dispatch_forward(x, position, out, stream):
+    o = _ops or _operators()
+    at = o.stream(x.device, stream)
+    given = out is not None
+    if not given:
+        if x.dim() != 2:
+            _not_matrices(x=x)
+        out = o.matrix(position.numel(), x.shape[1], x.dtype, x.device)
+    rc = o.dispatch_forward(_move(o, x, out, position), at)
+    if rc:
+        raise RedistError(rc, "redist_dispatch_forward")
+    if given:
+        o.written(out)
+    return out
+
+
+def dispatch_backward(drows, position, dx=None, stream=None):
+    """``redist_dispatch_backward``: ``dx`` (tokens, cols), a token's sum of its rows of ``drows`` (rows, cols)."""
+    if stream is not None:
+        with _allocating(stream):
+            return _dispatch_backward(drows, position, dx, stream)
+    return _dispatch_backward(drows, position, dx, None)
+
+
+def _dispatch_backward(drows, position, dx, stream):
+    o = _ops or _operators()
+    at = o.stream(drows.device, stream)
+    given = dx is not None
+    if not given:
+        if drows.dim() != 2:
+            _not_matrices(drows=drows)
+        dx = o.matrix(position.shape[0], drows.shape[1], drows.dtype, drows.device)
+    rc = o.dispatch_backward(_move(o, dx, drows, position), at)
+    if rc:
+        raise RedistError(rc, "redist_dispatch_backward")
+    if given:
+        o.written(dx)
+    return dx
+
+
+def combine_forward(rows, position, weights=None, residual=None, out=None, stream=None):
+    """``redist_combine_forward``: ``residual`` + the sum over a token's places of ``weights`` (tokens, k) float32 times the row of
+    ``rows`` (rows, cols) that ``position`` names; without ``weights`` the plain sum.  ``out`` may be ``residual`` itself."""
+    if stream is not None:
+        with _allocating(stream):
+            return _combine_forward(rows, position, weights, residual, out, stream)
+    return _combine_forward(rows, position, weights, residual, out, None)
+
+
+def _combine_forward(rows, position, weights, residual, out, stream):
+    o = _ops or _operators()
+    at = o.stream(rows.device, stream)
+    given = out is not None
+    if not given:
+        if rows.dim() != 2:
+            _not_matrices(rows=rows)
+        out = o.matrix(position.shape[0], rows.shape[1], rows.dtype, rows.device)
+    rc = o.combine_forward(_move(o, out, rows, position, residual, None, weights), at)
+    if rc:
+        raise RedistError(rc, "redist_combine_forward")
+    if given:
+        o.written(out)
+    return out
+
+
+def combine_backward(dy, rows, position, weights, drows=None, stream=None):
+    """``redist_combine_backward``: ``(drows, dweights)`` -- ``weights`` times a token's ``dy`` (tokens, cols) in its rows, and the
+    product of ``dy`` with each of them (float32, 0 in empty places).  Rows of ``drows`` that nobody names are left as they
+    were (in a new tensor: undefined)."""
+    if stream is not None:
+        with _allocating(stream):
+            return _combine_backward(dy, rows, position, weights, drows, stream)
+    return _combine_backward(dy, rows, position, weights, drows, None)
+
+
+def _combine_backward(dy, rows, position, weights, drows, stream):
+    o = _ops or _operators()
+    at = o.stream(dy.device, stream)
+    given = drows is not None
+    if not given:
+        if rows.dim() != 2:
+            _not_matrices(rows=rows)
+        drows = o.matrix(rows.shape[0], rows.shape[1], rows.dtype, rows.device)
+    if position.dim() != 2:
+        _not_matrices(position=position)
+    dweights = o.matrix(position.shape[0], position.shape[1], o.f32, dy.device)
+    rc = o.combine_backward(_move(o, dy, rows, position, None, drows, weights, dweights), at)
+    if rc:
+        raise RedistError(rc, "redist_combine_backward")
+    if given:
+        o.written(drows)
+    return drows, dweights
+
+
+def _stack(t, shape, dtype, device, what: str):
+    """``t`` as the fields of a redist_matrix and the distance from matrix to matrix, checked."""
+    if t is None:
+        return (0, 0, 0), 0
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        raise RedistError(1, f"{what} has to be {tuple(shape)} of {dtype} on {device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    apart, a, b = t.stride()
+    return (t.data_ptr(), a, b), apart
+
+
+def _not_stacks(**tensors) -> None:
+    for name, t in tensors.items():
+        if t.dim() != 3:
+            raise RedistError(1, f"{name} has to be a stack of matrices, not of {t.dim()} dimensions")
+
+
+def experts_forward(x, w, offsets, bias=None, activation: str = "none", out=None, pre=None, scratch=None, stream=None):
+    """``redist_experts_forward``: the linear layer with a weight per range of rows, ``activation(x[r] @ w[e].T + bias[e])`` for
+    rows ``offsets[e]`` to ``offsets[e + 1]``.
+
+    ``x`` (rows, in) and ``w`` (experts, out, in), bfloat16 or float16; ``offsets`` (experts + 1,) int32 on the device, not
+    decreasing; ``bias`` (experts, out) of any type; ``pre`` (rows, out), if given, receives ``x @ w.T + bias``.  Returns
+    ``out`` (rows, out); rows of no expert are left as they were (in a new tensor: undefined)."""
+    if stream is not None:
+        with _allocating(stream):
+            return _experts_forward(x, w, offsets, bias, activation, out, pre, scratch, stream)
+    return _experts_forward(x, w, offsets, bias, activation, out, pre, scratch, None)
+
+
+def _experts_forward(x, w, offsets, bias, activation, out, pre, scratch, stream):
+    o = _ops or _operators()
+    if x.dim() != 2 or w.dim() != 3:
+        _not_matrices(x=x)
+        _not_stacks(w=w)
+    rows, k = x.shape
+    experts, n = w.shape[0], w.shape[1]
+    device, dtype, shape = x.device, x.dtype, (rows, n)
+    at = o.stream(device, stream)
+    given = out is not None
+    if not given:
+        out = o.matrix(rows, n, dtype, device)
+    b, bt, bs = 0, 0, 0
+    if bias is not None:
+        if bias.shape != (experts, n) or bias.device != device or (n > 1 and bias.stride(1) != 1):
+            raise RedistError(1, f"bias has to be {experts} x {n} with contiguous rows on {device}")
+        b, bt, bs = bias.data_ptr(), _code(o, bias, "bias"), bias.stride(0)
+    weight, apart = _stack(w, (experts, n, k), dtype, device, "w")
+    op = _pack_experts(rows, k, n, experts, _code(o, x, "x"), bt, _activation(activation), x.data_ptr(), *x.stride(), *weight,
+                       *_matrix(out, shape, dtype, device, "out"), *_matrix(pre, shape, dtype, device, "pre"), apart, bs, b,
+                       _table(o, offsets, (experts + 1,), o.i32, device, "offsets"))
+    rc = o.experts_forward(op, None, 0, at) if scratch is None else _ESCRATCH
+    if rc == _ESCRATCH:                                      # operands off 16-byte boundaries: rare
+        keep, sp, sn = o.scratch(o.experts_scratch_bytes(op, None), scratch, device)
+        rc = o.experts_forward(op, sp, sn, at)
+    if rc:
+        raise RedistError(rc, "redist_experts_forward")
+    if pre is not None or given:
+        o.written([t for t in (pre, out if given else None) if t is not None])
+    return out
+
+
+def experts_backward(dy, x, w, offsets, pre=None, activation: str = "none", need=(True, True, True), dx=None, dw=None, dbias=None,
+                     scratch=None, stream=None):
+    """``redist_experts_backward``: ``(dx, dw, dbias)``, the gradients of :func:`experts_forward`; ``need`` says which of them are
+    wanted.  dx (rows, in) and dw (experts, out, in) have the type of ``dy``, dbias (experts, out) is float32.  Experts
+    without rows get zeros; rows of no expert are left as they were in dx (in a new tensor: undefined)."""
+    if stream is not None:
+        with _allocating(stream):
+            return _experts_backward(dy, x, w, offsets, pre, activation, need, dx, dw, dbias, scratch, stream)
+    return _experts_backward(dy, x, w, offsets, pre, activation, need, dx, dw, dbias, scratch, None)
+
+
+def _experts_backward(dy, x, w, offsets, pre, activation, need, dx, dw, dbias, scratch, stream):
+    o = _ops or _operators()
+    if dy.dim() != 2 or x.dim() != 2 or w.dim() != 3:
+        _not_matrices(dy=dy, x=x)
+        _not_stacks(w=w)
+    rows, n = dy.shape
+    experts, k = w.shape[0], x.shape[1]
+    device, dtype = dy.device, dy.dtype
+    at = o.stream(device, stream)
+    wide, tall, stack = (rows, n), (rows, k), (experts, n, k)
+    given = [t for t, wanted in zip((dx, dw, dbias), need) if wanted and t is not None]
+    if not need[0]:
+        dx = None
+    elif dx is None:
+        dx = o.matrix(rows, k, dtype, device)
+    if not need[1]:
+        dw = None
+    elif dw is None:
+        dw = o.strided(stack, (n * k, k, 1), dtype=dtype, device=device)
+    if not need[2]:
+        dbias = None
+    elif dbias is None:
+        dbias = o.matrix(experts, n, o.f32, device)
+    weight, apart = _stack(w, stack, dtype, device, "w")
+    grad, grad_apart = _stack(dw, stack, dtype, device, "dw")
+    op = _pack_experts(rows, k, n, experts, _code(o, dy, "dy"), 0, _activation(activation), *_matrix(x, tall, dtype, device, "x"), *weight, 0, 0, 0,
+                       *_matrix(pre, wide, dtype, device, "pre"), apart, 0, 0, _table(o, offsets, (experts + 1,), o.i32, device, "offsets"))
+    g = _pack_experts_grads(dy.data_ptr(), *dy.stride(), *_matrix(dx, tall, dtype, device, "dx"), *grad, grad_apart,
+                            0 if dbias is None else _table(o, dbias, (experts, n), o.f32, device, "dbias"))
+    keep, sp, sn = o.scratch(o.experts_scratch_bytes(op, g), scratch, device)
+    rc = o.experts_backward(op, g, sp, sn, at)
+    if rc:
+        raise RedistError(rc, "redist_experts_backward")
+    if given:
+        o.written(given)
+    return dx, dw, dbias
+
+
+# ---- the bound on a step's gradients ---------------------------------------------------------------------
+
+
+def _dense(t) -> bool:
+    """Whether the elements of ``t`` lie side by side, in whatever order of the dimensions."""
+    if t.is_contiguous():
+        return True
+    return t.permute(sorted(range(t.dim()), key=lambda d: (-t.stride(d), -t.shape[d]))).is_contiguous()
+
+
+def clip_gradients(tensors, max_norm, eps: float = 1e-6, out=None, scratch=None, stream=None):
+    """``redist_clip``: the norm over all elements of all ``tensors`` -- a 0-dimensional float32 tensor, returned -- and the
+    tensors times ``min(1, max_norm / (norm + eps))``, in place or into the tensors of ``out`` (same shapes, strides and
+    types).  ``max_norm`` None: the norm only.  bfloat16, float16 and float32 may be mixed; any shape whose elements lie
+    side by side."""
+    if stream is not None:
+        with _allocating(stream):
+            return _clip_gradients(tensors, max_norm, eps, out, scratch, stream)
+    return _clip_gradients(tensors, max_norm, eps, out, scratch, None)
+
+
+def _clip_gradients(tensors, max_norm, eps, out, scratch, stream):
+    o = _ops or _operators()
+    tensors = list(tensors)
+    if max_norm is not None and not max_norm >= 0:
+        raise RedistError(1, f"max_norm is not negative, or None, not {max_norm}")
+    if out is not None:
+        out = list(out)
+        if len(out) != len(tensors):
+            raise RedistError(1, f"{len(tensors)} tensors, but {len(out)} to write")
+    device = tensors[0].device if tensors else o.torch.device("cuda", o.current_device() if o.current_device else 0)
+    at = o.stream(device, stream)
+    codes, blocks = o.codes, []
+    for i, t in enumerate(tensors):
+        code = codes.get(t.dtype)
+        if code is None:
+            _code(o, t, "a gradient")
+        if t.device != device or not _dense(t):
+            raise RedistError(1, f"gradients have to be on one device with their elements side by side; number {i} is not")
+        to = 0
+        if out is not None:
+            v = out[i]
+            if v.shape != t.shape or v.dtype is not t.dtype or v.device != device or v.stride() != t.stride():
+                raise RedistError(1, f"out has to be like the gradients; number {i} is not")
+            to = v.data_ptr()
+        blocks.append(_pack_tensor(t.data_ptr(), to, t.numel(), code, 0))
+    norm = o.strided((), (), dtype=o.f32, device=device)
+    table = b"".join(blocks)
+    held = ctypes.c_char_p(table)
+    op = _pack_clip(ctypes.cast(held, ctypes.c_void_p).value or 0, len(tensors), -1.0 if max_norm is None else max_norm, eps, norm.data_ptr())
+    keep, sp, sn = o.scratch(o.clip_scratch_bytes(op), scratch, device)
+    rc = o.clip(op, sp, sn, at)
+    if rc:
+        raise RedistError(rc, "redist_clip")
+    if max_norm is not None and tensors:
+        o.written(tensors if out is None else out)
+    return norm
 
 
 def redist_product_timeouts() -> int:

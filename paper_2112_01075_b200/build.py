@@ -26,8 +26,9 @@ OBJ = os.path.join(HERE, "_obj")
 LIB = os.path.join(HERE, "libredist_b200.so")
 LIB_BOUNDS = os.path.join(HERE, "libredist_b200_bounds.so")
 SOURCES = ["api.cu", "kernels.cu", "static_scratch.cu", "planner.cpp", "descriptor.cpp", "describe.cpp", "multi_gpu.cpp",
-           "operators.cu", "product.cu", "few.cu", "rows.cu"]
-HEADERS = ["plan.hpp", "copy_params.h", "kernels.h", "product.h", "rows.h", "elements.cuh", "activation.cuh"]
+           "operators.cu", "product.cu", "few.cu", "rows.cu", "expert_operators.cu", "experts.cu", "routing.cu", "clip.cu"]
+HEADERS = ["plan.hpp", "copy_params.h", "kernels.h", "product.h", "rows.h", "elements.cuh", "activation.cuh", "tensor_core.cuh", "checks.h",
+           "experts.h", "routing.h", "clip.h"]
 CHECKED = ["kernels.cu"]          # sources that differ in the checked build
 # (source, object name, defines): the kernels compile as three parts side by side (see REDIST_PART in kernels.cu)
 UNITS = [(s, os.path.splitext(s)[0], []) for s in SOURCES if s != "kernels.cu"] + \

@@ -1,0 +1,765 @@
+// Matrix products grouped by expert: ranges of rows, each with a weight of its own (out), or each summed into one (gradients).
+//
+// The weight's features are the tall side of a tile (128 of them per SM, on the lanes of tensor memory), an expert's rows the
+// other (its columns): the tensor cores' time is proportional to the columns, so a range that ends inside a tile costs its
+// own length, rounded up to 16 (32 for a pair of SMs), and a few rows read a weight no differently from many.  An expert's
+// rows are cut into tiles of nearly equal width.  Blocks stay on their SM and take tiles in turn; every warp walks along the
+// offsets by itself, 32 experts at a time.  The rest is that of the plain product (product.cu): TMA ring, two accumulators,
+// eight storing warps, bounded waits.  Outputs leave tensor memory transposed: the fragments are turned by stmatrix.trans on
+// their way to the pieces that the TMA stores; where a range ends within a piece the warp stores its rows itself, so
+// neighbours' rows are not touched.
+// Sums over an expert's rows end in the middle of a box: every expert has tensor maps of its own, which end with its rows,
+// so that what follows is read as zeros -- products with the neighbours' rows would not do: zero times their infinities.
+#include "experts.h"
+
+#include <cuda.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cstring>
+
+#include "activation.cuh"
+#include "elements.cuh"
+#include "rows.h"
+#include "tensor_core.cuh"
+
+namespace redist {
+
+namespace {
+
+constexpr int kThreads = 384;           // warps 0 and 3 load, warp 1 multiplies, warp 2 owns tensor memory, warps 4-11 store
+constexpr int kRing = 196608;           // bytes of the ring of stages
+constexpr int kPiece = 2048;            // 32 rows of 32 16-bit outputs: 64 bytes, 64-byte swizzle
+constexpr int kEpiBytes = 8 * 2 * kPiece;
+constexpr int kBarBytes = 256;
+constexpr int kSmem = 1024 + kRing + kEpiBytes + kBarBytes;
+constexpr int kMostStages = 12;
+constexpr uint32_t kDrainPolls = 1 << 16, kCopyPolls = 1 << 10;         // as in the plain product
+
+__device__ unsigned int g_grouped_timeouts = 0;
+
+struct GroupedParams {
+    int32_t rows, m, n, experts, k_blocks;
+    int32_t tiles_m, tiles_n;           // tiles_n: SUMS only
+    int32_t a_along_rows, b_along_rows;
+    uint32_t idesc, wait_polls, test_extra_tx;
+    int32_t aligned_out, activation, type;
+    const int32_t *offsets;
+    const CUtensorMap *maps;            // SUMS: of a and b for every expert
+    void *out, *pre;
+    int64_t ld_out, out_batch, ld_pre, bias_stride;
+    const void *bias;
+    int32_t bias_type;
+};
+
+__device__ __forceinline__ int offset_at(const GroupedParams &p, int e) { return min(max(__ldg(p.offsets + e), 0), p.rows); }
+
+// ---- tiles ---------------------------------------------------------------------------------------
+
+struct GroupedTile {
+    int expert, tm, row0, count, k0, steps;     // rows row0 ... row0 + count - 1 of the result (SUMS: its rows, and where its sum begins)
+};
+
+// A warp's walk along the tiles, in increasing order.  ROWS: lane i knows the range of expert chunk + i and how many tiles
+// it has up to there.
+template <int CG, int BN, int KB, bool SUMS> struct Walk {
+    const GroupedParams &p;
+    int chunk = -32, lane;
+    int lo = 0, hi = 0, through = 0, before = 0, all = 0, carry = 0;    // before: tiles of earlier chunks; all: of this one
+
+    __device__ __forceinline__ Walk(const GroupedParams &params) : p(params), lane(int(threadIdx.x) & 31) {}
+
+    // The next 32 experts.  Offsets that decrease count as the largest before them.
+    __device__ __forceinline__ void next()
+    {
+        before += all;
+        chunk += 32;
+        const int e = chunk + lane;
+        int start = e < p.experts ? offset_at(p, e) : p.rows;
+        const int end = e < p.experts ? offset_at(p, e + 1) : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, start, d);
+            if (lane >= d) start = max(start, up);
+        }
+        lo = max(start, carry);
+        hi = max(lo, end);
+        carry = __shfl_sync(0xffffffffu, hi, 31);
+        through = e < p.experts ? (hi - lo + BN - 1) / BN * p.tiles_m : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, through, d);
+            if (lane >= d) through += up;
+        }
+        all = __shfl_sync(0xffffffffu, through, 31);
+    }
+
+    // Tile `t`, if there is one; all lanes get the answer.
+    __device__ __forceinline__ bool at(int t, GroupedTile &r)
+    {
+        if constexpr (SUMS) {
+            const int per = p.tiles_m * p.tiles_n;
+            if (t >= per * p.experts) return false;
+            r.expert = t / per;
+            int q = t - r.expert * per;
+            const int group = q / (8 * p.tiles_m), height = min(8, p.tiles_n - group * 8);
+            q -= group * 8 * p.tiles_m;
+            r.row0 = (group * 8 + q % height) * BN;
+            r.count = min(BN, p.n - r.row0);
+            r.tm = q / height;
+            r.k0 = offset_at(p, r.expert);
+            r.steps = (max(0, offset_at(p, r.expert + 1) - r.k0) + KB * kBK - 1) / (KB * kBK);
+            return true;
+        } else {
+            while (t >= before + all) {
+                if (chunk + 32 >= p.experts) return false;
+                next();
+            }
+            const int which = __ffs(__ballot_sync(0xffffffffu, before + through > t)) - 1;
+            const int from = __shfl_sync(0xffffffffu, lo, which), to = __shfl_sync(0xffffffffu, hi, which);
+            const int tiles = (to - from + BN - 1) / BN;
+            int q = t - before - (__shfl_sync(0xffffffffu, through, which) - tiles * p.tiles_m);
+            // columns of tiles in groups of eight, so that the blocks at work at one time share both operands in L2
+            const int group = q / (8 * p.tiles_m), height = min(8, tiles - group * 8);
+            q -= group * 8 * p.tiles_m;
+            const int width = ((to - from + tiles - 1) / tiles + 16 * CG - 1) / (16 * CG) * (16 * CG);
+            r.expert = chunk + which;
+            r.row0 = from + (group * 8 + q % height) * width;
+            r.count = max(0, min(width, to - r.row0));
+            r.tm = q / height;
+            r.k0 = 0;
+            r.steps = p.k_blocks;
+            return true;
+        }
+    }
+    // The columns that the tensor cores compute.
+    static __device__ __forceinline__ int columns(const GroupedTile &r) { return max(16 * CG, (r.count + 16 * CG - 1) / (16 * CG) * (16 * CG)); }
+};
+
+// ---- epilogue --------------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t piece_at(int r, int j) { return uint32_t(r * 64 + ((j ^ ((r >> 1) & 3)) << 4)); }
+
+// 16 lanes x 32 columns of tensor memory, as fragments: registers 4 i, 4 i + 1 are columns 8 i + 2 (lane % 4) and the next of
+// row lane / 4, registers 4 i + 2, 4 i + 3 those of row lane / 4 + 8.
+__device__ __forceinline__ void tmem_load_fragments(uint32_t addr, uint32_t *v)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+struct GroupedPieces {
+    uint8_t *smem;
+    uint32_t addr;
+    int turn = 0;
+
+    // Fills a piece -- rows are the result's rows, 32 of its columns each -- and sends it off.  v: the fragments of lanes 0-15
+    // and 16-31.  `rows` of them are stored, at row0 on; `left`: columns up to the end of the result.
+    template <typename T>
+    __device__ __forceinline__ void put(const float (&v)[32], const CUtensorMap *map, int aligned, void *out, int64_t ld, int lane, int64_t row0,
+                                        int rows, int col0, int left, int z, int64_t batch)
+    {
+        if (aligned) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        }
+        __syncwarp();
+        const uint32_t to = addr + turn * kPiece;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t at = to + piece_at(8 * i + (lane & 7), lane >> 3);
+            asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
+                         ::"r"(at), "r"(pack2<T>(v[4 * i], v[4 * i + 1])), "r"(pack2<T>(v[4 * i + 2], v[4 * i + 3])),
+                           "r"(pack2<T>(v[16 + 4 * i], v[16 + 4 * i + 1])), "r"(pack2<T>(v[16 + 4 * i + 2], v[16 + 4 * i + 3])) : "memory");
+        }
+        if (aligned && rows >= 32) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                             ::"l"(map), "r"(to), "r"(col0), "r"(int(row0)), "r"(z) : "memory");
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+            turn ^= 1;
+            return;
+        }
+        __syncwarp();
+        const uint8_t *piece = smem + turn * kPiece;
+        T *first = static_cast<T *>(out) + z * batch + row0 * ld + col0;
+        if (aligned) {
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                const int r = it * 8 + (lane >> 2), j = lane & 3;
+                if (r >= rows || 8 * j >= left) continue;
+                const uint4 u = *reinterpret_cast<const uint4 *>(piece + piece_at(r, j));
+                T *q = first + r * ld + 8 * j;
+                if (8 * j + 8 <= left) {
+                    *reinterpret_cast<uint4 *>(q) = u;
+                } else {
+                    for (int i = 0; 8 * j + i < left; ++i) q[i] = reinterpret_cast<const T *>(piece + piece_at(r, j))[i];
+                }
+            }
+        } else if (lane < left) {
+            for (int r = 0; r < min(rows, 32); ++r)
+                first[r * ld + lane] = *reinterpret_cast<const T *>(piece + piece_at(r, lane >> 3) + (lane & 7) * 2);
+        }
+        __syncwarp();
+    }
+};
+
+// ---- the kernel ------------------------------------------------------------------------------------
+
+template <int CG, int BN, int KB, bool SUMS>
+__global__ void __launch_bounds__(kThreads, 1)
+redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
+                      const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ GroupedParams p)
+{
+    constexpr int kRowsB = BN / CG;
+    constexpr int kSliceA = 128 * 128, kSliceB = kRowsB * 128, kStageA = KB * kSliceA, kStageB = KB * kSliceB, kStage = kStageA + kStageB;
+    constexpr int kStages = kRing / kStage < kMostStages ? kRing / kStage : kMostStages;
+    constexpr uint32_t kColumns = 2 * BN < 32 ? 32 : 2 * BN;
+    static_assert(8 * (2 * kStages + 5) + 8 <= kBarBytes, "barriers, tensor memory's address and the flag");
+    static_assert((kColumns & (kColumns - 1)) == 0 && kColumns <= 512, "tensor memory is allocated in powers of two");
+    static_assert(!SUMS || kRowsB % 64 == 0, "operands along their rows come in boxes of 64");
+
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
+    uint8_t *ring = raw + (base - smem_addr(raw));
+    const uint32_t bars = base + kRing + kEpiBytes;
+    auto full = [&](int s) { return bars + 8 * s; };
+    auto empty = [&](int s) { return bars + 8 * (kStages + s); };
+    auto acc_full = [&](int b) { return bars + 8 * (2 * kStages + b); };
+    auto acc_free = [&](int b) { return bars + 8 * (2 * kStages + 2 + b); };
+    const uint32_t drained = bars + 8 * (2 * kStages + 4);
+    const uint32_t tmem_at = bars + 8 * (2 * kStages + 5);
+    volatile uint32_t *tmem_word = reinterpret_cast<volatile uint32_t *>(ring + kRing + kEpiBytes + 8 * (2 * kStages + 5));
+    volatile uint32_t *failed = tmem_word + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 1 ? 0 : cluster_rank();
+    const int first = blockIdx.x / CG, step = gridDim.x / CG;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(full(s), 2);                           // both operands' bytes are announced
+            bar_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            bar_init(acc_full(b), 1);
+            bar_init(acc_free(b), 8 * CG);
+        }
+        bar_init(drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *failed = 0;
+    }
+    if (warp == 2) tmem_alloc<CG>(tmem_at, kColumns);
+    fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();
+    fence_after();
+    const uint32_t tmem = *tmem_word;
+    let_next_start();
+    wait_for_previous();
+
+    using Tiles = Walk<CG, BN, KB, SUMS>;
+    Tiles walk(p);
+    GroupedTile at;
+    bool ok = true;
+    if (warp == 0 || warp == 3) {
+        // Loads: warp 0 those of the features, warp 3 those of the rows.
+        const bool second = warp == 3;
+        int stage = 0;
+        uint32_t phase = 0, rounds = 0, polls = p.wait_polls;
+        const CUtensorMap *map = second ? &map_b : &map_a;
+        const int along_rows = SUMS ? 1 : second ? p.b_along_rows : p.a_along_rows;
+        const uint32_t announced = CG * (second ? kStageB : kStageA + p.test_extra_tx);
+        int expert = -1;
+        for (int t = first; walk.at(t, at); t += step) {
+            if (SUMS && at.expert != expert && at.steps) {
+                expert = at.expert;
+                map = p.maps + 2 * expert + second;
+                asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(map) : "memory");
+                __syncwarp();
+            }
+            const int row = second ? at.row0 + int(rank) * (Tiles::columns(at) / CG) : (at.tm * CG + int(rank)) * 128;
+            const int z = SUMS || second ? 0 : at.expert;
+            for (int kb = 0; kb < at.steps; ++kb) {
+                if (!bar_wait(empty(stage), phase ^ 1, polls)) {
+                    ok = false;
+                    polls = 1;
+                }
+                if (elected() && ok) {
+                    const uint32_t to = base + stage * kStage + (second ? kStageA : 0);
+                    const uint32_t bar = CG == 1 ? full(stage) : in_first(full(stage));
+                    if (rank == 0) bar_expect(full(stage), announced);
+#pragma unroll
+                    for (int k = 0; k < KB; ++k) {
+                        const int x = at.k0 + (kb * KB + k) * kBK;
+                        const uint32_t slice = to + k * (second ? kSliceB : kSliceA);
+                        if (!along_rows) {
+                            load_box<CG>(slice, map, bar, x, row, z);
+                        } else {
+                            const int boxes = second ? kRowsB / 64 : 2;
+                            for (int i = 0; i < boxes; ++i) load_box<CG>(slice + i * kBK * 128, map, bar, row + 64 * i, x, z);
+                        }
+                    }
+                }
+                if (ok && ++stage == kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                    rounds = 1;
+                }
+            }
+        }
+        // every stage's last use has to be over before this block may end: its products read, its copies landed
+        const int used = rounds ? kStages : stage;
+        auto use = [&](int i) { return rounds ? (stage + i) % kStages : i; };
+        auto last = [&](int s) { return s < stage ? phase : phase ^ 1; };   // the phase of the stage's last use
+        for (int i = 0; i < used && ok; ++i) ok = bar_wait(empty(use(i)), last(use(i)), p.wait_polls);
+        if (!ok && rank == 0)
+            for (int i = 0; i < used; ++i) bar_wait(full(use(i)), last(use(i)), kCopyPolls);
+        if (!ok && rank != 0)                                             // its copies report to the first block: give
+            for (int i = 0; i < 128; ++i) __nanosleep(1 << 15);           // them 4 ms to land in memory it still owns
+    } else if (warp == 1 && rank == 0) {
+        // Products.
+        int stage = 0;
+        uint32_t phase = 0, polls = p.wait_polls;
+        int use = 0;
+        const int a_along = SUMS ? 1 : p.a_along_rows, b_along = SUMS ? 1 : p.b_along_rows;
+        const uint64_t desc_a = slice_desc(base, a_along), desc_b = slice_desc(base + kStageA, b_along);
+        const uint64_t step_a = a_along ? 2048 >> 4 : 32 >> 4, step_b = b_along ? 2048 >> 4 : 32 >> 4;
+        for (int t = first; walk.at(t, at); t += step, ++use) {
+            const int buf = use & 1;
+            if (!bar_wait(acc_free(buf), ((use >> 1) & 1) ^ 1, polls)) {
+                ok = false;
+                polls = 1;
+            }
+            fence_after();
+            const uint32_t acc = tmem + buf * BN, idesc = p.idesc | uint32_t(Tiles::columns(at) >> 3) << 17;
+            for (int kb = 0; kb < at.steps; ++kb) {
+                if (!bar_wait(full(stage), phase, polls)) {
+                    ok = false;
+                    polls = 1;
+                }
+                fence_after();
+                if (elected() && ok) {
+                    const uint64_t da = desc_a + uint32_t(stage * (kStage >> 4)), db = desc_b + uint32_t(stage * (kStage >> 4));
+#pragma unroll
+                    for (int k = 0; k < KB; ++k)
+#pragma unroll
+                        for (int i = 0; i < kBK / 16; ++i)
+                            mma<CG>(acc, da + k * (kSliceA >> 4) + i * step_a, db + k * (kSliceB >> 4) + i * step_b, idesc, kb > 0 || k + i > 0);
+                    commit<CG>(empty(stage));
+                    if (kb + 1 == at.steps) commit<CG>(acc_full(buf));
+                }
+                if (++stage == kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+            if (at.steps == 0 && elected() && ok) commit<CG>(acc_full(buf));     // an expert without rows: zeros, not from here
+        }
+        if (!ok) {
+            *failed = 1;
+            if constexpr (CG == 2)
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_second(tmem_at + 4)), "r"(1u) : "memory");
+        }
+        // whatever became of the waits: what was issued reads the stages and writes tensor memory, of both blocks of a pair
+        if (elected()) commit<CG>(drained);
+        ok = bar_wait(drained, 0, kDrainPolls) && ok;
+    } else if (warp == 1) {
+        ok = bar_wait(drained, 0, kDrainPolls);                           // reported by the first block
+    } else if (warp >= 4) {
+        // outputs: a warp has 32 features (lanes of tensor memory) and every second piece of 32 columns
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        GroupedPieces pieces{ring + kRing + (warp - 4) * 2 * kPiece, base + kRing + (warp - 4) * 2 * kPiece};
+        int use = 0;
+        for (int t = first; walk.at(t, at); t += step, ++use) {
+            const int b = use & 1;
+            const int col0 = (at.tm * CG + int(rank)) * 128 + quarter * 32, left = p.m - col0;
+            float bias[4] = {};
+            if (!SUMS && p.bias) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int f = i * 8 + (lane >> 2);
+                    if (f < left) bias[i] = load_any(p.bias, p.bias_type, at.expert * p.bias_stride + col0 + f);
+                }
+            }
+            // This wait is for a whole tile's sum: the polls again for every 512 stages of it (0.4 ms at most), unless the
+            // multiplying warp has given up.  One answer for the warp: what follows is for all of its lanes.
+            bool ready = false;
+            for (int turns = 1 + at.steps / 512; turns > 0 && !ready; --turns) {
+                ready = __all_sync(0xffffffffu, bar_wait(acc_full(b), (use >> 1) & 1, p.wait_polls));
+                if (!ready && __any_sync(0xffffffffu, *failed)) break;
+            }
+            if (!ready) {
+                ok = false;
+                break;
+            }
+            fence_after();
+#pragma unroll 1
+            for (int c = half * 32; c < at.count && left > 0; c += 64) {
+                float v[32];
+                if (at.steps) {
+                    uint32_t u[32];
+                    const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + b * BN + c;
+                    tmem_load_fragments(from, u);
+                    tmem_load_fragments(from + (16u << 16), u + 16);
+                    tmem_load_wait();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+                }
+                const int rows = SUMS && p.aligned_out ? 32 : at.count - c;           // (the map of a stack ends with each matrix)
+                const int64_t row0 = at.row0 + c;
+                const int z = SUMS ? at.expert : 0;
+                auto store = [&](const CUtensorMap *map, void *out, int64_t ld) {
+                    if (p.type == T_BF16) pieces.put<__nv_bfloat16>(v, map, p.aligned_out, out, ld, lane, row0, rows, col0, left, z, p.out_batch);
+                    else pieces.put<__half>(v, map, p.aligned_out, out, ld, lane, row0, rows, col0, left, z, p.out_batch);
+                };
+                if constexpr (!SUMS) {
+                    if (p.bias)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] += bias[(i >> 4) * 2 + ((i >> 1) & 1)];
+                    if (p.pre) store(&map_pre, p.pre, p.ld_pre);
+                    activate32(v, p.activation);
+                }
+                store(&map_out, p.out, p.ld_out);
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (CG == 1)
+                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(acc_free(b)) : "memory");
+                else
+                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first(acc_free(b))) : "memory");
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    if (!ok) *failed = 1;
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();
+    fence_after();
+    if (threadIdx.x == 0 && *failed) atomicAdd(&g_grouped_timeouts, 1u);
+    if (warp == 2) tmem_free<CG>(tmem, kColumns);
+}
+
+// The maps of every expert's rows: copies of two that end with its last row.
+__global__ void __launch_bounds__(64) redist_expert_maps_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                                const __grid_constant__ GroupedParams p, CUtensorMap *maps)
+{
+    let_next_start();
+    wait_for_previous();
+    const int which = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31;
+    const int e = blockIdx.x, lo = offset_at(p, e), hi = offset_at(p, e + 1);
+    if (hi <= lo) return;                                   // never used
+    CUtensorMap *to = maps + 2 * e + which;
+    const uint32_t *from = reinterpret_cast<const uint32_t *>(which ? &map_b : &map_a);
+    reinterpret_cast<uint32_t *>(to)[lane] = from[lane];
+    __threadfence();
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("tensormap.replace.tile.global_dim.global.b1024.b32 [%0], 1, %1;" ::"l"(to), "r"(hi) : "memory");
+        asm volatile("fence.proxy.tensormap::generic.release.gpu;" ::: "memory");
+    }
+}
+
+// ---- dz and its sums ---------------------------------------------------------------------------------
+
+constexpr int kSlopeCols = 256;
+
+// Rows of a block of the slope kernel: as few as keep four blocks on each of 148 SMs (written here because scratch is asked for
+// by sizes alone), 8 to 128, more where the grid would grow beyond its limit.
+int64_t slope_rows(int64_t rows, int64_t cols)
+{
+    int64_t per = 128 * ((rows + 128 * 32768 - 1) / (128 * 32768));
+    while (per > 8 && ((rows + per - 1) / per) * ((cols + kSlopeCols - 1) / kSlopeCols) < 4 * 148) per /= 2;
+    return per;
+}
+
+// A block takes `per` rows by 256 columns, and within them one expert's rows after the other; a warp every eighth row, a lane
+// eight neighbours.  Chunk c's sums for expert e are part c + e: both only grow, so no two share one.
+template <typename T, bool ALIGNED> __global__ void __launch_bounds__(256, 4) redist_expert_slope_kernel(const ExpertSlope s, int64_t per)
+{
+    __shared__ float all[8][kSlopeCols];
+    let_next_start();
+    wait_for_previous();
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int64_t c = int64_t(blockIdx.x) * kSlopeCols + lane * 8;
+    const int64_t lo = int64_t(blockIdx.y) * per, hi = min(s.rows, lo + per);
+    const int count = int(min(s.cols - c, int64_t(8)));
+    auto offset = [&](int e) { return int64_t(min(max(int64_t(__ldg(s.offsets + e)), int64_t(0)), s.rows)); };
+    // the first expert that ends behind this block's first row
+    int e = 0;
+    for (int above = s.experts; e < above;) {
+        const int mid = (e + above) >> 1;
+        if (offset(mid + 1) > lo) above = mid;
+        else e = mid + 1;
+    }
+    for (; e < s.experts; ++e) {
+        const int64_t from = max(lo, offset(e)), to = min(hi, offset(e + 1));
+        if (offset(e) >= hi) break;
+        if (from >= to) continue;
+        float sums[8] = {};
+        if (count > 0)
+            for (int64_t row = from + w; row < to; row += 8) {
+                const T *src = static_cast<const T *>(s.dy) + row * s.ld_dy + c, *z = static_cast<const T *>(s.z) + row * s.ld_z + c;
+                uint4 u, y;
+                if (ALIGNED && count >= 8) {
+                    u = *reinterpret_cast<const uint4 *>(src);
+                    if (s.z) y = *reinterpret_cast<const uint4 *>(z);
+                } else {
+                    Blocks a, b = {};
+                    a.load(src, count * 2);
+                    if (s.z) b.load(z, count * 2);
+                    u = a.get(src);
+                    y = b.get(z);
+                }
+                float v[8], at[8];
+                const uint32_t wu[4] = {u.x, u.y, u.z, u.w}, wy[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = unpack2<T>(wu[i]), g = unpack2<T>(wy[i]);
+                    v[2 * i] = f.x;
+                    v[2 * i + 1] = f.y;
+                    at[2 * i] = g.x;
+                    at[2 * i + 1] = g.y;
+                }
+                if (s.z) {
+                    times_slope8(v, at, s.activation);
+                    // dz becomes an operand of two products: 16 bits, as the tensor cores take them (see the linear layer's)
+                    u = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sums[i] += v[i];
+                if (s.dst) *reinterpret_cast<uint4 *>(static_cast<T *>(s.dst) + row * s.ld_dst + c) = u;
+            }
+        if (!s.sums) continue;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) all[w][lane * 8 + i] = sums[i];
+        __syncthreads();
+        const int64_t cc = int64_t(blockIdx.x) * kSlopeCols + threadIdx.x;
+        if (cc < s.cols) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += all[i][threadIdx.x];
+            s.partials[(int64_t(blockIdx.y) + e) * s.cols + cc] = sum;
+        }
+    }
+}
+
+// The sums of an expert: its parts, in the order of the rows; a warp every eighth of them, a lane one column.
+__global__ void __launch_bounds__(256) redist_expert_sums_kernel(const ExpertSlope s, int64_t per)
+{
+    __shared__ float all[8][32];
+    let_next_start();
+    wait_for_previous();
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, e = blockIdx.y;
+    const int64_t c = int64_t(blockIdx.x) * 32 + lane;
+    auto offset = [&](int i) { return min(max(int64_t(__ldg(s.offsets + i)), int64_t(0)), s.rows); };
+    const int64_t from = offset(e), to = offset(e + 1);
+    float sum = 0.0f;
+    if (from < to && c < s.cols) {
+        const int64_t last = (to - 1) / per;
+#pragma unroll 4
+        for (int64_t q = from / per + w; q <= last; q += 8) sum += s.partials[(q + e) * s.cols + c];
+    }
+    all[w][lane] = sum;
+    __syncthreads();
+    if (w == 0 && c < s.cols) {
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += all[i][lane];
+        s.sums[e * s.cols + c] = sum;
+    }
+}
+
+// ---- host --------------------------------------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled()
+{
+    static std::atomic<void *> known{nullptr};
+    void *fn = known.load(std::memory_order_acquire);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return nullptr;
+        known.store(fn, std::memory_order_release);
+    }
+    return reinterpret_cast<EncodeTiled>(fn);
+}
+
+// A map of `depth` arrays of `lines` lines of `line` 16-bit elements, taken in boxes of box_lines x box_line.
+bool make_map(CUtensorMap *map, const void *data, int64_t line, int64_t lines, int64_t depth, int64_t ld, int64_t plane, int box_line, int box_lines,
+              CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promotion)
+{
+    EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[3] = {cuuint64_t(line), cuuint64_t(lines), cuuint64_t(depth)};
+    // strides that are never used: any legal value does
+    const int64_t pitch = lines > 1 ? ld : (line + 7) / 8 * 8, apart = depth > 1 ? plane : pitch;
+    const cuuint64_t strides[2] = {cuuint64_t(pitch) * 2, cuuint64_t(apart) * 2};
+    const cuuint32_t box[3] = {cuuint32_t(box_line), cuuint32_t(box_lines), 1}, one[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void *>(data), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                  promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool make_operand(CUtensorMap *map, const Operand &op, int64_t rows, int64_t cols, int64_t depth, int box_rows)
+{
+    return make_map(map, op.data, op.along_rows ? rows : cols, op.along_rows ? cols : rows, depth, op.ld, op.batch_stride, kBK, op.along_rows ? kBK : box_rows,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+}
+
+bool make_result(CUtensorMap *map, void *data, int64_t rows, int64_t cols, int64_t depth, int64_t ld, int64_t plane)
+{
+    return make_map(map, data, cols, rows, depth, ld, plane, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE);
+}
+
+bool on_16(const void *p, int64_t ld) { return p == nullptr || (uintptr_t(p) % 16 == 0 && ld % 8 == 0); }
+
+template <typename... P, typename... A>
+cudaError_t launch_any(void (*kernel)(P...), dim3 grid, int threads, int smem, int cluster, const LaunchOptions &o, cudaStream_t stream, const A &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(unsigned(threads));
+    cfg.dynamicSmemBytes = size_t(smem);
+    cfg.stream = stream;
+    cudaLaunchAttribute at[2];
+    int n_at = 0;
+    if (cluster > 1) {
+        at[n_at].id = cudaLaunchAttributeClusterDimension;
+        at[n_at].val.clusterDim.x = unsigned(cluster);
+        at[n_at].val.clusterDim.y = 1;
+        at[n_at].val.clusterDim.z = 1;
+        ++n_at;
+    }
+    if (o.pdl) {
+        at[n_at].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[n_at].val.programmaticStreamSerializationAllowed = 1;
+        ++n_at;
+    }
+    cfg.attrs = at;
+    cfg.numAttrs = unsigned(n_at);
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int CG, int BN, int KB, bool SUMS>
+cudaError_t launch(const Grouped &g, void *scratch, const LaunchOptions &o, int device, int sms, cudaStream_t stream)
+{
+    GroupedParams p;
+    std::memset(&p, 0, sizeof p);
+    p.rows = int32_t(g.rows);
+    p.m = int32_t(g.m);
+    p.n = int32_t(g.n);
+    p.experts = g.experts;
+    p.k_blocks = SUMS ? 0 : int32_t((g.k + KB * kBK - 1) / (KB * kBK));
+    p.tiles_m = int32_t((g.m + 128 * CG - 1) / (128 * CG));
+    p.tiles_n = SUMS ? int32_t((g.n + BN - 1) / BN) : 0;
+    p.a_along_rows = g.a.along_rows;
+    p.b_along_rows = g.b.along_rows;
+    const uint32_t format = g.type == T_BF16 ? 1 : 0;
+    // 32-bit accumulators, operand types, operand orders, tile height / 16; the kernel adds the tile's width / 8
+    p.idesc = (1u << 4) | (format << 7) | (format << 10) | (uint32_t(g.a.along_rows) << 15) | (uint32_t(g.b.along_rows) << 16) |
+              (uint32_t(128 * CG >> 4) << 24);
+    p.wait_polls = o.wait_polls;
+    p.test_extra_tx = o.test_extra_tx;
+    p.activation = g.activation;
+    p.type = g.type;
+    p.offsets = g.offsets;
+    p.maps = static_cast<const CUtensorMap *>(scratch);
+    p.out = g.out;
+    p.pre = g.pre;
+    p.ld_out = g.ld_out;
+    p.out_batch = g.out_batch;
+    p.ld_pre = g.ld_pre;
+    p.bias = g.bias;
+    p.bias_type = g.bias_type;
+    p.bias_stride = g.bias_stride;
+    p.aligned_out = on_16(g.out, g.ld_out) && (!SUMS || g.experts == 1 || g.out_batch % 8 == 0) && on_16(g.pre, g.ld_pre);
+
+    // a bound on the tiles: every expert with rows has at most one that is not full
+    const int64_t parts = SUMS ? int64_t(p.tiles_n) * g.experts : std::min<int64_t>(g.experts, g.rows) + g.rows / BN;
+    const int64_t tiles = parts * p.tiles_m;
+    if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
+
+    CUtensorMap ma, mb, mo, mp;
+    const int64_t features = SUMS ? g.n : g.rows, sum = SUMS ? g.rows : g.k;
+    if (!make_operand(&ma, g.a, g.m, sum, SUMS ? 1 : g.experts, 128) || !make_operand(&mb, g.b, features, sum, 1, BN / CG)) return cudaErrorInvalidValue;
+    std::memset(&mo, 0, sizeof mo);
+    std::memset(&mp, 0, sizeof mp);
+    if (p.aligned_out) {
+        if (!make_result(&mo, g.out, features, g.m, SUMS ? g.experts : 1, g.ld_out, g.out_batch)) return cudaErrorInvalidValue;
+        if (g.pre && !make_result(&mp, g.pre, features, g.m, 1, g.ld_pre, 0)) return cudaErrorInvalidValue;
+    }
+    if (SUMS) {
+        const cudaError_t ce = launch_any(redist_expert_maps_kernel, dim3(unsigned(g.experts)), 64, 0, 1, o, stream, ma, mb, p, static_cast<CUtensorMap *>(scratch));
+        if (ce != cudaSuccess) return ce;
+    }
+    auto *kernel = redist_grouped_kernel<CG, BN, KB, SUMS>;
+    static std::atomic<uint64_t> ready{0};                  // devices on which this kernel may use its shared memory
+    if (device >= 64 || !(ready.load(std::memory_order_relaxed) >> device & 1)) {
+        const cudaError_t ce = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (ce != cudaSuccess) return ce;
+        if (device < 64) ready.fetch_or(uint64_t(1) << device, std::memory_order_relaxed);
+    }
+    const int64_t groups = sms / CG;
+    return launch_any(kernel, dim3(unsigned(std::min(tiles, groups) * CG)), kThreads, kSmem, CG, o, stream, ma, mb, mo, mp, p);
+}
+
+}  // namespace
+
+int64_t grouped_scratch_bytes(const Grouped &g) { return g.sums ? int64_t(g.experts) * 2 * int64_t(sizeof(CUtensorMap)) : 0; }
+
+cudaError_t launch_grouped(const Grouped &g, void *scratch, const LaunchOptions &o, cudaStream_t stream)
+{
+    if (!g.sums && g.rows == 0) return cudaSuccess;
+    int device = 0, sms = 0;
+    const cudaError_t ce = current_device(&device, &sms);
+    if (ce != cudaSuccess) return ce;
+    if (g.sums) return launch<1, 128, 2, true>(g, scratch, o, device, sms, stream);
+    return launch<1, 128, 2, false>(g, scratch, o, device, sms, stream);
+}
+
+int64_t expert_partial_bytes(int64_t rows, int64_t cols, int experts)
+{
+    const int64_t per = slope_rows(rows, cols);
+    return ((rows + per - 1) / per + experts) * cols * 4;
+}
+
+cudaError_t launch_expert_slope(const ExpertSlope &s, const LaunchOptions &o, cudaStream_t stream)
+{
+    const int64_t per = slope_rows(s.rows, s.cols);
+    if (s.rows > 0) {
+        const dim3 grid(unsigned((s.cols + kSlopeCols - 1) / kSlopeCols), unsigned((s.rows + per - 1) / per));
+        const bool aligned = on_16(s.dy, s.ld_dy) && on_16(s.z, s.ld_z);
+        cudaError_t ce;
+        if (s.type == T_BF16)
+            ce = aligned ? launch_any(redist_expert_slope_kernel<__nv_bfloat16, true>, grid, 256, 0, 1, o, stream, s, per)
+                         : launch_any(redist_expert_slope_kernel<__nv_bfloat16, false>, grid, 256, 0, 1, o, stream, s, per);
+        else
+            ce = aligned ? launch_any(redist_expert_slope_kernel<__half, true>, grid, 256, 0, 1, o, stream, s, per)
+                         : launch_any(redist_expert_slope_kernel<__half, false>, grid, 256, 0, 1, o, stream, s, per);
+        if (ce != cudaSuccess) return ce;
+    }
+    if (!s.sums) return cudaSuccess;
+    return launch_any(redist_expert_sums_kernel, dim3(unsigned((s.cols + 31) / 32), unsigned(s.experts)), 256, 0, 1, o, stream, s, per);
+}
+
+cudaError_t read_grouped_timeouts(unsigned int *out) { return cudaMemcpyFromSymbol(out, g_grouped_timeouts, sizeof *out); }
+
+}  // namespace redist

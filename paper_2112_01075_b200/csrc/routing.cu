@@ -1,0 +1,569 @@
+// The router of a block of experts, and the moves of tokens to their experts' rows and back: kernels bound by the memory they
+// stream over, or by the latency of a launch.
+#include "routing.h"
+
+#include <algorithm>
+
+#include "elements.cuh"
+
+namespace redist {
+
+namespace {
+
+constexpr int kRouteThreads = 512, kRouteWarps = kRouteThreads / 32;
+constexpr int kCounters = 8192;         // of a block: experts times the warps that count
+
+// A logit as a number whose order is that of the choice: NaN first, minus infinity (and 0, for what has been chosen already)
+// never.  Both zeros are one.
+constexpr uint32_t kNever = 0x007fffffu;
+__device__ __forceinline__ uint32_t order_of(float v)
+{
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return v != v ? 0xffffffffu : b >> 31 ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key >> 31 ? key ^ 0x80000000u : ~key); }
+
+// L lanes share a token.
+template <int L> __device__ __forceinline__ float lane_sum(float v)
+{
+#pragma unroll
+    for (int d = L / 2; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+template <int L> __device__ __forceinline__ uint32_t lane_max(uint32_t v)
+{
+    if constexpr (L == 32) return __reduce_max_sync(0xffffffffu, v);
+#pragma unroll
+    for (int d = L / 2; d; d >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+
+struct RouteParams {
+    Route r;
+    int64_t per_block;                  // tokens
+    int32_t *counts;                    // [block][expert]; null: one block, which places the rows itself
+};
+
+// Exclusive sums of `n` counters in shared memory, in place, by the first warp; the total goes to `total`.
+__device__ __forceinline__ void scan_counts(int32_t *c, int n, int32_t *total)
+{
+    if (threadIdx.x >= 32) return;
+    const int lane = threadIdx.x;
+    int32_t carry = 0;
+    for (int at = 0; at < n; at += 32) {
+        const int32_t mine = at + lane < n ? c[at + lane] : 0;
+        int32_t sum = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int32_t up = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += up;
+        }
+        if (at + lane < n) c[at + lane] = carry + sum - mine;
+        carry += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    if (lane == 0) *total = carry;
+}
+
+// Rows for the places of tokens lo ... hi - 1, the next free row of expert e being base[e].  The warps that count take a
+// stretch of the places each: first they count their experts, then they know where theirs begin.
+__device__ __forceinline__ void place_rows(const Route &r, int64_t lo, int64_t hi, const int32_t *base, int32_t *counters)
+{
+    const int warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31, experts = r.experts;
+    const int counting = min(kRouteWarps, kCounters / experts);
+    const int64_t first = lo * r.chosen, places = (hi - lo) * r.chosen, share = (places + counting - 1) / counting;
+    const int64_t from = first + min(places, warp * share), to = first + min(places, (warp + 1) * share);
+    for (int i = threadIdx.x; i < counting * experts; i += kRouteThreads) counters[i] = 0;
+    __syncthreads();
+    int32_t *mine = counters + warp * experts;
+    if (warp < counting)
+        for (int64_t i = from + lane; i < to; i += 32) {
+            const int32_t e = r.choice[i];
+            if (e >= 0) atomicAdd(mine + e, 1);
+        }
+    __syncthreads();
+    for (int e = threadIdx.x; e < experts; e += kRouteThreads) {
+        int32_t next = base[e];
+        for (int w = 0; w < counting; ++w) {
+            const int32_t n = counters[w * experts + e];
+            counters[w * experts + e] = next;
+            next += n;
+        }
+    }
+    __syncthreads();
+    if (warp < counting)
+        for (int64_t at = from; at < to; at += 32) {
+            const int64_t i = at + lane;
+            const int32_t e = i < to ? r.choice[i] : -1;
+            const uint32_t same = __match_any_sync(0xffffffffu, e);
+            const int before = __popc(same & ((1u << lane) - 1));
+            const int32_t start = e >= 0 ? mine[e] : 0;
+            __syncwarp();
+            if (e >= 0 && before == 0) mine[e] = start + __popc(same);
+            __syncwarp();
+            if (i < to) r.position[i] = e >= 0 ? start + before : -1;
+        }
+}
+
+// The choice: L lanes hold PER logits of a token each, and agree `chosen` times on the largest that is left.  Blocks count
+// how many places each expert got among their tokens.
+template <typename T, int L, int PER>
+__global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const RouteParams p)
+{
+    __shared__ int32_t counts[kMostExperts], counters[kCounters];
+    const Route &r = p.r;
+    const int lane = int(threadIdx.x) & 31, at = lane % L, group = int(threadIdx.x) / L;
+    const uint32_t segment = L == 32 ? 0xffffffffu : ((1u << L) - 1) << (lane / L * L);
+    for (int e = threadIdx.x; e < r.experts; e += kRouteThreads) counts[e] = 0;
+    let_next_start();
+    wait_for_previous();
+    __syncthreads();
+    const int64_t lo = int64_t(blockIdx.x) * p.per_block, hi = min(r.tokens, lo + p.per_block);
+    for (int64_t base = lo; base < hi; base += kRouteThreads / L) {           // all lanes of a warp walk along
+        const int64_t t = base + group;
+        const bool in = t < hi;
+        const T *row = static_cast<const T *>(r.logits) + t * r.ld;
+        uint32_t key[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) key[j] = in && at + 32 * j < r.experts ? order_of(to_float(row[at + 32 * j])) : 0;
+        uint32_t best = 0, top = 0, own = 0;
+        int32_t own_choice = -1;
+        float every = 0.0f;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) best = max(best, key[j]);
+        for (int s = 0; s < r.chosen; ++s) {
+            const uint32_t most = lane_max<L>(best);
+            if (s == 0) {
+                top = most;
+                if (!r.normalize) {
+#pragma unroll
+                    for (int j = 0; j < PER; ++j)
+                        if (key[j] > kNever) every += expf(value_of(key[j]) - value_of(top));
+                }
+            }
+            int32_t which;
+            if constexpr (PER == 1) {
+                which = __ffs(__ballot_sync(0xffffffffu, best == most) & segment) - 1 - lane / L * L;
+            } else {
+                uint32_t index = 0xffffu;
+#pragma unroll
+                for (int j = PER - 1; j >= 0; --j)
+                    if (key[j] == most) index = uint32_t(at + 32 * j);
+                which = int32_t(__reduce_min_sync(0xffffffffu, index));
+            }
+            if (at == s) {
+                own = most;
+                own_choice = most > kNever ? which : -1;
+            }
+            if (which % 32 == at) {
+                best = 0;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    if (at + 32 * j == which) key[j] = 0;
+                    best = max(best, key[j]);
+                }
+            }
+        }
+        const float part = own_choice >= 0 ? expf(value_of(own) - value_of(top)) : 0.0f;
+        const float total = lane_sum<L>(r.normalize ? part : every);
+        if (in && at < r.chosen) {
+            r.weights[t * r.chosen + at] = own_choice >= 0 ? part / total : 0.0f;
+            r.choice[t * r.chosen + at] = own_choice;
+            if (own_choice >= 0) atomicAdd(counts + own_choice, 1);           // whole numbers: any order
+        }
+    }
+    __syncthreads();
+    if (p.counts) {
+        for (int e = threadIdx.x; e < r.experts; e += kRouteThreads) p.counts[int64_t(blockIdx.x) * r.experts + e] = counts[e];
+        return;
+    }
+    __shared__ int32_t total;
+    scan_counts(counts, r.experts, &total);
+    __syncthreads();
+    for (int e = threadIdx.x; e <= r.experts; e += kRouteThreads) r.offsets[e] = e < r.experts ? counts[e] : total;
+    place_rows(r, lo, hi, counts, counters);
+}
+
+// The second step where tokens are many: a block's rows of expert e follow those of lower experts and those of the blocks
+// before it.
+__global__ void __launch_bounds__(kRouteThreads) redist_place_kernel(const RouteParams p)
+{
+    __shared__ int32_t base[kMostExperts], counters[kCounters], total;
+    const Route &r = p.r;
+    let_next_start();
+    wait_for_previous();
+    int32_t before[kMostExperts / kRouteThreads] = {};
+#pragma unroll
+    for (int i = 0; i < kMostExperts / kRouteThreads; ++i) {
+        const int e = int(threadIdx.x) + i * kRouteThreads;
+        if (e < r.experts) {
+            int32_t sum = 0;
+#pragma unroll 8
+            for (int b = 0; b < int(gridDim.x); ++b) {
+                const int32_t n = p.counts[int64_t(b) * r.experts + e];
+                if (b < int(blockIdx.x)) before[i] += n;
+                sum += n;
+            }
+            base[e] = sum;
+        }
+    }
+    __syncthreads();
+    scan_counts(base, r.experts, &total);
+    __syncthreads();
+    if (blockIdx.x == 0)
+        for (int e = threadIdx.x; e <= r.experts; e += kRouteThreads) r.offsets[e] = e < r.experts ? base[e] : total;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kMostExperts / kRouteThreads; ++i) {
+        const int e = int(threadIdx.x) + i * kRouteThreads;
+        if (e < r.experts) base[e] += before[i];
+    }
+    __syncthreads();
+    const int64_t lo = int64_t(blockIdx.x) * p.per_block, hi = min(r.tokens, lo + p.per_block);
+    place_rows(r, min(lo, hi), hi, base, counters);
+}
+
+// A warp per token.
+template <typename T, int PER> __global__ void __launch_bounds__(256) redist_route_gradient_kernel(const Route r)
+{
+    const int lane = int(threadIdx.x) & 31;
+    const int64_t t = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    let_next_start();
+    wait_for_previous();
+    if (t >= r.tokens) return;
+    float w = 0.0f, d = 0.0f;
+    int32_t e = -1;
+    if (lane < r.chosen) {
+        e = r.choice[t * r.chosen + lane];
+        if (e >= 0) {
+            w = r.weights[t * r.chosen + lane];
+            d = r.dweights[t * r.chosen + lane];
+        }
+    }
+    const float mean = lane_sum<32>(w * d), own = r.normalize ? w * (d - mean) : w * d;
+    float v[PER];
+    if (r.normalize) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) v[j] = 0.0f;
+    } else {
+        const T *row = static_cast<const T *>(r.logits) + t * r.ld;
+        uint32_t key[PER], top = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            key[j] = lane + 32 * j < r.experts ? order_of(to_float(row[lane + 32 * j])) : 0;
+            top = max(top, key[j]);
+        }
+        top = lane_max<32>(top);
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            v[j] = key[j] > kNever ? expf(value_of(key[j]) - value_of(top)) : 0.0f;
+            sum += v[j];
+        }
+        const float scale = top > kNever ? -mean / lane_sum<32>(sum) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) v[j] *= scale;
+    }
+    for (int s = 0; s < r.chosen; ++s) {
+        const int32_t to = __shfl_sync(0xffffffffu, e, s);
+        const float g = __shfl_sync(0xffffffffu, own, s);
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (lane + 32 * j == to) v[j] += g;
+    }
+    T *out = static_cast<T *>(r.dlogits) + t * r.ld_dlogits;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+        if (lane + 32 * j < r.experts) out[lane + 32 * j] = from_float<T>(v[j]);
+}
+
+// ---- moves -----------------------------------------------------------------------------------------------
+
+// N neighbours, loaded and stored at once.
+template <typename T, int N> struct Some {
+    static constexpr int kBytes = N * int(sizeof(T));
+    union {
+        T v[N];
+        uint4 u4;
+        uint2 u2;
+        uint32_t u1;
+        uint16_t uh;
+    };
+    __device__ __forceinline__ Some() {}
+    __device__ __forceinline__ void load(const T *p)
+    {
+        if constexpr (kBytes == 16) u4 = *reinterpret_cast<const uint4 *>(p);
+        else if constexpr (kBytes == 8) u2 = *reinterpret_cast<const uint2 *>(p);
+        else if constexpr (kBytes == 4) u1 = *reinterpret_cast<const uint32_t *>(p);
+        else uh = *reinterpret_cast<const uint16_t *>(p);
+    }
+    __device__ __forceinline__ void store(T *p) const
+    {
+        if constexpr (kBytes == 16) *reinterpret_cast<uint4 *>(p) = u4;
+        else if constexpr (kBytes == 8) *reinterpret_cast<uint2 *>(p) = u2;
+        else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t *>(p) = u1;
+        else *reinterpret_cast<uint16_t *>(p) = uh;
+    }
+};
+
+__device__ __forceinline__ int64_t row_at(const Move &m, int64_t place)
+{
+    const int32_t p = m.position[place];
+    return p >= 0 && p < m.rows ? p : -1;
+}
+
+constexpr int kMoveThreads = 256, kHeld = 4;        // pieces a thread holds at a time
+
+// L threads take kHeld L pieces of a token (of its `pieces`): loaded once, stored to its rows.
+template <typename T, int N, int L> __global__ void __launch_bounds__(kMoveThreads) redist_dispatch_kernel(const Move m, int pieces)
+{
+    const int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + int(threadIdx.x) / L;
+    const int first = int(blockIdx.y) * kHeld * L + int(threadIdx.x) % L;
+    let_next_start();
+    wait_for_previous();
+    if (t >= m.tokens) return;
+    const T *from = static_cast<const T *>(m.token) + t * m.ld_token;
+    Some<T, N> v[kHeld];
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+        if (first + j * L < pieces) v[j].load(from + int64_t(first + j * L) * N);
+    for (int s = 0; s < m.chosen; ++s) {
+        const int64_t row = row_at(m, t * m.chosen + s);
+        if (row < 0) continue;
+        T *to = static_cast<T *>(m.row) + row * m.ld_row;
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            if (first + j * L < pieces) v[j].store(to + int64_t(first + j * L) * N);
+    }
+}
+
+// The other way: a token's rows, weighted and added in the order of its places.
+template <typename T, int N, int L> __global__ void __launch_bounds__(kMoveThreads) redist_combine_kernel(const Move m, int pieces)
+{
+    const int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + int(threadIdx.x) / L;
+    const int first = int(blockIdx.y) * kHeld * L + int(threadIdx.x) % L;
+    let_next_start();
+    wait_for_previous();
+    if (t >= m.tokens) return;
+    float sum[kHeld][N] = {};
+    if (m.residual) {
+        const T *from = static_cast<const T *>(m.residual) + t * m.ld_residual;
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            if (first + j * L < pieces) {
+                Some<T, N> v;
+                v.load(from + int64_t(first + j * L) * N);
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[j][i] = to_float(v.v[i]);
+            }
+    }
+#pragma unroll 2
+    for (int s = 0; s < m.chosen; ++s) {
+        const int64_t row = row_at(m, t * m.chosen + s);
+        if (row < 0) continue;
+        const float w = m.weights ? m.weights[t * m.chosen + s] : 1.0f;
+        const T *from = static_cast<const T *>(m.row) + row * m.ld_row;
+        Some<T, N> v[kHeld];
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            if (first + j * L < pieces) v[j].load(from + int64_t(first + j * L) * N);
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            if (first + j * L < pieces)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[j][i] = fmaf(w, to_float(v[j].v[i]), sum[j][i]);
+    }
+    T *to = static_cast<T *>(m.token) + t * m.ld_token;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+        if (first + j * L < pieces) {
+            Some<T, N> v;
+#pragma unroll
+            for (int i = 0; i < N; ++i) v.v[i] = from_float<T>(sum[j][i]);
+            v.store(to + int64_t(first + j * L) * N);
+        }
+}
+
+// The gradient of the latter: L threads take a whole token, because dweights are sums over its columns.
+template <typename T, int N, int L> __global__ void __launch_bounds__(kMoveThreads) redist_combine_gradient_kernel(const Move m, int pieces)
+{
+    __shared__ float dots[kMoveThreads / 32][kMostChosen];
+    const int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + int(threadIdx.x) / L;
+    const int at = int(threadIdx.x) % L, warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31;
+    let_next_start();
+    wait_for_previous();
+    const bool in = t < m.tokens;
+    const T *dy = static_cast<const T *>(m.token) + (in ? t : 0) * m.ld_token;
+    for (int s = 0; s < m.chosen; ++s) {
+        const int64_t row = in ? row_at(m, t * m.chosen + s) : -1;
+        float dot = 0.0f;
+        if (row >= 0) {
+            const float w = m.weights[t * m.chosen + s];
+            const T *y = static_cast<const T *>(m.row) + row * m.ld_row;
+            T *to = static_cast<T *>(m.drow) + row * m.ld_drow;
+            for (int first = at; first < pieces; first += kHeld * L) {
+                Some<T, N> d[kHeld], v[kHeld];
+#pragma unroll
+                for (int j = 0; j < kHeld; ++j)
+                    if (first + j * L < pieces) {
+                        d[j].load(dy + int64_t(first + j * L) * N);
+                        v[j].load(y + int64_t(first + j * L) * N);
+                    }
+#pragma unroll
+                for (int j = 0; j < kHeld; ++j)
+                    if (first + j * L < pieces) {
+                        Some<T, N> out;
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const float g = to_float(d[j].v[i]);
+                            dot = fmaf(g, to_float(v[j].v[i]), dot);
+                            out.v[i] = from_float<T>(w * g);
+                        }
+                        out.store(to + int64_t(first + j * L) * N);
+                    }
+            }
+        }
+        dot = lane_sum<32>(dot);
+        if (lane == 0) dots[warp][s] = dot;
+    }
+    if constexpr (L > 32) __syncthreads();
+    else __syncwarp();
+    for (int s = at; in && s < m.chosen; s += L) {
+        float sum = 0.0f;
+        for (int i = 0; i < L / 32; ++i) sum += dots[int(threadIdx.x) / L * (L / 32) + i][s];
+        m.dweights[t * m.chosen + s] = sum;
+    }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------
+
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, const LaunchOptions &o, cudaStream_t stream, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(unsigned(threads));
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = o.pdl ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// Blocks of the choice: one up to 128 tokens (a second launch costs more than it saves), one per SM and stretch of tokens above.
+int64_t tokens_per_block(int64_t tokens, int sms) { return std::max<int64_t>(128, (tokens + sms - 1) / sms); }
+
+template <typename T> cudaError_t launch_route_typed(const RouteParams &p, int64_t blocks, const LaunchOptions &o, cudaStream_t stream)
+{
+    const dim3 grid = dim3(unsigned(blocks));
+    const int e = p.r.experts;
+    if (e <= 8) return launch(redist_route_kernel<T, 8, 1>, grid, kRouteThreads, o, stream, p);
+    if (e <= 32) return launch(redist_route_kernel<T, 32, 1>, grid, kRouteThreads, o, stream, p);
+    if (e <= 64) return launch(redist_route_kernel<T, 32, 2>, grid, kRouteThreads, o, stream, p);
+    if (e <= 128) return launch(redist_route_kernel<T, 32, 4>, grid, kRouteThreads, o, stream, p);
+    if (e <= 256) return launch(redist_route_kernel<T, 32, 8>, grid, kRouteThreads, o, stream, p);
+    return launch(redist_route_kernel<T, 32, 32>, grid, kRouteThreads, o, stream, p);
+}
+
+template <typename T> cudaError_t launch_route_gradient_typed(const Route &r, const LaunchOptions &o, cudaStream_t stream)
+{
+    const dim3 grid = dim3(unsigned((r.tokens + 7) / 8));
+    const int e = r.experts;
+    if (e <= 32) return launch(redist_route_gradient_kernel<T, 1>, grid, 256, o, stream, r);
+    if (e <= 128) return launch(redist_route_gradient_kernel<T, 4>, grid, 256, o, stream, r);
+    if (e <= 256) return launch(redist_route_gradient_kernel<T, 8>, grid, 256, o, stream, r);
+    return launch(redist_route_gradient_kernel<T, 32>, grid, 256, o, stream, r);
+}
+
+// How many neighbours can be accessed at once: what the columns, the addresses and the strides are all multiples of.
+int together(int64_t cols, int type, std::initializer_list<std::pair<const void *, int64_t>> arrays)
+{
+    const int size = int(type_bytes(type));
+    uint64_t all = 16 | uint64_t(cols * size);
+    for (const auto &a : arrays)
+        if (a.first) all |= uint64_t(uintptr_t(a.first)) | uint64_t(a.second * size);
+    return int(all & (~all + 1)) / size;
+}
+
+enum Which { kDispatch, kCombine, kGradient };
+
+template <Which W, typename T, int N> cudaError_t launch_move_lanes(const Move &m, const LaunchOptions &o, cudaStream_t stream)
+{
+    const int64_t pieces = (m.cols + N - 1) / N;
+    // a warp per token (or stretch of it) for short rows, a block for longer ones
+    const bool wide = pieces > 32 * kHeld;
+    const int64_t tokens_per = wide ? 1 : kMoveThreads / 32, chunk = (wide ? kMoveThreads : 32) * kHeld;
+    const unsigned x = unsigned((m.tokens + tokens_per - 1) / tokens_per), y = unsigned(W == kGradient ? 1 : (pieces + chunk - 1) / chunk);
+    if (y > 65535 || pieces > INT32_MAX / 2) return cudaErrorInvalidValue;
+    const dim3 grid = dim3(x, y);
+    if constexpr (W == kDispatch) {
+        if (wide) return launch(redist_dispatch_kernel<T, N, kMoveThreads>, grid, kMoveThreads, o, stream, m, int(pieces));
+        return launch(redist_dispatch_kernel<T, N, 32>, grid, kMoveThreads, o, stream, m, int(pieces));
+    } else if constexpr (W == kCombine) {
+        if (wide) return launch(redist_combine_kernel<T, N, kMoveThreads>, grid, kMoveThreads, o, stream, m, int(pieces));
+        return launch(redist_combine_kernel<T, N, 32>, grid, kMoveThreads, o, stream, m, int(pieces));
+    } else {
+        if (wide) return launch(redist_combine_gradient_kernel<T, N, kMoveThreads>, grid, kMoveThreads, o, stream, m, int(pieces));
+        return launch(redist_combine_gradient_kernel<T, N, 32>, grid, kMoveThreads, o, stream, m, int(pieces));
+    }
+}
+
+template <Which W, typename T> cudaError_t launch_move_typed(const Move &m, int n, const LaunchOptions &o, cudaStream_t stream)
+{
+    constexpr int kMost = 16 / int(sizeof(T));
+    if (n >= kMost) return launch_move_lanes<W, T, kMost>(m, o, stream);
+    if (n >= kMost / 2) return launch_move_lanes<W, T, kMost / 2>(m, o, stream);
+    if constexpr (kMost == 8)
+        if (n >= 2) return launch_move_lanes<W, T, 2>(m, o, stream);
+    return launch_move_lanes<W, T, 1>(m, o, stream);
+}
+
+template <Which W> cudaError_t launch_move(const Move &m, const LaunchOptions &o, cudaStream_t stream)
+{
+    if (m.tokens == 0) return cudaSuccess;
+    const int n = together(m.cols, m.type, {{m.token, m.ld_token}, {m.row, m.ld_row}, {m.drow, m.ld_drow}, {m.residual, m.ld_residual}});
+    switch (m.type) {
+    case T_BF16: return launch_move_typed<W, __nv_bfloat16>(m, n, o, stream);
+    case T_F16: return launch_move_typed<W, __half>(m, n, o, stream);
+    default: return launch_move_typed<W, float>(m, n, o, stream);
+    }
+}
+
+}  // namespace
+
+int64_t route_scratch_bytes(int64_t tokens, int experts, int sms)
+{
+    const int64_t per = tokens_per_block(tokens, sms), blocks = (tokens + per - 1) / per;
+    return blocks > 1 ? blocks * experts * 4 : 0;
+}
+
+cudaError_t launch_route(const Route &r, void *scratch, int sms, const LaunchOptions &o, cudaStream_t stream)
+{
+    RouteParams p = {};
+    p.r = r;
+    p.per_block = tokens_per_block(r.tokens, sms);
+    const int64_t blocks = std::max<int64_t>(1, (r.tokens + p.per_block - 1) / p.per_block);
+    p.counts = blocks > 1 ? static_cast<int32_t *>(scratch) : nullptr;
+    const cudaError_t ce = r.type == T_BF16  ? launch_route_typed<__nv_bfloat16>(p, blocks, o, stream)
+                           : r.type == T_F16 ? launch_route_typed<__half>(p, blocks, o, stream)
+                                             : launch_route_typed<float>(p, blocks, o, stream);
+    if (ce != cudaSuccess || blocks == 1) return ce;
+    return launch(redist_place_kernel, dim3(unsigned(blocks)), kRouteThreads, o, stream, p);
+}
+
+cudaError_t launch_route_gradient(const Route &r, const LaunchOptions &o, cudaStream_t stream)
+{
+    if (r.tokens == 0) return cudaSuccess;
+    switch (r.type) {
+    case T_BF16: return launch_route_gradient_typed<__nv_bfloat16>(r, o, stream);
+    case T_F16: return launch_route_gradient_typed<__half>(r, o, stream);
+    default: return launch_route_gradient_typed<float>(r, o, stream);
+    }
+}
+
+cudaError_t launch_dispatch(const Move &m, const LaunchOptions &o, cudaStream_t stream) { return launch_move<kDispatch>(m, o, stream); }
+cudaError_t launch_combine(const Move &m, const LaunchOptions &o, cudaStream_t stream) { return launch_move<kCombine>(m, o, stream); }
+cudaError_t launch_combine_gradient(const Move &m, const LaunchOptions &o, cudaStream_t stream) { return launch_move<kGradient>(m, o, stream); }
+
+}  // namespace redist
