@@ -16,6 +16,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstring>
 
 #include "activation.cuh"
@@ -55,6 +56,9 @@ struct GroupedParams {
 __device__ __forceinline__ int offset_at(const GroupedParams &p, int e) { return min(max(__ldg(p.offsets + e), 0), p.rows); }
 
 // ---- tiles ---------------------------------------------------------------------------------------
+
+// Rows of the boxes in which a tile that is not full is loaded.
+template <int ROWS> constexpr int kPartRows = ROWS < 32 ? ROWS : 32;
 
 struct GroupedTile {
     int expert, tm, row0, count, k0, steps;     // rows row0 ... row0 + count - 1 of the result (SUMS: its rows, and where its sum begins)
@@ -214,10 +218,10 @@ struct GroupedPieces {
 
 template <int CG, int BN, int KB, bool SUMS>
 __global__ void __launch_bounds__(kThreads, 1)
-redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
-                      const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ GroupedParams p)
+redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_part,
+                      const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ GroupedParams p)
 {
-    constexpr int kRowsB = BN / CG;
+    constexpr int kRowsB = BN / CG, kPart = kPartRows<kRowsB>;
     constexpr int kSliceA = 128 * 128, kSliceB = kRowsB * 128, kStageA = KB * kSliceA, kStageB = KB * kSliceB, kStage = kStageA + kStageB;
     constexpr int kStages = kRing / kStage < kMostStages ? kRing / kStage : kMostStages;
     constexpr uint32_t kColumns = 2 * BN < 32 ? 32 : 2 * BN;
@@ -275,7 +279,6 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         uint32_t phase = 0, rounds = 0, polls = p.wait_polls;
         const CUtensorMap *map = second ? &map_b : &map_a;
         const int along_rows = SUMS ? 1 : second ? p.b_along_rows : p.a_along_rows;
-        const uint32_t announced = CG * (second ? kStageB : kStageA + p.test_extra_tx);
         int expert = -1;
         for (int t = first; walk.at(t, at); t += step) {
             if (SUMS && at.expert != expert && at.steps) {
@@ -284,8 +287,14 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(map) : "memory");
                 __syncwarp();
             }
-            const int row = second ? at.row0 + int(rank) * (Tiles::columns(at) / CG) : (at.tm * CG + int(rank)) * 128;
+            const int width = Tiles::columns(at) / CG, row = second ? at.row0 + int(rank) * width : (at.tm * CG + int(rank)) * 128;
             const int z = SUMS || second ? 0 : at.expert;
+            // a tile that is not full takes its rows in boxes of kPart, as many as it has
+            const bool part = !SUMS && second && kPart < kRowsB && width <= kRowsB - kPart;
+            if (!SUMS && second) map = part ? &map_part : &map_b;
+            const int boxes = along_rows ? (second ? (width + 63) / 64 : 2) : part ? (width + kPart - 1) / kPart : 1;
+            const uint32_t size = along_rows ? kBK * 128 : !second ? kSliceA : part ? kPart * 128 : kSliceB;
+            const uint32_t announced = CG * (KB * uint32_t(boxes) * size + (second ? 0 : p.test_extra_tx));
             for (int kb = 0; kb < at.steps; ++kb) {
                 if (!bar_wait(empty(stage), phase ^ 1, polls)) {
                     ok = false;
@@ -299,12 +308,10 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     for (int k = 0; k < KB; ++k) {
                         const int x = at.k0 + (kb * KB + k) * kBK;
                         const uint32_t slice = to + k * (second ? kSliceB : kSliceA);
-                        if (!along_rows) {
-                            load_box<CG>(slice, map, bar, x, row, z);
-                        } else {
-                            const int boxes = second ? kRowsB / 64 : 2;
-                            for (int i = 0; i < boxes; ++i) load_box<CG>(slice + i * kBK * 128, map, bar, row + 64 * i, x, z);
-                        }
+                        if (!along_rows)
+                            for (int i = 0; i < boxes; ++i) load_box<CG>(slice + i * size, map, bar, x, row + i * kPart, z);
+                        else
+                            for (int i = 0; i < boxes; ++i) load_box<CG>(slice + i * size, map, bar, row + 64 * i, x, z);
                     }
                 }
                 if (ok && ++stage == kStages) {
@@ -697,9 +704,11 @@ cudaError_t launch(const Grouped &g, void *scratch, const LaunchOptions &o, int 
     const int64_t tiles = parts * p.tiles_m;
     if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
 
-    CUtensorMap ma, mb, mo, mp;
+    CUtensorMap ma, mb, ms, mo, mp;
     const int64_t features = SUMS ? g.n : g.rows, sum = SUMS ? g.rows : g.k;
-    if (!make_operand(&ma, g.a, g.m, sum, SUMS ? 1 : g.experts, 128) || !make_operand(&mb, g.b, features, sum, 1, BN / CG)) return cudaErrorInvalidValue;
+    if (!make_operand(&ma, g.a, g.m, sum, SUMS ? 1 : g.experts, 128) || !make_operand(&mb, g.b, features, sum, 1, BN / CG) ||
+        !make_operand(&ms, g.b, features, sum, 1, kPartRows<BN / CG>))
+        return cudaErrorInvalidValue;
     std::memset(&mo, 0, sizeof mo);
     std::memset(&mp, 0, sizeof mp);
     if (p.aligned_out) {
@@ -718,7 +727,42 @@ cudaError_t launch(const Grouped &g, void *scratch, const LaunchOptions &o, int 
         if (device < 64) ready.fetch_or(uint64_t(1) << device, std::memory_order_relaxed);
     }
     const int64_t groups = sms / CG;
-    return launch_any(kernel, dim3(unsigned(std::min(tiles, groups) * CG)), kThreads, kSmem, CG, o, stream, ma, mb, mo, mp, p);
+    return launch_any(kernel, dim3(unsigned(std::min(tiles, groups) * CG)), kThreads, kSmem, CG, o, stream, ma, mb, ms, mo, mp, p);
+}
+
+// The tile shapes, and what they take: microseconds per 64 steps of a sum, `step` + `column` per column computed (at least
+// `least`; three quarters where all tiles fit on the GPU at once), and per launch besides.  Fitted to timings of some twenty
+// sizes from 500 x 512 -> 512 to 32768 x 4096 -> 4096.
+enum GroupedShape { kPair256, kPair128, kOne32, kOne128, kOne64 };
+struct GroupedCost {
+    int rows, cols, per_unit;
+    double step, column, least, launch;
+};
+constexpr GroupedCost kGroupedCosts[] = {{256, 256, 2, 0.044, 0.00147, 0.18, 5.5}, {256, 128, 2, 0.044, 0.00147, 0.18, 4.5}, {128, 32, 1, 0.185, 0.00066, 0, 3.4},
+                                         {128, 128, 1, 0.185, 0.00066, 0, 4.2}, {128, 64, 1, 0.185, 0.00066, 0, 3.6}};
+
+// The shape with the least time by these figures, or the one that computes least where memory sets the time.  How the rows
+// are spread over the experts is not known here: what a busy expert has is taken as one and a half times the mean.
+GroupedShape choose(const Grouped &g, int sms, const LaunchOptions &o)
+{
+    if (o.test_shape) return GroupedShape(o.test_shape - 1);
+    const double busy = double(std::min<int64_t>(g.experts, g.rows)), rows = 1.5 * double(g.rows) / busy;
+    const double bytes = 2.0 * (double(g.sums ? g.experts : busy) * double(g.m) * double(g.sums ? g.n : g.k) + double(g.rows) * double(g.m + (g.sums ? g.n : g.k)));
+    GroupedShape best = kPair256;
+    double least = 1e30;
+    for (int i = 0; i < 5; ++i) {
+        const GroupedCost &c = kGroupedCosts[i];
+        if (g.sums && c.cols < 64) continue;
+        const double features = std::ceil(double(g.m) / c.rows), cols = g.sums ? double(g.n) : rows, per = std::ceil(cols / c.cols);
+        const double tiles = features * per * (g.sums ? g.experts : busy), units = double(sms / c.per_unit);
+        const double steps = std::ceil((g.sums ? double(g.rows) / g.experts : double(g.k)) / 64), waves = tiles <= units ? 0.75 : tiles / units + 0.5;
+        const double compute = waves * steps * std::max(c.least, c.step + c.column * cols / per), time = c.launch + std::max(compute, bytes / 6.5e6) + 0.1 * compute;
+        if (time < least) {
+            least = time;
+            best = GroupedShape(i);
+        }
+    }
+    return best;
 }
 
 }  // namespace
@@ -731,8 +775,21 @@ cudaError_t launch_grouped(const Grouped &g, void *scratch, const LaunchOptions 
     int device = 0, sms = 0;
     const cudaError_t ce = current_device(&device, &sms);
     if (ce != cudaSuccess) return ce;
-    if (g.sums) return launch<1, 128, 2, true>(g, scratch, o, device, sms, stream);
-    return launch<1, 128, 2, false>(g, scratch, o, device, sms, stream);
+    if (g.sums) {
+        switch (choose(g, sms, o)) {
+        case kPair256: return launch<2, 256, 1, true>(g, scratch, o, device, sms, stream);
+        case kPair128: return launch<2, 128, 2, true>(g, scratch, o, device, sms, stream);
+        case kOne128: return launch<1, 128, 2, true>(g, scratch, o, device, sms, stream);
+        default: return launch<1, 64, 2, true>(g, scratch, o, device, sms, stream);
+        }
+    }
+    switch (choose(g, sms, o)) {
+    case kPair256: return launch<2, 256, 1, false>(g, scratch, o, device, sms, stream);
+    case kPair128: return launch<2, 128, 2, false>(g, scratch, o, device, sms, stream);
+    case kOne32: return launch<1, 32, 2, false>(g, scratch, o, device, sms, stream);
+    case kOne128: return launch<1, 128, 2, false>(g, scratch, o, device, sms, stream);
+    default: return launch<1, 64, 2, false>(g, scratch, o, device, sms, stream);
+    }
 }
 
 int64_t expert_partial_bytes(int64_t rows, int64_t cols, int experts)
