@@ -10,6 +10,7 @@ dimension ``k``, minor-to-major (Section 2.1 of the paper).
 """
 from __future__ import annotations
 
+import array
 import contextlib
 import ctypes
 import json
@@ -665,7 +666,6 @@ _pack_matrix = struct.Struct(_MATRIX).pack
 _pack_move = struct.Struct("3q2i" + _MATRIX * 4 + "3P").pack
 _pack_experts = struct.Struct("3q4i" + _MATRIX * 4 + "2q2P").pack
 _pack_experts_grads = struct.Struct(_MATRIX * 3 + "qP").pack
-_pack_tensor = struct.Struct("2Pq2i").pack
 _pack_clip = struct.Struct("Pq2fP").pack
 _ESCRATCH = 5
 
@@ -1029,8 +1029,10 @@ def _route_forward(logits, k, normalize, scratch, stream):
     offsets = o.strided((experts + 1,), (1,), dtype=o.i32, device=device)
     op = _pack_route(tokens, experts, k, _code(o, logits, "logits"), 1 if normalize else 0, logits.data_ptr(), *logits.stride(),
                      weights.data_ptr(), choice.data_ptr(), position.data_ptr(), offsets.data_ptr())
-    keep, sp, sn = o.scratch(o.route_scratch_bytes(op), scratch, device)
-    rc = o.route_forward(op, sp, sn, at)
+    rc = o.route_forward(op, None, 0, at) if scratch is None else _ESCRATCH
+    if rc == _ESCRATCH:                                      # many tokens
+        keep, sp, sn = o.scratch(o.route_scratch_bytes(op), scratch, device)
+        rc = o.route_forward(op, sp, sn, at)
     if rc:
         raise RedistError(rc, "redist_route_forward")
     return weights, choice, position, offsets
@@ -1069,6 +1071,9 @@ def _route_backward(dweights, logits, weights, choice, normalize, dlogits, strea
     return dlogits
 
 
+_ABSENT = (0, 0, 0)
+
+
 def _move(o, token, row, position, residual=None, drow=None, weights=None, dweights=None):
     """The packed block of the four moves."""
     if token.dim() != 2 or row.dim() != 2 or position.dim() != 2:
@@ -1077,7 +1082,8 @@ def _move(o, token, row, position, residual=None, drow=None, weights=None, dweig
     rows, k = row.shape[0], position.shape[1]
     places, wide = (tokens, k), (rows, cols)
     return _pack_move(tokens, rows, cols, _code(o, token, "tokens"), k, token.data_ptr(), *token.stride(), *_matrix(row, wide, dtype, device, "rows"),
-                      *_matrix(residual, (tokens, cols), dtype, device, "residual"), *_matrix(drow, wide, dtype, device, "drows"),
+                      *(_ABSENT if residual is None else _matrix(residual, (tokens, cols), dtype, device, "residual")),
+                      *(_ABSENT if drow is None else _matrix(drow, wide, dtype, device, "drows")),
                       _table(o, position, places, o.i32, device, "position"),
                       0 if weights is None else _table(o, weights, places, o.f32, device, "weights"),
                       0 if dweights is None else _table(o, dweights, places, o.f32, device, "dweights"))
@@ -1329,24 +1335,20 @@ def _clip_gradients(tensors, max_norm, eps, out, scratch, stream):
             raise RedistError(1, f"{len(tensors)} tensors, but {len(out)} to write")
     device = tensors[0].device if tensors else o.torch.device("cuda", o.current_device() if o.current_device else 0)
     at = o.stream(device, stream)
-    codes, blocks = o.codes, []
-    for i, t in enumerate(tensors):
-        code = codes.get(t.dtype)
-        if code is None:
-            _code(o, t, "a gradient")
-        if t.device != device or not _dense(t):
+    codes, entries, to = o.codes, [], 0
+    for i, t in enumerate(tensors):                          # (a list may be long: a line of Python is a line per tensor)
+        if t.device != device or not (t.is_contiguous() or _dense(t)):
             raise RedistError(1, f"gradients have to be on one device with their elements side by side; number {i} is not")
-        to = 0
         if out is not None:
             v = out[i]
             if v.shape != t.shape or v.dtype is not t.dtype or v.device != device or v.stride() != t.stride():
                 raise RedistError(1, f"out has to be like the gradients; number {i} is not")
             to = v.data_ptr()
-        blocks.append(_pack_tensor(t.data_ptr(), to, t.numel(), code, 0))
+        code = codes.get(t.dtype)
+        entries += (t.data_ptr(), to, t.numel(), _code(o, t, "a gradient") if code is None else code)
     norm = o.strided((), (), dtype=o.f32, device=device)
-    table = b"".join(blocks)
-    held = ctypes.c_char_p(table)
-    op = _pack_clip(ctypes.cast(held, ctypes.c_void_p).value or 0, len(tensors), -1.0 if max_norm is None else max_norm, eps, norm.data_ptr())
+    table = array.array("q", entries)                        # (type and reserved share the last word of an entry)
+    op = _pack_clip(table.buffer_info()[0], len(tensors), -1.0 if max_norm is None else max_norm, eps, norm.data_ptr())
     keep, sp, sn = o.scratch(o.clip_scratch_bytes(op), scratch, device)
     rc = o.clip(op, sp, sn, at)
     if rc:

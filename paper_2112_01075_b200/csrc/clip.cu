@@ -184,7 +184,7 @@ template <typename T> __device__ __forceinline__ void scale(const void *data, vo
                 w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
             else
                 w = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
-            *reinterpret_cast<uint4 *>(to + first) = w;
+            __stcs(reinterpret_cast<uint4 *>(to + first), w);       // (not wanted again before all else: L2 keeps what is read)
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)

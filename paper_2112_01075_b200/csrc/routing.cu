@@ -3,6 +3,7 @@
 #include "routing.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "elements.cuh"
 
@@ -10,7 +11,7 @@ namespace redist {
 
 namespace {
 
-constexpr int kRouteThreads = 512, kRouteWarps = kRouteThreads / 32;
+constexpr int kRouteThreads = 1024, kRouteWarps = kRouteThreads / 32;
 constexpr int kCounters = 8192;         // of a block: experts times the warps that count
 
 // A logit as a number whose order is that of the choice: NaN first, minus infinity (and 0, for what has been chosen already)
@@ -69,20 +70,27 @@ __device__ __forceinline__ void scan_counts(int32_t *c, int n, int32_t *total)
 __device__ __forceinline__ void place_rows(const Route &r, int64_t lo, int64_t hi, const int32_t *base, int32_t *counters)
 {
     const int warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31, experts = r.experts;
-    const int counting = min(kRouteWarps, kCounters / experts);
-    const int64_t first = lo * r.chosen, places = (hi - lo) * r.chosen, share = (places + counting - 1) / counting;
+    const int64_t first = lo * r.chosen, places = (hi - lo) * r.chosen;
+    // two turns of a warp, where there are warps for that: every warp's counters make the chain below longer
+    const int counting = max(1, int(min(int64_t(min(kRouteWarps, kCounters / experts)), (places + 63) / 64)));
+    const int64_t share = (places + counting - 1) / counting;
     const int64_t from = first + min(places, warp * share), to = first + min(places, (warp + 1) * share);
     for (int i = threadIdx.x; i < counting * experts; i += kRouteThreads) counters[i] = 0;
+    int32_t held[2];                    // the first two turns' experts
+#pragma unroll
+    for (int i = 0; i < 2; ++i) held[i] = warp < counting && from + 32 * i + lane < to ? r.choice[from + 32 * i + lane] : -1;
     __syncthreads();
     int32_t *mine = counters + warp * experts;
+    auto expert = [&](int64_t at) { return at == from ? held[0] : at == from + 32 ? held[1] : at + lane < to ? r.choice[at + lane] : -1; };
     if (warp < counting)
-        for (int64_t i = from + lane; i < to; i += 32) {
-            const int32_t e = r.choice[i];
+        for (int64_t at = from; at < to; at += 32) {
+            const int32_t e = expert(at);
             if (e >= 0) atomicAdd(mine + e, 1);
         }
     __syncthreads();
     for (int e = threadIdx.x; e < experts; e += kRouteThreads) {
         int32_t next = base[e];
+#pragma unroll 4
         for (int w = 0; w < counting; ++w) {
             const int32_t n = counters[w * experts + e];
             counters[w * experts + e] = next;
@@ -93,7 +101,7 @@ __device__ __forceinline__ void place_rows(const Route &r, int64_t lo, int64_t h
     if (warp < counting)
         for (int64_t at = from; at < to; at += 32) {
             const int64_t i = at + lane;
-            const int32_t e = i < to ? r.choice[i] : -1;
+            const int32_t e = expert(at);
             const uint32_t same = __match_any_sync(0xffffffffu, e);
             const int before = __popc(same & ((1u << lane) - 1));
             const int32_t start = e >= 0 ? mine[e] : 0;
@@ -104,11 +112,44 @@ __device__ __forceinline__ void place_rows(const Route &r, int64_t lo, int64_t h
         }
 }
 
+// A logit's place in the order of the choice, as the warp compares it.  The 16 bits of a 16-bit logit leave room for its
+// index: one maximum over the lanes then gives both, where 32 bits take a second step.
+template <typename T> struct Ranked {
+    static constexpr bool kIndexed = sizeof(T) == 2;
+    static __device__ __forceinline__ uint32_t of(T v, int index)
+    {
+        const uint32_t key = order_of(to_float(v));
+        if constexpr (!kIndexed) return key;
+        // (a bf16 is the upper half of its 32 bits; a f16 is ordered by its own)
+        if constexpr (std::is_same_v<T, __half>) {
+            const uint32_t b = __half_as_ushort(__hadd(v, __float2half_rn(0.0f)));
+            const uint32_t h = __hisnan(v) ? 0xffffu : b >> 15 ? (~b & 0xffffu) : b | 0x8000u;
+            return h << 16 | (0xffffu - uint32_t(index));
+        }
+        return (key & 0xffff0000u) | (0xffffu - uint32_t(index));
+    }
+    // What is never chosen: minus infinity and what has been taken.
+    static __device__ __forceinline__ bool never(uint32_t r)
+    {
+        if constexpr (!kIndexed) return r <= kNever;
+        else if constexpr (std::is_same_v<T, __half>) return r >> 16 <= 0x03ffu;
+        else return r >> 16 <= kNever >> 16;
+    }
+    static __device__ __forceinline__ float value(uint32_t r)
+    {
+        if constexpr (!kIndexed) return value_of(r);
+        const uint32_t h = r >> 16, b = h >> 15 ? h ^ 0x8000u : ~h & 0xffffu;
+        if constexpr (std::is_same_v<T, __half>) return __half2float(__ushort_as_half(uint16_t(b)));
+        return __uint_as_float(b << 16);
+    }
+};
+
 // The choice: L lanes hold PER logits of a token each, and agree `chosen` times on the largest that is left.  Blocks count
-// how many places each expert got among their tokens.
+// how many places each expert got among their tokens.  What bounds it is the number of instructions per token.
 template <typename T, int L, int PER>
 __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const RouteParams p)
 {
+    using R = Ranked<T>;
     __shared__ int32_t counts[kMostExperts], counters[kCounters];
     const Route &r = p.r;
     const int lane = int(threadIdx.x) & 31, at = lane % L, group = int(threadIdx.x) / L;
@@ -118,13 +159,21 @@ __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const Route
     wait_for_previous();
     __syncthreads();
     const int64_t lo = int64_t(blockIdx.x) * p.per_block, hi = min(r.tokens, lo + p.per_block);
+    T ahead[PER];
+    auto load = [&](int64_t t) {
+        const T *row = static_cast<const T *>(r.logits) + t * r.ld;
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (t < hi && at + 32 * j < r.experts) ahead[j] = row[at + 32 * j];
+    };
+    load(lo + group);
     for (int64_t base = lo; base < hi; base += kRouteThreads / L) {           // all lanes of a warp walk along
         const int64_t t = base + group;
         const bool in = t < hi;
-        const T *row = static_cast<const T *>(r.logits) + t * r.ld;
         uint32_t key[PER];
 #pragma unroll
-        for (int j = 0; j < PER; ++j) key[j] = in && at + 32 * j < r.experts ? order_of(to_float(row[at + 32 * j])) : 0;
+        for (int j = 0; j < PER; ++j) key[j] = in && at + 32 * j < r.experts ? R::of(ahead[j], at + 32 * j) : 0;
+        load(t + kRouteThreads / L);
         uint32_t best = 0, top = 0, own = 0;
         int32_t own_choice = -1;
         float every = 0.0f;
@@ -137,33 +186,49 @@ __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const Route
                 if (!r.normalize) {
 #pragma unroll
                     for (int j = 0; j < PER; ++j)
-                        if (key[j] > kNever) every += expf(value_of(key[j]) - value_of(top));
+                        if (!R::never(key[j])) every += expf(R::value(key[j]) - R::value(top));
                 }
             }
-            int32_t which;
-            if constexpr (PER == 1) {
-                which = __ffs(__ballot_sync(0xffffffffu, best == most) & segment) - 1 - lane / L * L;
+            if constexpr (R::kIndexed) {
+                if (at == s) own = most;
+                if (best == most) {                                           // (its own lane, or all are taken)
+                    best = 0;
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) {
+                        if (key[j] == most) key[j] = 0;
+                        best = max(best, key[j]);
+                    }
+                }
             } else {
-                uint32_t index = 0xffffu;
+                int32_t which;
+                if constexpr (PER == 1) {
+                    which = __ffs(__ballot_sync(0xffffffffu, best == most) & segment) - 1 - lane / L * L;
+                } else {
+                    uint32_t index = 0xffffu;
+                    if (best == most) {
 #pragma unroll
-                for (int j = PER - 1; j >= 0; --j)
-                    if (key[j] == most) index = uint32_t(at + 32 * j);
-                which = int32_t(__reduce_min_sync(0xffffffffu, index));
-            }
-            if (at == s) {
-                own = most;
-                own_choice = most > kNever ? which : -1;
-            }
-            if (which % 32 == at) {
-                best = 0;
+                        for (int j = PER - 1; j >= 0; --j)
+                            if (key[j] == most) index = uint32_t(at + 32 * j);
+                    }
+                    which = int32_t(__reduce_min_sync(0xffffffffu, index));
+                }
+                if (at == s) {
+                    own = most;
+                    own_choice = which;
+                }
+                if (which % 32 == at) {
+                    best = 0;
 #pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    if (at + 32 * j == which) key[j] = 0;
-                    best = max(best, key[j]);
+                    for (int j = 0; j < PER; ++j) {
+                        if (at + 32 * j == which) key[j] = 0;
+                        best = max(best, key[j]);
+                    }
                 }
             }
         }
-        const float part = own_choice >= 0 ? expf(value_of(own) - value_of(top)) : 0.0f;
+        if constexpr (R::kIndexed) own_choice = int32_t(0xffffu - (own & 0xffffu));
+        if (R::never(own)) own_choice = -1;
+        const float part = own_choice >= 0 ? expf(R::value(own) - R::value(top)) : 0.0f;
         const float total = lane_sum<L>(r.normalize ? part : every);
         if (in && at < r.chosen) {
             r.weights[t * r.chosen + at] = own_choice >= 0 ? part / total : 0.0f;
@@ -187,36 +252,33 @@ __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const Route
 // before it.
 __global__ void __launch_bounds__(kRouteThreads) redist_place_kernel(const RouteParams p)
 {
-    __shared__ int32_t base[kMostExperts], counters[kCounters], total;
+    __shared__ int32_t base[kMostExperts], before[kMostExperts], counters[kCounters], total;
     const Route &r = p.r;
     let_next_start();
     wait_for_previous();
-    int32_t before[kMostExperts / kRouteThreads] = {};
-#pragma unroll
-    for (int i = 0; i < kMostExperts / kRouteThreads; ++i) {
-        const int e = int(threadIdx.x) + i * kRouteThreads;
-        if (e < r.experts) {
-            int32_t sum = 0;
+    for (int e = threadIdx.x; e < r.experts; e += kRouteThreads) base[e] = before[e] = 0;
+    __syncthreads();
+    // the experts side by side, the blocks divided among the threads that are left
+    const int across = (r.experts + 31) / 32 * 32, parts = max(1, kRouteThreads / across), part = int(threadIdx.x) / across;
+    if (part < parts)
+        for (int e = int(threadIdx.x) - part * across; e < r.experts; e += kRouteThreads) {
+            int32_t sum = 0, early = 0;
 #pragma unroll 8
-            for (int b = 0; b < int(gridDim.x); ++b) {
+            for (int b = part; b < int(gridDim.x); b += parts) {
                 const int32_t n = p.counts[int64_t(b) * r.experts + e];
-                if (b < int(blockIdx.x)) before[i] += n;
                 sum += n;
+                if (b < int(blockIdx.x)) early += n;
             }
-            base[e] = sum;
+            atomicAdd(base + e, sum);                       // whole numbers: any order
+            atomicAdd(before + e, early);
         }
-    }
     __syncthreads();
     scan_counts(base, r.experts, &total);
     __syncthreads();
     if (blockIdx.x == 0)
         for (int e = threadIdx.x; e <= r.experts; e += kRouteThreads) r.offsets[e] = e < r.experts ? base[e] : total;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kMostExperts / kRouteThreads; ++i) {
-        const int e = int(threadIdx.x) + i * kRouteThreads;
-        if (e < r.experts) base[e] += before[i];
-    }
+    for (int e = threadIdx.x; e < r.experts; e += kRouteThreads) base[e] += before[e];
     __syncthreads();
     const int64_t lo = int64_t(blockIdx.x) * p.per_block, hi = min(r.tokens, lo + p.per_block);
     place_rows(r, min(lo, hi), hi, base, counters);
@@ -305,13 +367,14 @@ template <typename T, int N> struct Some {
     }
 };
 
-__device__ __forceinline__ int64_t row_at(const Move &m, int64_t place)
+__device__ __forceinline__ int32_t row_at(const Move &m, int64_t place)
 {
     const int32_t p = m.position[place];
     return p >= 0 && p < m.rows ? p : -1;
 }
 
 constexpr int kMoveThreads = 256, kHeld = 4;        // pieces a thread holds at a time
+constexpr int kGathered = 2;                        // ... of a row, where rows are read
 
 // L threads take kHeld L pieces of a token (of its `pieces`): loaded once, stored to its rows.
 template <typename T, int N, int L> __global__ void __launch_bounds__(kMoveThreads) redist_dispatch_kernel(const Move m, int pieces)
@@ -336,101 +399,147 @@ template <typename T, int N, int L> __global__ void __launch_bounds__(kMoveThrea
     }
 }
 
-// The other way: a token's rows, weighted and added in the order of its places.
-template <typename T, int N, int L> __global__ void __launch_bounds__(kMoveThreads) redist_combine_kernel(const Move m, int pieces)
+// K places of a token: their rows and weights.
+template <int K> struct Places {
+    int32_t row[K];
+    float weight[K];
+    __device__ __forceinline__ void load(const Move &m, int64_t t, int from)
+    {
+#pragma unroll
+        for (int i = 0; i < K; ++i) row[i] = t < m.tokens && from + i < m.chosen ? row_at(m, t * m.chosen + from + i) : -1;
+#pragma unroll
+        for (int i = 0; i < K; ++i) weight[i] = m.weights && t < m.tokens && from + i < m.chosen ? m.weights[t * m.chosen + from + i] : 1.0f;
+    }
+};
+
+// The other way: a token's rows, weighted and added in the order of its places.  L threads share a token (or a stretch of it)
+// and go on to others; K rows are on their way at a time, and the next token's places too, so that only one latency of
+// memory stands between tokens.
+template <typename T, int N, int L, int K> __global__ void __launch_bounds__(kMoveThreads, K > 2 ? 3 : 4) redist_combine_kernel(const Move m, int pieces)
 {
-    const int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + int(threadIdx.x) / L;
-    const int first = int(blockIdx.y) * kHeld * L + int(threadIdx.x) % L;
+    const int64_t step = int64_t(gridDim.x) * (kMoveThreads / L);
+    const int first = int(blockIdx.y) * kGathered * L + int(threadIdx.x) % L;
     let_next_start();
     wait_for_previous();
-    if (t >= m.tokens) return;
-    float sum[kHeld][N] = {};
-    if (m.residual) {
-        const T *from = static_cast<const T *>(m.residual) + t * m.ld_residual;
+    int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + int(threadIdx.x) / L;
+    Places<K> next;
+    next.load(m, t, 0);
+    for (; t < m.tokens; t += step) {
+        float sum[kGathered][N] = {};
+        Some<T, N> r[kGathered];
+        if (m.residual) {
+            const T *from = static_cast<const T *>(m.residual) + t * m.ld_residual;
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j)
+            for (int j = 0; j < kGathered; ++j)
+                if (first + j * L < pieces) r[j].load(from + int64_t(first + j * L) * N);
+        }
+        for (int s = 0; s < m.chosen; s += K) {
+            const Places<K> now = next;
+            Some<T, N> v[K][kGathered];
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                const T *from = static_cast<const T *>(m.row) + int64_t(now.row[i]) * m.ld_row;
+#pragma unroll
+                for (int j = 0; j < kGathered; ++j)
+                    if (now.row[i] >= 0 && first + j * L < pieces) v[i][j].load(from + int64_t(first + j * L) * N);
+            }
+            if (s + K < m.chosen) next.load(m, t, s + K);
+            else next.load(m, t + step, 0);
+            if (s == 0 && m.residual)
+#pragma unroll
+                for (int j = 0; j < kGathered; ++j)
+                    if (first + j * L < pieces)
+#pragma unroll
+                        for (int q = 0; q < N; ++q) sum[j][q] = to_float(r[j].v[q]);
+#pragma unroll
+            for (int i = 0; i < K; ++i)
+#pragma unroll
+                for (int j = 0; j < kGathered; ++j)
+                    if (now.row[i] >= 0 && first + j * L < pieces)
+#pragma unroll
+                        for (int q = 0; q < N; ++q) sum[j][q] = fmaf(now.weight[i], to_float(v[i][j].v[q]), sum[j][q]);
+        }
+        T *to = static_cast<T *>(m.token) + t * m.ld_token;
+#pragma unroll
+        for (int j = 0; j < kGathered; ++j)
             if (first + j * L < pieces) {
-                Some<T, N> v;
-                v.load(from + int64_t(first + j * L) * N);
+                Some<T, N> out;
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum[j][i] = to_float(v.v[i]);
+                for (int q = 0; q < N; ++q) out.v[q] = from_float<T>(sum[j][q]);
+                out.store(to + int64_t(first + j * L) * N);
             }
     }
-#pragma unroll 2
-    for (int s = 0; s < m.chosen; ++s) {
-        const int64_t row = row_at(m, t * m.chosen + s);
-        if (row < 0) continue;
-        const float w = m.weights ? m.weights[t * m.chosen + s] : 1.0f;
-        const T *from = static_cast<const T *>(m.row) + row * m.ld_row;
-        Some<T, N> v[kHeld];
-#pragma unroll
-        for (int j = 0; j < kHeld; ++j)
-            if (first + j * L < pieces) v[j].load(from + int64_t(first + j * L) * N);
-#pragma unroll
-        for (int j = 0; j < kHeld; ++j)
-            if (first + j * L < pieces)
-#pragma unroll
-                for (int i = 0; i < N; ++i) sum[j][i] = fmaf(w, to_float(v[j].v[i]), sum[j][i]);
-    }
-    T *to = static_cast<T *>(m.token) + t * m.ld_token;
-#pragma unroll
-    for (int j = 0; j < kHeld; ++j)
-        if (first + j * L < pieces) {
-            Some<T, N> v;
-#pragma unroll
-            for (int i = 0; i < N; ++i) v.v[i] = from_float<T>(sum[j][i]);
-            v.store(to + int64_t(first + j * L) * N);
-        }
 }
 
-// The gradient of the latter: L threads take a whole token, because dweights are sums over its columns.
-template <typename T, int N, int L> __global__ void __launch_bounds__(kMoveThreads) redist_combine_gradient_kernel(const Move m, int pieces)
+// The gradient of the latter: L threads take whole tokens, because dweights are sums over their columns.
+template <typename T, int N, int L, int K> __global__ void __launch_bounds__(kMoveThreads, 3) redist_combine_gradient_kernel(const Move m, int pieces)
 {
-    __shared__ float dots[kMoveThreads / 32][kMostChosen];
-    const int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + int(threadIdx.x) / L;
-    const int at = int(threadIdx.x) % L, warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31;
+    __shared__ float dots[2][kMoveThreads / 32][kMostChosen];
+    const int64_t step = int64_t(gridDim.x) * (kMoveThreads / L);
+    const int group = int(threadIdx.x) / L, at = int(threadIdx.x) % L, warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31;
     let_next_start();
     wait_for_previous();
-    const bool in = t < m.tokens;
-    const T *dy = static_cast<const T *>(m.token) + (in ? t : 0) * m.ld_token;
-    for (int s = 0; s < m.chosen; ++s) {
-        const int64_t row = in ? row_at(m, t * m.chosen + s) : -1;
-        float dot = 0.0f;
-        if (row >= 0) {
-            const float w = m.weights[t * m.chosen + s];
-            const T *y = static_cast<const T *>(m.row) + row * m.ld_row;
-            T *to = static_cast<T *>(m.drow) + row * m.ld_drow;
-            for (int first = at; first < pieces; first += kHeld * L) {
-                Some<T, N> d[kHeld], v[kHeld];
+    int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + group;
+    Places<K> next;
+    next.load(m, t, 0);
+    int turn = 0;
+    for (int64_t base = int64_t(blockIdx.x) * (kMoveThreads / L); base < m.tokens; base += step, t += step, turn ^= 1) {      // the block walks along
+        const bool in = t < m.tokens;
+        const T *dy = static_cast<const T *>(m.token) + (in ? t : 0) * m.ld_token;
+        for (int s = 0; s < m.chosen; s += K) {
+            const Places<K> now = next;
+            float dot[K] = {};
+            for (int first = at; first < pieces; first += kGathered * L) {
+                Some<T, N> d[kGathered], v[K][kGathered];
 #pragma unroll
-                for (int j = 0; j < kHeld; ++j)
-                    if (first + j * L < pieces) {
-                        d[j].load(dy + int64_t(first + j * L) * N);
-                        v[j].load(y + int64_t(first + j * L) * N);
-                    }
+                for (int j = 0; j < kGathered; ++j)
+                    if (in && first + j * L < pieces) d[j].load(dy + int64_t(first + j * L) * N);
 #pragma unroll
-                for (int j = 0; j < kHeld; ++j)
-                    if (first + j * L < pieces) {
-                        Some<T, N> out;
+                for (int i = 0; i < K; ++i) {
+                    const T *y = static_cast<const T *>(m.row) + int64_t(now.row[i]) * m.ld_row;
 #pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            const float g = to_float(d[j].v[i]);
-                            dot = fmaf(g, to_float(v[j].v[i]), dot);
-                            out.v[i] = from_float<T>(w * g);
+                    for (int j = 0; j < kGathered; ++j)
+                        if (now.row[i] >= 0 && first + j * L < pieces) v[i][j].load(y + int64_t(first + j * L) * N);
+                }
+                if (first == at) {
+                    if (s + K < m.chosen) next.load(m, t, s + K);
+                    else next.load(m, t + step, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < K; ++i) {
+                    T *to = static_cast<T *>(m.drow) + int64_t(now.row[i]) * m.ld_drow;
+#pragma unroll
+                    for (int j = 0; j < kGathered; ++j)
+                        if (now.row[i] >= 0 && first + j * L < pieces) {
+                            Some<T, N> out;
+#pragma unroll
+                            for (int q = 0; q < N; ++q) {
+                                const float g = to_float(d[j].v[q]);
+                                dot[i] = fmaf(g, to_float(v[i][j].v[q]), dot[i]);
+                                out.v[q] = from_float<T>(now.weight[i] * g);
+                            }
+                            out.store(to + int64_t(first + j * L) * N);
                         }
-                        out.store(to + int64_t(first + j * L) * N);
-                    }
+                }
+            }
+            if (at >= pieces) {                             // (a thread without pieces has not asked)
+                if (s + K < m.chosen) next.load(m, t, s + K);
+                else next.load(m, t + step, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                dot[i] = lane_sum<32>(dot[i]);
+                if (lane == 0 && s + i < m.chosen) dots[turn][warp][s + i] = dot[i];
             }
         }
-        dot = lane_sum<32>(dot);
-        if (lane == 0) dots[warp][s] = dot;
-    }
-    if constexpr (L > 32) __syncthreads();
-    else __syncwarp();
-    for (int s = at; in && s < m.chosen; s += L) {
-        float sum = 0.0f;
-        for (int i = 0; i < L / 32; ++i) sum += dots[int(threadIdx.x) / L * (L / 32) + i][s];
-        m.dweights[t * m.chosen + s] = sum;
+        // the next token writes to the other half: one barrier for each
+        if constexpr (L > 32) __syncthreads();
+        else __syncwarp();
+        for (int s = at; in && s < m.chosen; s += L) {
+            float sum = 0.0f;
+            for (int i = 0; i < L / 32; ++i) sum += dots[turn][group * (L / 32) + i][s];
+            m.dweights[t * m.chosen + s] = sum;
+        }
     }
 }
 
@@ -488,25 +597,41 @@ int together(int64_t cols, int type, std::initializer_list<std::pair<const void 
 
 enum Which { kDispatch, kCombine, kGradient };
 
+// Blocks that walk along the tokens: as many as fit on the GPU.
+unsigned walkers(int64_t tokens, int64_t tokens_per, unsigned across, int resident)
+{
+    return unsigned(std::max<int64_t>(1, std::min<int64_t>((tokens + tokens_per - 1) / tokens_per, (int64_t(resident) + across - 1) / across)));
+}
+
+template <Which W, typename T, int N, int L> cudaError_t launch_move_width(const Move &m, int pieces, int sms, const LaunchOptions &o, cudaStream_t stream)
+{
+    constexpr int kTokens = kMoveThreads / L;
+    if constexpr (W == kDispatch) {
+        const dim3 grid(unsigned((m.tokens + kTokens - 1) / kTokens), unsigned((pieces + kHeld * L - 1) / (kHeld * L)));
+        if (grid.y > 65535) return cudaErrorInvalidValue;
+        return launch(redist_dispatch_kernel<T, N, L>, grid, kMoveThreads, o, stream, m, pieces);
+    } else if constexpr (W == kCombine) {
+        const unsigned y = unsigned((pieces + kGathered * L - 1) / (kGathered * L));
+        if (y > 65535) return cudaErrorInvalidValue;
+        const dim3 grid(walkers(m.tokens, kTokens, y, sms * (m.chosen <= 2 ? 4 : 3)), y);
+        if (m.chosen <= 2) return launch(redist_combine_kernel<T, N, L, 2>, grid, kMoveThreads, o, stream, m, pieces);
+        return launch(redist_combine_kernel<T, N, L, 4>, grid, kMoveThreads, o, stream, m, pieces);
+    } else {
+        const dim3 grid(walkers(m.tokens, kTokens, 1, sms * 3));
+        return launch(redist_combine_gradient_kernel<T, N, L, 2>, grid, kMoveThreads, o, stream, m, pieces);
+    }
+}
+
 template <Which W, typename T, int N> cudaError_t launch_move_lanes(const Move &m, const LaunchOptions &o, cudaStream_t stream)
 {
     const int64_t pieces = (m.cols + N - 1) / N;
+    if (pieces > INT32_MAX / 2) return cudaErrorInvalidValue;
+    int device = 0, sms = 0;
+    const cudaError_t ce = current_device(&device, &sms);
+    if (ce != cudaSuccess) return ce;
     // a warp per token (or stretch of it) for short rows, a block for longer ones
-    const bool wide = pieces > 32 * kHeld;
-    const int64_t tokens_per = wide ? 1 : kMoveThreads / 32, chunk = (wide ? kMoveThreads : 32) * kHeld;
-    const unsigned x = unsigned((m.tokens + tokens_per - 1) / tokens_per), y = unsigned(W == kGradient ? 1 : (pieces + chunk - 1) / chunk);
-    if (y > 65535 || pieces > INT32_MAX / 2) return cudaErrorInvalidValue;
-    const dim3 grid = dim3(x, y);
-    if constexpr (W == kDispatch) {
-        if (wide) return launch(redist_dispatch_kernel<T, N, kMoveThreads>, grid, kMoveThreads, o, stream, m, int(pieces));
-        return launch(redist_dispatch_kernel<T, N, 32>, grid, kMoveThreads, o, stream, m, int(pieces));
-    } else if constexpr (W == kCombine) {
-        if (wide) return launch(redist_combine_kernel<T, N, kMoveThreads>, grid, kMoveThreads, o, stream, m, int(pieces));
-        return launch(redist_combine_kernel<T, N, 32>, grid, kMoveThreads, o, stream, m, int(pieces));
-    } else {
-        if (wide) return launch(redist_combine_gradient_kernel<T, N, kMoveThreads>, grid, kMoveThreads, o, stream, m, int(pieces));
-        return launch(redist_combine_gradient_kernel<T, N, 32>, grid, kMoveThreads, o, stream, m, int(pieces));
-    }
+    if (pieces > 32 * kHeld) return launch_move_width<W, T, N, kMoveThreads>(m, int(pieces), sms, o, stream);
+    return launch_move_width<W, T, N, 32>(m, int(pieces), sms, o, stream);
 }
 
 template <Which W, typename T> cudaError_t launch_move_typed(const Move &m, int n, const LaunchOptions &o, cudaStream_t stream)
