@@ -2,7 +2,7 @@
 //
 // Two passes over the data, the second only where it changes something or goes elsewhere.  The tensors' addresses travel as
 // arguments of the launch (nothing is copied to the device, so a call can be captured), up to 1000 of them.  The tensors are cut
-// into units of 16 KB; every block takes a stretch of units, adds their squares and leaves a partial sum in 64 bits; the
+// into units of 32 KB; every block takes a stretch of units, adds their squares and leaves a partial sum in 64 bits; the
 // blocks of the second pass all add all partial sums, in the same order, so that no block waits for another, and go through
 // their stretch backwards: what the first pass read last is still in L2.
 #include "clip.h"
@@ -16,7 +16,7 @@ namespace redist {
 
 namespace {
 
-constexpr int kThreads = 256, kPieces = 4, kUnit = kThreads * kPieces * 16, kBlocksPerSm = 4;
+constexpr int kThreads = 256, kPieces = 8, kUnit = kThreads * kPieces * 16, kBlocksPerSm = 3;
 
 template <int MOST> struct ClipTable {
     const void *data[MOST];
@@ -136,23 +136,15 @@ template <int MOST> __device__ __forceinline__ int tensor_of(const ClipTable<MOS
     return lo;
 }
 
-template <int MOST> __device__ __forceinline__ void stretch(const ClipTable<MOST> &c, int &from, int &to)
-{
-    const int64_t units = c.begin[c.count];
-    from = int(units * blockIdx.x / gridDim.x);
-    to = int(units * (blockIdx.x + 1) / gridDim.x);
-}
-
 template <int MOST> __global__ void __launch_bounds__(kThreads, kBlocksPerSm) redist_squares_kernel(const __grid_constant__ ClipTable<MOST> c, double *sums)
 {
     __shared__ double slot[kThreads / 32];
     let_next_start();
     wait_for_previous();
-    int from, to;
-    stretch(c, from, to);
+    const int units = c.begin[c.count];
     double sum = 0.0;
-    for (int u = from, i = from < to ? tensor_of(c, from) : 0; u < to; ++u) {
-        while (u >= c.begin[i + 1]) ++i;
+    for (int u = blockIdx.x; u < units; u += gridDim.x) {
+        const int i = tensor_of(c, u);
         const int64_t unit = u - c.begin[i];
         if (c.type[i] == T_BF16) sum += squares(Share<__nv_bfloat16>(c.data[i], c.elements[i], unit));
         else if (c.type[i] == T_F16) sum += squares(Share<__half>(c.data[i], c.elements[i], unit));
@@ -184,7 +176,7 @@ template <typename T> __device__ __forceinline__ void scale(const void *data, vo
                 w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
             else
                 w = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
-            __stcs(reinterpret_cast<uint4 *>(to + first), w);       // (not wanted again before all else: L2 keeps what is read)
+            *reinterpret_cast<uint4 *>(to + first) = w;
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
@@ -205,10 +197,8 @@ template <int MOST> __global__ void __launch_bounds__(kThreads, kBlocksPerSm) re
     if (c.max_norm < 0.0f) return;
     float factor = c.max_norm / (norm + c.eps);
     if (factor > 1.0f) factor = 1.0f;                       // (a NaN stays)
-    int from, to;
-    stretch(c, from, to);
-    for (int u = to - 1, i = from < to ? tensor_of(c, to - 1) : 0; u >= from; --u) {
-        while (u < c.begin[i]) --i;
+    for (int u = c.begin[c.count] - 1 - int(blockIdx.x); u >= 0; u -= gridDim.x) {
+        const int i = tensor_of(c, u);
         if (factor == 1.0f && c.out[i] == c.data[i]) continue;
         const int64_t unit = u - c.begin[i];
         if (c.type[i] == T_BF16) scale<__nv_bfloat16>(c.data[i], c.out[i], c.elements[i], unit, factor);

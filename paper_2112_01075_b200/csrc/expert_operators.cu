@@ -164,6 +164,18 @@ redist_status check_experts_backward(const redist_experts &q, const redist_exper
     return on(g.dbias, 4) ? REDIST_OK : REDIST_EALIGN;
 }
 
+// Operands to lay anew, up to three in one launch.
+struct Lays {
+    Lay list[3];
+    int count = 0;
+    redist_status launch(const LaunchOptions &o, cudaStream_t stream)
+    {
+        const int n = count;
+        count = 0;
+        return cuda(launch_lay(list, n, o, stream));
+    }
+};
+
 // A stack as an operand: as it lies, or laid out anew in scratch.
 struct PlacedStack {
     Lines from;
@@ -177,15 +189,15 @@ struct PlacedStack {
         plane = fits ? stride : from.lines * ld;
         if (!fits) copy = pieces.take(count * plane * 2);
     }
-    cudaError_t lay(int type, const LaunchOptions &o, cudaStream_t stream) const
+    // Adds what lays it anew to `lays`, which goes off when it is full.
+    redist_status lay(int type, Lays &lays, const LaunchOptions &o, cudaStream_t stream) const
     {
-        if (fits) return cudaSuccess;
+        if (fits) return REDIST_OK;
         const bool even = count == 1 || stride == from.lines * from.ld;        // one long matrix
-        Lay list[3] = {};
-        int n = 0;
-        cudaError_t ce = cudaSuccess;
-        for (i64 i = 0; i < (even ? 1 : count) && ce == cudaSuccess; ++i) {
-            Lay &l = list[n++];
+        for (i64 i = 0; i < (even ? 1 : count); ++i) {
+            if (lays.count == 3) TRY(lays.launch(o, stream));
+            Lay &l = lays.list[lays.count++];
+            l = Lay{};
             l.rows = even ? count * from.lines : from.lines;
             l.cols = from.line;
             l.type = type;
@@ -193,17 +205,26 @@ struct PlacedStack {
             l.ld_src = from.ld;
             l.dst = static_cast<char *>(copy) + i * plane * 2;
             l.ld_dst = ld;
-            if (n == 3 || i + 1 == (even ? 1 : count)) {
-                ce = launch_lay(list, n, o, stream);
-                n = 0;
-            }
         }
-        return ce;
+        return REDIST_OK;
     }
     Operand operand(bool rows_survive) const { return Operand{fits ? from.data : copy, ld, plane, from.by_rows == rows_survive ? 0 : 1}; }
 };
 
 const redist_matrix kAbsent = {nullptr, 1, 1};
+
+// A forward call of a few rows reads its operands as they lie and needs no scratch: up to eight rows, where its blocks are more
+// than the tiles and start sooner (2 rows of 8 experts, 4096 -> 4096: 15.7 us against 18; 6 rows of 128, 1024 -> 1024: 6.4 and 9.2),
+// and up to 32 where the weights they meet are small (32 rows of 4, 512 -> 512: 4.3 and 5.4, but 32 of 8, 4096 -> 4096: 52 and 49)
+// and on 16-byte boundaries (513 -> 511: 11.6 and 9.6).
+bool few_expert_rows(const redist_experts &q, const LaunchOptions &o)
+{
+    if (o.test_shape || q.rows > kFewRows || !row_major(q.x, q.rows, q.in_features) || !row_major(q.w, q.out_features, q.in_features)) return false;
+    if (q.rows <= 8) return true;
+    const double met = double(std::min<i64>(q.rows, q.experts)) * double(q.in_features) * double(q.out_features);
+    return met <= double(1 << 23) && operand_fits(q.x.data, row_stride(q.x, q.rows, q.in_features), 0, 1) &&
+           operand_fits(q.w.data, row_stride(q.w, q.out_features, q.in_features), q.w_stride, int(std::min<i64>(q.experts, 2)));
+}
 
 struct ExpertsForward {
     Placed x;
@@ -424,7 +445,7 @@ size_t redist_experts_scratch_bytes(const redist_experts *op, const redist_exper
     if (!op) return 0;
     Pieces p{0};
     if (!grads) {
-        if (check_experts_forward(*op) != REDIST_OK || op->rows == 0) return 0;
+        if (check_experts_forward(*op) != REDIST_OK || op->rows == 0 || few_expert_rows(*op, options())) return 0;
         ExpertsForward f(*op, p);
     } else {
         if (check_experts_backward(*op, *grads) != REDIST_OK || op->rows == 0) return 0;
@@ -443,25 +464,20 @@ redist_status redist_experts_forward(const redist_experts *op, void *scratch, si
         const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
         const LaunchOptions o = options();
         Pieces p{uintptr_t(scratch)};
-        const ExpertsForward f(q, p);
+        const bool few = few_expert_rows(q, o);
+        Pieces none{0};
+        const ExpertsForward f(q, few ? none : p);
         const Extent outs[3] = {extent(q.out, q.rows, q.out_features, 2), extent(q.pre, q.pre.data ? q.rows : 0, q.out_features, 2), extent(scratch, p.used)};
         const Extent ins[4] = {extent(q.x, q.rows, q.in_features, 2), extent(q.w, q.out_features, q.in_features, 2, q.experts, q.w_stride),
                                extent(q.bias, ((q.experts - 1) * q.bias_stride + q.out_features) * type_bytes(q.bias_type)), extent(q.offsets, i64(q.experts + 1) * 4)};
         TRY(apart(outs, 3, ins, 4));
         TRY(check_scratch(scratch, scratch_bytes, p.used));
-        Lay list[1];
-        int lays = 0;
-        f.x.lay(q.type, list, lays);
-        TRY(cuda(launch_lay(list, lays, o, stream)));
-        TRY(cuda(f.w.lay(q.type, o, stream)));
         Grouped g = {};
         g.rows = q.rows;
         g.m = q.out_features;
         g.k = q.in_features;
         g.experts = q.experts;
         g.type = q.type;
-        g.a = f.w.operand(true);
-        g.b = f.x.operand(true);
         g.offsets = q.offsets;
         g.out = q.out.data;
         g.ld_out = row_stride(q.out, q.rows, q.out_features);
@@ -471,6 +487,17 @@ redist_status redist_experts_forward(const redist_experts *op, void *scratch, si
         g.bias_type = q.bias_type;
         g.bias_stride = q.bias_stride;
         g.activation = q.activation;
+        if (few) {
+            g.a = Operand{f.w.from.data, f.w.from.ld, q.w_stride, 0};
+            g.b = Operand{f.x.from.data, f.x.from.ld, 0, 0};
+            return cuda(launch_few_grouped(g, o, stream));
+        }
+        Lays lays;
+        f.x.lay(q.type, lays.list, lays.count);
+        TRY(f.w.lay(q.type, lays, o, stream));
+        TRY(lays.launch(o, stream));
+        g.a = f.w.operand(true);
+        g.b = f.x.operand(true);
         return cuda(launch_grouped(g, nullptr, o, stream));
     } catch (...) {
         return REDIST_EINTERNAL;
@@ -527,6 +554,10 @@ redist_status redist_experts_backward(const redist_experts *op, const redist_exp
             s.partials = b.partials;
             TRY(cuda(launch_expert_slope(s, o, stream)));
         }
+        Lays lays;
+        if (g.dw.data) b.x.lay(q.type, lays.list, lays.count);
+        if (g.dx.data) TRY(b.w.lay(q.type, lays, o, stream));
+        TRY(lays.launch(o, stream));
         const void *dz = b.fresh ? b.dz : g.dy.data;
         Grouped d = {};
         d.rows = q.rows;
@@ -535,7 +566,6 @@ redist_status redist_experts_backward(const redist_experts *op, const redist_exp
         d.offsets = q.offsets;
         d.activation = ACT_NONE;
         if (g.dx.data) {
-            TRY(cuda(b.w.lay(q.type, o, stream)));
             Grouped x = d;
             x.m = q.in_features;
             x.k = q.out_features;
@@ -546,10 +576,6 @@ redist_status redist_experts_backward(const redist_experts *op, const redist_exp
             TRY(cuda(launch_grouped(x, nullptr, o, stream)));
         }
         if (g.dw.data) {
-            Lay list[1];
-            int lays = 0;
-            b.x.lay(q.type, list, lays);
-            TRY(cuda(launch_lay(list, lays, o, stream)));
             Grouped w = d;
             w.sums = 1;
             w.m = q.in_features;

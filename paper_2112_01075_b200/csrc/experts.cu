@@ -39,12 +39,18 @@ constexpr uint32_t kDrainPolls = 1 << 16, kCopyPolls = 1 << 10;         // as in
 
 __device__ unsigned int g_grouped_timeouts = 0;
 
+// Quotients of small numbers without a division, of which a warp's every tile would take four: a thousand cycles, in which
+// neither products nor stores are under way.
+struct Divider {
+    uint32_t mul, shift;                // mul 0: by one
+};
 struct GroupedParams {
     int32_t rows, m, n, experts, k_blocks;
     int32_t tiles_m, tiles_n;           // tiles_n: SUMS only
     int32_t a_along_rows, b_along_rows;
+    Divider by_group, by_matrix;        // 8 tiles_m; SUMS: tiles_m tiles_n
     uint32_t idesc, wait_polls, test_extra_tx;
-    int32_t aligned_out, activation, type;
+    int32_t aligned_out, activation, type, run;      // run: SUMS: log2 of the tiles that a block takes one after the other
     const int32_t *offsets;
     const CUtensorMap *maps;            // SUMS: of a and b for every expert
     void *out, *pre;
@@ -64,14 +70,31 @@ struct GroupedTile {
     int expert, tm, row0, count, k0, steps;     // rows row0 ... row0 + count - 1 of the result (SUMS: its rows, and where its sum begins)
 };
 
+__device__ __forceinline__ int quotient(int n, const Divider &d) { return d.mul ? int(__umulhi(uint32_t(n), d.mul) >> d.shift) : n; }    // n >= 0
+__device__ __forceinline__ int by_height(int n, int height)      // 1 to 8; n < 2^29
+{
+    if (height == 8) return n >> 3;
+    if (height == 1) return n;
+    return int(__umulhi(uint32_t(n), height == 2 ? 0x80000000u : height == 3 ? 0x55555556u : height == 4 ? 0x40000000u : height == 5 ? 0x33333334u
+                                     : height == 6 ? 0x2aaaaaabu : 0x24924925u));
+}
+
 // A warp's walk along the tiles, in increasing order.  ROWS: lane i knows the range of expert chunk + i and how many tiles
 // it has up to there.
 template <int CG, int BN, int KB, bool SUMS> struct Walk {
     const GroupedParams &p;
-    int chunk = -32, lane;
-    int lo = 0, hi = 0, through = 0, before = 0, all = 0, carry = 0;    // before: tiles of earlier chunks; all: of this one
+    int chunk = -32, lane, first, step;
+    int lo = 0, hi = 0, parts = 0, width = 0, through = 0, before = 0, all = 0, carry = 0;  // before: tiles of earlier chunks; all: of this one
+    int expert = -1, k0 = 0, steps = 0;
 
-    __device__ __forceinline__ Walk(const GroupedParams &params) : p(params), lane(int(threadIdx.x) & 31) {}
+    __device__ __forceinline__ Walk(const GroupedParams &params) : p(params), lane(int(threadIdx.x) & 31), first(blockIdx.x / CG), step(gridDim.x / CG) {}
+
+    // The n-th tile of this block, if there is one; all lanes get the answer.
+    __device__ __forceinline__ bool next_at(int n, GroupedTile &r)
+    {
+        if constexpr (SUMS) return at(((((n >> p.run) * step) + first) << p.run) + (n & ((1 << p.run) - 1)), r);
+        else return at(first + n * step, r);
+    }
 
     // The next 32 experts.  Offsets that decrease count as the largest before them.
     __device__ __forceinline__ void next()
@@ -89,7 +112,9 @@ template <int CG, int BN, int KB, bool SUMS> struct Walk {
         lo = max(start, carry);
         hi = max(lo, end);
         carry = __shfl_sync(0xffffffffu, hi, 31);
-        through = e < p.experts ? (hi - lo + BN - 1) / BN * p.tiles_m : 0;
+        parts = e < p.experts ? (hi - lo + BN - 1) / BN : 0;
+        width = parts ? ((hi - lo + parts - 1) / parts + 16 * CG - 1) / (16 * CG) * (16 * CG) : 0;
+        through = parts * p.tiles_m;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int up = __shfl_up_sync(0xffffffffu, through, d);
@@ -98,21 +123,26 @@ template <int CG, int BN, int KB, bool SUMS> struct Walk {
         all = __shfl_sync(0xffffffffu, through, 31);
     }
 
-    // Tile `t`, if there is one; all lanes get the answer.
+    // Tile `t`, if there is one.  Tiles of an expert in groups of eight parts of the rows (SUMS: of the result's rows), so that the
+    // blocks at work at one time share both operands in L2.
     __device__ __forceinline__ bool at(int t, GroupedTile &r)
     {
         if constexpr (SUMS) {
-            const int per = p.tiles_m * p.tiles_n;
-            if (t >= per * p.experts) return false;
-            r.expert = t / per;
-            int q = t - r.expert * per;
-            const int group = q / (8 * p.tiles_m), height = min(8, p.tiles_n - group * 8);
+            r.expert = quotient(t, p.by_matrix);
+            if (r.expert >= p.experts) return false;
+            int q = t - r.expert * p.tiles_m * p.tiles_n;
+            const int group = quotient(q, p.by_group), height = min(8, p.tiles_n - group * 8);
             q -= group * 8 * p.tiles_m;
-            r.row0 = (group * 8 + q % height) * BN;
+            r.tm = by_height(q, height);
+            r.row0 = (group * 8 + q - r.tm * height) * BN;
             r.count = min(BN, p.n - r.row0);
-            r.tm = q / height;
-            r.k0 = offset_at(p, r.expert);
-            r.steps = (max(0, offset_at(p, r.expert + 1) - r.k0) + KB * kBK - 1) / (KB * kBK);
+            if (r.expert != expert) {
+                expert = r.expert;
+                k0 = offset_at(p, expert);
+                steps = (max(0, offset_at(p, expert + 1) - k0) + KB * kBK - 1) / (KB * kBK);
+            }
+            r.k0 = k0;
+            r.steps = steps;
             return true;
         } else {
             while (t >= before + all) {
@@ -121,16 +151,14 @@ template <int CG, int BN, int KB, bool SUMS> struct Walk {
             }
             const int which = __ffs(__ballot_sync(0xffffffffu, before + through > t)) - 1;
             const int from = __shfl_sync(0xffffffffu, lo, which), to = __shfl_sync(0xffffffffu, hi, which);
-            const int tiles = (to - from + BN - 1) / BN;
+            const int tiles = __shfl_sync(0xffffffffu, parts, which), wide = __shfl_sync(0xffffffffu, width, which);
             int q = t - before - (__shfl_sync(0xffffffffu, through, which) - tiles * p.tiles_m);
-            // columns of tiles in groups of eight, so that the blocks at work at one time share both operands in L2
-            const int group = q / (8 * p.tiles_m), height = min(8, tiles - group * 8);
+            const int group = quotient(q, p.by_group), height = min(8, tiles - group * 8);
             q -= group * 8 * p.tiles_m;
-            const int width = ((to - from + tiles - 1) / tiles + 16 * CG - 1) / (16 * CG) * (16 * CG);
             r.expert = chunk + which;
-            r.row0 = from + (group * 8 + q % height) * width;
-            r.count = max(0, min(width, to - r.row0));
-            r.tm = q / height;
+            r.tm = by_height(q, height);
+            r.row0 = from + (group * 8 + q - r.tm * height) * wide;
+            r.count = max(0, min(wide, to - r.row0));
             r.k0 = 0;
             r.steps = p.k_blocks;
             return true;
@@ -244,7 +272,6 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 1 ? 0 : cluster_rank();
-    const int first = blockIdx.x / CG, step = gridDim.x / CG;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -280,7 +307,7 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         const CUtensorMap *map = second ? &map_b : &map_a;
         const int along_rows = SUMS ? 1 : second ? p.b_along_rows : p.a_along_rows;
         int expert = -1;
-        for (int t = first; walk.at(t, at); t += step) {
+        for (int n = 0; walk.next_at(n, at); ++n) {
             if (SUMS && at.expert != expert && at.steps) {
                 expert = at.expert;
                 map = p.maps + 2 * expert + second;
@@ -338,7 +365,7 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         const int a_along = SUMS ? 1 : p.a_along_rows, b_along = SUMS ? 1 : p.b_along_rows;
         const uint64_t desc_a = slice_desc(base, a_along), desc_b = slice_desc(base + kStageA, b_along);
         const uint64_t step_a = a_along ? 2048 >> 4 : 32 >> 4, step_b = b_along ? 2048 >> 4 : 32 >> 4;
-        for (int t = first; walk.at(t, at); t += step, ++use) {
+        for (; walk.next_at(use, at); ++use) {
             const int buf = use & 1;
             if (!bar_wait(acc_free(buf), ((use >> 1) & 1) ^ 1, polls)) {
                 ok = false;
@@ -384,7 +411,7 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         GroupedPieces pieces{ring + kRing + (warp - 4) * 2 * kPiece, base + kRing + (warp - 4) * 2 * kPiece};
         int use = 0;
-        for (int t = first; walk.at(t, at); t += step, ++use) {
+        for (; walk.next_at(use, at); ++use) {
             const int b = use & 1;
             const int col0 = (at.tm * CG + int(rank)) * 128 + quarter * 32, left = p.m - col0;
             float bias[4] = {};
@@ -441,10 +468,12 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             fence_before();
             __syncwarp();
             if (lane == 0) {
+                // (relaxed: what is handed back is tensor memory, whose loads are over.  A release to the cluster would wait for the stores
+                // to memory as well, 1450 cycles a tile.)
                 if constexpr (CG == 1)
                     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(acc_free(b)) : "memory");
                 else
-                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first(acc_free(b))) : "memory");
+                    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first(acc_free(b))) : "memory");
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -665,6 +694,15 @@ cudaError_t launch_any(void (*kernel)(P...), dim3 grid, int threads, int smem, i
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// The smallest power of two that makes the quotient exact for numerators below 2^31.
+Divider divider(int64_t d)
+{
+    if (d <= 1) return Divider{0, 0};
+    int lg = 0;
+    while ((int64_t(1) << lg) < d) ++lg;
+    return Divider{uint32_t(((uint64_t(1) << (31 + lg)) + uint64_t(d) - 1) / uint64_t(d)), uint32_t(lg - 1)};
+}
+
 template <int CG, int BN, int KB, bool SUMS>
 cudaError_t launch(const Grouped &g, void *scratch, const LaunchOptions &o, int device, int sms, cudaStream_t stream)
 {
@@ -702,7 +740,9 @@ cudaError_t launch(const Grouped &g, void *scratch, const LaunchOptions &o, int 
     // a bound on the tiles: every expert with rows has at most one that is not full
     const int64_t parts = SUMS ? int64_t(p.tiles_n) * g.experts : std::min<int64_t>(g.experts, g.rows) + g.rows / BN;
     const int64_t tiles = parts * p.tiles_m;
-    if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
+    if (tiles > INT32_MAX / 8 || int64_t(p.tiles_m) * 8 >= INT32_MAX / 8) return cudaErrorInvalidValue;
+    p.by_group = divider(int64_t(p.tiles_m) * 8);
+    p.by_matrix = divider(int64_t(p.tiles_m) * std::max(p.tiles_n, 1));
 
     CUtensorMap ma, mb, ms, mo, mp;
     const int64_t features = SUMS ? g.n : g.rows, sum = SUMS ? g.rows : g.k;
@@ -727,19 +767,26 @@ cudaError_t launch(const Grouped &g, void *scratch, const LaunchOptions &o, int 
         if (device < 64) ready.fetch_or(uint64_t(1) << device, std::memory_order_relaxed);
     }
     const int64_t groups = sms / CG;
+    // Every other expert costs the loading warps a fence and the fetch of a tensor map: where sums are short, blocks take a few
+    // tiles of one expert after the other (64 gradients of 1024 x 2048 over 256 rows: 56 -> 53 us on pairs, 70 -> 65 on single SMs;
+    // more of them leave SMs idle at the end).
+    if (SUMS) {
+        const int64_t steps = std::max<int64_t>(1, g.rows / g.experts / kBK);
+        while (p.run < (CG == 2 ? 1 : 3) && (steps << p.run) < 4 && (groups << (p.run + 1)) <= tiles) ++p.run;
+    }
     return launch_any(kernel, dim3(unsigned(std::min(tiles, groups) * CG)), kThreads, kSmem, CG, o, stream, ma, mb, ms, mo, mp, p);
 }
 
 // The tile shapes, and what they take: microseconds per 64 steps of a sum, `step` + `column` per column computed (at least
-// `least`; three quarters where all tiles fit on the GPU at once), and per launch besides.  Fitted to timings of some twenty
+// `least`; three quarters where all tiles fit on the GPU at once), but at least `tile` a tile (its stores), and per launch besides.  Fitted to timings of some twenty
 // sizes from 500 x 512 -> 512 to 32768 x 4096 -> 4096.
 enum GroupedShape { kPair256, kPair128, kOne32, kOne128, kOne64 };
 struct GroupedCost {
     int rows, cols, per_unit;
-    double step, column, least, launch;
+    double step, column, least, tile, launch;
 };
-constexpr GroupedCost kGroupedCosts[] = {{256, 256, 2, 0.044, 0.00147, 0.18, 5.5}, {256, 128, 2, 0.044, 0.00147, 0.18, 4.5}, {128, 32, 1, 0.185, 0.00066, 0, 3.4},
-                                         {128, 128, 1, 0.185, 0.00066, 0, 4.2}, {128, 64, 1, 0.185, 0.00066, 0, 3.6}};
+constexpr GroupedCost kGroupedCosts[] = {{256, 256, 2, 0.044, 0.00147, 0.18, 1.6, 5.5}, {256, 128, 2, 0.044, 0.00147, 0.18, 1.0, 4.5}, {128, 32, 1, 0.185, 0.00066, 0, 0.5, 3.4},
+                                         {128, 128, 1, 0.185, 0.00066, 0, 1.05, 4.2}, {128, 64, 1, 0.185, 0.00066, 0, 0.75, 3.6}};
 
 // The shape with the least time by these figures, or the one that computes least where memory sets the time.  How the rows
 // are spread over the experts is not known here: what a busy expert has is taken as one and a half times the mean.
@@ -756,7 +803,7 @@ GroupedShape choose(const Grouped &g, int sms, const LaunchOptions &o)
         const double features = std::ceil(double(g.m) / c.rows), cols = g.sums ? double(g.n) : rows, per = std::ceil(cols / c.cols);
         const double tiles = features * per * (g.sums ? g.experts : busy), units = double(sms / c.per_unit);
         const double steps = std::ceil((g.sums ? double(g.rows) / g.experts : double(g.k)) / 64), waves = tiles <= units ? 0.75 : tiles / units + 0.5;
-        const double compute = waves * steps * std::max(c.least, c.step + c.column * cols / per), time = c.launch + std::max(compute, bytes / 6.5e6) + 0.1 * compute;
+        const double compute = waves * std::max(steps * std::max(c.least, c.step + c.column * cols / per), c.tile), time = c.launch + std::max(compute, bytes / 6.5e6) + 0.1 * compute;
         if (time < least) {
             least = time;
             best = GroupedShape(i);

@@ -30,6 +30,9 @@ struct Grouped {
 int64_t grouped_scratch_bytes(const Grouped &g);
 cudaError_t launch_grouped(const Grouped &g, void *scratch, const LaunchOptions &o, cudaStream_t stream);
 
+// ROWS for up to kFewRows rows, both operands contiguous along the sum, at any alignment (few.cu).
+cudaError_t launch_few_grouped(const Grouped &g, const LaunchOptions &o, cudaStream_t stream);
+
 // dz = dy times the activation's slope at z for the rows of the experts (dst or null: not kept), and the sums of an expert's
 // rows (sums[e][col], or null), of the unrounded values in a fixed order.
 struct ExpertSlope {

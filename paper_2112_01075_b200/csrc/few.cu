@@ -18,6 +18,7 @@
 
 #include "activation.cuh"
 #include "elements.cuh"
+#include "experts.h"
 
 namespace redist {
 
@@ -32,6 +33,10 @@ struct Few {
     int64_t ld_x, ld_w;
     int64_t k_per_block;        // a multiple of 64
     Epilogue e;
+    // rows by expert
+    const int32_t *offsets;
+    int32_t experts, by_row;
+    int64_t w_batch, bias_stride;
 };
 
 template <typename T> __device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
@@ -95,9 +100,31 @@ __device__ __forceinline__ uint32_t cluster_size()
     return r;
 }
 
-// MT * 16 rows of w per block, NT * 8 rows of x.
-template <typename T, int MT, int NT, int ALIGN>
-__global__ void __launch_bounds__(32 * kWarps, NT > 2 || ALIGN == 0 ? 3 : 4) redist_few_rows_kernel(const Few f)
+// An expert and its rows, of `rows`: expert `y` itself, or (by row: fewer rows than experts) the one whose first row is y; no rows
+// where there is none.  Offsets that decrease count as the largest before them.
+__device__ __forceinline__ int range_of(const int32_t *offsets, int experts, bool by_row, int y, int rows, int &lo, int &hi)
+{
+    const int lane = int(threadIdx.x) & 31;
+    int e = y, most = 0;
+    if (by_row) {
+        uint32_t next = uint32_t(experts) + 1;              // the first offset beyond row y: where its expert ends
+        for (int i = lane; i <= experts && next > uint32_t(experts); i += 32)
+            if (__ldg(offsets + i) > y) next = uint32_t(i);
+        e = int(__reduce_min_sync(0xffffffffu, next)) - 1;
+    }
+    lo = hi = 0;
+    if (e < 0 || e >= experts) return 0;
+    for (int i = lane; i <= e; i += 32) most = max(most, __ldg(offsets + i));
+    lo = min(__reduce_max_sync(0xffffffffu, most), rows);
+    hi = max(lo, min(__ldg(offsets + e + 1), rows));
+    if (by_row && lo != y) lo = hi;
+    return e;
+}
+
+// MT * 16 rows of w per block, NT * 8 rows of x at a time.  GROUPED: a weight (and bias) for each range of rows of x; the
+// second dimension of the grid are the experts, or the rows.
+template <typename T, int MT, int NT, int ALIGN, bool GROUPED>
+__global__ void __launch_bounds__(32 * kWarps, NT > 2 || ALIGN == 0 ? 3 : 4) redist_few_rows_kernel(Few f)
 {
     constexpr int kOut = MT * 16 * NT * 8;
     __shared__ float parts[kWarps][kOut];
@@ -108,7 +135,15 @@ __global__ void __launch_bounds__(32 * kWarps, NT > 2 || ALIGN == 0 ? 3 : 4) red
     const uint32_t splits = cluster_size(), rank = cluster_rank();
     const int64_t n0 = int64_t(blockIdx.x / splits) * MT * 16;
     const int64_t lo = int64_t(rank) * f.k_per_block, hi = min(f.k, lo + f.k_per_block);
-    const T *x = static_cast<const T *>(f.x), *w = static_cast<const T *>(f.w);
+    int from = 0, to = f.rows, expert = 0;
+    if constexpr (GROUPED) {
+        expert = range_of(f.offsets, f.experts, f.by_row, blockIdx.y, f.rows, from, to);
+        if (from == to) return;                             // all blocks of a cluster
+    }
+#pragma unroll 1
+    do {
+    const int rows = GROUPED ? min(to - from, NT * 8) : f.rows;
+    const T *x = static_cast<const T *>(f.x) + (GROUPED ? from * f.ld_x : 0), *w = static_cast<const T *>(f.w) + (GROUPED ? expert * f.w_batch : 0);
     float acc[MT][NT][4] = {};
     constexpr int kPairs = 2, kTurn = kPairs * 64;
 #pragma unroll 1
@@ -133,7 +168,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT > 2 || ALIGN == 0 ? 3 : 4) red
                 const int64_t c = at + u * 64 + t * 16;
                 const int row = j * 8 + g;
                 uint4 b[2];
-                sixteen<ALIGN, false>(x + int64_t(row) * f.ld_x, row < f.rows ? c : hi, hi, b[0], b[1]);
+                sixteen<ALIGN, false>(x + int64_t(row) * f.ld_x, row < rows ? c : hi, hi, b[0], b[1]);
 #pragma unroll
                 for (int q = 0; q < 2; ++q)
 #pragma unroll
@@ -182,29 +217,35 @@ __global__ void __launch_bounds__(32 * kWarps, NT > 2 || ALIGN == 0 ? 3 : 4) red
         } else {
             v[0] = total[o];
         }
-        if (row >= f.rows || col >= f.n) continue;
-        if (e.bias) v[0] += load_any(e.bias, e.bias_type, col);
-        if (e.pre) static_cast<T *>(e.pre)[row * e.ld_pre + col] = from_float<T>(v[0]);
+        if (row >= rows || col >= f.n) continue;
+        if (e.bias) v[0] += load_any(e.bias, e.bias_type, (GROUPED ? expert * f.bias_stride : 0) + col);
+        const int64_t at = GROUPED ? from + row : row;
+        if (e.pre) static_cast<T *>(e.pre)[at * e.ld_pre + col] = from_float<T>(v[0]);
         activate8(v, e.activation);
-        if (e.residual) v[0] += to_float(static_cast<const T *>(e.residual)[row * e.ld_residual + col]);
-        static_cast<T *>(e.out)[row * e.ld_out + col] = from_float<T>(v[0]);
+        if (!GROUPED && e.residual) v[0] += to_float(static_cast<const T *>(e.residual)[at * e.ld_residual + col]);
+        static_cast<T *>(e.out)[at * e.ld_out + col] = from_float<T>(v[0]);
     }
     if (splits > 1) {                                     // the others read this block's shared memory
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else if (GROUPED) {
+        __syncthreads();
     }
+    from += NT * 8;
+    } while (GROUPED && from < to);
 }
 
-template <typename T, int MT, int NT, int ALIGN>
+template <typename T, int MT, int NT, int ALIGN, bool GROUPED>
 cudaError_t launch(Few f, int sms, const LaunchOptions &o, cudaStream_t stream)
 {
-    const int64_t groups = (f.n + MT * 16 - 1) / (MT * 16);
+    const int64_t groups = (f.n + MT * 16 - 1) / (MT * 16), busy = std::min(f.experts, f.rows);
     // Blocks for two per SM, as long as a warp keeps two turns of the sum.
     int64_t splits = 1;
-    while (splits < kMostCluster && groups * splits < 2 * sms && f.k >= splits * 2 * kWarps * kStep) splits *= 2;
+    while (splits < kMostCluster && groups * busy * splits < 2 * sms && f.k >= splits * 2 * kWarps * kStep) splits *= 2;
     f.k_per_block = (f.k + splits * 64 - 1) / (splits * 64) * 64;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(groups * splits));
+    cfg.gridDim = dim3(unsigned(groups * splits), unsigned(busy));
+    f.by_row = f.rows < f.experts;
     cfg.blockDim = dim3(32 * kWarps);
     cfg.stream = stream;
     cudaLaunchAttribute at[2];
@@ -223,21 +264,24 @@ cudaError_t launch(Few f, int sms, const LaunchOptions &o, cudaStream_t stream)
     }
     cfg.attrs = at;
     cfg.numAttrs = unsigned(n_at);
-    return cudaLaunchKernelEx(&cfg, redist_few_rows_kernel<T, MT, NT, ALIGN>, f);
+    return cudaLaunchKernelEx(&cfg, redist_few_rows_kernel<T, MT, NT, ALIGN, GROUPED>, f);
 }
 
-template <typename T, int ALIGN> cudaError_t launch_rows(const Few &f, int sms, const LaunchOptions &o, cudaStream_t stream)
+template <typename T, int ALIGN, bool GROUPED> cudaError_t launch_rows(const Few &f, int sms, const LaunchOptions &o, cudaStream_t stream)
 {
-    if (f.rows <= 8) return launch<T, 1, 1, ALIGN>(f, sms, o, stream);
-    if (f.rows <= 16) return launch<T, 1, 2, ALIGN>(f, sms, o, stream);
-    return launch<T, 1, 4, ALIGN>(f, sms, o, stream);
+    // (by expert: the experts' rows in turns of eight, unless they have more on average)
+    if (f.rows <= (GROUPED ? 8 * f.experts : 8)) return launch<T, 1, 1, ALIGN, GROUPED>(f, sms, o, stream);
+    if (f.rows <= 16) return launch<T, 1, 2, ALIGN, GROUPED>(f, sms, o, stream);
+    return launch<T, 1, 4, ALIGN, GROUPED>(f, sms, o, stream);
 }
 
-template <typename T> cudaError_t launch_typed(const Few &f, int sms, const LaunchOptions &o, cudaStream_t stream)
+template <typename T, bool GROUPED> cudaError_t launch_typed(const Few &f, int sms, const LaunchOptions &o, cudaStream_t stream)
 {
-    const bool on16 = f.k % 8 == 0 && operand_fits(f.x, f.ld_x, 0, 1) && operand_fits(f.w, f.ld_w, 0, 1);
-    if (on16 && f.k % 16 == 0 && uintptr_t(f.w) % 32 == 0 && f.ld_w % 16 == 0) return launch_rows<T, 32>(f, sms, o, stream);
-    return on16 ? launch_rows<T, 16>(f, sms, o, stream) : launch_rows<T, 0>(f, sms, o, stream);
+    const int matrices = std::min(f.experts, 2);
+    const bool on16 = f.k % 8 == 0 && operand_fits(f.x, f.ld_x, 0, 1) && operand_fits(f.w, f.ld_w, f.w_batch, matrices);
+    if (on16 && f.k % 16 == 0 && uintptr_t(f.w) % 32 == 0 && f.ld_w % 16 == 0 && (matrices == 1 || f.w_batch % 16 == 0))
+        return launch_rows<T, 32, GROUPED>(f, sms, o, stream);
+    return on16 ? launch_rows<T, 16, GROUPED>(f, sms, o, stream) : launch_rows<T, 0, GROUPED>(f, sms, o, stream);
 }
 
 }  // namespace
@@ -256,7 +300,35 @@ cudaError_t launch_few_rows(const Product &p, const LaunchOptions &o, cudaStream
     f.ld_x = p.a.ld;
     f.ld_w = p.b.ld;
     f.e = p.e;
-    return p.type == T_BF16 ? launch_typed<__nv_bfloat16>(f, sms, o, stream) : launch_typed<__half>(f, sms, o, stream);
+    f.experts = 1;
+    return p.type == T_BF16 ? launch_typed<__nv_bfloat16, false>(f, sms, o, stream) : launch_typed<__half, false>(f, sms, o, stream);
+}
+
+cudaError_t launch_few_grouped(const Grouped &g, const LaunchOptions &o, cudaStream_t stream)
+{
+    int device = 0, sms = 0;
+    const cudaError_t ce = current_device(&device, &sms);
+    if (ce != cudaSuccess) return ce;
+    Few f = {};
+    f.n = g.m;
+    f.k = g.k;
+    f.rows = int32_t(g.rows);
+    f.x = g.b.data;
+    f.w = g.a.data;
+    f.ld_x = g.b.ld;
+    f.ld_w = g.a.ld;
+    f.w_batch = g.a.batch_stride;
+    f.offsets = g.offsets;
+    f.experts = g.experts;
+    f.bias_stride = g.bias_stride;
+    f.e.out = g.out;
+    f.e.ld_out = g.ld_out;
+    f.e.pre = g.pre;
+    f.e.ld_pre = g.ld_pre;
+    f.e.bias = g.bias;
+    f.e.bias_type = g.bias_type;
+    f.e.activation = g.activation;
+    return g.type == T_BF16 ? launch_typed<__nv_bfloat16, true>(f, sms, o, stream) : launch_typed<__half, true>(f, sms, o, stream);
 }
 
 }  // namespace redist
