@@ -164,18 +164,6 @@ redist_status check_experts_backward(const redist_experts &q, const redist_exper
     return on(g.dbias, 4) ? REDIST_OK : REDIST_EALIGN;
 }
 
-// Operands to lay anew, up to three in one launch.
-struct Lays {
-    Lay list[3];
-    int count = 0;
-    redist_status launch(const LaunchOptions &o, cudaStream_t stream)
-    {
-        const int n = count;
-        count = 0;
-        return cuda(launch_lay(list, n, o, stream));
-    }
-};
-
 // A stack as an operand: as it lies, or laid out anew in scratch.
 struct PlacedStack {
     Lines from;
@@ -189,25 +177,7 @@ struct PlacedStack {
         plane = fits ? stride : from.lines * ld;
         if (!fits) copy = pieces.take(count * plane * 2);
     }
-    // Adds what lays it anew to `lays`, which goes off when it is full.
-    redist_status lay(int type, Lays &lays, const LaunchOptions &o, cudaStream_t stream) const
-    {
-        if (fits) return REDIST_OK;
-        const bool even = count == 1 || stride == from.lines * from.ld;        // one long matrix
-        for (i64 i = 0; i < (even ? 1 : count); ++i) {
-            if (lays.count == 3) TRY(lays.launch(o, stream));
-            Lay &l = lays.list[lays.count++];
-            l = Lay{};
-            l.rows = even ? count * from.lines : from.lines;
-            l.cols = from.line;
-            l.type = type;
-            l.src = static_cast<const char *>(from.data) + i * stride * 2;
-            l.ld_src = from.ld;
-            l.dst = static_cast<char *>(copy) + i * plane * 2;
-            l.ld_dst = ld;
-        }
-        return REDIST_OK;
-    }
+    StackLay lay() const { return StackLay{from.data, copy, count, from.lines, from.line, from.ld, stride, ld, plane}; }
     Operand operand(bool rows_survive) const { return Operand{fits ? from.data : copy, ld, plane, from.by_rows == rows_survive ? 0 : 1}; }
 };
 
@@ -227,10 +197,9 @@ bool few_expert_rows(const redist_experts &q, const LaunchOptions &o)
 }
 
 struct ExpertsForward {
-    Placed x;
-    PlacedStack w;
+    PlacedStack x, w;
     ExpertsForward(const redist_experts &q, Pieces &p)
-        : x(q.x, q.rows, q.in_features, p), w(q.w, q.out_features, q.in_features, q.experts, q.w_stride, p)
+        : x(q.x, q.rows, q.in_features, 1, 0, p), w(q.w, q.out_features, q.in_features, q.experts, q.w_stride, p)
     {
     }
 };
@@ -240,22 +209,16 @@ struct ExpertsBackward {
     i64 ld_dz;
     void *dz = nullptr, *maps = nullptr;
     float *partials = nullptr;
-    Placed x;
-    PlacedStack w;
+    PlacedStack x, w;
     ExpertsBackward(const redist_experts &q, const redist_experts_grads &g, Pieces &p)
         : fresh((g.dx.data || g.dw.data) && (q.activation != REDIST_ACT_NONE || !operand_fits(g.dy.data, lines_of(g.dy, q.rows, q.out_features).ld, 0, 1))),
-          x(g.dw.data ? q.x : kAbsent, g.dw.data ? q.rows : 0, g.dw.data ? q.in_features : 0, p),
+          x(g.dw.data ? q.x : kAbsent, g.dw.data ? q.rows : 0, g.dw.data ? q.in_features : 0, 1, 0, p),
           w(g.dx.data ? q.w : kAbsent, g.dx.data ? q.out_features : 0, g.dx.data ? q.in_features : 0, g.dx.data ? q.experts : 1, g.dx.data ? q.w_stride : 0, p)
     {
         ld_dz = fresh ? round_up(q.out_features, 64) : lines_of(g.dy, q.rows, q.out_features).ld;
         if (fresh) dz = p.take(q.rows * ld_dz * 2);
         if (g.dbias) partials = static_cast<float *>(p.take(expert_partial_bytes(q.rows, q.out_features, q.experts)));
-        if (g.dw.data) {
-            Grouped s = {};
-            s.experts = q.experts;
-            s.sums = 1;
-            maps = p.take(grouped_scratch_bytes(s));
-        }
+        if (g.dw.data) maps = p.take(grouped_maps_bytes(q.experts));
     }
 };
 
@@ -492,13 +455,14 @@ redist_status redist_experts_forward(const redist_experts *op, void *scratch, si
             g.b = Operand{f.x.from.data, f.x.from.ld, 0, 0};
             return cuda(launch_few_grouped(g, o, stream));
         }
-        Lays lays;
-        f.x.lay(q.type, lays.list, lays.count);
-        TRY(f.w.lay(q.type, lays, o, stream));
-        TRY(lays.launch(o, stream));
+        Prepare before = {};
+        before.type = q.type;
+        before.lay[0] = f.w.lay();
+        before.lay[1] = f.x.lay();
+        TRY(cuda(launch_prepare(before, o, stream)));
         g.a = f.w.operand(true);
         g.b = f.x.operand(true);
-        return cuda(launch_grouped(g, nullptr, o, stream));
+        return cuda(launch_grouped(g, nullptr, nullptr, o, stream));
     } catch (...) {
         return REDIST_EINTERNAL;
     }
@@ -533,60 +497,64 @@ redist_status redist_experts_backward(const redist_experts *op, const redist_exp
                                extent(q.x, g.dw.data ? q.rows : 0, q.in_features, 2), extent(q.offsets, i64(q.experts + 1) * 4)};
         TRY(apart(outs, 4, ins, 5));
         TRY(check_scratch(scratch, scratch_bytes, p.used));
-        const i64 ld_dy = row_stride(g.dy, q.rows, q.out_features);
+        const void *dz = b.fresh ? b.dz : g.dy.data;
+        Grouped x = {};
+        x.rows = q.rows;
+        x.experts = q.experts;
+        x.type = q.type;
+        x.offsets = q.offsets;
+        x.activation = ACT_NONE;
+        Grouped w = x;
+        x.m = q.in_features;
+        x.k = q.out_features;
+        x.a = b.w.operand(false);
+        x.b = Operand{dz, b.ld_dz, 0, 0};
+        x.out = g.dx.data;
+        x.ld_out = row_stride(g.dx, q.rows, q.in_features);
+        w.sums = 1;
+        w.m = q.in_features;
+        w.n = q.out_features;
+        w.a = b.x.operand(false);
+        w.b = Operand{dz, b.ld_dz, 0, 1};
+        w.out = g.dw.data;
+        w.ld_out = row_stride(g.dw, q.out_features, q.in_features);
+        w.out_batch = g.dw_stride;
+
+        Prepare before = {};
+        before.type = q.type;
         if (b.fresh || g.dbias) {
-            ExpertSlope s = {};
+            ExpertSlope &s = before.slope;
             s.rows = q.rows;
             s.cols = q.out_features;
             s.experts = q.experts;
-            s.type = q.type;
             s.activation = q.activation;
             s.offsets = q.offsets;
             s.dy = g.dy.data;
-            s.ld_dy = ld_dy;
+            s.ld_dy = row_stride(g.dy, q.rows, q.out_features);
             if (q.activation != REDIST_ACT_NONE) {
                 s.z = q.pre.data;
                 s.ld_z = row_stride(q.pre, q.rows, q.out_features);
             }
             s.dst = b.dz;
             s.ld_dst = b.ld_dz;
-            s.sums = g.dbias;
             s.partials = b.partials;
-            TRY(cuda(launch_expert_slope(s, o, stream)));
         }
-        Lays lays;
-        if (g.dw.data) b.x.lay(q.type, lays.list, lays.count);
-        if (g.dx.data) TRY(b.w.lay(q.type, lays, o, stream));
-        TRY(lays.launch(o, stream));
-        const void *dz = b.fresh ? b.dz : g.dy.data;
-        Grouped d = {};
-        d.rows = q.rows;
-        d.experts = q.experts;
-        d.type = q.type;
-        d.offsets = q.offsets;
-        d.activation = ACT_NONE;
-        if (g.dx.data) {
-            Grouped x = d;
-            x.m = q.in_features;
-            x.k = q.out_features;
-            x.a = b.w.operand(false);
-            x.b = Operand{dz, b.ld_dz, 0, 0};
-            x.out = g.dx.data;
-            x.ld_out = row_stride(g.dx, q.rows, q.in_features);
-            TRY(cuda(launch_grouped(x, nullptr, o, stream)));
-        }
-        if (g.dw.data) {
-            Grouped w = d;
-            w.sums = 1;
-            w.m = q.in_features;
-            w.n = q.out_features;
-            w.a = b.x.operand(false);
-            w.b = Operand{dz, b.ld_dz, 0, 1};
-            w.out = g.dw.data;
-            w.ld_out = row_stride(g.dw, q.out_features, q.in_features);
-            w.out_batch = g.dw_stride;
-            TRY(cuda(launch_grouped(w, b.maps, o, stream)));
-        }
+        before.lay[0] = b.w.lay();
+        before.lay[1] = b.x.lay();
+        if (g.dw.data) before.sums = &w;
+        before.maps = b.maps;
+        TRY(cuda(launch_prepare(before, o, stream)));
+        ExpertSums sums = {};
+        sums.rows = q.rows;
+        sums.cols = q.out_features;
+        sums.per = slope_rows(q.rows, q.out_features);
+        sums.experts = q.experts;
+        sums.offsets = q.offsets;
+        sums.partials = b.partials;
+        sums.sums = g.dbias;
+        if (g.dx.data) TRY(cuda(launch_grouped(x, nullptr, &sums, o, stream)));
+        if (g.dw.data) TRY(cuda(launch_grouped(w, b.maps, &sums, o, stream)));
+        if (sums.sums) TRY(cuda(launch_expert_sums(sums, o, stream)));
         return REDIST_OK;
     } catch (...) {
         return REDIST_EINTERNAL;

@@ -57,6 +57,7 @@ struct GroupedParams {
     int64_t ld_out, out_batch, ld_pre, bias_stride;
     const void *bias;
     int32_t bias_type;
+    ExpertSums columns;                 // computed in passing, by the warp that has nothing else to do
 };
 
 __device__ __forceinline__ int offset_at(const GroupedParams &p, int e) { return min(max(__ldg(p.offsets + e), 0), p.rows); }
@@ -242,6 +243,28 @@ struct GroupedPieces {
     }
 };
 
+// The sums of the experts' rows from their parts, in the order of the rows: warp `first` of `warps`, a lane one column.
+__device__ __forceinline__ void expert_sums(const ExpertSums &s, int64_t first, int64_t warps, int lane)
+{
+    const int64_t across = (s.cols + 31) / 32, all = across * s.experts;
+    for (int64_t q = first; q < all; q += warps) {
+        const int64_t e = q / across, c = (q - e * across) * 32 + lane;
+        const int64_t from = min(max(int64_t(__ldg(s.offsets + e)), int64_t(0)), s.rows), to = min(max(int64_t(__ldg(s.offsets + e + 1)), int64_t(0)), s.rows);
+        if (c >= s.cols) continue;
+        float part[8] = {}, sum = 0.0f;                     // every eighth part: the order of the kernel for the sums alone
+        if (from < to) {
+            const int64_t last = (to - 1) / s.per + e;
+            for (int64_t at = from / s.per + e; at <= last; at += 8)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (at + i <= last) part[i] += s.partials[(at + i) * s.cols + c];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += part[i];
+        s.sums[e * s.cols + c] = sum;
+    }
+}
+
 // ---- the kernel ------------------------------------------------------------------------------------
 
 template <int CG, int BN, int KB, bool SUMS>
@@ -406,6 +429,8 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         ok = bar_wait(drained, 0, kDrainPolls) && ok;
     } else if (warp == 1) {
         ok = bar_wait(drained, 0, kDrainPolls);                           // reported by the first block
+    } else if (warp == 2) {
+        if (p.columns.sums) expert_sums(p.columns, blockIdx.x, gridDim.x, lane);
     } else if (warp >= 4) {
         // outputs: a warp has 32 features (lanes of tensor memory) and every second piece of 32 columns
         const int quarter = warp & 3, half = (warp - 4) >> 2;
@@ -488,68 +513,45 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     if (warp == 2) tmem_free<CG>(tmem, kColumns);
 }
 
-// The maps of every expert's rows: copies of two that end with its last row.
-__global__ void __launch_bounds__(64) redist_expert_maps_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                                const __grid_constant__ GroupedParams p, CUtensorMap *maps)
-{
-    let_next_start();
-    wait_for_previous();
-    const int which = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31;
-    const int e = blockIdx.x, lo = offset_at(p, e), hi = offset_at(p, e + 1);
-    if (hi <= lo) return;                                   // never used
-    CUtensorMap *to = maps + 2 * e + which;
-    const uint32_t *from = reinterpret_cast<const uint32_t *>(which ? &map_b : &map_a);
-    reinterpret_cast<uint32_t *>(to)[lane] = from[lane];
-    __threadfence();
-    __syncwarp();
-    if (lane == 0) {
-        asm volatile("tensormap.replace.tile.global_dim.global.b1024.b32 [%0], 1, %1;" ::"l"(to), "r"(hi) : "memory");
-        asm volatile("fence.proxy.tensormap::generic.release.gpu;" ::: "memory");
-    }
-}
+// ---- before the products ----------------------------------------------------------------------------
 
-// ---- dz and its sums ---------------------------------------------------------------------------------
+struct PrepareParams {
+    Prepare p;
+    int64_t slope_per, slope_across;            // rows of a block, blocks side by side
+    int64_t slope_blocks, lay_blocks[2], map_blocks;
+    int32_t aligned;                            // dy and z: every row starts on a 16-byte boundary
+    int32_t rows, experts;                      // of the maps
+    const int32_t *offsets;
+};
 
-constexpr int kSlopeCols = 256;
+constexpr int kPrepareCols = 256;           // a warp's columns
 
-// Rows of a block of the slope kernel: as few as keep four blocks on each of 148 SMs (written here because scratch is asked for
-// by sizes alone), 8 to 128, more where the grid would grow beyond its limit.
-int64_t slope_rows(int64_t rows, int64_t cols)
-{
-    int64_t per = 128 * ((rows + 128 * 32768 - 1) / (128 * 32768));
-    while (per > 8 && ((rows + per - 1) / per) * ((cols + kSlopeCols - 1) / kSlopeCols) < 4 * 148) per /= 2;
-    return per;
-}
+__device__ __forceinline__ int64_t offset_in(const int32_t *offsets, int e, int64_t rows) { return min(max(int64_t(__ldg(offsets + e)), int64_t(0)), rows); }
 
 // A block takes `per` rows by 256 columns, and within them one expert's rows after the other; a warp every eighth row, a lane
 // eight neighbours.  Chunk c's sums for expert e are part c + e: both only grow, so no two share one.
-template <typename T, bool ALIGNED> __global__ void __launch_bounds__(256, 4) redist_expert_slope_kernel(const ExpertSlope s, int64_t per)
+template <typename T> __device__ __forceinline__ void slope_block(const ExpertSlope &s, int64_t chunk, int64_t column, int64_t per, bool aligned, float (&all)[8][kPrepareCols])
 {
-    __shared__ float all[8][kSlopeCols];
-    let_next_start();
-    wait_for_previous();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const int64_t c = int64_t(blockIdx.x) * kSlopeCols + lane * 8;
-    const int64_t lo = int64_t(blockIdx.y) * per, hi = min(s.rows, lo + per);
+    const int64_t c = column * kPrepareCols + lane * 8, lo = chunk * per, hi = min(s.rows, lo + per);
     const int count = int(min(s.cols - c, int64_t(8)));
-    auto offset = [&](int e) { return int64_t(min(max(int64_t(__ldg(s.offsets + e)), int64_t(0)), s.rows)); };
     // the first expert that ends behind this block's first row
     int e = 0;
     for (int above = s.experts; e < above;) {
         const int mid = (e + above) >> 1;
-        if (offset(mid + 1) > lo) above = mid;
+        if (offset_in(s.offsets, mid + 1, s.rows) > lo) above = mid;
         else e = mid + 1;
     }
     for (; e < s.experts; ++e) {
-        const int64_t from = max(lo, offset(e)), to = min(hi, offset(e + 1));
-        if (offset(e) >= hi) break;
+        const int64_t begin = offset_in(s.offsets, e, s.rows), from = max(lo, begin), to = min(hi, offset_in(s.offsets, e + 1, s.rows));
+        if (begin >= hi) break;
         if (from >= to) continue;
         float sums[8] = {};
         if (count > 0)
             for (int64_t row = from + w; row < to; row += 8) {
                 const T *src = static_cast<const T *>(s.dy) + row * s.ld_dy + c, *z = static_cast<const T *>(s.z) + row * s.ld_z + c;
-                uint4 u, y;
-                if (ALIGNED && count >= 8) {
+                uint4 u, y = make_uint4(0, 0, 0, 0);
+                if (aligned && count >= 8) {
                     u = *reinterpret_cast<const uint4 *>(src);
                     if (s.z) y = *reinterpret_cast<const uint4 *>(z);
                 } else {
@@ -578,36 +580,96 @@ template <typename T, bool ALIGNED> __global__ void __launch_bounds__(256, 4) re
                 for (int i = 0; i < 8; ++i) sums[i] += v[i];
                 if (s.dst) *reinterpret_cast<uint4 *>(static_cast<T *>(s.dst) + row * s.ld_dst + c) = u;
             }
-        if (!s.sums) continue;
+        if (!s.partials) continue;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 8; ++i) all[w][lane * 8 + i] = sums[i];
         __syncthreads();
-        const int64_t cc = int64_t(blockIdx.x) * kSlopeCols + threadIdx.x;
+        const int64_t cc = column * kPrepareCols + threadIdx.x;
         if (cc < s.cols) {
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += all[i][threadIdx.x];
-            s.partials[(int64_t(blockIdx.y) + e) * s.cols + cc] = sum;
+            s.partials[(chunk + e) * s.cols + cc] = sum;
         }
     }
 }
 
-// The sums of an expert: its parts, in the order of the rows; a warp every eighth of them, a lane one column.
-__global__ void __launch_bounds__(256) redist_expert_sums_kernel(const ExpertSlope s, int64_t per)
+// A warp takes a line at a time, four stretches of 256 columns of it under way.
+__device__ __forceinline__ void lay_block(const StackLay &l, int64_t block, int64_t blocks)
+{
+    constexpr int kAhead = 4;
+    const int lane = threadIdx.x & 31;
+    const int64_t all = l.count * l.lines;
+    for (int64_t line = block * 8 + (threadIdx.x >> 5); line < all; line += blocks * 8) {
+        const int64_t matrix = l.count > 1 ? line / l.lines : 0, at = line - matrix * l.lines;
+        const uint16_t *src = static_cast<const uint16_t *>(l.src) + matrix * l.plane_src + at * l.ld_src;
+        uint16_t *dst = static_cast<uint16_t *>(l.dst) + matrix * l.plane_dst + at * l.ld_dst;
+        for (int64_t c = lane * 8; c < l.line; c += kAhead * kPrepareCols) {
+            Blocks b[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int64_t count = min(l.line - c - i * kPrepareCols, int64_t(8));
+                if (count > 0) b[i].load(src + c + i * kPrepareCols, int(count) * 2);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (c + i * kPrepareCols < l.line) *reinterpret_cast<uint4 *>(dst + c + i * kPrepareCols) = b[i].get(src + c + i * kPrepareCols);
+        }
+    }
+}
+
+// The maps of every expert's rows: copies of two that end with its last row.  A warp makes one.
+__device__ __forceinline__ void map_block(const PrepareParams &p, const CUtensorMap &map_a, const CUtensorMap &map_b, int64_t block)
+{
+    const int lane = int(threadIdx.x) & 31;
+    const int64_t which = block * 8 + (threadIdx.x >> 5), e = which >> 1;
+    if (e >= p.experts) return;
+    const int64_t lo = offset_in(p.offsets, int(e), p.rows), hi = offset_in(p.offsets, int(e) + 1, p.rows);
+    if (hi <= lo) return;                                   // never used
+    CUtensorMap *to = static_cast<CUtensorMap *>(p.p.maps) + which;
+    const uint32_t *from = reinterpret_cast<const uint32_t *>(which & 1 ? &map_b : &map_a);
+    reinterpret_cast<uint32_t *>(to)[lane] = from[lane];
+    __threadfence();
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("tensormap.replace.tile.global_dim.global.b1024.b32 [%0], 1, %1;" ::"l"(to), "r"(int(hi)) : "memory");
+        asm volatile("fence.proxy.tensormap::generic.release.gpu;" ::: "memory");
+    }
+}
+
+// Each of the four has blocks of its own: what these small works cost is mostly a launch.
+template <typename T> __global__ void __launch_bounds__(256, 4)
+redist_expert_prepare_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ PrepareParams p)
+{
+    __shared__ float all[8][kPrepareCols];
+    let_next_start();
+    wait_for_previous();
+    int64_t b = blockIdx.x;
+    if (b < p.slope_blocks) {
+        slope_block<T>(p.p.slope, b / p.slope_across, b % p.slope_across, p.slope_per, p.aligned, all);
+        return;
+    }
+    b -= p.slope_blocks;
+    if (b < p.lay_blocks[0]) return lay_block(p.p.lay[0], b, p.lay_blocks[0]);
+    b -= p.lay_blocks[0];
+    if (b < p.lay_blocks[1]) return lay_block(p.p.lay[1], b, p.lay_blocks[1]);
+    map_block(p, map_a, map_b, b - p.lay_blocks[1]);
+}
+
+// The sums on their own: eight warps share the parts of 32 columns.
+__global__ void __launch_bounds__(256) redist_expert_sums_kernel(const ExpertSums s)
 {
     __shared__ float all[8][32];
     let_next_start();
     wait_for_previous();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, e = blockIdx.y;
-    const int64_t c = int64_t(blockIdx.x) * 32 + lane;
-    auto offset = [&](int i) { return min(max(int64_t(__ldg(s.offsets + i)), int64_t(0)), s.rows); };
-    const int64_t from = offset(e), to = offset(e + 1);
+    const int64_t c = int64_t(blockIdx.x) * 32 + lane, from = offset_in(s.offsets, e, s.rows), to = offset_in(s.offsets, e + 1, s.rows);
     float sum = 0.0f;
     if (from < to && c < s.cols) {
-        const int64_t last = (to - 1) / per;
+        const int64_t last = (to - 1) / s.per + e;
 #pragma unroll 4
-        for (int64_t q = from / per + w; q <= last; q += 8) sum += s.partials[(q + e) * s.cols + c];
+        for (int64_t part = from / s.per + e + w; part <= last; part += 8) sum += s.partials[part * s.cols + c];
     }
     all[w][lane] = sum;
     __syncthreads();
@@ -694,6 +756,11 @@ cudaError_t launch_any(void (*kernel)(P...), dim3 grid, int threads, int smem, i
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// The sums that a block of a product computes in passing: groups of 32 columns, and parts of an expert's rows on average, at most.
+// More could take longer than its tiles (8192 x 1024 -> 1024 of 64 experts, backward, with 14 groups a block 97 us, with a
+// launch for them 89).
+constexpr int kPassing = 8, kPassingParts = 24;
+
 // The smallest power of two that makes the quotient exact for numerators below 2^31.
 Divider divider(int64_t d)
 {
@@ -704,7 +771,7 @@ Divider divider(int64_t d)
 }
 
 template <int CG, int BN, int KB, bool SUMS>
-cudaError_t launch(const Grouped &g, void *scratch, const LaunchOptions &o, int device, int sms, cudaStream_t stream)
+cudaError_t launch(const Grouped &g, void *scratch, ExpertSums *columns, const LaunchOptions &o, int device, int sms, cudaStream_t stream)
 {
     GroupedParams p;
     std::memset(&p, 0, sizeof p);
@@ -755,10 +822,6 @@ cudaError_t launch(const Grouped &g, void *scratch, const LaunchOptions &o, int 
         if (!make_result(&mo, g.out, features, g.m, SUMS ? g.experts : 1, g.ld_out, g.out_batch)) return cudaErrorInvalidValue;
         if (g.pre && !make_result(&mp, g.pre, features, g.m, 1, g.ld_pre, 0)) return cudaErrorInvalidValue;
     }
-    if (SUMS) {
-        const cudaError_t ce = launch_any(redist_expert_maps_kernel, dim3(unsigned(g.experts)), 64, 0, 1, o, stream, ma, mb, p, static_cast<CUtensorMap *>(scratch));
-        if (ce != cudaSuccess) return ce;
-    }
     auto *kernel = redist_grouped_kernel<CG, BN, KB, SUMS>;
     static std::atomic<uint64_t> ready{0};                  // devices on which this kernel may use its shared memory
     if (device >= 64 || !(ready.load(std::memory_order_relaxed) >> device & 1)) {
@@ -767,6 +830,12 @@ cudaError_t launch(const Grouped &g, void *scratch, const LaunchOptions &o, int 
         if (device < 64) ready.fetch_or(uint64_t(1) << device, std::memory_order_relaxed);
     }
     const int64_t groups = sms / CG;
+    const unsigned blocks = unsigned(std::min(tiles, groups) * CG);
+    if (columns && columns->sums && (columns->cols + 31) / 32 * columns->experts <= int64_t(blocks) * kPassing &&
+        columns->rows <= columns->per * columns->experts * kPassingParts) {
+        p.columns = *columns;
+        columns->sums = nullptr;                            // done
+    }
     // Every other expert costs the loading warps a fence and the fetch of a tensor map: where sums are short, blocks take a few
     // tiles of one expert after the other (64 gradients of 1024 x 2048 over 256 rows: 56 -> 53 us on pairs, 70 -> 65 on single SMs;
     // more of them leave SMs idle at the end).
@@ -774,7 +843,7 @@ cudaError_t launch(const Grouped &g, void *scratch, const LaunchOptions &o, int 
         const int64_t steps = std::max<int64_t>(1, g.rows / g.experts / kBK);
         while (p.run < (CG == 2 ? 1 : 3) && (steps << p.run) < 4 && (groups << (p.run + 1)) <= tiles) ++p.run;
     }
-    return launch_any(kernel, dim3(unsigned(std::min(tiles, groups) * CG)), kThreads, kSmem, CG, o, stream, ma, mb, ms, mo, mp, p);
+    return launch_any(kernel, dim3(blocks), kThreads, kSmem, CG, o, stream, ma, mb, ms, mo, mp, p);
 }
 
 // The tile shapes, and what they take: microseconds per 64 steps of a sum, `step` + `column` per column computed (at least
@@ -814,9 +883,9 @@ GroupedShape choose(const Grouped &g, int sms, const LaunchOptions &o)
 
 }  // namespace
 
-int64_t grouped_scratch_bytes(const Grouped &g) { return g.sums ? int64_t(g.experts) * 2 * int64_t(sizeof(CUtensorMap)) : 0; }
+int64_t grouped_maps_bytes(int experts) { return int64_t(experts) * 2 * int64_t(sizeof(CUtensorMap)); }
 
-cudaError_t launch_grouped(const Grouped &g, void *scratch, const LaunchOptions &o, cudaStream_t stream)
+cudaError_t launch_grouped(const Grouped &g, void *scratch, ExpertSums *columns, const LaunchOptions &o, cudaStream_t stream)
 {
     if (!g.sums && g.rows == 0) return cudaSuccess;
     int device = 0, sms = 0;
@@ -824,19 +893,33 @@ cudaError_t launch_grouped(const Grouped &g, void *scratch, const LaunchOptions 
     if (ce != cudaSuccess) return ce;
     if (g.sums) {
         switch (choose(g, sms, o)) {
-        case kPair256: return launch<2, 256, 1, true>(g, scratch, o, device, sms, stream);
-        case kPair128: return launch<2, 128, 2, true>(g, scratch, o, device, sms, stream);
-        case kOne128: return launch<1, 128, 2, true>(g, scratch, o, device, sms, stream);
-        default: return launch<1, 64, 2, true>(g, scratch, o, device, sms, stream);
+        case kPair256: return launch<2, 256, 1, true>(g, scratch, columns, o, device, sms, stream);
+        case kPair128: return launch<2, 128, 2, true>(g, scratch, columns, o, device, sms, stream);
+        case kOne128: return launch<1, 128, 2, true>(g, scratch, columns, o, device, sms, stream);
+        default: return launch<1, 64, 2, true>(g, scratch, columns, o, device, sms, stream);
         }
     }
     switch (choose(g, sms, o)) {
-    case kPair256: return launch<2, 256, 1, false>(g, scratch, o, device, sms, stream);
-    case kPair128: return launch<2, 128, 2, false>(g, scratch, o, device, sms, stream);
-    case kOne32: return launch<1, 32, 2, false>(g, scratch, o, device, sms, stream);
-    case kOne128: return launch<1, 128, 2, false>(g, scratch, o, device, sms, stream);
-    default: return launch<1, 64, 2, false>(g, scratch, o, device, sms, stream);
+    case kPair256: return launch<2, 256, 1, false>(g, scratch, columns, o, device, sms, stream);
+    case kPair128: return launch<2, 128, 2, false>(g, scratch, columns, o, device, sms, stream);
+    case kOne32: return launch<1, 32, 2, false>(g, scratch, columns, o, device, sms, stream);
+    case kOne128: return launch<1, 128, 2, false>(g, scratch, columns, o, device, sms, stream);
+    default: return launch<1, 64, 2, false>(g, scratch, columns, o, device, sms, stream);
     }
+}
+
+cudaError_t launch_expert_sums(const ExpertSums &s, const LaunchOptions &o, cudaStream_t stream)
+{
+    return launch_any(redist_expert_sums_kernel, dim3(unsigned((s.cols + 31) / 32), unsigned(s.experts)), 256, 0, 1, o, stream, s);
+}
+
+// Rows of a block of the slope: as few as keep four blocks on each of 148 SMs (written here because scratch is asked for by
+// sizes alone), 8 to 128, more where the grid would grow beyond its limit.
+int64_t slope_rows(int64_t rows, int64_t cols)
+{
+    int64_t per = 128 * ((rows + 128 * 32768 - 1) / (128 * 32768));
+    while (per > 8 && ((rows + per - 1) / per) * ((cols + kPrepareCols - 1) / kPrepareCols) < 4 * 148) per /= 2;
+    return per;
 }
 
 int64_t expert_partial_bytes(int64_t rows, int64_t cols, int experts)
@@ -845,23 +928,38 @@ int64_t expert_partial_bytes(int64_t rows, int64_t cols, int experts)
     return ((rows + per - 1) / per + experts) * cols * 4;
 }
 
-cudaError_t launch_expert_slope(const ExpertSlope &s, const LaunchOptions &o, cudaStream_t stream)
+cudaError_t launch_prepare(const Prepare &p, const LaunchOptions &o, cudaStream_t stream)
 {
-    const int64_t per = slope_rows(s.rows, s.cols);
-    if (s.rows > 0) {
-        const dim3 grid(unsigned((s.cols + kSlopeCols - 1) / kSlopeCols), unsigned((s.rows + per - 1) / per));
-        const bool aligned = on_16(s.dy, s.ld_dy) && on_16(s.z, s.ld_z);
-        cudaError_t ce;
-        if (s.type == T_BF16)
-            ce = aligned ? launch_any(redist_expert_slope_kernel<__nv_bfloat16, true>, grid, 256, 0, 1, o, stream, s, per)
-                         : launch_any(redist_expert_slope_kernel<__nv_bfloat16, false>, grid, 256, 0, 1, o, stream, s, per);
-        else
-            ce = aligned ? launch_any(redist_expert_slope_kernel<__half, true>, grid, 256, 0, 1, o, stream, s, per)
-                         : launch_any(redist_expert_slope_kernel<__half, false>, grid, 256, 0, 1, o, stream, s, per);
-        if (ce != cudaSuccess) return ce;
+    PrepareParams q;
+    std::memset(static_cast<void *>(&q), 0, sizeof q);
+    q.p = p;
+    if (p.slope.dy && p.slope.rows > 0) {
+        q.slope_per = slope_rows(p.slope.rows, p.slope.cols);
+        q.slope_across = (p.slope.cols + kPrepareCols - 1) / kPrepareCols;
+        q.slope_blocks = (p.slope.rows + q.slope_per - 1) / q.slope_per * q.slope_across;
+        q.aligned = on_16(p.slope.dy, p.slope.ld_dy) && on_16(p.slope.z, p.slope.ld_z);
     }
-    if (!s.sums) return cudaSuccess;
-    return launch_any(redist_expert_sums_kernel, dim3(unsigned((s.cols + 31) / 32), unsigned(s.experts)), 256, 0, 1, o, stream, s, per);
+    for (int i = 0; i < 2; ++i)
+        if (p.lay[i].dst) {
+            // (a line for each warp: there are more blocks than fit at once, and a warp's line hides little)
+            q.lay_blocks[i] = std::min<int64_t>((p.lay[i].count * p.lay[i].lines + 7) / 8, 1 << 20);
+        }
+    CUtensorMap ma, mb;
+    std::memset(&ma, 0, sizeof ma);
+    std::memset(&mb, 0, sizeof mb);
+    if (p.sums) {
+        const Grouped &g = *p.sums;
+        if (!make_operand(&ma, g.a, g.m, g.rows, 1, 128) || !make_operand(&mb, g.b, g.n, g.rows, 1, 128)) return cudaErrorInvalidValue;
+        q.rows = int32_t(g.rows);
+        q.experts = g.experts;
+        q.offsets = g.offsets;
+        q.map_blocks = (int64_t(g.experts) * 2 + 7) / 8;
+    }
+    const int64_t blocks = q.slope_blocks + q.lay_blocks[0] + q.lay_blocks[1] + q.map_blocks;
+    if (blocks == 0) return cudaSuccess;
+    if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+    return p.type == T_BF16 ? launch_any(redist_expert_prepare_kernel<__nv_bfloat16>, dim3(unsigned(blocks)), 256, 0, 1, o, stream, ma, mb, q)
+                            : launch_any(redist_expert_prepare_kernel<__half>, dim3(unsigned(blocks)), 256, 0, 1, o, stream, ma, mb, q);
 }
 
 cudaError_t read_grouped_timeouts(unsigned int *out) { return cudaMemcpyFromSymbol(out, g_grouped_timeouts, sizeof *out); }
