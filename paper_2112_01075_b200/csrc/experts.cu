@@ -235,9 +235,20 @@ struct GroupedPieces {
                     for (int i = 0; 8 * j + i < left; ++i) q[i] = reinterpret_cast<const T *>(piece + piece_at(r, j))[i];
                 }
             }
-        } else if (lane < left) {
-            for (int r = 0; r < min(rows, 32); ++r)
-                first[r * ld + lane] = *reinterpret_cast<const T *>(piece + piece_at(r, lane >> 3) + (lane & 7) * 2);
+        } else {
+            // Rows that start anywhere: a row with one instruction, although it stores no more than 64 bytes.  What counts is how
+            // many sectors of L2 the instructions touch, and whole blocks of 16 bytes, the row's ends on their own, touch more.
+            T *to = first + lane;
+            if (lane < left && rows >= 32) {
+                T held[32];
+#pragma unroll
+                for (int r = 0; r < 32; ++r) held[r] = *reinterpret_cast<const T *>(piece + piece_at(r, lane >> 3) + (lane & 7) * 2);
+#pragma unroll
+                for (int r = 0; r < 32; ++r, to += ld) *to = held[r];
+            } else if (lane < left) {
+#pragma unroll 4
+                for (int r = 0; r < rows; ++r) to[r * ld] = *reinterpret_cast<const T *>(piece + piece_at(r, lane >> 3) + (lane & 7) * 2);
+            }
         }
         __syncwarp();
     }
@@ -595,8 +606,8 @@ template <typename T> __device__ __forceinline__ void slope_block(const ExpertSl
     }
 }
 
-// A warp takes a line at a time, four stretches of 256 columns of it under way.
-__device__ __forceinline__ void lay_block(const StackLay &l, int64_t block, int64_t blocks)
+// A warp takes a line at a time, four stretches of 256 columns of it under way ...
+__device__ __forceinline__ void lay_long(const StackLay &l, int64_t block, int64_t blocks)
 {
     constexpr int kAhead = 4;
     const int lane = threadIdx.x & 31;
@@ -617,6 +628,40 @@ __device__ __forceinline__ void lay_block(const StackLay &l, int64_t block, int6
                 if (c + i * kPrepareCols < l.line) *reinterpret_cast<uint4 *>(dst + c + i * kPrepareCols) = b[i].get(src + c + i * kPrepareCols);
         }
     }
+}
+
+// ... and of lines of up to 128 columns as many as fill it, twice.
+__device__ __forceinline__ int lay_lanes(int64_t line)       // of a line of up to 128 columns
+{
+    int lanes = 16;
+    while (lanes > 1 && (lanes / 2) * 8 >= line) lanes /= 2;
+    return lanes;
+}
+__device__ __forceinline__ void lay_short(const StackLay &l, int64_t block, int64_t blocks)
+{
+    const int lanes = lay_lanes(l.line), group = 32 / lanes, lane = threadIdx.x & 31, c = lane % lanes * 8;
+    const int64_t all = l.count * l.lines;
+    for (int64_t line0 = (block * 8 + (threadIdx.x >> 5)) * 2 * group + lane / lanes; line0 < all; line0 += blocks * 8 * 2 * group) {
+        Blocks b[2];
+        const uint16_t *src[2];
+        uint16_t *dst[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int64_t line = line0 + i * group, matrix = l.count > 1 ? line / l.lines : 0, at = line - matrix * l.lines;
+            src[i] = static_cast<const uint16_t *>(l.src) + matrix * l.plane_src + at * l.ld_src + c;
+            dst[i] = line < all && c < l.line ? static_cast<uint16_t *>(l.dst) + matrix * l.plane_dst + at * l.ld_dst + c : nullptr;
+            if (dst[i]) b[i].load(src[i], int(min(l.line - c, int64_t(8))) * 2);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (dst[i]) *reinterpret_cast<uint4 *>(dst[i]) = b[i].get(src[i]);
+    }
+}
+
+__device__ __forceinline__ void lay_block(const StackLay &l, int64_t block, int64_t blocks)
+{
+    if (l.line > 128) lay_long(l, block, blocks);
+    else lay_short(l, block, blocks);
 }
 
 // The maps of every expert's rows: copies of two that end with its last row.  A warp makes one.
@@ -941,8 +986,9 @@ cudaError_t launch_prepare(const Prepare &p, const LaunchOptions &o, cudaStream_
     }
     for (int i = 0; i < 2; ++i)
         if (p.lay[i].dst) {
-            // (a line for each warp: there are more blocks than fit at once, and a warp's line hides little)
-            q.lay_blocks[i] = std::min<int64_t>((p.lay[i].count * p.lay[i].lines + 7) / 8, 1 << 20);
+            // a turn for each warp: there are more blocks than fit at once, and a warp's turn hides little
+            const int64_t line = p.lay[i].line, turn = line > 128 ? 1 : line > 64 ? 4 : 8;
+            q.lay_blocks[i] = std::min<int64_t>((p.lay[i].count * p.lay[i].lines + 8 * turn - 1) / (8 * turn), 1 << 20);
         }
     CUtensorMap ma, mb;
     std::memset(&ma, 0, sizeof ma);

@@ -159,6 +159,7 @@ __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const Route
     wait_for_previous();
     __syncthreads();
     const int64_t lo = int64_t(blockIdx.x) * p.per_block, hi = min(r.tokens, lo + p.per_block);
+    constexpr bool kAhead = PER <= 8;                        // (more of them do not fit into the registers)
     T ahead[PER];
     auto load = [&](int64_t t) {
         const T *row = static_cast<const T *>(r.logits) + t * r.ld;
@@ -166,14 +167,15 @@ __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const Route
         for (int j = 0; j < PER; ++j)
             if (t < hi && at + 32 * j < r.experts) ahead[j] = row[at + 32 * j];
     };
-    load(lo + group);
+    if (kAhead) load(lo + group);
     for (int64_t base = lo; base < hi; base += kRouteThreads / L) {           // all lanes of a warp walk along
         const int64_t t = base + group;
         const bool in = t < hi;
+        if (!kAhead) load(t);
         uint32_t key[PER];
 #pragma unroll
         for (int j = 0; j < PER; ++j) key[j] = in && at + 32 * j < r.experts ? R::of(ahead[j], at + 32 * j) : 0;
-        load(t + kRouteThreads / L);
+        if (kAhead) load(t + kRouteThreads / L);
         uint32_t best = 0, top = 0, own = 0;
         int32_t own_choice = -1;
         float every = 0.0f;
@@ -543,6 +545,199 @@ template <typename T, int N, int L, int K> __global__ void __launch_bounds__(kMo
     }
 }
 
+// ---- moves of rows that start anywhere --------------------------------------------------------------------
+
+// Where rows of 16-bit elements have no more in common than that: a row that is written is cut into the pieces that its own
+// 16-byte boundaries make; what it is made of is loaded from any address and shifted.
+template <typename T> struct Cut {
+    static constexpr int N = 16 / int(sizeof(T));
+    int head, cols;                     // elements before the first boundary
+    __device__ __forceinline__ Cut(const T *row, int64_t columns) : cols(int(columns))
+    {
+        head = min(int((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / int(sizeof(T)), cols);
+    }
+    // Piece p begins at element at(p) and has count(p) of them, none beyond the end.
+    __device__ __forceinline__ int at(int p) const { return p == 0 ? 0 : head + (p - 1) * N; }
+    __device__ __forceinline__ int count(int p) const { return p == 0 ? head : max(0, min(N, cols - at(p))); }
+};
+// Blocks together, shifted by an offset that all lanes of a warp share (a warp is at one row): one branch, then four
+// instructions, where lanes with offsets of their own take thirty.
+template <int WORD> __device__ __forceinline__ uint4 joined(const Blocks &b, bool half)
+{
+    const uint32_t w[8] = {b.a.x, b.a.y, b.a.z, b.a.w, b.b.x, b.b.y, b.b.z, b.b.w};
+    if (!half) return make_uint4(w[WORD], w[WORD + 1], w[WORD + 2], w[WORD + 3]);
+    return make_uint4(__funnelshift_r(w[WORD], w[WORD + 1], 16), __funnelshift_r(w[WORD + 1], w[WORD + 2], 16),
+                      __funnelshift_r(w[WORD + 2], w[WORD + 3], 16), __funnelshift_r(w[WORD + 3], w[WORD + 4], 16));
+}
+__device__ __forceinline__ uint4 joined(const Blocks &b, const void *p)
+{
+    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p) & 15);
+    if (off == 0) return b.a;
+    if (off < 4) return joined<0>(b, off & 2);
+    if (off < 8) return joined<1>(b, off & 2);
+    if (off < 12) return joined<2>(b, off & 2);
+    return joined<3>(b, off & 2);
+}
+template <typename T> __device__ __forceinline__ void floats(const uint4 &u, float (&v)[16 / sizeof(T)])
+{
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            v[i] = __uint_as_float(w[i]);
+        } else {
+            const float2 f = unpack2<T>(w[i]);
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+    }
+}
+template <typename T> __device__ __forceinline__ uint4 rounded(const float (&v)[16 / sizeof(T)])
+{
+    if constexpr (sizeof(T) == 4) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    else return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+}
+template <typename T> __device__ __forceinline__ void store_some(T *to, const uint4 &u, int count)
+{
+    if (count == 16 / int(sizeof(T))) {
+        *reinterpret_cast<uint4 *>(to) = u;
+        return;
+    }
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 16 / int(sizeof(T)); ++i) {
+        if (i >= count) continue;
+        if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(to)[i] = w[i];
+        else reinterpret_cast<uint16_t *>(to)[i] = uint16_t(w[i >> 1] >> ((i & 1) * 16));
+    }
+}
+
+constexpr int kCut = 2;                 // pieces under way per thread
+
+template <typename T, int L> __global__ void __launch_bounds__(kMoveThreads) redist_dispatch_any_kernel(const Move m)
+{
+    const int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + int(threadIdx.x) / L;
+    const int first = int(blockIdx.y) * kCut * L + int(threadIdx.x) % L;
+    let_next_start();
+    wait_for_previous();
+    if (t >= m.tokens) return;
+    const T *from = static_cast<const T *>(m.token) + t * m.ld_token;
+    for (int s = 0; s < m.chosen; ++s) {
+        const int64_t row = row_at(m, t * m.chosen + s);
+        if (row < 0) continue;
+        T *to = static_cast<T *>(m.row) + row * m.ld_row;
+        const Cut<T> cut(to, m.cols);
+        Blocks b[kCut];
+#pragma unroll
+        for (int j = 0; j < kCut; ++j)
+            if (cut.count(first + j * L) > 0) b[j].load(from + cut.at(first + j * L), cut.count(first + j * L) * int(sizeof(T)));
+#pragma unroll
+        for (int j = 0; j < kCut; ++j)
+            if (cut.count(first + j * L) > 0) store_some(to + cut.at(first + j * L), joined(b[j], from + cut.at(first + j * L)), cut.count(first + j * L));
+    }
+}
+
+template <typename T, int L> __global__ void __launch_bounds__(kMoveThreads, 3) redist_combine_any_kernel(const Move m)
+{
+    constexpr int N = Cut<T>::N, K = 2;
+    const int64_t step = int64_t(gridDim.x) * (kMoveThreads / L);
+    const int first = int(blockIdx.y) * L + int(threadIdx.x) % L;
+    let_next_start();
+    wait_for_previous();
+    int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + int(threadIdx.x) / L;
+    Places<K> next;
+    next.load(m, t, 0);
+    for (; t < m.tokens; t += step) {
+        T *to = static_cast<T *>(m.token) + t * m.ld_token;
+        const Cut<T> cut(to, m.cols);
+        const int at = cut.at(first), count = cut.count(first), bytes = count * int(sizeof(T));
+        const T *residual = static_cast<const T *>(m.residual) + t * m.ld_residual + at;
+        Blocks r;
+        if (m.residual && count > 0) r.load(residual, bytes);
+        float sum[N] = {};
+        for (int s = 0; s < m.chosen; s += K) {
+            const Places<K> now = next;
+            Blocks b[K];
+#pragma unroll
+            for (int i = 0; i < K; ++i)
+                if (now.row[i] >= 0 && count > 0) b[i].load(static_cast<const T *>(m.row) + int64_t(now.row[i]) * m.ld_row + at, bytes);
+            if (s + K < m.chosen) next.load(m, t, s + K);
+            else next.load(m, t + step, 0);
+            if (s == 0 && m.residual && count > 0) floats<T>(joined(r, residual), sum);
+#pragma unroll
+            for (int i = 0; i < K; ++i)
+                if (now.row[i] >= 0 && count > 0) {
+                    float v[N];
+                    floats<T>(joined(b[i], static_cast<const T *>(m.row) + int64_t(now.row[i]) * m.ld_row + at), v);
+#pragma unroll
+                    for (int q = 0; q < N; ++q) sum[q] = fmaf(now.weight[i], v[q], sum[q]);
+                }
+        }
+        if (count > 0) store_some(to + at, rounded<T>(sum), count);
+    }
+}
+
+template <typename T, int L> __global__ void __launch_bounds__(kMoveThreads, 3) redist_combine_gradient_any_kernel(const Move m, int pieces)
+{
+    constexpr int N = Cut<T>::N;
+    __shared__ float dots[2][kMoveThreads / 32][kMostChosen];
+    const int64_t step = int64_t(gridDim.x) * (kMoveThreads / L);
+    const int group = int(threadIdx.x) / L, lane_at = int(threadIdx.x) % L, warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31;
+    let_next_start();
+    wait_for_previous();
+    int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + group;
+    int turn = 0;
+    for (int64_t base = int64_t(blockIdx.x) * (kMoveThreads / L); base < m.tokens; base += step, t += step, turn ^= 1) {      // the block walks along
+        const bool in = t < m.tokens;
+        const T *dy = static_cast<const T *>(m.token) + (in ? t : 0) * m.ld_token;
+#pragma unroll 1
+        for (int s = 0; s < m.chosen; ++s) {
+            const int64_t row = in ? row_at(m, t * m.chosen + s) : -1;
+            float dot = 0.0f;
+            if (row >= 0) {
+                const float weight = m.weights[t * m.chosen + s];
+                const T *y = static_cast<const T *>(m.row) + row * m.ld_row;
+                T *to = static_cast<T *>(m.drow) + row * m.ld_drow;
+                const Cut<T> cut(to, m.cols);
+                for (int p = lane_at; p < pieces; p += kCut * L) {
+                    Blocks d[kCut], v[kCut];
+#pragma unroll
+                    for (int j = 0; j < kCut; ++j) {
+                        const int at = cut.at(p + j * L), bytes = cut.count(p + j * L) * int(sizeof(T));
+                        if (bytes > 0) {
+                            d[j].load(dy + at, bytes);
+                            v[j].load(y + at, bytes);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < kCut; ++j) {
+                        const int at = cut.at(p + j * L), count = cut.count(p + j * L);
+                        if (count <= 0) continue;
+                        float g[N], x[N];
+                        floats<T>(joined(d[j], dy + at), g);
+                        floats<T>(joined(v[j], y + at), x);
+#pragma unroll
+                        for (int q = 0; q < N; ++q) {
+                            if (q < count) dot = fmaf(g[q], x[q], dot);
+                            g[q] *= weight;
+                        }
+                        store_some(to + at, rounded<T>(g), count);
+                    }
+                }
+            }
+            dot = lane_sum<32>(dot);
+            if (lane == 0) dots[turn][warp][s] = dot;
+        }
+        if constexpr (L > 32) __syncthreads();
+        else __syncwarp();
+        for (int s = lane_at; in && s < m.chosen; s += L) {
+            float sum = 0.0f;
+            for (int i = 0; i < L / 32; ++i) sum += dots[turn][group * (L / 32) + i][s];
+            m.dweights[t * m.chosen + s] = sum;
+        }
+    }
+}
+
 // ---- host --------------------------------------------------------------------------------------------------
 
 template <typename... P, typename... A>
@@ -560,8 +755,12 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, const LaunchOpt
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// Blocks of the choice: one up to 128 tokens (a second launch costs more than it saves), one per SM and stretch of tokens above.
-int64_t tokens_per_block(int64_t tokens, int sms) { return std::max<int64_t>(128, (tokens + sms - 1) / sms); }
+// Tokens of a block of the choice: those of one turn of its warps up to as many as are worth a second launch (the more the
+// fewer the experts are), or one stretch per SM.
+int64_t tokens_per_block(int64_t tokens, int experts, int sms)
+{
+    return std::max<int64_t>(experts <= 128 ? 128 : experts <= 256 ? 64 : 32, (tokens + sms - 1) / sms);
+}
 
 template <typename T> cudaError_t launch_route_typed(const RouteParams &p, int64_t blocks, const LaunchOptions &o, cudaStream_t stream)
 {
@@ -572,6 +771,7 @@ template <typename T> cudaError_t launch_route_typed(const RouteParams &p, int64
     if (e <= 64) return launch(redist_route_kernel<T, 32, 2>, grid, kRouteThreads, o, stream, p);
     if (e <= 128) return launch(redist_route_kernel<T, 32, 4>, grid, kRouteThreads, o, stream, p);
     if (e <= 256) return launch(redist_route_kernel<T, 32, 8>, grid, kRouteThreads, o, stream, p);
+    if (e <= 512) return launch(redist_route_kernel<T, 32, 16>, grid, kRouteThreads, o, stream, p);
     return launch(redist_route_kernel<T, 32, 32>, grid, kRouteThreads, o, stream, p);
 }
 
@@ -582,6 +782,7 @@ template <typename T> cudaError_t launch_route_gradient_typed(const Route &r, co
     if (e <= 32) return launch(redist_route_gradient_kernel<T, 1>, grid, 256, o, stream, r);
     if (e <= 128) return launch(redist_route_gradient_kernel<T, 4>, grid, 256, o, stream, r);
     if (e <= 256) return launch(redist_route_gradient_kernel<T, 8>, grid, 256, o, stream, r);
+    if (e <= 512) return launch(redist_route_gradient_kernel<T, 16>, grid, 256, o, stream, r);
     return launch(redist_route_gradient_kernel<T, 32>, grid, 256, o, stream, r);
 }
 
@@ -634,9 +835,30 @@ template <Which W, typename T, int N> cudaError_t launch_move_lanes(const Move &
     return launch_move_width<W, T, N, 32>(m, int(pieces), sms, o, stream);
 }
 
+template <Which W, typename T, int L> cudaError_t launch_move_any(const Move &m, const LaunchOptions &o, cudaStream_t stream)
+{
+    constexpr int kTokens = kMoveThreads / L;
+    int device = 0, sms = 0;
+    const cudaError_t ce = current_device(&device, &sms);
+    if (ce != cudaSuccess) return ce;
+    const int64_t pieces = 1 + (m.cols + Cut<T>::N - 1) / Cut<T>::N;        // at most
+    const int64_t y = W == kGradient ? 1 : (pieces + L * (W == kDispatch ? kCut : 1) - 1) / (L * (W == kDispatch ? kCut : 1));
+    if (y > 65535) return cudaErrorInvalidValue;
+    if constexpr (W == kDispatch)
+        return launch(redist_dispatch_any_kernel<T, L>, dim3(unsigned((m.tokens + kTokens - 1) / kTokens), unsigned(y)), kMoveThreads, o, stream, m);
+    else if constexpr (W == kCombine)
+        return launch(redist_combine_any_kernel<T, L>, dim3(walkers(m.tokens, kTokens, unsigned(y), sms * 3), unsigned(y)), kMoveThreads, o, stream, m);
+    else
+        return launch(redist_combine_gradient_any_kernel<T, L>, dim3(walkers(m.tokens, kTokens, 1, sms * 3)), kMoveThreads, o, stream, m, int(pieces));
+}
+
 template <Which W, typename T> cudaError_t launch_move_typed(const Move &m, int n, const LaunchOptions &o, cudaStream_t stream)
 {
     constexpr int kMost = 16 / int(sizeof(T));
+    // 8000 x 4095, two rows each, forward and backward: 295 us cut and shifted, 441 by single elements; but with two elements of
+    // 16 bits or one of 32 at a time the latter take less (4094: 280 against 289; 1021 of 32 bits: 207 against 261)
+    if (sizeof(T) == 2 && n == 1 && m.cols >= 2 * kMost)
+        return m.cols > 32 * kMost ? launch_move_any<W, T, kMoveThreads>(m, o, stream) : launch_move_any<W, T, 32>(m, o, stream);
     if (n >= kMost) return launch_move_lanes<W, T, kMost>(m, o, stream);
     if (n >= kMost / 2) return launch_move_lanes<W, T, kMost / 2>(m, o, stream);
     if constexpr (kMost == 8)
@@ -659,7 +881,7 @@ template <Which W> cudaError_t launch_move(const Move &m, const LaunchOptions &o
 
 int64_t route_scratch_bytes(int64_t tokens, int experts, int sms)
 {
-    const int64_t per = tokens_per_block(tokens, sms), blocks = (tokens + per - 1) / per;
+    const int64_t per = tokens_per_block(tokens, experts, sms), blocks = (tokens + per - 1) / per;
     return blocks > 1 ? blocks * experts * 4 : 0;
 }
 
@@ -667,7 +889,7 @@ cudaError_t launch_route(const Route &r, void *scratch, int sms, const LaunchOpt
 {
     RouteParams p = {};
     p.r = r;
-    p.per_block = tokens_per_block(r.tokens, sms);
+    p.per_block = tokens_per_block(r.tokens, r.experts, sms);
     const int64_t blocks = std::max<int64_t>(1, (r.tokens + p.per_block - 1) / p.per_block);
     p.counts = blocks > 1 ? static_cast<int32_t *>(scratch) : nullptr;
     const cudaError_t ce = r.type == T_BF16  ? launch_route_typed<__nv_bfloat16>(p, blocks, o, stream)

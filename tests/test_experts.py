@@ -244,6 +244,10 @@ GROUPS = [  # rows of each expert, rows before and behind them, in, out
     ([128, 129, 127], 0, 0, 136, 640), ([257, 0, 1, 300, 64], 0, 50, 512, 520), ([16, 17, 15, 33, 31, 32, 0, 1], 7, 0, 1000, 130),
     ([1000], 0, 0, 72, 2000), ([i % 4 for i in range(70)], 0, 0, 264, 300), ([90, 400, 12], 1, 1, 1021, 515), ([700, 5, 513], 0, 0, 777, 771),
     ([0] * 40 + [3] + [0] * 40 + [260], 0, 0, 128, 256), ([2100, 1800], 0, 100, 256, 768),
+    # a few rows: the kernel for those, by row and by expert
+    ([0, 0, 2, 0, 1, 0, 0, 3, 0, 0], 1, 2, 520, 130), ([5, 0, 27], 0, 0, 64, 96), ([1, 0, 0, 0, 0, 0, 1], 0, 0, 4096, 520), ([1, 0, 2], 0, 1, 333, 77),
+    # several tiles for every block, several of one expert one after the other
+    ([5000, 100, 3000], 0, 0, 192, 1536), ([i % 7 for i in range(100)], 0, 0, 512, 512), ([9] * 30, 5, 0, 90, 1000),
 ]
 
 
@@ -256,6 +260,26 @@ def ragged(counts, before, behind):
 @pytest.mark.parametrize("case", range(len(GROUPS)))
 @pytest.mark.parametrize("dtype", [BF16, F16])
 def test_experts_forward(case, dtype):
+    check_forward(case, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", range(len(GROUPS)))
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_experts_backward(case, dtype):
+    check_backward(case, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", [2, 4, 6, 7, 9, 10, 11, 18, 19, 20])
+@pytest.mark.parametrize("shape", [1, 2, 3, 4, 5])
+def test_experts_on_every_tile_shape(case, shape):
+    with api.tuning(test_product_shape=shape):
+        check_forward(case, (BF16, F16)[shape % 2])
+        check_backward(case, (F16, BF16)[shape % 2])
+
+
+def check_forward(case, dtype):
     counts, before, behind, k, n = GROUPS[case]
     offsets, rows = ragged(counts, before, behind)
     g, e = gen(case), len(counts)
@@ -281,10 +305,7 @@ def test_experts_forward(case, dtype):
         assert bool((t[:before] == 7).all()) and bool((t[rows - behind:] == 7).all())
 
 
-@pytest.mark.gpu
-@pytest.mark.parametrize("case", range(len(GROUPS)))
-@pytest.mark.parametrize("dtype", [BF16, F16])
-def test_experts_backward(case, dtype):
+def check_backward(case, dtype):
     counts, before, behind, k, n = GROUPS[case]
     offsets, rows = ragged(counts, before, behind)
     g, e = gen(case + 100), len(counts)
@@ -384,6 +405,13 @@ def test_experts_with_offsets_that_are_none():
             dx, dw, db = api.experts_backward(dy, x, w, offsets, pre, act)
         torch.cuda.synchronize()
         assert bool((room[:32] == 7).all()) and bool((room[-32:] == 7).all())
+    for bad in ([0, 5, 2, 9, 3], [-7, 5, 10, 2, 10 ** 9], [2 ** 31 - 1] * 5, [-2 ** 31] * 5, [8, 6, 4, 2, 0], [0, 8, 0, 8, 0]):     # a few rows
+        for experts in (4, 12):                                              # (by expert and by row)
+            offsets = torch.tensor(bad + bad[-1:] * (experts - 4), dtype=I32, device="cuda")
+            room = torch.full((8 + 64, n), 7.0, dtype=BF16, device="cuda")
+            api.experts_forward(x[:8], w.repeat(3, 1, 1)[:experts], offsets, out=room[32:-32])
+            torch.cuda.synchronize()
+            assert bool((room[:32] == 7).all()) and bool((room[-32:] == 7).all())
 
 
 @pytest.mark.gpu
