@@ -60,7 +60,8 @@ struct GroupedParams {
     ExpertSums columns;                 // computed in passing, by the warp that has nothing else to do
 };
 
-__device__ __forceinline__ int offset_at(const GroupedParams &p, int e) { return min(max(__ldg(p.offsets + e), 0), p.rows); }
+// (Plain loads: the offsets come from a kernel that may still be running when this one has begun to wait for it.)
+__device__ __forceinline__ int offset_at(const GroupedParams &p, int e) { return min(max(p.offsets[e], 0), p.rows); }
 
 // ---- tiles ---------------------------------------------------------------------------------------
 
@@ -236,8 +237,9 @@ struct GroupedPieces {
                 }
             }
         } else {
-            // Rows that start anywhere: a row with one instruction, although it stores no more than 64 bytes.  What counts is how
-            // many sectors of L2 the instructions touch, and whole blocks of 16 bytes, the row's ends on their own, touch more.
+            // Rows that start anywhere: one instruction per row, all values at hand before the first (55 gradients of 514 x 4849: 112
+            // us, with a loop of loads and stores 203).  Whole blocks of 16 bytes and the rows' ends on their own are more requests
+            // to L2 for the same bytes, and took longer, in pieces of 64 columns too.
             T *to = first + lane;
             if (lane < left && rows >= 32) {
                 T held[32];
@@ -260,7 +262,7 @@ __device__ __forceinline__ void expert_sums(const ExpertSums &s, int64_t first, 
     const int64_t across = (s.cols + 31) / 32, all = across * s.experts;
     for (int64_t q = first; q < all; q += warps) {
         const int64_t e = q / across, c = (q - e * across) * 32 + lane;
-        const int64_t from = min(max(int64_t(__ldg(s.offsets + e)), int64_t(0)), s.rows), to = min(max(int64_t(__ldg(s.offsets + e + 1)), int64_t(0)), s.rows);
+        const int64_t from = min(max(int64_t(s.offsets[e]), int64_t(0)), s.rows), to = min(max(int64_t(s.offsets[e + 1]), int64_t(0)), s.rows);
         if (c >= s.cols) continue;
         float part[8] = {}, sum = 0.0f;                     // every eighth part: the order of the kernel for the sums alone
         if (from < to) {
@@ -537,7 +539,7 @@ struct PrepareParams {
 
 constexpr int kPrepareCols = 256;           // a warp's columns
 
-__device__ __forceinline__ int64_t offset_in(const int32_t *offsets, int e, int64_t rows) { return min(max(int64_t(__ldg(offsets + e)), int64_t(0)), rows); }
+__device__ __forceinline__ int64_t offset_in(const int32_t *offsets, int e, int64_t rows) { return min(max(int64_t(offsets[e]), int64_t(0)), rows); }
 
 // A block takes `per` rows by 256 columns, and within them one expert's rows after the other; a warp every eighth row, a lane
 // eight neighbours.  Chunk c's sums for expert e are part c + e: both only grow, so no two share one.

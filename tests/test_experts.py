@@ -455,6 +455,77 @@ def test_experts_gradient_against_differences(activation):
         assert abs(float((d.double() * v.double()).sum() - slope)) <= size * 2 * 2.0 ** -11 / h + reach + grads * 2 * 2.0 ** -11
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("stride", [(1 << 26) + 8, (1 << 26) + 1])
+def test_rows_far_apart(stride):
+    """40 rows 2^26 elements apart, and five weights 2^30: offsets pass 2^31 elements and 2^32 bytes, on 16-byte boundaries and off
+    them."""
+    g = gen(30)
+    buffer = torch.zeros(40 * stride, dtype=BF16, device="cuda")
+    far = lambda t: buffer.as_strided(t.shape, (stride, 1)).copy_(t)                     # noqa: E731
+    room = lambda *s: buffer.as_strided(s, (stride, 1)).zero_()                          # noqa: E731
+    offsets, rows = ragged([9, 0, 20, 11, 0], 0, 0)
+    x, w, dy, pre = rand(g, 40, 72, dtype=BF16), rand(g, 5, 56, 72, dtype=BF16), rand(g, 40, 56, dtype=BF16), rand(g, 40, 56, dtype=BF16)
+    few = torch.tensor([0, 3, 3, 8, 8, 8], dtype=I32, device="cuda")
+    want, want_few = api.experts_forward(x, w, offsets, activation="gelu"), api.experts_forward(x[:8], w, few)
+    assert torch.equal(api.experts_forward(far(x), w, offsets, activation="gelu"), want)
+    assert torch.equal(api.experts_forward(far(x)[:8], w, few), want_few)
+    assert torch.equal(api.experts_forward(x, w, offsets, activation="gelu", out=room(40, 56)), want)
+    assert torch.equal(api.experts_forward(x[:8], w, few, out=room(8, 56)), want_few)
+    z = room(40, 56)
+    api.experts_forward(x, w, offsets, activation="gelu", pre=z)
+    assert torch.equal(z, api.experts_forward(x, w, offsets))
+    grads = api.experts_backward(dy, x, w, offsets, pre, "silu")
+    for got in (api.experts_backward(far(dy), x, w, offsets, pre, "silu"), api.experts_backward(dy, far(x), w, offsets, pre, "silu"),
+                api.experts_backward(dy, x, w, offsets, far(pre), "silu"), api.experts_backward(dy, x, w, offsets, pre, "silu", dx=room(40, 72))):
+        assert all(torch.equal(a, b) for a, b in zip(got, grads))
+    apart = (1 << 29) + (stride & 15)
+    stack = lambda: buffer.as_strided((5, 56, 72), (apart, 72, 1))                       # noqa: E731
+    assert 4 * apart + 56 * 72 <= buffer.numel()
+    assert torch.equal(api.experts_forward(x, stack().copy_(w), offsets, activation="gelu"), want)
+    assert torch.equal(api.experts_forward(x[:8], stack(), few), want_few)
+    assert all(torch.equal(a, b) for a, b in zip(api.experts_backward(dy, x, stack(), offsets, pre, "silu"), grads))
+    assert torch.equal(api.experts_backward(dy, x, w, offsets, pre, "silu", dw=stack().zero_())[1], grads[1])
+    # moves: 20 tokens with two rows each
+    p = torch.randperm(40, generator=g, device="cuda").view(20, 2).to(I32)
+    t, y, weights = x[:20], rand(g, 40, 72, dtype=BF16), rand(g, 20, 2)
+    sent, joined, back = api.dispatch_forward(t, p), api.combine_forward(y, p, weights, residual=t), api.combine_backward(t, y, p, weights)
+    assert torch.equal(api.dispatch_forward(far(t), p), sent) and torch.equal(api.dispatch_forward(t, p, out=room(40, 72)), sent)
+    assert torch.equal(api.combine_forward(far(y), p, weights, residual=t), joined) and torch.equal(api.combine_forward(y, p, weights, residual=far(t)), joined)
+    assert torch.equal(api.combine_forward(y, p, weights, residual=t, out=room(20, 72)), joined)
+    near = dict(rtol=1e-5, atol=1e-4)                        # (the order of a sum goes by the alignment)
+    for got in (api.combine_backward(far(t), y, p, weights), api.combine_backward(t, far(y), p, weights), api.combine_backward(t, y, p, weights, drows=room(40, 72))):
+        assert torch.equal(got[0], back[0]) and torch.allclose(got[1], back[1], **near)
+    assert torch.equal(api.dispatch_backward(y, p, dx=room(20, 72)), api.dispatch_backward(y, p))
+    logits = rand(g, 40, 24, dtype=BF16)
+    routes = api.route_forward(logits, 3, normalize=False)
+    assert all(torch.equal(a, b) for a, b in zip(api.route_forward(far(logits), 3, normalize=False), routes))
+    dw = rand(g, 40, 3)
+    d = api.route_backward(dw, logits, routes[0], routes[1], normalize=False)
+    assert torch.equal(api.route_backward(dw, far(logits), routes[0], routes[1], normalize=False), d)
+    assert torch.equal(api.route_backward(dw, logits, routes[0], routes[1], normalize=False, dlogits=room(40, 24)), d)
+
+
+@pytest.mark.gpu
+def test_more_than_two_to_the_31_elements():
+    """Rows by expert of 140000 x 16000; from the beginning, the middle and the end."""
+    g = gen(31)
+    counts = [60000, 0, 79990]
+    offsets, rows = ragged(counts, 0, 10)
+    x, w = rand(g, rows, 64, dtype=BF16), rand(g, 3, 16000, 64, scale=0.1, dtype=BF16)
+    y = torch.zeros((rows, 16000), dtype=BF16, device="cuda")
+    api.experts_forward(x, w, offsets, activation="relu", out=y)
+    for at, e in ((0, 0), (59950, 0), (60000, 2), (134215, 2), (139890, 2)):             # 134218 x 16000 is 2^31
+        part = slice(at, at + 50)
+        z, slack = products(x[part], w[e])
+        within(y[part], act64(z, "relu"), slack, BF16)
+    assert not bool(y[139990:].any())
+    p = torch.arange(rows, device="cuda", dtype=I32).flip(0).view(-1, 1).contiguous()
+    back = api.combine_forward(y, p)
+    for at in (0, 5785, 70000, 139950):
+        assert torch.equal(back[at:at + 50], y[rows - at - 50:rows - at].flip(0))
+
+
 # ---- the bound on the gradients -------------------------------------------------------------------------------------------
 
 def norm64(tensors):
