@@ -1335,20 +1335,24 @@ def _clip_gradients(tensors, max_norm, eps, out, scratch, stream):
             raise RedistError(1, f"{len(tensors)} tensors, but {len(out)} to write")
     device = tensors[0].device if tensors else o.torch.device("cuda", o.current_device() if o.current_device else 0)
     at = o.stream(device, stream)
-    codes, entries, to = o.codes, [], 0
-    for i, t in enumerate(tensors):                          # (a list may be long: a line of Python is a line per tensor)
-        if t.device != device or not (t.is_contiguous() or _dense(t)):
-            raise RedistError(1, f"gradients have to be on one device with their elements side by side; number {i} is not")
-        if out is not None:
-            v = out[i]
+    # (a list may be long: what can be asked of all tensors at once is)
+    T, n, codes = o.torch.Tensor, len(tensors), o.codes
+    if any(map(device.index.__ne__, map(T.get_device, tensors))) or not (all(map(T.is_contiguous, tensors)) or all(map(_dense, tensors))):
+        raise RedistError(1, "gradients have to be on one device, the elements of each side by side")
+    types = [codes.get(t.dtype) for t in tensors]
+    if None in types:
+        _code(o, tensors[types.index(None)], "a gradient")
+    table = array.array("q", bytes(32 * n))                  # entries of four words: data, out, elements, type and reserved
+    table[0::4] = array.array("q", list(map(T.data_ptr, tensors)))
+    table[2::4] = array.array("q", list(map(T.numel, tensors)))
+    table[3::4] = array.array("q", types)
+    if out is not None:
+        for i, (t, v) in enumerate(zip(tensors, out)):
             if v.shape != t.shape or v.dtype is not t.dtype or v.device != device or v.stride() != t.stride():
                 raise RedistError(1, f"out has to be like the gradients; number {i} is not")
-            to = v.data_ptr()
-        code = codes.get(t.dtype)
-        entries += (t.data_ptr(), to, t.numel(), _code(o, t, "a gradient") if code is None else code)
+        table[1::4] = array.array("q", list(map(T.data_ptr, out)))
     norm = o.strided((), (), dtype=o.f32, device=device)
-    table = array.array("q", entries)                        # (type and reserved share the last word of an entry)
-    op = _pack_clip(table.buffer_info()[0], len(tensors), -1.0 if max_norm is None else max_norm, eps, norm.data_ptr())
+    op = _pack_clip(table.buffer_info()[0], n, -1.0 if max_norm is None else max_norm, eps, norm.data_ptr())
     keep, sp, sn = o.scratch(o.clip_scratch_bytes(op), scratch, device)
     rc = o.clip(op, sp, sn, at)
     if rc:

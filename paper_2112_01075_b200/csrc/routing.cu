@@ -65,23 +65,35 @@ __device__ __forceinline__ void scan_counts(int32_t *c, int n, int32_t *total)
     if (lane == 0) *total = carry;
 }
 
-// Rows for the places of tokens lo ... hi - 1, the next free row of expert e being base[e].  The warps that count take a
-// stretch of the places each: first they count their experts, then they know where theirs begin.
-__device__ __forceinline__ void place_rows(const Route &r, int64_t lo, int64_t hi, const int32_t *base, int32_t *counters)
+// The places of tokens lo ... hi - 1 are shared by warps that take a stretch of them each.
+struct Stretch {
+    int counting;                       // warps
+    int64_t from, to;                   // this warp's places
+    int32_t held[2];                    // the experts of the first two turns
+    __device__ __forceinline__ Stretch(const Route &r, int64_t lo, int64_t hi)
+    {
+        const int warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31;
+        const int64_t first = lo * r.chosen, places = (hi - lo) * r.chosen;
+        // two turns of a warp, where there are warps for that: every warp's counters make the chain of the counts longer
+        counting = max(1, int(min(int64_t(min(kRouteWarps, kCounters / r.experts)), (places + 63) / 64)));
+        const int64_t share = (places + counting - 1) / counting;
+        from = first + min(places, warp * share);
+        to = first + min(places, (warp + 1) * share);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) held[i] = warp < counting && from + 32 * i + lane < to ? r.choice[from + 32 * i + lane] : -1;
+    }
+};
+// Rows for the places, the next free row of expert e being base[e]: first the warps count the experts of their stretch, then they
+// know where theirs begin.
+__device__ __forceinline__ void place_rows(const Route &r, const Stretch &own, const int32_t *base, int32_t *counters)
 {
     const int warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31, experts = r.experts;
-    const int64_t first = lo * r.chosen, places = (hi - lo) * r.chosen;
-    // two turns of a warp, where there are warps for that: every warp's counters make the chain below longer
-    const int counting = max(1, int(min(int64_t(min(kRouteWarps, kCounters / experts)), (places + 63) / 64)));
-    const int64_t share = (places + counting - 1) / counting;
-    const int64_t from = first + min(places, warp * share), to = first + min(places, (warp + 1) * share);
+    const int counting = own.counting;
+    const int64_t from = own.from, to = own.to;
     for (int i = threadIdx.x; i < counting * experts; i += kRouteThreads) counters[i] = 0;
-    int32_t held[2];                    // the first two turns' experts
-#pragma unroll
-    for (int i = 0; i < 2; ++i) held[i] = warp < counting && from + 32 * i + lane < to ? r.choice[from + 32 * i + lane] : -1;
     __syncthreads();
     int32_t *mine = counters + warp * experts;
-    auto expert = [&](int64_t at) { return at == from ? held[0] : at == from + 32 ? held[1] : at + lane < to ? r.choice[at + lane] : -1; };
+    auto expert = [&](int64_t at) { return at == from ? own.held[0] : at == from + 32 ? own.held[1] : at + lane < to ? r.choice[at + lane] : -1; };
     if (warp < counting)
         for (int64_t at = from; at < to; at += 32) {
             const int32_t e = expert(at);
@@ -144,12 +156,58 @@ template <typename T> struct Ranked {
     }
 };
 
-// The choice: L lanes hold PER logits of a token each, and agree `chosen` times on the largest that is left.  Blocks count
-// how many places each expert got among their tokens.  What bounds it is the number of instructions per token.
+// A lane's logits in descending order, each with its index where it does not hold it: what is taken is the first, and taking it
+// moves the others up.  (Of equal ones the lower index comes first: neighbours only change places when they are out of order,
+// and the pairs of the networks are ordered by index to begin with.)
+template <bool INDEXED, int PER> struct Sorted {
+    uint32_t key[PER];
+    uint16_t index[INDEXED ? 1 : PER];
+    __device__ __forceinline__ void order(int a, int b)     // a < b
+    {
+        bool swap = key[b] > key[a];
+        if constexpr (!INDEXED) swap = swap || (key[b] == key[a] && index[b] < index[a]);
+        const uint32_t k = swap ? key[b] : key[a];
+        key[b] = swap ? key[a] : key[b];
+        key[a] = k;
+        if constexpr (!INDEXED) {
+            const uint16_t i = swap ? index[b] : index[a];
+            index[b] = swap ? index[a] : index[b];
+            index[a] = i;
+        }
+    }
+    __device__ __forceinline__ void sort()                  // odd-even merges
+    {
+#pragma unroll
+        for (int p = 1; p < PER; p *= 2)
+#pragma unroll
+            for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+                for (int j = k % p; j + k < PER; j += 2 * k)
+#pragma unroll
+                    for (int i = 0; i < k; ++i)
+                        if ((i + j) / (2 * p) == (i + j + k) / (2 * p) && i + j + k < PER) order(i + j, i + j + k);
+    }
+    __device__ __forceinline__ void take(bool mine)
+    {
+#pragma unroll
+        for (int j = 0; j + 1 < PER; ++j) {
+            key[j] = mine ? key[j + 1] : key[j];
+            if constexpr (!INDEXED) index[j] = mine ? index[j + 1] : index[j];
+        }
+        key[PER - 1] = mine ? 0 : key[PER - 1];
+    }
+};
+
+// The choice: L lanes hold PER logits of a token each, and agree `chosen` times on the largest that is left.  Blocks count how
+// many places each expert got among their tokens.  What bounds it is the number of instructions per token: 16384 tokens, 8 of
+// 128 experts, 10.2 us, and 12.8 when the lane whose logit was taken looked through the others again, a dozen instructions with all
+// lanes waiting.
 template <typename T, int L, int PER>
 __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const RouteParams p)
 {
     using R = Ranked<T>;
+    constexpr int kTurn = kRouteThreads / L;                 // tokens of a block side by side
+    constexpr bool kSorted = PER <= 8, kAhead = PER <= 8;    // (more of them do not fit into the registers, or take longer to sort)
     __shared__ int32_t counts[kMostExperts], counters[kCounters];
     const Route &r = p.r;
     const int lane = int(threadIdx.x) & 31, at = lane % L, group = int(threadIdx.x) / L;
@@ -159,7 +217,6 @@ __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const Route
     wait_for_previous();
     __syncthreads();
     const int64_t lo = int64_t(blockIdx.x) * p.per_block, hi = min(r.tokens, lo + p.per_block);
-    constexpr bool kAhead = PER <= 8;                        // (more of them do not fit into the registers)
     T ahead[PER];
     auto load = [&](int64_t t) {
         const T *row = static_cast<const T *>(r.logits) + t * r.ld;
@@ -168,37 +225,42 @@ __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const Route
             if (t < hi && at + 32 * j < r.experts) ahead[j] = row[at + 32 * j];
     };
     if (kAhead) load(lo + group);
-    for (int64_t base = lo; base < hi; base += kRouteThreads / L) {           // all lanes of a warp walk along
+    for (int64_t base = lo; base < hi; base += kTurn) {                       // all lanes of a warp walk along
         const int64_t t = base + group;
         const bool in = t < hi;
         if (!kAhead) load(t);
-        uint32_t key[PER];
-#pragma unroll
-        for (int j = 0; j < PER; ++j) key[j] = in && at + 32 * j < r.experts ? R::of(ahead[j], at + 32 * j) : 0;
-        if (kAhead) load(t + kRouteThreads / L);
+        Sorted<R::kIndexed, PER> mine;
         uint32_t best = 0, top = 0, own = 0;
         int32_t own_choice = -1;
         float every = 0.0f;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) best = max(best, key[j]);
-        for (int s = 0; s < r.chosen; ++s) {
-            const uint32_t most = lane_max<L>(best);
-            if (s == 0) {
-                top = most;
-                if (!r.normalize) {
+        for (int j = 0; j < PER; ++j) {
+            mine.key[j] = in && at + 32 * j < r.experts ? R::of(ahead[j], at + 32 * j) : 0;
+            if constexpr (!R::kIndexed) mine.index[j] = uint16_t(at + 32 * j);
+            best = max(best, mine.key[j]);
+        }
+        if (kAhead) load(t + kTurn);
+        if (!r.normalize) {
+            top = lane_max<L>(best);
 #pragma unroll
-                    for (int j = 0; j < PER; ++j)
-                        if (!R::never(key[j])) every += expf(R::value(key[j]) - R::value(top));
-                }
-            }
+            for (int j = 0; j < PER; ++j)
+                if (!R::never(mine.key[j])) every += expf(R::value(mine.key[j]) - R::value(top));
+        }
+        if constexpr (kSorted) mine.sort();
+        for (int s = 0; s < r.chosen; ++s) {
+            if constexpr (kSorted) best = mine.key[0];
+            const uint32_t most = lane_max<L>(best);
+            if (s == 0) top = most;
             if constexpr (R::kIndexed) {
                 if (at == s) own = most;
-                if (best == most) {                                           // (its own lane, or all are taken)
+                if constexpr (kSorted) {
+                    mine.take(best == most);                                  // (its own lane, or all are taken)
+                } else if (best == most) {
                     best = 0;
 #pragma unroll
                     for (int j = 0; j < PER; ++j) {
-                        if (key[j] == most) key[j] = 0;
-                        best = max(best, key[j]);
+                        if (mine.key[j] == most) mine.key[j] = 0;
+                        best = max(best, mine.key[j]);
                     }
                 }
             } else {
@@ -207,10 +269,12 @@ __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const Route
                     which = __ffs(__ballot_sync(0xffffffffu, best == most) & segment) - 1 - lane / L * L;
                 } else {
                     uint32_t index = 0xffffu;
-                    if (best == most) {
+                    if constexpr (kSorted) {
+                        if (best == most) index = mine.index[0];
+                    } else if (best == most) {
 #pragma unroll
                         for (int j = PER - 1; j >= 0; --j)
-                            if (key[j] == most) index = uint32_t(at + 32 * j);
+                            if (mine.key[j] == most) index = uint32_t(at + 32 * j);
                     }
                     which = int32_t(__reduce_min_sync(0xffffffffu, index));
                 }
@@ -218,12 +282,14 @@ __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const Route
                     own = most;
                     own_choice = which;
                 }
-                if (which % 32 == at) {
+                if constexpr (kSorted) {
+                    mine.take(which % 32 == at);
+                } else if (which % 32 == at) {
                     best = 0;
 #pragma unroll
                     for (int j = 0; j < PER; ++j) {
-                        if (at + 32 * j == which) key[j] = 0;
-                        best = max(best, key[j]);
+                        if (at + 32 * j == which) mine.key[j] = 0;
+                        best = max(best, mine.key[j]);
                     }
                 }
             }
@@ -247,7 +313,7 @@ __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const Route
     scan_counts(counts, r.experts, &total);
     __syncthreads();
     for (int e = threadIdx.x; e <= r.experts; e += kRouteThreads) r.offsets[e] = e < r.experts ? counts[e] : total;
-    place_rows(r, lo, hi, counts, counters);
+    place_rows(r, Stretch(r, lo, hi), counts, counters);
 }
 
 // The second step where tokens are many: a block's rows of expert e follow those of lower experts and those of the blocks
@@ -258,6 +324,8 @@ __global__ void __launch_bounds__(kRouteThreads) redist_place_kernel(const Route
     const Route &r = p.r;
     let_next_start();
     wait_for_previous();
+    const int64_t lo = int64_t(blockIdx.x) * p.per_block, hi = min(r.tokens, lo + p.per_block);
+    const Stretch own(r, min(lo, hi), hi);                  // on its way while the counts are
     for (int e = threadIdx.x; e < r.experts; e += kRouteThreads) base[e] = before[e] = 0;
     __syncthreads();
     // the experts side by side, the blocks divided among the threads that are left
@@ -282,8 +350,7 @@ __global__ void __launch_bounds__(kRouteThreads) redist_place_kernel(const Route
     __syncthreads();
     for (int e = threadIdx.x; e < r.experts; e += kRouteThreads) base[e] += before[e];
     __syncthreads();
-    const int64_t lo = int64_t(blockIdx.x) * p.per_block, hi = min(r.tokens, lo + p.per_block);
-    place_rows(r, min(lo, hi), hi, base, counters);
+    place_rows(r, own, base, counters);
 }
 
 // A warp per token.
