@@ -806,7 +806,9 @@ def test_more_move_refusals(name, change, status):
     (dict(w=(None, 16, 1)), 1), (dict(w_stride=383), 1), (dict(w_stride=0), 1), (dict(w_stride=-384), 1), (dict(w=(0x20001, 16, 1)), 7),
     (dict(out=(0x30000, 23, 1)), 1), (dict(out=(0x10010, 24, 1)), 6), (dict(pre=(0x30010, 24, 1)), 6), (dict(out=(0x20800, 24, 1)), 6),
     (dict(bias=0x50001), 7), (dict(bias=0x50000, bias_type=3), 1), (dict(bias=0x50000, bias_stride=-1), 1), (dict(bias=0x30010), 6),
-    (dict(offsets=0x30010), 6), (dict(rows=1 << 31), 10), (dict(x=(0x10002, 16, 1)), 5), (dict(w=(0x20002, 16, 1)), 5), (dict(w_stride=388), 5),
+    (dict(offsets=0x30010), 6), (dict(rows=1 << 31), 10),
+    # (a few rows need no scratch)
+    (dict(rows=40, x=(0x10002, 16, 1)), 5), (dict(rows=40, w=(0x20002, 16, 1)), 5), (dict(rows=40, w_stride=388), 5),
 ])
 def test_experts_refusals(change, status):
     assert api.load().redist_experts_forward(api._Experts(*{**EXPERTS, **change}.values()), None, 0, None) == status
