@@ -177,23 +177,28 @@ struct PlacedStack {
         plane = fits ? stride : from.lines * ld;
         if (!fits) copy = pieces.take(count * plane * 2);
     }
-    StackLay lay() const { return StackLay{from.data, copy, count, from.lines, from.line, from.ld, stride, ld, plane}; }
+    StackLay lay(const int32_t *offsets) const { return StackLay{from.data, copy, count, from.lines, from.line, from.ld, stride, ld, plane, offsets}; }
     Operand operand(bool rows_survive) const { return Operand{fits ? from.data : copy, ld, plane, from.by_rows == rows_survive ? 0 : 1}; }
 };
 
 const redist_matrix kAbsent = {nullptr, 1, 1};
 
 // A forward call of a few rows reads its operands as they lie and needs no scratch: up to eight rows, where its blocks are more
-// than the tiles and start sooner (2 rows of 8 experts, 4096 -> 4096: 15.7 us against 18; 6 rows of 128, 1024 -> 1024: 6.4 and 9.2),
-// and up to 32 where the weights they meet are small (32 rows of 4, 512 -> 512: 4.3 and 5.4, but 32 of 8, 4096 -> 4096: 52 and 49)
-// and on 16-byte boundaries (513 -> 511: 11.6 and 9.6).
+// than the tiles and start sooner (2 rows of 8 experts, 4096 -> 4096: 15.4 us against 18; 6 rows of 128, 1024 -> 1024: 6.4 and 9.2;
+// 4 of 8, 81 -> 153: 6.7 and 8.6), and up to 32 where the weights they meet are small or sums long, of which a tile takes one step
+// after the other (32 rows of 4, 512 -> 512: 4.3 and 5.4; 20 of 2, 2576 -> 90: 6.1 and 10.2; but 9 of 2, 256 -> 6795: 7.4 and 6.2, and 32
+// of 8, 4096 -> 4096: 52 and 49).  Off 16-byte boundaries shifting costs more, so only with a few rows for each expert or very long
+// sums with few results (26 rows of 16, 555 -> 121: 6.9 and 8.5; 32 of 40, 5619 -> 73: 24 and 31; but 26 of one, 1037 -> 68: 16 and 10).
 bool few_expert_rows(const redist_experts &q, const LaunchOptions &o)
 {
     if (o.test_shape || q.rows > kFewRows || !row_major(q.x, q.rows, q.in_features) || !row_major(q.w, q.out_features, q.in_features)) return false;
     if (q.rows <= 8) return true;
-    const double met = double(std::min<i64>(q.rows, q.experts)) * double(q.in_features) * double(q.out_features);
-    return met <= double(1 << 23) && operand_fits(q.x.data, row_stride(q.x, q.rows, q.in_features), 0, 1) &&
-           operand_fits(q.w.data, row_stride(q.w, q.out_features, q.in_features), q.w_stride, int(std::min<i64>(q.experts, 2)));
+    const i64 busy = std::min<i64>(q.rows, q.experts);
+    const double met = double(busy) * double(q.in_features) * double(q.out_features);
+    if (operand_fits(q.x.data, row_stride(q.x, q.rows, q.in_features), 0, 1) &&
+        operand_fits(q.w.data, row_stride(q.w, q.out_features, q.in_features), q.w_stride, int(std::min<i64>(q.experts, 2))))
+        return met <= double(q.in_features >= 2048 ? 1 << 22 : 1 << 20);
+    return (met <= double(1 << 20) && q.rows <= 4 * busy) || (q.in_features >= 4096 && q.out_features <= 256);
 }
 
 struct ExpertsForward {
@@ -457,8 +462,8 @@ redist_status redist_experts_forward(const redist_experts *op, void *scratch, si
         }
         Prepare before = {};
         before.type = q.type;
-        before.lay[0] = f.w.lay();
-        before.lay[1] = f.x.lay();
+        before.lay[0] = f.w.lay(q.offsets);
+        before.lay[1] = f.x.lay(nullptr);
         TRY(cuda(launch_prepare(before, o, stream)));
         g.a = f.w.operand(true);
         g.b = f.x.operand(true);
@@ -539,8 +544,8 @@ redist_status redist_experts_backward(const redist_experts *op, const redist_exp
             s.ld_dst = b.ld_dz;
             s.partials = b.partials;
         }
-        before.lay[0] = b.w.lay();
-        before.lay[1] = b.x.lay();
+        before.lay[0] = b.w.lay(q.offsets);
+        before.lay[1] = b.x.lay(nullptr);
         if (g.dw.data) before.sums = &w;
         before.maps = b.maps;
         TRY(cuda(launch_prepare(before, o, stream)));

@@ -543,20 +543,28 @@ __device__ __forceinline__ int64_t offset_in(const int32_t *offsets, int e, int6
 
 // A block takes `per` rows by 256 columns, and within them one expert's rows after the other; a warp every eighth row, a lane
 // eight neighbours.  Chunk c's sums for expert e are part c + e: both only grow, so no two share one.
-template <typename T> __device__ __forceinline__ void slope_block(const ExpertSlope &s, int64_t chunk, int64_t column, int64_t per, bool aligned, float (&all)[8][kPrepareCols])
+constexpr int kHeldOffsets = 512;           // of so many experts the offsets are looked up in shared memory
+template <typename T> __device__ __forceinline__ void slope_block(const ExpertSlope &s, int64_t chunk, int64_t column, int64_t per, bool aligned, float (&all)[8][kPrepareCols],
+                                                                  int32_t (&offsets)[kHeldOffsets + 1])
 {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int64_t c = column * kPrepareCols + lane * 8, lo = chunk * per, hi = min(s.rows, lo + per);
     const int count = int(min(s.cols - c, int64_t(8)));
+    const bool held = s.experts <= kHeldOffsets;            // (a chain of searches and steps: a latency of L2 each otherwise)
+    if (held) {
+        for (int i = threadIdx.x; i <= s.experts; i += 256) offsets[i] = int32_t(offset_in(s.offsets, i, s.rows));
+        __syncthreads();
+    }
+    auto offset = [&](int i) { return held ? int64_t(offsets[i]) : offset_in(s.offsets, i, s.rows); };
     // the first expert that ends behind this block's first row
     int e = 0;
     for (int above = s.experts; e < above;) {
         const int mid = (e + above) >> 1;
-        if (offset_in(s.offsets, mid + 1, s.rows) > lo) above = mid;
+        if (offset(mid + 1) > lo) above = mid;
         else e = mid + 1;
     }
     for (; e < s.experts; ++e) {
-        const int64_t begin = offset_in(s.offsets, e, s.rows), from = max(lo, begin), to = min(hi, offset_in(s.offsets, e + 1, s.rows));
+        const int64_t begin = offset(e), from = max(lo, begin), to = min(hi, offset(e + 1));
         if (begin >= hi) break;
         if (from >= to) continue;
         float sums[8] = {};
@@ -616,6 +624,7 @@ __device__ __forceinline__ void lay_long(const StackLay &l, int64_t block, int64
     const int64_t all = l.count * l.lines;
     for (int64_t line = block * 8 + (threadIdx.x >> 5); line < all; line += blocks * 8) {
         const int64_t matrix = l.count > 1 ? line / l.lines : 0, at = line - matrix * l.lines;
+        if (l.offsets && l.offsets[matrix + 1] <= l.offsets[matrix]) continue;
         const uint16_t *src = static_cast<const uint16_t *>(l.src) + matrix * l.plane_src + at * l.ld_src;
         uint16_t *dst = static_cast<uint16_t *>(l.dst) + matrix * l.plane_dst + at * l.ld_dst;
         for (int64_t c = lane * 8; c < l.line; c += kAhead * kPrepareCols) {
@@ -632,37 +641,40 @@ __device__ __forceinline__ void lay_long(const StackLay &l, int64_t block, int64
     }
 }
 
-// ... and of lines of up to 128 columns as many as fill it, twice.
-__device__ __forceinline__ int lay_lanes(int64_t line)       // of a line of up to 128 columns
+// ... and of lines of up to 256 columns as many as fill it, four times.
+constexpr int kShortLines = 4;
+__host__ __device__ __forceinline__ int lay_lanes(int64_t line)       // of a line of up to 256 columns
 {
-    int lanes = 16;
+    int lanes = 32;
     while (lanes > 1 && (lanes / 2) * 8 >= line) lanes /= 2;
     return lanes;
 }
 __device__ __forceinline__ void lay_short(const StackLay &l, int64_t block, int64_t blocks)
 {
     const int lanes = lay_lanes(l.line), group = 32 / lanes, lane = threadIdx.x & 31, c = lane % lanes * 8;
-    const int64_t all = l.count * l.lines;
-    for (int64_t line0 = (block * 8 + (threadIdx.x >> 5)) * 2 * group + lane / lanes; line0 < all; line0 += blocks * 8 * 2 * group) {
-        Blocks b[2];
-        const uint16_t *src[2];
-        uint16_t *dst[2];
+    const int64_t all = l.count * l.lines, turn = kShortLines * group;
+    for (int64_t line0 = (block * 8 + (threadIdx.x >> 5)) * turn + lane / lanes; line0 < all; line0 += blocks * 8 * turn) {
+        Blocks b[kShortLines];
+        const uint16_t *src[kShortLines];
+        uint16_t *dst[kShortLines];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t line = line0 + i * group, matrix = l.count > 1 ? line / l.lines : 0, at = line - matrix * l.lines;
+        for (int i = 0; i < kShortLines; ++i) {
+            const int64_t line = line0 + i * group;
+            const int64_t matrix = l.count == 1 ? 0 : all < INT32_MAX ? int64_t(uint32_t(line) / uint32_t(l.lines)) : line / l.lines, at = line - matrix * l.lines;
+            const bool some = line < all && c < l.line && !(l.offsets && l.offsets[matrix + 1] <= l.offsets[matrix]);
             src[i] = static_cast<const uint16_t *>(l.src) + matrix * l.plane_src + at * l.ld_src + c;
-            dst[i] = line < all && c < l.line ? static_cast<uint16_t *>(l.dst) + matrix * l.plane_dst + at * l.ld_dst + c : nullptr;
-            if (dst[i]) b[i].load(src[i], int(min(l.line - c, int64_t(8))) * 2);
+            dst[i] = some ? static_cast<uint16_t *>(l.dst) + matrix * l.plane_dst + at * l.ld_dst + c : nullptr;
+            if (some) b[i].load(src[i], int(min(l.line - c, int64_t(8))) * 2);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kShortLines; ++i)
             if (dst[i]) *reinterpret_cast<uint4 *>(dst[i]) = b[i].get(src[i]);
     }
 }
 
 __device__ __forceinline__ void lay_block(const StackLay &l, int64_t block, int64_t blocks)
 {
-    if (l.line > 128) lay_long(l, block, blocks);
+    if (l.line > kPrepareCols) lay_long(l, block, blocks);
     else lay_short(l, block, blocks);
 }
 
@@ -690,11 +702,12 @@ template <typename T> __global__ void __launch_bounds__(256, 4)
 redist_expert_prepare_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ PrepareParams p)
 {
     __shared__ float all[8][kPrepareCols];
+    __shared__ int32_t offsets[kHeldOffsets + 1];
     let_next_start();
     wait_for_previous();
     int64_t b = blockIdx.x;
     if (b < p.slope_blocks) {
-        slope_block<T>(p.p.slope, b / p.slope_across, b % p.slope_across, p.slope_per, p.aligned, all);
+        slope_block<T>(p.p.slope, b / p.slope_across, b % p.slope_across, p.slope_per, p.aligned, all, offsets);
         return;
     }
     b -= p.slope_blocks;
@@ -803,11 +816,6 @@ cudaError_t launch_any(void (*kernel)(P...), dim3 grid, int threads, int smem, i
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// The sums that a block of a product computes in passing: groups of 32 columns, and parts of an expert's rows on average, at most.
-// More could take longer than its tiles (8192 x 1024 -> 1024 of 64 experts, backward, with 14 groups a block 97 us, with a
-// launch for them 89).
-constexpr int kPassing = 8, kPassingParts = 24;
-
 // The smallest power of two that makes the quotient exact for numerators below 2^31.
 Divider divider(int64_t d)
 {
@@ -878,8 +886,14 @@ cudaError_t launch(const Grouped &g, void *scratch, ExpertSums *columns, const L
     }
     const int64_t groups = sms / CG;
     const unsigned blocks = unsigned(std::min(tiles, groups) * CG);
-    if (columns && columns->sums && (columns->cols + 31) / 32 * columns->experts <= int64_t(blocks) * kPassing &&
-        columns->rows <= columns->per * columns->experts * kPassingParts) {
+    // The sums of 32 columns of an expert take two latencies of memory and one for every eight of its parts; a product computes them
+    // in passing where that hides behind its tiles (8192 x 1024 -> 1024 of 64 experts with 14 such groups a block: 97 us, with a
+    // launch for them 89; 832 x 96 <- 865 of 7 with 7 of them: 21 us for the product, 7 alone).
+    const double share = columns ? std::ceil(double((columns->cols + 31) / 32) * columns->experts / blocks) : 0;
+    const double rows = columns ? double(columns->rows) / std::min<int64_t>(columns->experts, columns->rows) : 0;
+    const double passing = columns ? share * (1.2 + 0.6 * std::ceil(1.5 * rows / double(columns->per) / 8)) : 0;
+    const double own = 4 + 0.2 * std::ceil(double(tiles) / double(groups)) * (SUMS ? std::ceil(rows / 64) : double(g.k) / 64);
+    if (columns && columns->sums && passing <= own) {
         p.columns = *columns;
         columns->sums = nullptr;                            // done
     }
@@ -989,7 +1003,7 @@ cudaError_t launch_prepare(const Prepare &p, const LaunchOptions &o, cudaStream_
     for (int i = 0; i < 2; ++i)
         if (p.lay[i].dst) {
             // a turn for each warp: there are more blocks than fit at once, and a warp's turn hides little
-            const int64_t line = p.lay[i].line, turn = line > 128 ? 1 : line > 64 ? 4 : 8;
+            const int64_t line = p.lay[i].line, turn = line > kPrepareCols ? 1 : kShortLines * (32 / lay_lanes(line));
             q.lay_blocks[i] = std::min<int64_t>((p.lay[i].count * p.lay[i].lines + 8 * turn - 1) / (8 * turn), 1 << 20);
         }
     CUtensorMap ma, mb;

@@ -58,11 +58,13 @@ struct ExpertSlope {
     float *partials;                    // expert_partial_bytes
 };
 
-// `count` matrices of `lines` lines laid out anew on 16-byte boundaries (dst null: none).
+// `count` matrices of `lines` lines laid out anew on 16-byte boundaries (dst null: none); with offsets only those of experts that
+// have rows.
 struct StackLay {
     const void *src;
     void *dst;
     int64_t count, lines, line, ld_src, plane_src, ld_dst, plane_dst;
+    const int32_t *offsets;             // or null
 };
 
 struct Prepare {

@@ -543,9 +543,10 @@ template <typename T, int N, int L, int K> __global__ void __launch_bounds__(kMo
 // The gradient of the latter: L threads take whole tokens, because dweights are sums over their columns.
 template <typename T, int N, int L, int K> __global__ void __launch_bounds__(kMoveThreads, 3) redist_combine_gradient_kernel(const Move m, int pieces)
 {
-    __shared__ float dots[2][kMoveThreads / 32][kMostChosen];
+    constexpr int kLanes = L < 32 ? L : 32;                  // that add up a dot before it goes through shared memory
+    __shared__ float dots[2][kMoveThreads / kLanes][kMostChosen];
     const int64_t step = int64_t(gridDim.x) * (kMoveThreads / L);
-    const int group = int(threadIdx.x) / L, at = int(threadIdx.x) % L, warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31;
+    const int group = int(threadIdx.x) / L, at = int(threadIdx.x) % L, slot = int(threadIdx.x) / kLanes, lane = int(threadIdx.x) % kLanes;
     let_next_start();
     wait_for_previous();
     int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + group;
@@ -597,8 +598,8 @@ template <typename T, int N, int L, int K> __global__ void __launch_bounds__(kMo
             }
 #pragma unroll
             for (int i = 0; i < K; ++i) {
-                dot[i] = lane_sum<32>(dot[i]);
-                if (lane == 0 && s + i < m.chosen) dots[turn][warp][s + i] = dot[i];
+                dot[i] = lane_sum<kLanes>(dot[i]);
+                if (lane == 0 && s + i < m.chosen) dots[turn][slot][s + i] = dot[i];
             }
         }
         // the next token writes to the other half: one barrier for each
@@ -606,7 +607,7 @@ template <typename T, int N, int L, int K> __global__ void __launch_bounds__(kMo
         else __syncwarp();
         for (int s = at; in && s < m.chosen; s += L) {
             float sum = 0.0f;
-            for (int i = 0; i < L / 32; ++i) sum += dots[turn][group * (L / 32) + i][s];
+            for (int i = 0; i < L / kLanes; ++i) sum += dots[turn][group * (L / kLanes) + i][s];
             m.dweights[t * m.chosen + s] = sum;
         }
     }
@@ -747,9 +748,10 @@ template <typename T, int L> __global__ void __launch_bounds__(kMoveThreads, 3) 
 template <typename T, int L> __global__ void __launch_bounds__(kMoveThreads, 3) redist_combine_gradient_any_kernel(const Move m, int pieces)
 {
     constexpr int N = Cut<T>::N;
-    __shared__ float dots[2][kMoveThreads / 32][kMostChosen];
+    constexpr int kLanes = L < 32 ? L : 32;
+    __shared__ float dots[2][kMoveThreads / kLanes][kMostChosen];
     const int64_t step = int64_t(gridDim.x) * (kMoveThreads / L);
-    const int group = int(threadIdx.x) / L, lane_at = int(threadIdx.x) % L, warp = int(threadIdx.x) >> 5, lane = int(threadIdx.x) & 31;
+    const int group = int(threadIdx.x) / L, lane_at = int(threadIdx.x) % L, slot = int(threadIdx.x) / kLanes, lane = int(threadIdx.x) % kLanes;
     let_next_start();
     wait_for_previous();
     int64_t t = int64_t(blockIdx.x) * (kMoveThreads / L) + group;
@@ -792,14 +794,14 @@ template <typename T, int L> __global__ void __launch_bounds__(kMoveThreads, 3) 
                     }
                 }
             }
-            dot = lane_sum<32>(dot);
-            if (lane == 0) dots[turn][warp][s] = dot;
+            dot = lane_sum<kLanes>(dot);
+            if (lane == 0) dots[turn][slot][s] = dot;
         }
         if constexpr (L > 32) __syncthreads();
         else __syncwarp();
         for (int s = lane_at; in && s < m.chosen; s += L) {
             float sum = 0.0f;
-            for (int i = 0; i < L / 32; ++i) sum += dots[turn][group * (L / 32) + i][s];
+            for (int i = 0; i < L / kLanes; ++i) sum += dots[turn][group * (L / kLanes) + i][s];
             m.dweights[t * m.chosen + s] = sum;
         }
     }
@@ -897,9 +899,11 @@ template <Which W, typename T, int N> cudaError_t launch_move_lanes(const Move &
     int device = 0, sms = 0;
     const cudaError_t ce = current_device(&device, &sms);
     if (ce != cudaSuccess) return ce;
-    // a warp per token (or stretch of it) for short rows, a block for longer ones
+    // eight or sixteen lanes per token for the shortest rows, a warp (per stretch) for short ones, a block for longer ones
     if (pieces > 32 * kHeld) return launch_move_width<W, T, N, kMoveThreads>(m, int(pieces), sms, o, stream);
-    return launch_move_width<W, T, N, 32>(m, int(pieces), sms, o, stream);
+    if (pieces > 16 && pieces <= 32) return launch_move_width<W, T, N, 16>(m, int(pieces), sms, o, stream);
+    if (pieces > 16) return launch_move_width<W, T, N, 32>(m, int(pieces), sms, o, stream);
+    return launch_move_width<W, T, N, 8>(m, int(pieces), sms, o, stream);
 }
 
 template <Which W, typename T, int L> cudaError_t launch_move_any(const Move &m, const LaunchOptions &o, cudaStream_t stream)
@@ -925,7 +929,10 @@ template <Which W, typename T> cudaError_t launch_move_typed(const Move &m, int 
     // 8000 x 4095, two rows each, forward and backward: 295 us cut and shifted, 441 by single elements; but with two elements of
     // 16 bits or one of 32 at a time the latter take less (4094: 280 against 289; 1021 of 32 bits: 207 against 261)
     if (sizeof(T) == 2 && n == 1 && m.cols >= 2 * kMost)
-        return m.cols > 32 * kMost ? launch_move_any<W, T, kMoveThreads>(m, o, stream) : launch_move_any<W, T, 32>(m, o, stream);
+        return m.cols > 32 * kHeld * kMost ? launch_move_any<W, T, kMoveThreads>(m, o, stream)
+               : m.cols > 31 * kMost       ? launch_move_any<W, T, 32>(m, o, stream)
+               : m.cols > 15 * kMost       ? launch_move_any<W, T, 16>(m, o, stream)
+                                           : launch_move_any<W, T, 8>(m, o, stream);
     if (n >= kMost) return launch_move_lanes<W, T, kMost>(m, o, stream);
     if (n >= kMost / 2) return launch_move_lanes<W, T, kMost / 2>(m, o, stream);
     if constexpr (kMost == 8)
