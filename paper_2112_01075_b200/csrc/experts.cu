@@ -541,14 +541,49 @@ constexpr int kPrepareCols = 256;           // a warp's columns
 
 __device__ __forceinline__ int64_t offset_in(const int32_t *offsets, int e, int64_t rows) { return min(max(int64_t(offsets[e]), int64_t(0)), rows); }
 
-// A block takes `per` rows by 256 columns, and within them one expert's rows after the other; a warp every eighth row, a lane
-// eight neighbours.  Chunk c's sums for expert e are part c + e: both only grow, so no two share one.
 constexpr int kHeldOffsets = 512;           // of so many experts the offsets are looked up in shared memory
-template <typename T> __device__ __forceinline__ void slope_block(const ExpertSlope &s, int64_t chunk, int64_t column, int64_t per, bool aligned, float (&all)[8][kPrepareCols],
-                                                                  int32_t (&offsets)[kHeldOffsets + 1])
+
+// A lane's eight neighbours of one row: dz, stored, and as it is before it is rounded.
+template <typename T> __device__ __forceinline__ void slope_row(const ExpertSlope &s, int64_t row, int64_t c, int count, bool aligned, float (&v)[8])
+{
+    const T *src = static_cast<const T *>(s.dy) + row * s.ld_dy + c, *z = static_cast<const T *>(s.z) + row * s.ld_z + c;
+    uint4 u, y = make_uint4(0, 0, 0, 0);
+    if (aligned && count >= 8) {
+        u = *reinterpret_cast<const uint4 *>(src);
+        if (s.z) y = *reinterpret_cast<const uint4 *>(z);
+    } else {
+        Blocks a, b = {};
+        a.load(src, count * 2);
+        if (s.z) b.load(z, count * 2);
+        u = a.get(src);
+        y = b.get(z);
+    }
+    float at[8];
+    const uint32_t wu[4] = {u.x, u.y, u.z, u.w}, wy[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpack2<T>(wu[i]), g = unpack2<T>(wy[i]);
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+        at[2 * i] = g.x;
+        at[2 * i + 1] = g.y;
+    }
+    if (s.z) {
+        times_slope8(v, at, s.activation);
+        // dz becomes an operand of two products: 16 bits, as the tensor cores take them (see the linear layer's)
+        u = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+    }
+    if (s.dst) *reinterpret_cast<uint4 *>(static_cast<T *>(s.dst) + row * s.ld_dst + c) = u;
+}
+
+// A block takes `per` rows by 256 columns, and within them one expert's rows after the other; a warp every eighth row, a lane
+// eight neighbours.  Chunk c's sums for expert e are part c + e: both only grow, so no two share one.  SMALL: eight rows, a
+// warp each, whatever their experts are (one expert after the other, each a latency of memory, 8 rows of 72 experts took 14 us).
+template <typename T, bool SMALL> __device__ __forceinline__ void slope_block(const ExpertSlope &s, int64_t chunk, int64_t column, int64_t per, bool aligned,
+                                                                              float (&all)[8][kPrepareCols], int32_t (&offsets)[kHeldOffsets + 1])
 {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const int64_t c = column * kPrepareCols + lane * 8, lo = chunk * per, hi = min(s.rows, lo + per);
+    const int64_t c = column * kPrepareCols + lane * 8, lo = chunk * per, hi = min(s.rows, lo + per), cc = column * kPrepareCols + threadIdx.x;
     const int count = int(min(s.cols - c, int64_t(8)));
     const bool held = s.experts <= kHeldOffsets;            // (a chain of searches and steps: a latency of L2 each otherwise)
     if (held) {
@@ -556,57 +591,55 @@ template <typename T> __device__ __forceinline__ void slope_block(const ExpertSl
         __syncthreads();
     }
     auto offset = [&](int i) { return held ? int64_t(offsets[i]) : offset_in(s.offsets, i, s.rows); };
-    // the first expert that ends behind this block's first row
-    int e = 0;
-    for (int above = s.experts; e < above;) {
-        const int mid = (e + above) >> 1;
-        if (offset(mid + 1) > lo) above = mid;
-        else e = mid + 1;
+    auto first_behind = [&](int64_t row) {                  // the first expert that ends behind it
+        int e = 0;
+        for (int above = s.experts; e < above;) {
+            const int mid = (e + above) >> 1;
+            if (offset(mid + 1) > row) above = mid;
+            else e = mid + 1;
+        }
+        return e;
+    };
+    if constexpr (SMALL) {
+        __shared__ int32_t owner[8];
+        const int64_t row = lo + w;
+        int e = row < hi ? first_behind(row) : s.experts;
+        if (e < s.experts && offset(e) > row) e = s.experts;
+        float v[8] = {};
+        if (e < s.experts && count > 0) slope_row<T>(s, row, c, count, aligned, v);
+        if (!s.partials) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) all[w][lane * 8 + i] = v[i];
+        if (lane == 0) owner[w] = e;
+        __syncthreads();
+        if (cc >= s.cols) return;
+        float sum = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const int here = owner[r];
+            sum += all[r][threadIdx.x];
+            if (here < s.experts && (r == 7 || owner[r + 1] != here)) s.partials[(chunk + here) * s.cols + cc] = sum;
+            if (r == 7 || owner[r + 1] != here) sum = 0.0f;
+        }
+        return;
     }
-    for (; e < s.experts; ++e) {
+    for (int e = first_behind(lo); e < s.experts; ++e) {
         const int64_t begin = offset(e), from = max(lo, begin), to = min(hi, offset(e + 1));
         if (begin >= hi) break;
         if (from >= to) continue;
         float sums[8] = {};
         if (count > 0)
             for (int64_t row = from + w; row < to; row += 8) {
-                const T *src = static_cast<const T *>(s.dy) + row * s.ld_dy + c, *z = static_cast<const T *>(s.z) + row * s.ld_z + c;
-                uint4 u, y = make_uint4(0, 0, 0, 0);
-                if (aligned && count >= 8) {
-                    u = *reinterpret_cast<const uint4 *>(src);
-                    if (s.z) y = *reinterpret_cast<const uint4 *>(z);
-                } else {
-                    Blocks a, b = {};
-                    a.load(src, count * 2);
-                    if (s.z) b.load(z, count * 2);
-                    u = a.get(src);
-                    y = b.get(z);
-                }
-                float v[8], at[8];
-                const uint32_t wu[4] = {u.x, u.y, u.z, u.w}, wy[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 f = unpack2<T>(wu[i]), g = unpack2<T>(wy[i]);
-                    v[2 * i] = f.x;
-                    v[2 * i + 1] = f.y;
-                    at[2 * i] = g.x;
-                    at[2 * i + 1] = g.y;
-                }
-                if (s.z) {
-                    times_slope8(v, at, s.activation);
-                    // dz becomes an operand of two products: 16 bits, as the tensor cores take them (see the linear layer's)
-                    u = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
-                }
+                float v[8];
+                slope_row<T>(s, row, c, count, aligned, v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sums[i] += v[i];
-                if (s.dst) *reinterpret_cast<uint4 *>(static_cast<T *>(s.dst) + row * s.ld_dst + c) = u;
             }
         if (!s.partials) continue;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 8; ++i) all[w][lane * 8 + i] = sums[i];
         __syncthreads();
-        const int64_t cc = column * kPrepareCols + threadIdx.x;
         if (cc < s.cols) {
             float sum = 0.0f;
 #pragma unroll
@@ -698,7 +731,7 @@ __device__ __forceinline__ void map_block(const PrepareParams &p, const CUtensor
 }
 
 // Each of the four has blocks of its own: what these small works cost is mostly a launch.
-template <typename T> __global__ void __launch_bounds__(256, 4)
+template <typename T, bool SMALL> __global__ void __launch_bounds__(256, 4)
 redist_expert_prepare_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ PrepareParams p)
 {
     __shared__ float all[8][kPrepareCols];
@@ -707,7 +740,7 @@ redist_expert_prepare_kernel(const __grid_constant__ CUtensorMap map_a, const __
     wait_for_previous();
     int64_t b = blockIdx.x;
     if (b < p.slope_blocks) {
-        slope_block<T>(p.p.slope, b / p.slope_across, b % p.slope_across, p.slope_per, p.aligned, all, offsets);
+        slope_block<T, SMALL>(p.p.slope, b / p.slope_across, b % p.slope_across, p.slope_per, p.aligned, all, offsets);
         return;
     }
     b -= p.slope_blocks;
@@ -1020,8 +1053,12 @@ cudaError_t launch_prepare(const Prepare &p, const LaunchOptions &o, cudaStream_
     const int64_t blocks = q.slope_blocks + q.lay_blocks[0] + q.lay_blocks[1] + q.map_blocks;
     if (blocks == 0) return cudaSuccess;
     if (blocks > INT32_MAX) return cudaErrorInvalidValue;
-    return p.type == T_BF16 ? launch_any(redist_expert_prepare_kernel<__nv_bfloat16>, dim3(unsigned(blocks)), 256, 0, 1, o, stream, ma, mb, q)
-                            : launch_any(redist_expert_prepare_kernel<__half>, dim3(unsigned(blocks)), 256, 0, 1, o, stream, ma, mb, q);
+    const dim3 grid = dim3(unsigned(blocks));
+    if (q.slope_per == 8)
+        return p.type == T_BF16 ? launch_any(redist_expert_prepare_kernel<__nv_bfloat16, true>, grid, 256, 0, 1, o, stream, ma, mb, q)
+                                : launch_any(redist_expert_prepare_kernel<__half, true>, grid, 256, 0, 1, o, stream, ma, mb, q);
+    return p.type == T_BF16 ? launch_any(redist_expert_prepare_kernel<__nv_bfloat16, false>, grid, 256, 0, 1, o, stream, ma, mb, q)
+                            : launch_any(redist_expert_prepare_kernel<__half, false>, grid, 256, 0, 1, o, stream, ma, mb, q);
 }
 
 cudaError_t read_grouped_timeouts(unsigned int *out) { return cudaMemcpyFromSymbol(out, g_grouped_timeouts, sizeof *out); }
