@@ -147,96 +147,96 @@ __global__ void __launch_bounds__(32 * kWarps, NT > 2 || ALIGN == 0 ? 3 : 4) red
     }
 #pragma unroll 1
     do {
-    const int rows = GROUPED ? min(to - from, NT * 8) : f.rows;
-    const T *x = static_cast<const T *>(f.x) + (GROUPED ? from * f.ld_x : 0), *w = static_cast<const T *>(f.w) + (GROUPED ? expert * f.w_batch : 0);
-    float acc[MT][NT][4] = {};
-    constexpr int kPairs = 2, kTurn = kPairs * 64;
+        const int rows = GROUPED ? min(to - from, NT * 8) : f.rows;
+        const T *x = static_cast<const T *>(f.x) + (GROUPED ? from * f.ld_x : 0), *w = static_cast<const T *>(f.w) + (GROUPED ? expert * f.w_batch : 0);
+        float acc[MT][NT][4] = {};
+        constexpr int kPairs = 2, kTurn = kPairs * 64;
 #pragma unroll 1
-    for (int64_t at = lo + warp * kTurn; at < hi; at += kTurn * kWarps) {
-        uint4 a[kPairs][MT][2][2];
+        for (int64_t at = lo + warp * kTurn; at < hi; at += kTurn * kWarps) {
+            uint4 a[kPairs][MT][2][2];
 #pragma unroll
-        for (int u = 0; u < kPairs; ++u) {
-            const int64_t c = at + u * 64 + t * 16;
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int64_t row = n0 + i * 16 + h * 8 + g;
-                    sixteen<ALIGN, true, !GROUPED>(w + row * f.ld_w, row < f.n ? c : hi, hi, a[u][i][h][0], a[u][i][h][1]);
-                }
-        }
-        // x is in L1 or L2: it is fetched while w is under way, and does not take registers from that
-#pragma unroll
-        for (int u = 0; u < kPairs; ++u)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
+            for (int u = 0; u < kPairs; ++u) {
                 const int64_t c = at + u * 64 + t * 16;
-                const int row = j * 8 + g;
-                uint4 b[2];
-                sixteen<ALIGN, false, !GROUPED>(x + int64_t(row) * f.ld_x, row < rows ? c : hi, hi, b[0], b[1]);
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
+                for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        const uint4 &a0 = a[u][i][0][q], &a1 = a[u][i][1][q];
-                        mma16<T>(acc[i][j], a0.x, a1.x, a0.y, a1.y, b[q].x, b[q].y);
-                        mma16<T>(acc[i][j], a0.z, a1.z, a0.w, a1.w, b[q].z, b[q].w);
+                    for (int h = 0; h < 2; ++h) {
+                        const int64_t row = n0 + i * 16 + h * 8 + g;
+                        sixteen<ALIGN, true, !GROUPED>(w + row * f.ld_w, row < f.n ? c : hi, hi, a[u][i][h][0], a[u][i][h][1]);
                     }
             }
-    }
-    // parts[warp][row of x][row of w]
+            // x is in L1 or L2: it is fetched while w is under way, and does not take registers from that
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+            for (int u = 0; u < kPairs; ++u)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+                for (int j = 0; j < NT; ++j) {
+                    const int64_t c = at + u * 64 + t * 16;
+                    const int row = j * 8 + g;
+                    uint4 b[2];
+                    sixteen<ALIGN, false, !GROUPED>(x + int64_t(row) * f.ld_x, row < rows ? c : hi, hi, b[0], b[1]);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) parts[warp][(j * 8 + 2 * t + (q & 1)) * MT * 16 + i * 16 + g + (q >> 1) * 8] = acc[i][j][q];
-    __syncthreads();
-    for (int o = threadIdx.x; o < kOut; o += 32 * kWarps) {
-        float s = 0.0f;
+                    for (int q = 0; q < 2; ++q)
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) s += parts[i][o];
-        total[o] = s;
-    }
-    if (splits > 1) {
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    } else {
-        __syncthreads();
-    }
-    // each block of the cluster finishes its share of the outputs
-    const Epilogue &e = f.e;
-    for (int o = int(rank) * 32 * kWarps + threadIdx.x; o < kOut; o += int(splits) * 32 * kWarps) {
-        const int row = o / (MT * 16);
-        const int64_t col = n0 + o % (MT * 16);
-        float v[8] = {};
-        if (splits > 1) {
-            const uint32_t here = uint32_t(__cvta_generic_to_shared(&total[o]));
-            for (uint32_t s = 0; s < splits; ++s) {
-                uint32_t there;
-                float part;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here), "r"(s));
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part) : "r"(there) : "memory");
-                v[0] += part;
-            }
-        } else {
-            v[0] = total[o];
+                        for (int i = 0; i < MT; ++i) {
+                            const uint4 &a0 = a[u][i][0][q], &a1 = a[u][i][1][q];
+                            mma16<T>(acc[i][j], a0.x, a1.x, a0.y, a1.y, b[q].x, b[q].y);
+                            mma16<T>(acc[i][j], a0.z, a1.z, a0.w, a1.w, b[q].z, b[q].w);
+                        }
+                }
         }
-        if (row >= rows || col >= f.n) continue;
-        if (e.bias) v[0] += load_any(e.bias, e.bias_type, (GROUPED ? expert * f.bias_stride : 0) + col);
-        const int64_t at = GROUPED ? from + row : row;
-        if (e.pre) static_cast<T *>(e.pre)[at * e.ld_pre + col] = from_float<T>(v[0]);
-        activate8(v, e.activation);
-        if (!GROUPED && e.residual) v[0] += to_float(static_cast<const T *>(e.residual)[at * e.ld_residual + col]);
-        static_cast<T *>(e.out)[at * e.ld_out + col] = from_float<T>(v[0]);
-    }
-    if (splits > 1) {                                     // the others read this block's shared memory
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    } else if (GROUPED) {
+        // parts[warp][row of x][row of w]
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) parts[warp][(j * 8 + 2 * t + (q & 1)) * MT * 16 + i * 16 + g + (q >> 1) * 8] = acc[i][j][q];
         __syncthreads();
-    }
-    from += NT * 8;
+        for (int o = threadIdx.x; o < kOut; o += 32 * kWarps) {
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) s += parts[i][o];
+            total[o] = s;
+        }
+        if (splits > 1) {
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        } else {
+            __syncthreads();
+        }
+        // each block of the cluster finishes its share of the outputs
+        const Epilogue &e = f.e;
+        for (int o = int(rank) * 32 * kWarps + threadIdx.x; o < kOut; o += int(splits) * 32 * kWarps) {
+            const int row = o / (MT * 16);
+            const int64_t col = n0 + o % (MT * 16);
+            float v[8] = {};
+            if (splits > 1) {
+                const uint32_t here = uint32_t(__cvta_generic_to_shared(&total[o]));
+                for (uint32_t s = 0; s < splits; ++s) {
+                    uint32_t there;
+                    float part;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here), "r"(s));
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part) : "r"(there) : "memory");
+                    v[0] += part;
+                }
+            } else {
+                v[0] = total[o];
+            }
+            if (row >= rows || col >= f.n) continue;
+            if (e.bias) v[0] += load_any(e.bias, e.bias_type, (GROUPED ? expert * f.bias_stride : 0) + col);
+            const int64_t at = GROUPED ? from + row : row;
+            if (e.pre) static_cast<T *>(e.pre)[at * e.ld_pre + col] = from_float<T>(v[0]);
+            activate8(v, e.activation);
+            if (!GROUPED && e.residual) v[0] += to_float(static_cast<const T *>(e.residual)[at * e.ld_residual + col]);
+            static_cast<T *>(e.out)[at * e.ld_out + col] = from_float<T>(v[0]);
+        }
+        if (splits > 1) {                                     // the others read this block's shared memory
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        } else if (GROUPED) {
+            __syncthreads();
+        }
+        from += NT * 8;
     } while (GROUPED && from < to);
 }
 

@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(kRouteThreads) redist_route_kernel(const Route
 }
 
 // The second step where tokens are many: a block's rows of expert e follow those of lower experts and those of the blocks
-// before it.
+// before it.  Two chains bound it, the blocks' counts (2 us) and the stretches' (3), at 16384 tokens with 8 of 128 experts.
 __global__ void __launch_bounds__(kRouteThreads) redist_place_kernel(const RouteParams p)
 {
     __shared__ int32_t base[kMostExperts], before[kMostExperts], counters[kCounters], total;
@@ -408,6 +408,10 @@ template <typename T, int PER> __global__ void __launch_bounds__(256) redist_rou
 }
 
 // ---- moves -----------------------------------------------------------------------------------------------
+
+// All of them are bound by memory: 16384 tokens of 4096 bf16 to two rows each 57 us (7.0 TB/s), back with weights and a residual 85
+// (6.3), their gradients 58 and 100 (6.7), against 6.56 for a plain copy.  Shorter rows share a warp; how many elements are
+// accessed at once goes by what columns, addresses and strides have in common.
 
 // N neighbours, loaded and stored at once.
 template <typename T, int N> struct Some {
