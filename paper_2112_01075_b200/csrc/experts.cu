@@ -537,7 +537,6 @@ struct PrepareParams {
     Prepare p;
     int64_t slope_per, slope_across;            // rows of a block, blocks side by side
     int64_t slope_blocks, lay_blocks[2], map_blocks;
-    int32_t aligned;                            // dy and z: every row starts on a 16-byte boundary
     int32_t rows, experts;                      // of the maps
     const int32_t *offsets;
 };
@@ -548,44 +547,48 @@ __device__ __forceinline__ int64_t offset_in(const int32_t *offsets, int e, int6
 
 constexpr int kHeldOffsets = 512;           // of so many experts the offsets are looked up in shared memory
 
-// A lane's eight neighbours of one row: dz, stored, and as it is before it is rounded.
-template <typename T> __device__ __forceinline__ void slope_row(const ExpertSlope &s, int64_t row, int64_t c, int count, bool aligned, float (&v)[8])
-{
-    const T *src = static_cast<const T *>(s.dy) + row * s.ld_dy + c, *z = static_cast<const T *>(s.z) + row * s.ld_z + c;
-    uint4 u, y = make_uint4(0, 0, 0, 0);
-    if (aligned && count >= 8) {
-        u = *reinterpret_cast<const uint4 *>(src);
-        if (s.z) y = *reinterpret_cast<const uint4 *>(z);
-    } else {
-        Blocks a, b = {};
-        a.load(src, count * 2);
-        if (s.z) b.load(z, count * 2);
-        u = a.get(src);
-        y = b.get(z);
+// A lane's eight neighbours of one row: asked for, and dz of them, stored, and as it is before it is rounded.
+template <typename T, bool ALIGNED> struct SlopeRow {
+    Blocks dy, z;
+    __device__ __forceinline__ void load(const ExpertSlope &s, int64_t row, int64_t c, int count)
+    {
+        const T *from = static_cast<const T *>(s.dy) + row * s.ld_dy + c, *at = static_cast<const T *>(s.z) + row * s.ld_z + c;
+        if (ALIGNED) {                                      // (the end of a row is in the same block)
+            dy.a = *reinterpret_cast<const uint4 *>(from);
+            if (s.z) z.a = *reinterpret_cast<const uint4 *>(at);
+        } else {
+            dy.load(from, count * 2);
+            if (s.z) z.load(at, count * 2);
+        }
     }
-    float at[8];
-    const uint32_t wu[4] = {u.x, u.y, u.z, u.w}, wy[4] = {y.x, y.y, y.z, y.w};
+    __device__ __forceinline__ void take(const ExpertSlope &s, int64_t row, int64_t c, float (&v)[8]) const
+    {
+        uint4 u = ALIGNED ? dy.a : dy.get(static_cast<const T *>(s.dy) + row * s.ld_dy + c);
+        const uint4 y = !s.z ? make_uint4(0, 0, 0, 0) : ALIGNED ? z.a : z.get(static_cast<const T *>(s.z) + row * s.ld_z + c);
+        float at[8];
+        const uint32_t wu[4] = {u.x, u.y, u.z, u.w}, wy[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = unpack2<T>(wu[i]), g = unpack2<T>(wy[i]);
-        v[2 * i] = f.x;
-        v[2 * i + 1] = f.y;
-        at[2 * i] = g.x;
-        at[2 * i + 1] = g.y;
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack2<T>(wu[i]), g = unpack2<T>(wy[i]);
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+            at[2 * i] = g.x;
+            at[2 * i + 1] = g.y;
+        }
+        if (s.z) {
+            times_slope8(v, at, s.activation);
+            // dz becomes an operand of two products: 16 bits, as the tensor cores take them (see the linear layer's)
+            u = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+        }
+        if (s.dst) *reinterpret_cast<uint4 *>(static_cast<T *>(s.dst) + row * s.ld_dst + c) = u;
     }
-    if (s.z) {
-        times_slope8(v, at, s.activation);
-        // dz becomes an operand of two products: 16 bits, as the tensor cores take them (see the linear layer's)
-        u = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
-    }
-    if (s.dst) *reinterpret_cast<uint4 *>(static_cast<T *>(s.dst) + row * s.ld_dst + c) = u;
-}
+};
 
 // A block takes `per` rows by 256 columns, and within them one expert's rows after the other; a warp every eighth row, a lane
 // eight neighbours.  Chunk c's sums for expert e are part c + e: both only grow, so no two share one.  SMALL: eight rows, a
 // warp each, whatever their experts are (one expert after the other, each a latency of memory, 8 rows of 72 experts took 14 us).
-template <typename T, bool SMALL> __device__ __forceinline__ void slope_block(const ExpertSlope &s, int64_t chunk, int64_t column, int64_t per, bool aligned,
-                                                                              float (&all)[8][kPrepareCols], int32_t (&offsets)[kHeldOffsets + 1])
+template <typename T, bool SMALL, bool ALIGNED> __device__ __forceinline__ void slope_block(const ExpertSlope &s, int64_t chunk, int64_t column, int64_t per,
+                                                                                           float (&all)[8][kPrepareCols], int32_t (&offsets)[kHeldOffsets + 1])
 {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int64_t c = column * kPrepareCols + lane * 8, lo = chunk * per, hi = min(s.rows, lo + per), cc = column * kPrepareCols + threadIdx.x;
@@ -611,7 +614,11 @@ template <typename T, bool SMALL> __device__ __forceinline__ void slope_block(co
         int e = row < hi ? first_behind(row) : s.experts;
         if (e < s.experts && offset(e) > row) e = s.experts;
         float v[8] = {};
-        if (e < s.experts && count > 0) slope_row<T>(s, row, c, count, aligned, v);
+        if (e < s.experts && count > 0) {
+            SlopeRow<T, ALIGNED> one;
+            one.load(s, row, c, count);
+            one.take(s, row, c, v);
+        }
         if (!s.partials) return;
 #pragma unroll
         for (int i = 0; i < 8; ++i) all[w][lane * 8 + i] = v[i];
@@ -633,10 +640,14 @@ template <typename T, bool SMALL> __device__ __forceinline__ void slope_block(co
         if (begin >= hi) break;
         if (from >= to) continue;
         float sums[8] = {};
+        SlopeRow<T, ALIGNED> next;                          // a row ahead
+        if (count > 0 && from + w < to) next.load(s, from + w, c, count);
         if (count > 0)
             for (int64_t row = from + w; row < to; row += 8) {
                 float v[8];
-                slope_row<T>(s, row, c, count, aligned, v);
+                const SlopeRow<T, ALIGNED> now = next;
+                if (row + 8 < to) next.load(s, row + 8, c, count);
+                now.take(s, row, c, v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sums[i] += v[i];
             }
@@ -679,8 +690,8 @@ __device__ __forceinline__ void lay_long(const StackLay &l, int64_t block, int64
     }
 }
 
-// ... and of lines of up to 256 columns as many as fill it, four times.
-constexpr int kShortLines = 4;
+// ... and of lines of up to 256 columns as many as fill it, twice.
+constexpr int kShortLines = 2;
 __host__ __device__ __forceinline__ int lay_lanes(int64_t line)       // of a line of up to 256 columns
 {
     int lanes = 32;
@@ -736,7 +747,7 @@ __device__ __forceinline__ void map_block(const PrepareParams &p, const CUtensor
 }
 
 // Each of the four has blocks of its own: what these small works cost is mostly a launch.
-template <typename T, bool SMALL> __global__ void __launch_bounds__(256, 4)
+template <typename T, bool SMALL, bool ALIGNED> __global__ void __launch_bounds__(256, 4)
 redist_expert_prepare_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ PrepareParams p)
 {
     __shared__ float all[8][kPrepareCols];
@@ -745,7 +756,7 @@ redist_expert_prepare_kernel(const __grid_constant__ CUtensorMap map_a, const __
     wait_for_previous();
     int64_t b = blockIdx.x;
     if (b < p.slope_blocks) {
-        slope_block<T, SMALL>(p.p.slope, b / p.slope_across, b % p.slope_across, p.slope_per, p.aligned, all, offsets);
+        slope_block<T, SMALL, ALIGNED>(p.p.slope, b / p.slope_across, b % p.slope_across, p.slope_per, all, offsets);
         return;
     }
     b -= p.slope_blocks;
@@ -1036,7 +1047,6 @@ cudaError_t launch_prepare(const Prepare &p, const LaunchOptions &o, cudaStream_
         q.slope_per = slope_rows(p.slope.rows, p.slope.cols);
         q.slope_across = (p.slope.cols + kPrepareCols - 1) / kPrepareCols;
         q.slope_blocks = (p.slope.rows + q.slope_per - 1) / q.slope_per * q.slope_across;
-        q.aligned = on_16(p.slope.dy, p.slope.ld_dy) && on_16(p.slope.z, p.slope.ld_z);
     }
     for (int i = 0; i < 2; ++i)
         if (p.lay[i].dst) {
@@ -1059,11 +1069,15 @@ cudaError_t launch_prepare(const Prepare &p, const LaunchOptions &o, cudaStream_
     if (blocks == 0) return cudaSuccess;
     if (blocks > INT32_MAX) return cudaErrorInvalidValue;
     const dim3 grid = dim3(unsigned(blocks));
-    if (q.slope_per == 8)
-        return p.type == T_BF16 ? launch_any(redist_expert_prepare_kernel<__nv_bfloat16, true>, grid, 256, 0, 1, o, stream, ma, mb, q)
-                                : launch_any(redist_expert_prepare_kernel<__half, true>, grid, 256, 0, 1, o, stream, ma, mb, q);
-    return p.type == T_BF16 ? launch_any(redist_expert_prepare_kernel<__nv_bfloat16, false>, grid, 256, 0, 1, o, stream, ma, mb, q)
-                            : launch_any(redist_expert_prepare_kernel<__half, false>, grid, 256, 0, 1, o, stream, ma, mb, q);
+    const bool aligned = on_16(p.slope.dy, p.slope.ld_dy) && on_16(p.slope.z, p.slope.ld_z), small = q.slope_per == 8;
+    auto go = [&](auto t) {
+        using T = decltype(t);
+        if (small) return aligned ? launch_any(redist_expert_prepare_kernel<T, true, true>, grid, 256, 0, 1, o, stream, ma, mb, q)
+                                  : launch_any(redist_expert_prepare_kernel<T, true, false>, grid, 256, 0, 1, o, stream, ma, mb, q);
+        return aligned ? launch_any(redist_expert_prepare_kernel<T, false, true>, grid, 256, 0, 1, o, stream, ma, mb, q)
+                       : launch_any(redist_expert_prepare_kernel<T, false, false>, grid, 256, 0, 1, o, stream, ma, mb, q);
+    };
+    return p.type == T_BF16 ? go(__nv_bfloat16()) : go(__half());
 }
 
 cudaError_t read_grouped_timeouts(unsigned int *out) { return cudaMemcpyFromSymbol(out, g_grouped_timeouts, sizeof *out); }
