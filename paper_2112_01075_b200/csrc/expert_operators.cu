@@ -177,7 +177,10 @@ struct PlacedStack {
         plane = fits ? stride : from.lines * ld;
         if (!fits) copy = pieces.take(count * plane * 2);
     }
-    StackLay lay(const int32_t *offsets) const { return StackLay{from.data, copy, count, from.lines, from.line, from.ld, stride, ld, plane, offsets}; }
+    StackLay lay(const int32_t *offsets, i64 rows) const
+    {
+        return StackLay{from.data, copy, count, from.lines, from.line, from.ld, stride, ld, plane, offsets, rows, 0};
+    }
     Operand operand(bool rows_survive) const { return Operand{fits ? from.data : copy, ld, plane, from.by_rows == rows_survive ? 0 : 1}; }
 };
 
@@ -462,8 +465,8 @@ redist_status redist_experts_forward(const redist_experts *op, void *scratch, si
         }
         Prepare before = {};
         before.type = q.type;
-        before.lay[0] = f.w.lay(q.offsets);
-        before.lay[1] = f.x.lay(nullptr);
+        before.lay[0] = f.w.lay(q.offsets, q.rows);
+        before.lay[1] = f.x.lay(nullptr, 0);
         TRY(cuda(launch_prepare(before, o, stream)));
         g.a = f.w.operand(true);
         g.b = f.x.operand(true);
@@ -544,8 +547,8 @@ redist_status redist_experts_backward(const redist_experts *op, const redist_exp
             s.ld_dst = b.ld_dz;
             s.partials = b.partials;
         }
-        before.lay[0] = b.w.lay(q.offsets);
-        before.lay[1] = b.x.lay(nullptr);
+        before.lay[0] = b.w.lay(q.offsets, q.rows);
+        before.lay[1] = b.x.lay(nullptr, 0);
         if (g.dw.data) before.sums = &w;
         before.maps = b.maps;
         TRY(cuda(launch_prepare(before, o, stream)));

@@ -536,7 +536,7 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
 struct PrepareParams {
     Prepare p;
     int64_t slope_per, slope_across;            // rows of a block, blocks side by side
-    int64_t slope_blocks, lay_blocks[2], map_blocks;
+    int64_t slope_blocks, lay_blocks[2], lay_share[2], map_blocks;      // lay_share: blocks of one matrix
     int32_t rows, experts;                      // of the maps
     const int32_t *offsets;
 };
@@ -665,32 +665,25 @@ template <typename T, bool SMALL, bool ALIGNED> __device__ __forceinline__ void 
     }
 }
 
-// A warp takes a line at a time, four stretches of 256 columns of it under way ...
-__device__ __forceinline__ void lay_long(const StackLay &l, int64_t block, int64_t blocks)
+// The matrix that a group of blocks lays out: of experts only those that have rows (-1: none).  By row, where rows are fewer than
+// experts: the expert whose first row is `slot`, so that the idle ones need no blocks.
+__device__ __forceinline__ int64_t matrix_of(const StackLay &l, int64_t slot)
 {
-    constexpr int kAhead = 4;
-    const int lane = threadIdx.x & 31;
-    const int64_t all = l.count * l.lines;
-    for (int64_t line = block * 8 + (threadIdx.x >> 5); line < all; line += blocks * 8) {
-        const int64_t matrix = l.count > 1 ? line / l.lines : 0, at = line - matrix * l.lines;
-        if (l.offsets && l.offsets[matrix + 1] <= l.offsets[matrix]) continue;
-        const uint16_t *src = static_cast<const uint16_t *>(l.src) + matrix * l.plane_src + at * l.ld_src;
-        uint16_t *dst = static_cast<uint16_t *>(l.dst) + matrix * l.plane_dst + at * l.ld_dst;
-        for (int64_t c = lane * 8; c < l.line; c += kAhead * kPrepareCols) {
-            Blocks b[kAhead];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int64_t count = min(l.line - c - i * kPrepareCols, int64_t(8));
-                if (count > 0) b[i].load(src + c + i * kPrepareCols, int(count) * 2);
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (c + i * kPrepareCols < l.line) *reinterpret_cast<uint4 *>(dst + c + i * kPrepareCols) = b[i].get(src + c + i * kPrepareCols);
-        }
-    }
+    if (!l.offsets) return slot;
+    if (!l.by_row) return l.offsets[slot + 1] > l.offsets[slot] ? slot : -1;
+    const int lane = threadIdx.x & 31, experts = int(l.count);
+    uint32_t next = uint32_t(experts) + 1;                  // the first offset beyond the row: where its expert ends
+    for (int i = lane; i <= experts && next > uint32_t(experts); i += 32)
+        if (l.offsets[i] > slot) next = uint32_t(i);
+    const int e = int(__reduce_min_sync(0xffffffffu, next)) - 1;
+    if (e < 0 || e >= experts) return -1;
+    int most = 0;
+    for (int i = lane; i <= e; i += 32) most = max(most, l.offsets[i]);
+    return __reduce_max_sync(0xffffffffu, most) == slot ? e : -1;
 }
 
-// ... and of lines of up to 256 columns as many as fill it, twice.
+// Lines of up to 256 columns: a warp takes as many as fill it, twice; longer ones one at a time, four stretches of 256 columns
+// under way.
 constexpr int kShortLines = 2;
 __host__ __device__ __forceinline__ int lay_lanes(int64_t line)       // of a line of up to 256 columns
 {
@@ -698,33 +691,46 @@ __host__ __device__ __forceinline__ int lay_lanes(int64_t line)       // of a li
     while (lanes > 1 && (lanes / 2) * 8 >= line) lanes /= 2;
     return lanes;
 }
-__device__ __forceinline__ void lay_short(const StackLay &l, int64_t block, int64_t blocks)
+
+// Block `block` of the `blocks` that share a matrix.
+__device__ __forceinline__ void lay_block(const StackLay &l, int64_t matrix, int64_t block, int64_t blocks)
 {
-    const int lanes = lay_lanes(l.line), group = 32 / lanes, lane = threadIdx.x & 31, c = lane % lanes * 8;
-    const int64_t all = l.count * l.lines, turn = kShortLines * group;
-    for (int64_t line0 = (block * 8 + (threadIdx.x >> 5)) * turn + lane / lanes; line0 < all; line0 += blocks * 8 * turn) {
-        Blocks b[kShortLines];
-        const uint16_t *src[kShortLines];
-        uint16_t *dst[kShortLines];
+    if (matrix < 0) return;
+    const uint16_t *from = static_cast<const uint16_t *>(l.src) + matrix * l.plane_src;
+    uint16_t *to = static_cast<uint16_t *>(l.dst) + matrix * l.plane_dst;
+    const int lane = threadIdx.x & 31;
+    const int64_t first = block * 8 + (threadIdx.x >> 5), step = blocks * 8;
+    if (l.line > kPrepareCols) {
+        constexpr int kAhead = 4;
+        for (int64_t line = first; line < l.lines; line += step) {
+            const uint16_t *src = from + line * l.ld_src;
+            uint16_t *dst = to + line * l.ld_dst;
+            for (int64_t c = lane * 8; c < l.line; c += kAhead * kPrepareCols) {
+                Blocks b[kAhead];
 #pragma unroll
-        for (int i = 0; i < kShortLines; ++i) {
-            const int64_t line = line0 + i * group;
-            const int64_t matrix = l.count == 1 ? 0 : all < INT32_MAX ? int64_t(uint32_t(line) / uint32_t(l.lines)) : line / l.lines, at = line - matrix * l.lines;
-            const bool some = line < all && c < l.line && !(l.offsets && l.offsets[matrix + 1] <= l.offsets[matrix]);
-            src[i] = static_cast<const uint16_t *>(l.src) + matrix * l.plane_src + at * l.ld_src + c;
-            dst[i] = some ? static_cast<uint16_t *>(l.dst) + matrix * l.plane_dst + at * l.ld_dst + c : nullptr;
-            if (some) b[i].load(src[i], int(min(l.line - c, int64_t(8))) * 2);
+                for (int i = 0; i < kAhead; ++i) {
+                    const int64_t count = min(l.line - c - i * kPrepareCols, int64_t(8));
+                    if (count > 0) b[i].load(src + c + i * kPrepareCols, int(count) * 2);
+                }
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+                    if (c + i * kPrepareCols < l.line) *reinterpret_cast<uint4 *>(dst + c + i * kPrepareCols) = b[i].get(src + c + i * kPrepareCols);
+            }
         }
+        return;
+    }
+    const int lanes = lay_lanes(l.line), group = 32 / lanes, c = lane % lanes * 8, turn = kShortLines * group;
+    if (c >= l.line) return;
+    for (int64_t line0 = first * turn + lane / lanes; line0 < l.lines; line0 += step * turn) {
+        Blocks b[kShortLines];
 #pragma unroll
         for (int i = 0; i < kShortLines; ++i)
-            if (dst[i]) *reinterpret_cast<uint4 *>(dst[i]) = b[i].get(src[i]);
+            if (line0 + i * group < l.lines) b[i].load(from + (line0 + i * group) * l.ld_src + c, int(min(l.line - c, int64_t(8))) * 2);
+#pragma unroll
+        for (int i = 0; i < kShortLines; ++i)
+            if (line0 + i * group < l.lines)
+                *reinterpret_cast<uint4 *>(to + (line0 + i * group) * l.ld_dst + c) = b[i].get(from + (line0 + i * group) * l.ld_src + c);
     }
-}
-
-__device__ __forceinline__ void lay_block(const StackLay &l, int64_t block, int64_t blocks)
-{
-    if (l.line > kPrepareCols) lay_long(l, block, blocks);
-    else lay_short(l, block, blocks);
 }
 
 // The maps of every expert's rows: copies of two that end with its last row.  A warp makes one.
@@ -760,9 +766,9 @@ redist_expert_prepare_kernel(const __grid_constant__ CUtensorMap map_a, const __
         return;
     }
     b -= p.slope_blocks;
-    if (b < p.lay_blocks[0]) return lay_block(p.p.lay[0], b, p.lay_blocks[0]);
+    if (b < p.lay_blocks[0]) return lay_block(p.p.lay[0], matrix_of(p.p.lay[0], b / p.lay_share[0]), b % p.lay_share[0], p.lay_share[0]);
     b -= p.lay_blocks[0];
-    if (b < p.lay_blocks[1]) return lay_block(p.p.lay[1], b, p.lay_blocks[1]);
+    if (b < p.lay_blocks[1]) return lay_block(p.p.lay[1], matrix_of(p.p.lay[1], b / p.lay_share[1]), b % p.lay_share[1], p.lay_share[1]);
     map_block(p, map_a, map_b, b - p.lay_blocks[1]);
 }
 
@@ -1051,8 +1057,12 @@ cudaError_t launch_prepare(const Prepare &p, const LaunchOptions &o, cudaStream_
     for (int i = 0; i < 2; ++i)
         if (p.lay[i].dst) {
             // a turn for each warp: there are more blocks than fit at once, and a warp's turn hides little
-            const int64_t line = p.lay[i].line, turn = line > kPrepareCols ? 1 : kShortLines * (32 / lay_lanes(line));
-            q.lay_blocks[i] = std::min<int64_t>((p.lay[i].count * p.lay[i].lines + 8 * turn - 1) / (8 * turn), 1 << 20);
+            StackLay &l = q.p.lay[i];
+            const int64_t turn = l.line > kPrepareCols ? 1 : kShortLines * (32 / lay_lanes(l.line));
+            l.by_row = l.offsets && l.rows < l.count && l.count <= 4096;        // (every block looks through the offsets then)
+            const int64_t slots = l.by_row ? l.rows : l.count;
+            q.lay_share[i] = std::max<int64_t>(1, std::min<int64_t>((l.lines + 8 * turn - 1) / (8 * turn), (int64_t(1) << 22) / slots));
+            q.lay_blocks[i] = slots * q.lay_share[i];
         }
     CUtensorMap ma, mb;
     std::memset(&ma, 0, sizeof ma);

@@ -65,6 +65,8 @@ struct StackLay {
     void *dst;
     int64_t count, lines, line, ld_src, plane_src, ld_dst, plane_dst;
     const int32_t *offsets;             // or null
+    int64_t rows;                       // of all experts
+    int32_t by_row;                     // set by launch_prepare
 };
 
 struct Prepare {
