@@ -1076,17 +1076,23 @@ _ABSENT = (0, 0, 0)
 
 def _move(o, token, row, position, residual=None, drow=None, weights=None, dweights=None):
     """The packed block of the four moves."""
-    if token.dim() != 2 or row.dim() != 2 or position.dim() != 2:
+    try:
+        tokens, cols = token.shape
+        rows, width = row.shape
+        places, k = position.shape
+    except ValueError:
         _not_matrices(tokens=token, rows=row, position=position)
-    (tokens, cols), dtype, device = token.shape, token.dtype, token.device
-    rows, k = row.shape[0], position.shape[1]
-    places, wide = (tokens, k), (rows, cols)
-    return _pack_move(tokens, rows, cols, _code(o, token, "tokens"), k, token.data_ptr(), *token.stride(), *_matrix(row, wide, dtype, device, "rows"),
+        raise
+    dtype, device, shape = token.dtype, token.device, (tokens, k)
+    if width != cols or row.dtype is not dtype or row.device != device:
+        _matrix(row, (rows, cols), dtype, device, "rows")                    # says what is wrong
+    if places != tokens or position.dtype is not o.i32 or position.device != device or not position.is_contiguous():
+        _table(o, position, shape, o.i32, device, "position")
+    return _pack_move(tokens, rows, cols, _code(o, token, "tokens"), k, token.data_ptr(), *token.stride(), row.data_ptr(), *row.stride(),
                       *(_ABSENT if residual is None else _matrix(residual, (tokens, cols), dtype, device, "residual")),
-                      *(_ABSENT if drow is None else _matrix(drow, wide, dtype, device, "drows")),
-                      _table(o, position, places, o.i32, device, "position"),
-                      0 if weights is None else _table(o, weights, places, o.f32, device, "weights"),
-                      0 if dweights is None else _table(o, dweights, places, o.f32, device, "dweights"))
+                      *(_ABSENT if drow is None else _matrix(drow, (rows, cols), dtype, device, "drows")), position.data_ptr(),
+                      0 if weights is None else _table(o, weights, shape, o.f32, device, "weights"),
+                      0 if dweights is None else dweights.data_ptr())
 
 
 def dispatch_forward(x, position, out=None, stream=None):
