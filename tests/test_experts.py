@@ -539,7 +539,7 @@ LISTS = [[1], [5, 0, 7], [4096], [100000, 3, 64, 1 << 20], [17] * 40, [1 + i % 5
 @pytest.mark.parametrize("case", range(len(LISTS)))
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32", "mixed", "off the blocks"])
 def test_clip(case, kind):
-    """Up to 32 squares are added in 32 bits (their sums then in 64): 33 2^-24 of the norm's square, half of it of the norm, and
+    """Up to 64 squares are added in 32 bits (their sums then in 64): 65 2^-24 of the norm's square, half of it of the norm, and
     its rounding; the factor takes three roundings more."""
     g = gen(case)
     types = {"bf16": [BF16], "f16": [F16], "f32": [F32]}.get(kind, [F32, BF16, F16])
@@ -548,7 +548,7 @@ def test_clip(case, kind):
         shift = i % 9 if kind == "off the blocks" else 0
         grads.append(rand(g, n + shift, scale=0.05, dtype=types[i % len(types)])[shift:])
     total = norm64(grads)
-    off = (33 / 2 + 1) * 2.0 ** -24
+    off = (65 / 2 + 1) * 2.0 ** -24
     keep = [t.clone() for t in grads]
     norm = api.clip_gradients(grads, None)
     assert norm.shape == () and norm.dtype is F32 and abs(float(norm) - total) <= total * off * 1.01
