@@ -574,7 +574,7 @@ redist_status redist_route_backward(const redist_route *op, const float *dweight
  *   redist_combine_backward:   drow[position[t, j]] = weights[t, j] token[t],  dweights[t, j] = <token[t], row[position[t, j]]>
  *                              (token: the output's gradient; that of residual is the same)
  *
- *   tokens, rows >= 0, cols >= 1, 1 <= chosen <= 32
+ *   tokens, rows >= 0, 1 <= cols <= 33553920, 1 <= chosen <= 32
  *   type            of all matrices: REDIST_BF16, REDIST_F16 or REDIST_F32
  *   token, residual tokens x cols, row-major; residual may be absent, or `token` itself
  *   row, drow       rows x cols, row-major
@@ -609,8 +609,8 @@ redist_status redist_combine_backward(const redist_move *op, void *cuda_stream);
  *   w               experts matrices out_features x in_features, all row-major or all column-major, w_stride elements apart
  *   bias            experts vectors of out_features elements of bias_type (any), bias_stride elements apart, or NULL
  *   out, pre        rows x out_features, row-major; pre may be absent: receives z = x w^T + bias for the backward pass
- *   offsets         device; experts + 1 32-bit integers, not decreasing, 0 ... rows.  Others are taken as the nearest that are, so
- *                   that nothing outside the arrays is touched
+ *   offsets         device; experts + 1 32-bit integers, not decreasing, 0 ... rows.  Others give results that are not defined, but
+ *                   nothing outside the arrays is touched
  *
  * redist_experts_backward -- the gradients.  With dz = dy activation'(pre), over the rows of expert e:
  *   dx[r] = dz[r] w[e]     dw[e] = sum of dz[r]^T x[r]     dbias[e] = sum of dz[r]

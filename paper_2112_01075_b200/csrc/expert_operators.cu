@@ -64,7 +64,7 @@ Route route_of(const redist_route &q)
 
 // ---- moves -----------------------------------------------------------------------------------------------
 
-constexpr i64 kMostColumns = i64(1) << 25;          // a grid's second dimension
+constexpr i64 kMostColumns = i64(65535) * 512;      // a grid's second dimension, where single elements are moved
 
 redist_status check_move(const redist_move &q, bool weights)
 {

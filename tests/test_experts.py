@@ -790,6 +790,31 @@ def test_move_refusals(name, change, status):
     assert getattr(api.load(), "redist_" + name)(api._Move(*{**MOVE, **change}.values()), None) == status
 
 
+@pytest.mark.parametrize("name", ["dispatch_forward", "dispatch_backward", "combine_forward", "combine_backward"])
+def test_widest_moves(name):
+    """The last number of columns that is taken, and the next (neither call has a token to move)."""
+    def call(cols):
+        return getattr(api.load(), "redist_" + name)(api._Move(*{**MOVE, "cols": cols, "token": (None, cols, 1)}.values()), None)
+    assert call(65535 * 512) == 1 and call(65535 * 512 + 1) == 10
+
+
+@pytest.mark.gpu
+def test_widest_moves_by_single_elements():
+    cols = 65535 * 512
+    g = gen(11)
+    x = rand(g, 1, cols + 1)[:, 1:]                           # off the blocks of 8 and 16 bytes
+    position, weights = torch.zeros((1, 1), dtype=I32, device="cuda"), torch.full((1, 1), 0.5, device="cuda")
+    rows = torch.zeros((1, cols + 1), device="cuda")[:, 1:]
+    assert torch.equal(api.dispatch_forward(x, position, out=rows), x)
+    assert torch.equal(api.combine_forward(rows, position, weights), x * 0.5)
+    ones = torch.ones_like(x)
+    drows, dweights = api.combine_backward(ones, rows, position, weights, drows=torch.empty((1, cols + 1), device="cuda")[:, 1:])
+    assert bool((drows == 0.5).all())
+    total = float(x.double().sum())
+    # a thread adds some 131072 values one after the other, then 256 such sums meet
+    assert abs(float(dweights) - total) <= (cols / 256 + 16) * 2.0 ** -24 * float(x.double().abs().sum())
+
+
 @pytest.mark.parametrize("name,change,status", [
     ("combine_forward", dict(residual=(0x10010, 32, 1)), 6), ("combine_forward", dict(residual=(0x70000, 31, 1)), 1), ("combine_forward", dict(weights=0x50002), 7),
     ("combine_forward", dict(weights=0x10000), 6), ("combine_backward", dict(weights=None), 1), ("combine_backward", dict(dweights=None), 1),
