@@ -81,7 +81,7 @@ def draw(rng):
                 return dict(kind=kind, type=rng.choice(("bf16", "bf16", "f16", "f32")), tokens=t, k=k, cols=c,
                             masked=rng.choice((0.0, 0.1)), residual=rng.random() < 0.5, grad=rng.random() < 0.5)
     if kind == "clip":
-        return dict(kind=kind, type=rng.choice(("bf16", "f16", "f32", "mixed")), tensors=_size(rng, 1, 60), most=_size(rng, 64, 1 << 22),
+        return dict(kind=kind, type=rng.choice(("bf16", "f16", "f32", "mixed")), tensors=_size(rng, 1, 600), most=_size(rng, 64, 1 << 22),
                     clip=rng.random() < 0.7)
     grad = kind == "experts_grad"
     while True:
