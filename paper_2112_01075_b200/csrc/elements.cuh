@@ -129,6 +129,9 @@ __device__ __forceinline__ uint4 load16_any(const void *p, int bytes)
     return v.get(p);
 }
 
+// A kernel starts while the one before it may still run, and waits here before it touches memory.  What it reads then may have been
+// written by that kernel, in the lifetime of this one: loads are plain ones, never __ldg or ld.global.nc, which take for granted that
+// nobody writes there as long as the kernel lives (and which the compiler may move up across the wait).
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

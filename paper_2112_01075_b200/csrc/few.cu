@@ -54,26 +54,24 @@ __device__ __forceinline__ void mma16<__half>(float (&c)[4], uint32_t a0, uint32
 }
 
 // 16 neighbours of a row in two blocks, zero beyond its end.  ALIGN 32: rows start on 32-byte boundaries and their length
-// is a multiple of 16 elements; 16: 16 bytes and 8 elements; 0: any.  STREAM: read once, not kept in L1.  FIXED: not written
-// while this kernel runs, the time included in which it waits for the one before it.
-template <int ALIGN, bool STREAM, bool FIXED, typename T> __device__ __forceinline__ void sixteen(const T *row, int64_t at, int64_t end, uint4 &u, uint4 &v)
+// is a multiple of 16 elements; 16: 16 bytes and 8 elements; 0: any.  STREAM: read once, not kept in L1.  Plain loads
+// (ld.global.nc is for what nobody writes while a kernel runs, and the kernel before, which may have written x and w, is
+// still running when this one has begun to wait for it).
+template <int ALIGN, bool STREAM, typename T> __device__ __forceinline__ void sixteen(const T *row, int64_t at, int64_t end, uint4 &u, uint4 &v)
 {
     u = v = make_uint4(0, 0, 0, 0);
     const int64_t left = end - at;
     if (left <= 0) return;
-    auto load = [](const uint4 *p) { return FIXED ? __ldg(p) : *p; };
-    if constexpr (ALIGN == 32 && STREAM && !FIXED) {
+    if constexpr (ALIGN == 32 && STREAM) {
         asm volatile("ld.global.L1::no_allocate.v8.u32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                      : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w), "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + at));
-    } else if constexpr (ALIGN == 32 && STREAM) {
-        asm volatile("ld.global.nc.L1::no_allocate.v8.u32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w), "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + at));
     } else if constexpr (ALIGN == 32) {
-        u = load(reinterpret_cast<const uint4 *>(row + at));
-        v = load(reinterpret_cast<const uint4 *>(row + at) + 1);
+        // (kept where it stands: loads of x that the compiler moved up together spilled, 16 x 4096 -> 16384 41 us for 37)
+        asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(row + at));
+        asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + at + 8));
     } else if constexpr (ALIGN == 16) {
-        u = load(reinterpret_cast<const uint4 *>(row + at));
-        if (left > 8) v = load(reinterpret_cast<const uint4 *>(row + at) + 1);
+        u = *reinterpret_cast<const uint4 *>(row + at);
+        if (left > 8) v = *(reinterpret_cast<const uint4 *>(row + at) + 1);
     } else {
         const int n = int(left < 16 ? left : 16);
         u = load16_any(row + at, min(n, 8) * 2);
@@ -162,7 +160,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT > 2 || ALIGN == 0 ? 3 : 4) red
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int64_t row = n0 + i * 16 + h * 8 + g;
-                        sixteen<ALIGN, true, !GROUPED>(w + row * f.ld_w, row < f.n ? c : hi, hi, a[u][i][h][0], a[u][i][h][1]);
+                        sixteen<ALIGN, true>(w + row * f.ld_w, row < f.n ? c : hi, hi, a[u][i][h][0], a[u][i][h][1]);
                     }
             }
             // x is in L1 or L2: it is fetched while w is under way, and does not take registers from that
@@ -173,7 +171,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT > 2 || ALIGN == 0 ? 3 : 4) red
                     const int64_t c = at + u * 64 + t * 16;
                     const int row = j * 8 + g;
                     uint4 b[2];
-                    sixteen<ALIGN, false, !GROUPED>(x + int64_t(row) * f.ld_x, row < rows ? c : hi, hi, b[0], b[1]);
+                    sixteen<ALIGN, false>(x + int64_t(row) * f.ld_x, row < rows ? c : hi, hi, b[0], b[1]);
 #pragma unroll
                     for (int q = 0; q < 2; ++q)
 #pragma unroll

@@ -712,7 +712,7 @@ __global__ void __launch_bounds__(kSumThreads) redist_column_sum_kernel(const fl
     float s = 0.0f;
     if (out && c < cols)
 #pragma unroll 8
-        for (int q = w; q < parts; q += kSumThreads / 32) s += __ldg(p + q * stride + c);
+        for (int q = w; q < parts; q += kSumThreads / 32) s += p[q * stride + c];            // (plain: see wait_for_previous)
     all[w][lane] = s;
     __syncthreads();
     // the warps' sums of column `w` of the block
@@ -834,7 +834,7 @@ template <typename T, bool ALIGNED, typename F> __device__ __forceinline__ void 
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int i = 0; i < kRaw; ++i) u[k][i] = __ldg(reinterpret_cast<const uint4 *>(p + k * 256) + i);
+                for (int i = 0; i < kRaw; ++i) u[k][i] = *(reinterpret_cast<const uint4 *>(p + k * 256) + i);      // (plain: see wait_for_previous)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 float v[8];
