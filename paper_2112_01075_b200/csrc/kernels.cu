@@ -140,7 +140,9 @@ __device__ __forceinline__ uint32_t fdiv(uint32_t n, const FastDiv &f)
 
 // Programmatic dependent launch: a kernel may start while the previous kernel of the stream still runs;
 // it must not touch global memory before this wait (kernel parameters and shared memory are free), so
-// every body decodes its first work item first and waits just before its first load.
+// every body decodes its first work item first and waits just before its first load.  What it loads may
+// have been written by that kernel, in the lifetime of this one: loads are plain ones, never __ldg or
+// ld.global.nc, which take for granted that nobody writes there as long as the kernel lives.
 __device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // streaming accesses: the data is touched once
@@ -179,9 +181,9 @@ __device__ __forceinline__ uint4 ld_shifted(const char *src)
 {
     const uint32_t m = uint32_t(reinterpret_cast<uintptr_t>(src)) & 15u;
     const uint4 *p = reinterpret_cast<const uint4 *>(src - m);
-    const uint4 a = __ldg(p);
+    const uint4 a = *p;
     if (m == 0) return a;
-    return funnel_shift16(a, __ldg(p + 1), m);
+    return funnel_shift16(a, p[1], m);
 }
 
 // Copy `count` pieces of `unit` bytes (unit = 1, 2, 4 or 8; all addresses are multiples of it) from
@@ -477,7 +479,7 @@ __device__ __forceinline__ void units_walk(const CopyParams<NT> &P, RowEntry *ro
                 }
                 d2[k] = b.o2 + a2;
                 ok[k] = ok[k] && CHK_SRC(P, b.sbase + a1, uint32_t(sizeof(T)));
-                if (ok[k]) v[k] = __ldg(reinterpret_cast<const T *>(b.sbase + a1));
+                if (ok[k]) v[k] = *reinterpret_cast<const T *>(b.sbase + a1);
             }
             for (uint32_t f = 0; f < fanout; ++f) {
                 char *dbase = b.dtab[f];
@@ -568,7 +570,7 @@ __device__ __forceinline__ uint4 gather_chunk(const CopyParams<NT> &P, const Box
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const T *sp = gather_src<LONG_DST, T, NT>(P, b, e, j, x + uint32_t(i * sizeof(T)));
-        u.t[i] = CHK_SRC(P, sp, uint32_t(sizeof(T))) ? __ldg(sp) : T();
+        u.t[i] = CHK_SRC(P, sp, uint32_t(sizeof(T))) ? *sp : T();
     }
     return u.v;
 }
@@ -647,7 +649,7 @@ __device__ __forceinline__ void gather_body(const CopyParams<NT> &P, RowEntry *r
                     const uint32_t x = (is_head ? 0u : toff) + slot * uint32_t(sizeof(T));
                     const T *sp = gather_src<LONG_DST, T, NT>(P, b, e, j, x);
                     if (!CHK_SRC(P, sp, uint32_t(sizeof(T)))) continue;
-                    const T val = __ldg(sp);
+                    const T val = *sp;
                     for (uint32_t f = 0; f < fanout; ++f) {
                         char *dbase = LONG_DST ? b.dtab[f] : P.dst[(b.t2 + j * g.gl_ts) * fanout + f];
                         if (CHK_DST(P, dbase + b.o2 + e.s2 + x, uint32_t(sizeof(T)))) *reinterpret_cast<T *>(dbase + b.o2 + e.s2 + x) = val;

@@ -9,15 +9,17 @@ import glob
 import os
 import re
 
+import numpy as np
 import pytest
 
+import oracle
 from paper_2112_01075_b200 import api
 
 torch = pytest.importorskip("torch")
 
 BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
 CSRC = os.path.join(os.path.dirname(api.__file__), "csrc")
-WAITS = "wait_for_previous()"
+WAITS = re.compile(r"\bwait_for_previous(_kernel)?\(\)")
 
 
 def code_of(path):
@@ -26,7 +28,7 @@ def code_of(path):
 
 
 def sources_that_wait():
-    kernels = [p for p in sorted(glob.glob(os.path.join(CSRC, "*.cu"))) if WAITS in code_of(p)]
+    kernels = [p for p in sorted(glob.glob(os.path.join(CSRC, "*.cu"))) if WAITS.search(code_of(p))]
     return kernels + sorted(glob.glob(os.path.join(CSRC, "*.cuh")))
 
 
@@ -36,9 +38,9 @@ def test_no_load_takes_the_read_only_path(path):
     assert not found, found
 
 
-def test_the_sources_of_the_operators_are_looked_through():
+def test_the_sources_of_all_kernels_are_looked_through():
     names = {os.path.basename(p) for p in sources_that_wait()}
-    assert {"few.cu", "rows.cu", "product.cu", "experts.cu", "routing.cu", "clip.cu", "elements.cuh", "activation.cuh"} <= names
+    assert {"kernels.cu", "few.cu", "rows.cu", "product.cu", "experts.cu", "routing.cu", "clip.cu", "elements.cuh", "activation.cuh"} <= names
 
 
 def gen(seed):
@@ -133,3 +135,37 @@ def test_orthogonalisation_of_what_a_product_has_written(n, m):
         pause()
         api.orthogonalize(x, out=out)
     back_to_back(calls, [x, out], 9)
+
+
+MOVES = [  # mesh, source, target, bytes of an element, mode: several launches, and runs of few bytes, ragged or interleaved
+    ((2, 3, 2), ((12, 12, 8), ((0,), (1,), ())), ((12, 12, 8), ((1,), (), (0,))), 4, api.FUSE_NONE),
+    ((4, 2), ((8 * 37, 8 * 101), ((0,), (1,))), ((8 * 37, 8 * 101), ((1,), (0,))), 2, api.NAIVE),
+    ((4,), ((36, 44, 28), ((0,), (), ())), ((36, 44, 28), ((), (), (0,))), 2, api.FUSE_ADJACENT),
+    ((4, 4, 4), ((8, 12, 4, 28, 20, 12), ((), (1,), (), (2,), (), ())), ((8, 12, 4, 28, 20, 12), ((2,), (), (), (), (0,), (1,))), 4, api.FUSE_NONE),
+    ((2, 3), ((30, 66), ((0,), (1,))), ((30, 66), ((1,), (0,))), 1, api.FUSE_NONE),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mesh,src,dst,e,mode", MOVES)
+def test_redistributions_one_after_the_other(mesh, src, dst, e, mode):
+    """There and back again over the same tiles, with other data every time that a kernel has written just before."""
+    there, back = api.Plan(mesh, src, dst, e, mode), api.Plan(mesh, dst, src, e, mode)
+    n = there.n_devices
+    rng = np.random.default_rng(n + e)
+    arrays = [rng.integers(0, 256, size=src[0] + (e,), dtype=np.uint8) for _ in range(3)]
+    stored = [[torch.from_numpy(np.ascontiguousarray(t).reshape(-1)).cuda() for t in oracle.reslice(mesh, src, a)] for a in arrays]
+    wanted = [[torch.from_numpy(np.ascontiguousarray(t).reshape(-1)).cuda() for t in oracle.reslice(mesh, dst, a)] for a in arrays]
+    a, b, c = ([torch.zeros(p.local_elems(i) * e, dtype=torch.uint8, device="cuda") for _ in range(n)] for p, i in ((there, 0), (there, 1), (back, 1)))
+    spaces = there.alloc_scratch(), back.alloc_scratch()
+    for i in range(30):
+        for t, s in zip(a, stored[i % 3]):
+            t.copy_(s)
+        there.execute(a, b, spaces[0])
+        back.execute(b, c, spaces[1])
+        there.execute(c, b, spaces[0])
+        back.execute(b, a, spaces[1])
+        there.execute(a, b, spaces[0])
+        got = [t.clone() for t in a], [t.clone() for t in b], [t.clone() for t in c]
+        assert all(torch.equal(x, y) for x, y in zip(got[0], stored[i % 3])) and all(torch.equal(x, y) for x, y in zip(got[2], stored[i % 3]))
+        assert all(torch.equal(x, y) for x, y in zip(got[1], wanted[i % 3])), i
