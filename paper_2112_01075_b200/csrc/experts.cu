@@ -445,8 +445,6 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         // whatever became of the waits: what was issued reads the stages and writes tensor memory, of both blocks of a pair
         if (elected()) commit<CG>(drained);
         ok = bar_wait(drained, 0, kDrainPolls) && ok;
-    } else if (warp == 1) {
-        ok = bar_wait(drained, 0, kDrainPolls);                           // reported by the first block
     } else if (warp == 2) {
         if (p.columns.sums) expert_sums(p.columns, blockIdx.x, gridDim.x, lane);
     } else if (warp >= 4) {
@@ -527,7 +525,12 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     __syncthreads();
     if constexpr (CG == 2) cluster_sync();
     fence_after();
-    if (threadIdx.x == 0 && *failed) atomicAdd(&g_grouped_timeouts, 1u);
+    // The end of the products is reported to both blocks of a pair, so the second one's memory has to last until then.  It asks now
+    // that the first has seen that end: a wait from the beginning would have to be as long as all tiles together.
+    const bool second = CG == 2 && rank != 0;
+    bool late = false;
+    if (second && warp == 1) late = !bar_wait(drained, 0, kDrainPolls);
+    if (threadIdx.x == (second ? 32 : 0) && (late || *failed)) atomicAdd(&g_grouped_timeouts, 1u);
     if (warp == 2) tmem_free<CG>(tmem, kColumns);
 }
 
