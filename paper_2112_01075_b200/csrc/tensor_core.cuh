@@ -41,6 +41,28 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t
     return done != 0;
 }
 
+// The same where threads of either block of a pair arrive and nothing but tensor memory is handed over: an order of execution, of
+// no other memory.  By PTX's description of tcgen05.fence, ::before_thread_sync and ::after_thread_sync need no more than that
+// between them: they compose with instructions that order the execution of threads, and then order the tcgen05 instructions on
+// either side.  (Its canonical patterns for different threads have mbarrier.arrive.relaxed.cluster behind the one and
+// mbarrier.try_wait.relaxed.cluster before the other.)
+__device__ __forceinline__ bool bar_wait_order(uint32_t bar, uint32_t parity, uint32_t polls)
+{
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, %3;\n"
+        "POLL:\n\t"
+        "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "@p bra DONE;\n\t"
+        "sub.u32 n, n, 1;\n\t"
+        "setp.ne.u32 q, n, 0;\n\t"
+        "@q bra POLL;\n"
+        "DONE:\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(done) : "r"(bar), "r"(parity), "r"(polls) : "memory");
+    return done != 0;
+}
+
 // One lane of a convergent warp, always the same.
 __device__ __forceinline__ bool elected()
 {
