@@ -622,7 +622,8 @@ template <typename T, int N, int L, int K> __global__ void __launch_bounds__(kMo
 // Where rows of 16-bit elements have no more in common than that: a row that is written is cut into the pieces that its own
 // 16-byte boundaries make; what it is made of is loaded from any address and shifted.
 template <typename T> struct Cut {
-    static constexpr int N = 16 / int(sizeof(T));
+    static_assert(sizeof(T) == 2, "words are taken apart into halves");
+    static constexpr int N = 8;
     int head, cols;                     // elements before the first boundary
     __device__ __forceinline__ Cut(const T *row, int64_t columns) : cols(int(columns))
     {
@@ -650,38 +651,30 @@ __device__ __forceinline__ uint4 joined(const Blocks &b, const void *p)
     if (off < 12) return joined<2>(b, off & 2);
     return joined<3>(b, off & 2);
 }
-template <typename T> __device__ __forceinline__ void floats(const uint4 &u, float (&v)[16 / sizeof(T)])
+template <typename T> __device__ __forceinline__ void floats(const uint4 &u, float (&v)[8])
 {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 4) {
-            v[i] = __uint_as_float(w[i]);
-        } else {
-            const float2 f = unpack2<T>(w[i]);
-            v[2 * i] = f.x;
-            v[2 * i + 1] = f.y;
-        }
+        const float2 f = unpack2<T>(w[i]);
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
     }
 }
-template <typename T> __device__ __forceinline__ uint4 rounded(const float (&v)[16 / sizeof(T)])
+template <typename T> __device__ __forceinline__ uint4 rounded(const float (&v)[8])
 {
-    if constexpr (sizeof(T) == 4) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-    else return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+    return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
 }
 template <typename T> __device__ __forceinline__ void store_some(T *to, const uint4 &u, int count)
 {
-    if (count == 16 / int(sizeof(T))) {
+    if (count == 8) {
         *reinterpret_cast<uint4 *>(to) = u;
         return;
     }
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 16 / int(sizeof(T)); ++i) {
-        if (i >= count) continue;
-        if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(to)[i] = w[i];
-        else reinterpret_cast<uint16_t *>(to)[i] = uint16_t(w[i >> 1] >> ((i & 1) * 16));
-    }
+    for (int i = 0; i < 8; ++i)
+        if (i < count) reinterpret_cast<uint16_t *>(to)[i] = uint16_t(w[i >> 1] >> ((i & 1) * 16));
 }
 
 constexpr int kCut = 2;                 // pieces under way per thread
@@ -904,9 +897,12 @@ template <Which W, typename T, int N> cudaError_t launch_move_lanes(const Move &
     const cudaError_t ce = current_device(&device, &sms);
     if (ce != cudaSuccess) return ce;
     // eight or sixteen lanes per token for the shortest rows, a warp (per stretch) for short ones, a block for longer ones
-    if (pieces > 32 * kHeld) return launch_move_width<W, T, N, kMoveThreads>(m, int(pieces), sms, o, stream);
-    if (pieces > 16 && pieces <= 32) return launch_move_width<W, T, N, 16>(m, int(pieces), sms, o, stream);
-    if (pieces > 16) return launch_move_width<W, T, N, 32>(m, int(pieces), sms, o, stream);
+    // (single elements of 16 bits: rows of up to 15 only, see launch_move_typed)
+    if constexpr (N * sizeof(T) > 2) {
+        if (pieces > 32 * kHeld) return launch_move_width<W, T, N, kMoveThreads>(m, int(pieces), sms, o, stream);
+        if (pieces > 16 && pieces <= 32) return launch_move_width<W, T, N, 16>(m, int(pieces), sms, o, stream);
+        if (pieces > 16) return launch_move_width<W, T, N, 32>(m, int(pieces), sms, o, stream);
+    }
     return launch_move_width<W, T, N, 8>(m, int(pieces), sms, o, stream);
 }
 
@@ -932,11 +928,12 @@ template <Which W, typename T> cudaError_t launch_move_typed(const Move &m, int 
     constexpr int kMost = 16 / int(sizeof(T));
     // 8000 x 4095, two rows each, forward and backward: 295 us cut and shifted, 441 by single elements; but with two elements of
     // 16 bits or one of 32 at a time the latter take less (4094: 280 against 289; 1021 of 32 bits: 207 against 261)
-    if (sizeof(T) == 2 && n == 1 && m.cols >= 2 * kMost)
-        return m.cols > 32 * kHeld * kMost ? launch_move_any<W, T, kMoveThreads>(m, o, stream)
-               : m.cols > 31 * kMost       ? launch_move_any<W, T, 32>(m, o, stream)
-               : m.cols > 15 * kMost       ? launch_move_any<W, T, 16>(m, o, stream)
-                                           : launch_move_any<W, T, 8>(m, o, stream);
+    if constexpr (sizeof(T) == 2)
+        if (n == 1 && m.cols >= 2 * kMost)
+            return m.cols > 32 * kHeld * kMost ? launch_move_any<W, T, kMoveThreads>(m, o, stream)
+                   : m.cols > 31 * kMost       ? launch_move_any<W, T, 32>(m, o, stream)
+                   : m.cols > 15 * kMost       ? launch_move_any<W, T, 16>(m, o, stream)
+                                               : launch_move_any<W, T, 8>(m, o, stream);
     if (n >= kMost) return launch_move_lanes<W, T, kMost>(m, o, stream);
     if (n >= kMost / 2) return launch_move_lanes<W, T, kMost / 2>(m, o, stream);
     if constexpr (kMost == 8)
