@@ -650,8 +650,8 @@ redist_status redist_experts_backward(const redist_experts *op, const redist_exp
  *   eps             >= 0 (1e-6 is usual)
  *   norm            device; one 32-bit float, or NULL
  * Squares are summed in a fixed order and without overflow or underflow for every finite input (64 bits where 32 would not
- * hold them).  The factor follows the formula for all inputs: an infinite norm gives 0 (and NaN where an element is
- * infinite), a NaN gives NaN throughout.  Errors: also EUNSUPPORTED for more than 2^40 elements in a tensor.
+ * hold them).  The factor follows the formula for all inputs, also where 32 bits hold neither it nor the norm (of which `norm`
+ * receives infinity then): an infinite element gives 0 (and NaN where it stands), a NaN gives NaN throughout.  Errors: also EUNSUPPORTED for more than 2^40 elements in a tensor.
  */
 typedef struct redist_tensor {
     void *data, *out;

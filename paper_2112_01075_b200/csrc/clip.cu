@@ -154,7 +154,7 @@ template <int MOST> __global__ void __launch_bounds__(kThreads, kBlocksPerSm) re
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
 }
 
-template <typename T> __device__ __forceinline__ void scale(const void *data, void *out, int64_t elements, int64_t unit, float factor)
+template <typename T, typename F> __device__ __forceinline__ void scale(const void *data, void *out, int64_t elements, int64_t unit, F factor)
 {
     constexpr int N = Share<T>::N;
     const Share<T> s(data, elements, unit);
@@ -168,7 +168,7 @@ template <typename T> __device__ __forceinline__ void scale(const void *data, vo
         float v[N];
         values<T>(u[j], v);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] *= factor;
+        for (int i = 0; i < N; ++i) v[i] = float(F(v[i]) * factor);
         const int64_t first = s.block(j) * N;
         if (aligned && s.whole(j)) {
             uint4 w;
@@ -185,6 +185,18 @@ template <typename T> __device__ __forceinline__ void scale(const void *data, vo
     }
 }
 
+template <int MOST, typename F> __device__ __forceinline__ void scale_all(const ClipTable<MOST> &c, F factor)
+{
+    for (int u = c.begin[c.count] - 1 - int(blockIdx.x); u >= 0; u -= gridDim.x) {
+        const int i = tensor_of(c, u);
+        if (factor == F(1) && c.out[i] == c.data[i]) continue;
+        const int64_t unit = u - c.begin[i];
+        if (c.type[i] == T_BF16) scale<__nv_bfloat16>(c.data[i], c.out[i], c.elements[i], unit, factor);
+        else if (c.type[i] == T_F16) scale<__half>(c.data[i], c.out[i], c.elements[i], unit, factor);
+        else scale<float>(c.data[i], c.out[i], c.elements[i], unit, factor);
+    }
+}
+
 template <int MOST> __global__ void __launch_bounds__(kThreads, kBlocksPerSm) redist_clip_kernel(const __grid_constant__ ClipTable<MOST> c)
 {
     __shared__ double slot[kThreads / 32];
@@ -192,19 +204,19 @@ template <int MOST> __global__ void __launch_bounds__(kThreads, kBlocksPerSm) re
     wait_for_previous();
     double sum = 0.0;
     for (int i = threadIdx.x; i < c.partials; i += kThreads) sum += c.sums[i];
-    const float norm = float(sqrt(block_sum(sum, slot)));
+    const double exact = sqrt(block_sum(sum, slot));
+    const float norm = float(exact);
     if (c.norm && blockIdx.x == 0 && threadIdx.x == 0) *c.norm = norm;
     if (c.max_norm < 0.0f) return;
     float factor = c.max_norm / (norm + c.eps);
-    if (factor > 1.0f) factor = 1.0f;                       // (a NaN stays)
-    for (int u = c.begin[c.count] - 1 - int(blockIdx.x); u >= 0; u -= gridDim.x) {
-        const int i = tensor_of(c, u);
-        if (factor == 1.0f && c.out[i] == c.data[i]) continue;
-        const int64_t unit = u - c.begin[i];
-        if (c.type[i] == T_BF16) scale<__nv_bfloat16>(c.data[i], c.out[i], c.elements[i], unit, factor);
-        else if (c.type[i] == T_F16) scale<__half>(c.data[i], c.out[i], c.elements[i], unit, factor);
-        else scale<float>(c.data[i], c.out[i], c.elements[i], unit, factor);
+    if (!(factor >= 0x1p-100f) && exact <= 0x1p1000) {
+        // a finite norm that 32 bits do not hold, or a quotient for which they have a few bits or none
+        const double quotient = double(c.max_norm) / (exact + double(c.eps));
+        if (quotient > 0.0 && quotient < 0x1p-100) return scale_all(c, quotient);
+        factor = float(quotient);
     }
+    if (factor > 1.0f) factor = 1.0f;                       // (a NaN stays)
+    scale_all(c, factor);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------
