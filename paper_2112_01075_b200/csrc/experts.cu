@@ -197,9 +197,11 @@ struct GroupedPieces {
     int turn = 0;
 
     // Fills a piece -- rows are the result's rows, 32 of its columns each -- and sends it off.  v: the fragments of lanes 0-15
-    // and 16-31.  `rows` of them are stored, at row0 on; `left`: columns up to the end of the result.
+    // and 16-31.  `rows` of them are stored, at row0 on, or (`ends`) as many as the map has; `left`: columns up to the end of the
+    // result.  The TMA writes whole 16 bytes: where a row ends within, what lies behind it would become zero (seen with 35 columns
+    // 40 apart), so the warp stores such a piece itself.
     template <typename T>
-    __device__ __forceinline__ void put(const float (&v)[32], const CUtensorMap *map, int aligned, void *out, int64_t ld, int lane, int64_t row0,
+    __device__ __forceinline__ void put(const float (&v)[32], const CUtensorMap *map, int aligned, bool ends, void *out, int64_t ld, int lane, int64_t row0,
                                         int rows, int col0, int left, int z, int64_t batch)
     {
         if (aligned) {
@@ -214,7 +216,7 @@ struct GroupedPieces {
                          ::"r"(at), "r"(pack2<T>(v[4 * i], v[4 * i + 1])), "r"(pack2<T>(v[4 * i + 2], v[4 * i + 3])),
                            "r"(pack2<T>(v[16 + 4 * i], v[16 + 4 * i + 1])), "r"(pack2<T>(v[16 + 4 * i + 2], v[16 + 4 * i + 3])) : "memory");
         }
-        if (aligned && rows >= 32) {
+        if (aligned && (ends || rows >= 32) && (left >= 32 || (left & 7) == 0)) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
@@ -490,12 +492,13 @@ redist_grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = 0.0f;
                 }
-                const int rows = SUMS && p.aligned_out ? 32 : at.count - c;           // (the map of a stack ends with each matrix)
+                const int rows = at.count - c;
                 const int64_t row0 = at.row0 + c;
                 const int z = SUMS ? at.expert : 0;
+                // (SUMS: a stack's map ends with each matrix, so whole boxes go out)
                 auto store = [&](const CUtensorMap *map, void *out, int64_t ld) {
-                    if (p.type == T_BF16) pieces.put<__nv_bfloat16>(v, map, p.aligned_out, out, ld, lane, row0, rows, col0, left, z, p.out_batch);
-                    else pieces.put<__half>(v, map, p.aligned_out, out, ld, lane, row0, rows, col0, left, z, p.out_batch);
+                    if (p.type == T_BF16) pieces.put<__nv_bfloat16>(v, map, p.aligned_out, SUMS, out, ld, lane, row0, rows, col0, left, z, p.out_batch);
+                    else pieces.put<__half>(v, map, p.aligned_out, SUMS, out, ld, lane, row0, rows, col0, left, z, p.out_batch);
                 };
                 if constexpr (!SUMS) {
                     if (p.bias)
