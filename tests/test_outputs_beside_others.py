@@ -70,3 +70,44 @@ def test_gradients_of_weights_of_one_row(k, experts):
             at = slice(int(offsets[i]), int(offsets[i + 1]))
             want, slack = products(dy[at].T.contiguous(), x[at].T.contiguous())
             within(dw.t[i], want, slack, BF16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", range(0, 6))
+@pytest.mark.parametrize("rows,k,n", [(40, 96, 35), (300, 35, 270), (700, 65, 1), (130, 1, 100), (33, 1604, 513), (1, 2055, 40), (513, 200, 7)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_linear_layers(rows, k, n, shape, dtype):
+    g = gen(rows + k + n)
+    x, w, r = rand(g, rows, k, dtype=dtype), rand(g, n, k, scale=k ** -0.5, dtype=dtype), rand(g, rows, n, dtype=dtype)
+    pre, dy = rand(g, rows, n, dtype=dtype), rand(g, rows, n, dtype=dtype)
+    z, slack = products(x, w)
+    d = dy.double()
+    dz = d * slope64(pre.double(), "silu")
+    off = dz.abs() * HALF_ULP[dtype] + d.abs() * 2.0 ** -20 + TINY[dtype]
+    for more in (0, 1):
+        y, p, dx, dw = (room(*s, dtype=dtype, more=more) for s in ((rows, n), (rows, n), (rows, k), (n, k)))
+        joined = room(rows, n, dtype=dtype, more=more)
+        beside = room(rows, n, dtype=dtype, more=more)
+        beside.t.copy_(r)
+        with api.tuning(test_product_shape=shape):
+            api.linear_forward(x, w, out=y.t, pre=p.t)
+            api.linear_forward(x, w, residual=beside.t, out=joined.t)
+            api.linear_forward(x, w, residual=beside.t, out=beside.t)
+            api.linear_backward(dy, x, w, pre, "silu", dx=dx.t, dw=dw.t)
+        assert all(t.intact() for t in (y, p, dx, dw, joined, beside))
+        within(y.t, z, slack, dtype)
+        assert torch.equal(y.t, p.t) and torch.equal(joined.t, beside.t)
+        within(joined.t, z + r.double(), slack + 2.0 ** -23 * (z + r.double()).abs(), dtype)
+        within(dx.t, dz @ w.double(), off @ w.double().abs() + (n + 2) * 2.0 ** -23 * (dz.abs() @ w.double().abs()), dtype)
+        within(dw.t, dz.T @ x.double(), off.T @ x.double().abs() + (rows + 2) * 2.0 ** -23 * (dz.abs().T @ x.double().abs()), dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,m,n", [(1, 130, 35), (1, 260, 513), (3, 64, 100), (2, 33, 7), (1, 1, 41), (2, 1, 20)])
+def test_orthogonalisation(batch, m, n):
+    x = rand(gen(m + n), batch, m, n, dtype=BF16)
+    want = api.orthogonalize(x)
+    for more, apart in ((0, 0), (1, 0), (0, 2)):
+        out = room(batch, m, n, dtype=BF16, more=more, apart=apart)
+        api.orthogonalize(x, out=out.t)
+        assert out.intact() and torch.equal(out.t, want)
