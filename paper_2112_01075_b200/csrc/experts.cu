@@ -6,8 +6,8 @@
 // rows are cut into tiles of nearly equal width.  Blocks stay on their SM and take tiles in turn; every warp walks along the
 // offsets by itself, 32 experts at a time.  The rest is that of the plain product (product.cu): TMA ring, two accumulators,
 // eight storing warps, bounded waits.  Outputs leave tensor memory transposed: the fragments are turned by stmatrix.trans on
-// their way to the pieces that the TMA stores; where a range ends within a piece the warp stores its rows itself, so
-// neighbours' rows are not touched.
+// their way to the pieces that the TMA stores; where a range ends within a piece, or a row within 16 bytes, the warp stores the
+// piece itself, so neighbours' rows and elements are not touched.
 // Sums over an expert's rows end in the middle of a box: every expert has tensor maps of its own, which end with its rows,
 // so that what follows is read as zeros -- products with the neighbours' rows would not do: zero times their infinities.
 //

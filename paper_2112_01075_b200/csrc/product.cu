@@ -5,16 +5,16 @@
 // shared-memory stages by TMA (128-byte swizzle), one thread issues the tcgen05.mma that consume them, and eight
 // warps turn the finished accumulator of the previous tile into outputs while the next one runs: tensor memory holds
 // two accumulators of BN columns.  Operands may be contiguous along the sum or along their rows (the gradients need
-// both): only the boxes and the shared-memory descriptors differ.  Ragged sizes cost nothing extra: the TMA fills
-// what lies outside an operand with zeros, and the epilogue stores what lies inside the result.
+// both): only the boxes and the shared-memory descriptors differ.  Ragged sizes cost nothing extra in the operands: the TMA
+// fills what lies outside one with zeros.  The epilogue stores what lies inside the result.
 //
 // What bounds it: large products the tensor cores and, in long runs, the power they may draw -- 8192 x 4096 -> 8192 with
 // GELU keeps their pipe busy 96 % of the cycles at 1.43 GHz; 16384 x 4096 -> 16384 takes 1370 us in a run of 50 ms and 1600
 // in one of two seconds (1605 and 1372 TFLOP/s; a library product 1649 at its best and 1372 sustained), with bias and GELU
 // 1385 and 1615.  A stack of 2048 x 2048 squares keeps the pipe busy 64-70 %: 32 stages of sum do not hide the last epilogue.  Small
 // products: the 2 us of a launch, 1 us to the first operands, 0.1-0.15 us per 64 steps of the sum, 1-3 us for the last
-// epilogue (512^3: 4.4 us, 1024^3: 6.0).  Rows of outputs or residuals off 16-byte boundaries cost about 20 us per
-// 4096 x 4096 outputs in the epilogue's stores.
+// epilogue (512^3: 4.4 us, 1024^3: 6.0).  Rows of outputs or residuals that start off 16-byte boundaries, and of outputs that end off
+// them, cost about 20 us per 4096 x 4096 outputs in the epilogue's stores.
 //
 // Every wait on an mbarrier is bounded, the storing warps' by polls that grow with a tile's sum.  A role whose wait runs
 // out leaves its loop, so the others' waits run out too; products already issued are awaited, as they are in a healthy
